@@ -61,7 +61,12 @@ typedef enum {
                                the fp16 range (see Precision)                  */
 } fsx_status;
 
-typedef enum { FSX_F32 = 0, FSX_BF16 = 1 } fsx_dtype;
+typedef enum {
+  FSX_F32 = 0,
+  FSX_BF16 = 1,
+  FSX_F16 = 2,  /* only where an entry point says so */
+  FSX_E4M3 = 3  /* 8-bit cache codes with scales (fsx_cache_write_e4m3); only where an entry point says so */
+} fsx_dtype;
 
 /* Model and capacity description, fixed at fsx_create. */
 typedef struct {
@@ -471,6 +476,100 @@ void* fsx_session_append_stream(fsx_session s);
 /* Waits for every append and tick enqueued so far. */
 fsx_status fsx_session_sync(fsx_session s);
 void fsx_session_destroy(fsx_session s);
+
+/* ================================================================ prompts and 8-bit caches
+ * The operators around a backbone's cache that neither the tick nor the append covers: the
+ * attention of whole prompts, whose rows fill a cache; a cache in 8 bits, which holds twice the
+ * rows in the same bytes; and the attention of a few drafted tokens over either cache. The paper
+ * leaves the backbone's prefill and decoding to its serving stack (Sec. 3.3).
+ * Shared conventions:
+ *   - Queries have n_heads heads, keys and values n_kv_heads; head h reads kv head
+ *     h / (n_heads / n_kv_heads). n_heads is a multiple of n_kv_heads, at most 64 times it.
+ *     head_dim is 128.
+ *   - Rows are packed: sequence b owns rows offsets[b] .. offsets[b+1]-1. Strides are in
+ *     elements between rows, so q, k and v may be columns of one projection's output; a row's
+ *     heads lie back to back. Rows are 16-byte aligned (base pointers, and strides a multiple of
+ *     16 bytes); outputs and caches are contiguous. Offsets may exceed 32 bits in elements.
+ *   - d_status: DEVICE int, not NULL, that the caller zeroes once and reads when it likes. A
+ *     call that finds an error writes its code there unless one is there already; no call clears it.
+ *   - Softmax statistics and sums are fp32. Weights of the values are rounded to the type of the
+ *     values, or for e4m3 caches to a sum of e4m3 parts that carries as many bits as the type.
+ *   - A key that a row does not see has no effect on it, whatever the key and value hold (NaN and
+ *     infinities too). A row that sees no key gets zeros and a log-sum-exp of -infinity.
+ *   - Asynchronous on `stream`; nothing is allocated. */
+
+/* Write n_rows rows of keys and values into an 8-bit cache: per row and kv head the scale is
+ * the smallest power of two s (at least 2^-126) with max|x| / s <= 448, and the code is x / s
+ * rounded to e4m3 (nearest, ties to even). A row of zeros has scale 1.
+ *   d_k, d_v   : DEVICE [n_rows] rows of `dtype` (FSX_F32, FSX_BF16, FSX_F16), kv_stride apart.
+ *   d_rows     : DEVICE int64 [n_rows]: the cache row that row i goes to; NULL: row i. Rows that
+ *                repeat leave one of their values.
+ *   d_k_cache, d_v_cache : DEVICE e4m3 [cache_rows, n_kv_heads, 128].
+ *   d_k_scale, d_v_scale : DEVICE fp32 [n_kv_heads, cache_rows].
+ * A destination outside 0 .. cache_rows-1 sets the status to FSX_ERR_DEVICE_ARG and its row is
+ * left out. A value that is not finite sets FSX_ERR_RANGE: it is stored as the NaN code, the
+ * others of its row with the scale of the finite ones. */
+fsx_status fsx_cache_write_e4m3(const void* d_k, const void* d_v, long long kv_stride, int dtype,
+                                const int64_t* d_rows, long long n_rows, int n_kv_heads, int head_dim,
+                                void* d_k_cache, void* d_v_cache, float* d_k_scale, float* d_v_scale,
+                                long long cache_rows, int* d_status, void* stream);
+
+/* Read n_rows rows of an 8-bit cache back: code times scale, rounded to `dtype` (FSX_F32, FSX_BF16,
+ * FSX_F16). Arguments as fsx_cache_write_e4m3, d_k and d_v being outputs. A cache row outside
+ * 0 .. cache_rows-1 sets FSX_ERR_DEVICE_ARG and leaves its output row unwritten. */
+fsx_status fsx_cache_read_e4m3(const void* d_k_cache, const void* d_v_cache, const float* d_k_scale,
+                               const float* d_v_scale, long long cache_rows, const int64_t* d_rows,
+                               long long n_rows, int n_kv_heads, int head_dim, void* d_k, void* d_v,
+                               long long kv_stride, int dtype, int* d_status, void* stream);
+
+/* Attention over whole prompts: O_i = softmax_j(q_i . k_j / sqrt(128)) v_j for every packed
+ * sequence and head. The queries of a sequence are its last tokens: with Lq queries and Lk keys,
+ * query i sees keys 0 .. Lk - Lq + i if `causal`, else all of them (Lk > Lq: a chunk behind rows
+ * that are there already; Lk < Lq: the first queries see nothing).
+ *   d_q        : DEVICE [q_rows] rows of `dtype` (FSX_BF16 or FSX_F16), q_stride apart.
+ *   d_k, d_v   : DEVICE [kv_rows] rows of the same type, kv_stride apart.
+ *   d_q_offsets, d_kv_offsets : DEVICE int64 [B+1], non-decreasing, within 0 .. q_rows / kv_rows.
+ *                B is 1 .. 1024; q_rows and kv_rows are below 2^31.
+ *   d_out      : DEVICE [q_rows, n_heads, 128] of `dtype`; rows of no sequence stay unwritten.
+ *   d_lse      : DEVICE fp32 [n_heads, q_rows], natural log-sum-exp of the scaled scores, or NULL.
+ * A sequence whose offsets are negative, decrease or pass the rows sets FSX_ERR_DEVICE_ARG and
+ * gets no output row; the others are written. */
+fsx_status fsx_prompt_attention(const void* d_q, long long q_stride, const void* d_k, const void* d_v,
+                                long long kv_stride, int dtype, const int64_t* d_q_offsets,
+                                const int64_t* d_kv_offsets, int B, long long q_rows, long long kv_rows,
+                                int n_heads, int n_kv_heads, int head_dim, int causal, void* d_out, float* d_lse,
+                                int* d_status, void* stream);
+
+/* Attention of a few new tokens of each request, a tree of drafts or a single token, over the
+ * request's cache rows and over those of its new tokens that a mask names, in one softmax.
+ *   d_q, d_k_new, d_v_new : DEVICE [new_rows] rows of `dtype` (FSX_BF16 or FSX_F16); q_stride and
+ *                new_stride apart.
+ *   d_new_offsets : DEVICE int64 [B+1], non-decreasing, within 0 .. new_rows: request b's new tokens,
+ *                at most 64 (0 is allowed).
+ *   d_mask     : DEVICE uint64 [new_rows]: bit j of a token's word: it sees its request's j-th new
+ *                token (set a token's own bit, and its ancestors' in the tree). Bits past the
+ *                request's tokens are ignored.
+ *   d_k_cache, d_v_cache : DEVICE [cache_rows, n_kv_heads, 128] of cache_dtype: `dtype` itself, or
+ *                FSX_E4M3 with d_k_scale, d_v_scale as fsx_cache_write_e4m3 leaves them (any finite
+ *                positive scales; NULL for a 16-bit cache). May be NULL if cache_rows is 0.
+ *   d_starts, d_offsets : as fsx_tick_ranges: request b reads cache rows d_starts[b] .. d_starts[b] +
+ *                L_b - 1, L_b = d_offsets[b+1] - d_offsets[b]; NULL d_starts: from row d_offsets[b].
+ *   B          : 1 .. 1024; cache_rows and new_rows are below 2^31.
+ *   d_out      : DEVICE [new_rows, n_heads, 128] of `dtype`; rows of no request stay unwritten.
+ *   d_lse      : DEVICE fp32 [n_heads, new_rows] as fsx_prompt_attention, or NULL.
+ *   d_workspace : DEVICE scratch of fsx_tree_attention_workspace_bytes(...) bytes, 256-byte aligned,
+ *                zeroed by the caller once before its first use; a call leaves it ready for the next. Calls
+ *                that overlap on the GPU must not share it. Zero it again after FSX_ERR_TIMEOUT.
+ * A request whose offsets are negative, decrease, pass the rows or name more than 64 new tokens
+ * sets FSX_ERR_DEVICE_ARG and gets no output row; the others are written. */
+size_t fsx_tree_attention_workspace_bytes(int B, long long new_rows, int n_heads, int n_kv_heads);
+fsx_status fsx_tree_attention(const void* d_q, long long q_stride, const void* d_k_new, const void* d_v_new,
+                              long long new_stride, int dtype, const int64_t* d_new_offsets, const uint64_t* d_mask,
+                              long long new_rows, const void* d_k_cache, const void* d_v_cache,
+                              const float* d_k_scale, const float* d_v_scale, int cache_dtype,
+                              long long cache_rows, const int64_t* d_starts, const int64_t* d_offsets, int B,
+                              int n_heads, int n_kv_heads, int head_dim, void* d_out, float* d_lse,
+                              void* d_workspace, size_t workspace_bytes, int* d_status, void* stream);
 
 #ifdef __cplusplus
 }

@@ -27,6 +27,8 @@ FSX_ERR_DEVICE_ARG = 6
 FSX_ERR_RANGE = 7
 FSX_F32 = 0
 FSX_BF16 = 1
+FSX_F16 = 2
+FSX_E4M3 = 3
 FSX_SCHED_SERIAL = 0
 FSX_SCHED_CONCURRENT = 1
 
@@ -84,6 +86,7 @@ def _load():
     vp, i32, i64p = ctypes.c_void_p, ctypes.c_int, ctypes.POINTER(ctypes.c_int64)
     vpp = ctypes.POINTER(ctypes.c_void_p)
     fp = ctypes.POINTER(ctypes.c_float)
+    ll = ctypes.c_longlong
     sig = {
         "fsx_create": (i32, [ctypes.POINTER(Config), ctypes.POINTER(Weights), i32, ctypes.POINTER(vp)]),
         "fsx_tick": (i32, [vp, vpp, vpp, vp, i32, vp, vp, vp]),
@@ -124,6 +127,13 @@ def _load():
         "fsx_append_get_status": (i32, [vp, vp]),
         "fsx_append_weight_bytes": (ctypes.c_longlong, [vp]),
         "fsx_append_destroy": (None, [vp]),
+        "fsx_cache_write_e4m3": (i32, [vp, vp, ll, i32, vp, ll, i32, i32, vp, vp, vp, vp, ll, vp, vp]),
+        "fsx_cache_read_e4m3": (i32, [vp, vp, vp, vp, ll, vp, ll, i32, i32, vp, vp, ll, i32, vp, vp]),
+        "fsx_prompt_attention": (i32, [vp, ll, vp, vp, ll, i32, vp, vp, i32, ll, ll, i32, i32, i32, i32, vp, vp, vp,
+                                       vp]),
+        "fsx_tree_attention_workspace_bytes": (ctypes.c_size_t, [i32, ll, i32, i32]),
+        "fsx_tree_attention": (i32, [vp, ll, vp, vp, ll, i32, vp, vp, ll, vp, vp, vp, vp, i32, ll, vp, vp, i32, i32,
+                                     i32, i32, vp, vp, vp, ctypes.c_size_t, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -151,7 +161,8 @@ def declared_symbols() -> list[str]:
             "fsx_append_get_status", "fsx_append_weight_bytes", "fsx_append_destroy", "fsx_append_set_concurrent",
             "fsx_session_create", "fsx_session_append", "fsx_session_tick", "fsx_session_committed",
             "fsx_session_reserved", "fsx_session_tick_stream", "fsx_session_append_stream", "fsx_session_sync",
-            "fsx_session_destroy", "fsx_set_wait_limit"]
+            "fsx_session_destroy", "fsx_set_wait_limit", "fsx_cache_write_e4m3", "fsx_cache_read_e4m3",
+            "fsx_prompt_attention", "fsx_tree_attention_workspace_bytes", "fsx_tree_attention"]
 
 
 def last_error() -> str:
@@ -334,6 +345,126 @@ def attention_noalloc_status(stream=None) -> int:
     """fsx_attention_noalloc_status: synchronises the stream, returns and clears the
     device status word of the static scratch (FSX_OK, FSX_ERR_DEVICE_ARG or FSX_ERR_TIMEOUT)."""
     return int(lib().fsx_attention_noalloc_status(_stream(stream)))
+
+
+_DTYPE_CODE = {"torch.float32": FSX_F32, "torch.bfloat16": FSX_BF16, "torch.float16": FSX_F16,
+               "torch.float8_e4m3fn": FSX_E4M3, "torch.uint8": FSX_E4M3}
+
+
+def _code(t) -> int:
+    """fsx_dtype of a tensor; e4m3 caches may be held as bytes."""
+    code = _DTYPE_CODE.get(str(t.dtype))
+    if code is None:
+        raise FsxError(FSX_ERR_UNSUPPORTED, f"dtype {t.dtype}")
+    return code
+
+
+def _same(ok: bool, what: str):
+    if not ok:
+        raise FsxError(FSX_ERR_INVALID_ARG, what)
+
+
+def _rows_of(t, what: str) -> int:
+    """Row stride of [rows, heads, 128] whose rows are contiguous."""
+    _same(t.dim() == 3 and t.stride(2) == 1 and (t.shape[1] == 1 or t.stride(1) == t.shape[2]),
+          f"{what}: [rows, heads, head_dim] with contiguous rows")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1] * t.shape[2])
+
+
+def _one_stride(a, b, what: str) -> int:
+    sa, sb = _rows_of(a, what), _rows_of(b, what)
+    _same(a.shape == b.shape and a.dtype == b.dtype and sa == sb, f"{what}: same shape, dtype and row stride")
+    return sa
+
+
+def _whole(t, what: str, dtype: str | None = None, shape=None):
+    _same(t.is_contiguous() and (dtype is None or str(t.dtype) == dtype) and
+          (shape is None or tuple(t.shape) == tuple(shape)), f"{what}: contiguous {dtype or ''} {shape or ''}")
+
+
+def _cache8(k_cache, v_cache, k_scale, v_scale):
+    _whole(k_cache, "k_cache")
+    _whole(v_cache, "v_cache", None, k_cache.shape)
+    _same(k_cache.dim() == 3 and k_cache.dtype == v_cache.dtype and _code(k_cache) == FSX_E4M3,
+          "8-bit caches: [rows, kv heads, 128] of float8_e4m3fn or uint8")
+    for t in (k_scale, v_scale):
+        _whole(t, "scales", "torch.float32", (k_cache.shape[1], k_cache.shape[0]))
+
+
+def cache_write(k, v, rows, k_cache, v_cache, k_scale, v_scale, status, stream=None):
+    """fsx_cache_write_e4m3: rows k, v [n, kv heads, 128] into cache rows `rows` (int64 [n]; None: 0 .. n - 1)."""
+    _cache8(k_cache, v_cache, k_scale, v_scale)
+    stride = _one_stride(k, v, "k, v")
+    _same(k.shape[1:] == k_cache.shape[1:], "k, v and the caches: same heads")
+    if rows is not None:
+        _whole(rows, "rows", "torch.int64", (k.shape[0],))
+    check(lib().fsx_cache_write_e4m3(_ptr(k), _ptr(v), stride, _code(k), _ptr(rows), k.shape[0], k.shape[1], k.shape[2],
+                                     _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), k_cache.shape[0],
+                                     _ptr(status), _stream(stream)))
+
+
+def cache_read(k_cache, v_cache, k_scale, v_scale, rows, k, v, status, stream=None):
+    """fsx_cache_read_e4m3: cache rows `rows` (int64 [n]; None: 0 .. n - 1) into k, v [n, kv heads, 128]."""
+    _cache8(k_cache, v_cache, k_scale, v_scale)
+    stride = _one_stride(k, v, "k, v")
+    _same(k.shape[1:] == k_cache.shape[1:], "k, v and the caches: same heads")
+    if rows is not None:
+        _whole(rows, "rows", "torch.int64", (k.shape[0],))
+    check(lib().fsx_cache_read_e4m3(_ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), k_cache.shape[0],
+                                    _ptr(rows), k.shape[0], k.shape[1], k.shape[2], _ptr(k), _ptr(v), stride, _code(k),
+                                    _ptr(status), _stream(stream)))
+    return k, v
+
+
+def prompt_attention(q, k, v, q_offsets, kv_offsets, out, status, lse=None, causal=True, stream=None):
+    """fsx_prompt_attention: packed q [rows, heads, 128], k and v [rows, kv heads, 128], int64 offsets [B + 1]."""
+    stride = _one_stride(k, v, "k, v")
+    _same(q.dtype == k.dtype and q.dtype == out.dtype and q.shape[2] == k.shape[2], "q, k, v, out: same dtype and head_dim")
+    _whole(out, "out", None, q.shape)
+    _whole(q_offsets, "q_offsets", "torch.int64")
+    _whole(kv_offsets, "kv_offsets", "torch.int64", q_offsets.shape)
+    if lse is not None:
+        _whole(lse, "lse", "torch.float32", (q.shape[1], q.shape[0]))
+    check(lib().fsx_prompt_attention(_ptr(q), _rows_of(q, "q"), _ptr(k), _ptr(v), stride, _code(q), _ptr(q_offsets),
+                                     _ptr(kv_offsets), q_offsets.shape[0] - 1, q.shape[0], k.shape[0], q.shape[1],
+                                     k.shape[1], q.shape[2], int(causal), _ptr(out), _ptr(lse), _ptr(status),
+                                     _stream(stream)))
+    return out
+
+
+def tree_attention_workspace_bytes(B: int, new_rows: int, n_heads: int, n_kv_heads: int) -> int:
+    return int(lib().fsx_tree_attention_workspace_bytes(B, new_rows, n_heads, n_kv_heads))
+
+
+def tree_attention(q, k_new, v_new, new_offsets, mask, k_cache, v_cache, offsets, out, status, workspace, k_scale=None,
+                   v_scale=None, starts=None, lse=None, stream=None):
+    """fsx_tree_attention: the new tokens' q [rows, heads, 128], k_new and v_new [rows, kv heads, 128], mask int64
+    [rows], over caches [rows, kv heads, 128] of q's dtype or e4m3 (then with scales [kv heads, rows])."""
+    stride = _one_stride(k_new, v_new, "k_new, v_new")
+    _same(q.dtype == k_new.dtype and q.dtype == out.dtype and q.shape[0] == k_new.shape[0] and
+          q.shape[2] == k_new.shape[2], "q, k_new, v_new, out: same dtype, rows and head_dim")
+    _whole(out, "out", None, q.shape)
+    _whole(new_offsets, "new_offsets", "torch.int64")
+    _whole(mask, "mask", "torch.int64", (q.shape[0],))
+    _whole(offsets, "offsets", "torch.int64", new_offsets.shape)
+    _whole(k_cache, "k_cache")
+    _whole(v_cache, "v_cache", str(k_cache.dtype), k_cache.shape)
+    _same(k_cache.dim() == 3 and k_cache.shape[1:] == k_new.shape[1:], "caches: [rows, kv heads, head_dim]")
+    code = _code(k_cache)
+    if code == FSX_E4M3:
+        _same(k_scale is not None and v_scale is not None, "8-bit caches need their scales")
+        _cache8(k_cache, v_cache, k_scale, v_scale)
+    if starts is not None:
+        _whole(starts, "starts", "torch.int64", (new_offsets.shape[0] - 1,))
+    if lse is not None:
+        _whole(lse, "lse", "torch.float32", (q.shape[1], q.shape[0]))
+    check(lib().fsx_tree_attention(_ptr(q), _rows_of(q, "q"), _ptr(k_new), _ptr(v_new), stride, _code(q),
+                                   _ptr(new_offsets), _ptr(mask), q.shape[0], _ptr(k_cache), _ptr(v_cache),
+                                   _ptr(k_scale), _ptr(v_scale), code, k_cache.shape[0], _ptr(starts), _ptr(offsets),
+                                   new_offsets.shape[0] - 1, q.shape[1], k_new.shape[1], q.shape[2], _ptr(out),
+                                   _ptr(lse), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                   _ptr(status), _stream(stream)))
+    return out
 
 
 class Append:
