@@ -1,66 +1,551 @@
 // Attention of a few new tokens of each request over its cache and over one another
-// (fsx_tree_attention).
+// (fsx_tree_attention), for up to 8 NT rows (token, head of the group) an item.
 //
-// A warp per (new token, head): lane l holds dims 4 l .. 4 l + 3 of the query and of the output; the
-// cache rows, then the new tokens that the mask names, are taken one at a time with a running maximum and sum.
+// Bound by the cache's bytes: each is read once, from global memory straight into the registers that
+// the matrix instructions take it from; no shared memory lies between. A warp takes 16 keys at a time:
+//   S^T = K Q^T      m16n8k16, keys as M, 8 rows as N: with one row the other form (rows as M) spends twice
+//                    the instructions and registers on rows that are not there
+//   O^T += V^T P^T   dims as M: P^T comes out of S^T by a transposing move of its packed 8 x 8 tiles
+// Which 4 dims a lane holds of a K = 16 step, and which 2 of an M = 16 tile, is free as long as both
+// operands agree: a lane takes whole 16-byte units of a row, so a warp's loads cover 64 to 128 bytes a row.
+//   lane (g, c) = (lane / 4, lane % 4): K of keys g, g + 8; V of keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9;
+//   scores and weights of keys g, g + 8 for rows 2 c, 2 c + 1; outputs of rows 2 c, 2 c + 1 for 16 dims.
+// 8-bit caches: codes become fp16 exactly, queries fp16 times a power of two per row (exact for bf16, whose
+// 8 bits fit; components 2^-22 below the row's largest may lose their last bits), a key's scale multiplies its
+// score, a value's scale its weight, relative to the largest value scale so far (`vs`). Weights are then fp16,
+// also for bf16 queries. 16-bit caches and the new tokens use their own type, weights rounded to it.
+// The running maximum moves only when a score exceeds it by more than 2^8, seen by one vote a step.
+//
+// The 4 warps of a CTA take every fourth 16 keys of a chunk of 64 and are put together in shared memory.
+#include <math_constants.h>
+
 #include <type_traits>
 
-#include "attention_rows.cuh"
 #include "fsx.h"
 #include "kernels.h"
 #include "llm.h"
+#include "tc_attention.cuh"
+#include "tree_schedule.cuh"
 
 namespace fsx {
 
 namespace {
 
-template <typename T, bool C8>
-__global__ void __launch_bounds__(128) tree_rows_kernel(const TreeArgs p) {
-  using CT = typename std::conditional<C8, unsigned char, T>::type;
-  const int b = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & 31;
-  const int kvh = h / (p.n_heads / p.n_kv_heads);
-  const long long t0 = p.new_offsets[b], t1 = p.new_offsets[b + 1];
-  const long long c0 = p.starts != nullptr ? p.starts[b] : p.offsets[b], len = p.offsets[b + 1] - p.offsets[b];
-  if (t0 < 0 || t1 < t0 || t1 > p.new_rows || t1 - t0 > kMaxDrafts || c0 < 0 || len < 0 || c0 > p.cache_rows ||
-      len > p.cache_rows - c0) {
-    if (threadIdx.x == 0) set_status(p.status, kStatusDeviceArg);
-    return;
-  }
-  const int n = static_cast<int>(t1 - t0);
-  for (int i = blockIdx.x * 4 + (threadIdx.x >> 5); i < n; i += gridDim.x * 4) {
-    RowState st;
-    row_query(st, static_cast<const T*>(p.q) + (t0 + i) * p.q_stride + h * kHeadDim + lane * 4);
-    for (long long j = 0; j < len; ++j) {
-      const long long at = ((c0 + j) * p.n_kv_heads + kvh) * kHeadDim + lane * 4;
-      float4 k = load4(static_cast<const CT*>(p.k_cache) + at), v = load4(static_cast<const CT*>(p.v_cache) + at);
-      if (C8) {
-        k = scaled(k, p.k_scale[kvh * p.cache_rows + c0 + j]);
-        v = scaled(v, p.v_scale[kvh * p.cache_rows + c0 + j]);
-      }
-      row_key(st, k, v);
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kChunk = 16 * kWarps;
+constexpr int kD = kHeadDim;
+
+__device__ __forceinline__ uint4 load_once(const void* p) {  // 16 bytes that no other warp of the SM reads
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p));
+  return v;
+}
+__device__ __forceinline__ uint32_t e4m3x2_to_half2(uint32_t two) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(two)));
+  return h;
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {  // 8 x 8 16-bit tile, packed pairs along a row
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+template <bool BF>
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if (BF)
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    mma_f16_16816(d, a0, a1, a2, a3, b0, b1);
+}
+__device__ __forceinline__ uint32_t word(const uint4& u, int i) { return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w; }
+
+// 16 keys on their way: K of keys g, g + 8 and V of keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9
+template <bool C8>
+struct Raw {
+  static constexpr int kK = C8 ? 2 : 4, kV = C8 ? 1 : 2;  // 16-byte units per row and lane
+  uint4 k[2][kK], v[4][kV];
+  float ks[2], vs[2];
+};
+
+template <int NT>
+struct State {
+  float o[8][NT][4];  // [dim pair][8 rows]: (dim 0; row 2 c, 2 c + 1), (dim 1; the same)
+  float m[NT][2], l[NT][2];
+  float vs;           // C8: o is in units of it
+};
+
+// Scores s[nt][key half * 2 + row] of 16 keys -> weights into the state, P^T packed for O^T. vs_of: the
+// scales of values of keys g, g + 8. BF: type of the weights.
+template <bool BF, bool C8, int NT>
+__device__ __forceinline__ void softmax_step(State<NT>& st, float (&s)[NT][4], const float (&vs_of)[2], uint32_t (&pt)[NT][2]) {
+  bool move = C8 && fmaxf(vs_of[0], vs_of[1]) > st.vs;
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int r = 0; r < 2; ++r) move = move || fmaxf(s[t][r], s[t][2 + r]) > st.m[t][r] + 8.f;
+  if (__any_sync(0xffffffffu, move)) {
+    float ratio = 1.f;
+    if (C8) {
+      float v = fmaxf(vs_of[0], vs_of[1]);
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+      v = fmaxf(v, st.vs);
+      ratio = v > 0.f ? st.vs / v : 1.f;
+      st.vs = v;
     }
-    const uint64_t mask = p.mask[t0 + i];
-    for (int j = 0; j < n; ++j)
-      if ((mask >> j) & 1u) {
-        const long long at = (t0 + j) * p.new_stride + kvh * kHeadDim + lane * 4;
-        row_key(st, load4(static_cast<const T*>(p.k_new) + at), load4(static_cast<const T*>(p.v_new) + at));
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        float top = fmaxf(s[t][r], s[t][2 + r]);
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float m = fmaxf(st.m[t][r], top);
+        const float alpha = m == st.m[t][r] ? 1.f : exp2_fast(st.m[t][r] - m);
+        st.m[t][r] = m;
+        st.l[t][r] *= alpha;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          st.o[j][t][r] *= alpha * ratio;
+          st.o[j][t][2 + r] *= alpha * ratio;
+        }
       }
-    row_finish(st, static_cast<T*>(p.out) + ((t0 + i) * p.n_heads + h) * kHeadDim + lane * 4,
-               p.lse != nullptr ? p.lse + h * p.new_rows + t0 + i : nullptr, lane);
   }
+  const float inv = C8 ? (st.vs > 0.f ? 1.f / st.vs : 0.f) : 1.f;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float w[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        w[r] = exp2_fast(s[t][2 * h + r] - (st.m[t][r] == -CUDART_INF_F ? 0.f : st.m[t][r]));
+        st.l[t][r] += w[r];
+        if (C8) w[r] *= vs_of[h] * inv;
+      }
+      pt[t][h] = transpose8x8(pack16<BF>(w[0], w[1]));
+    }
+  }
+}
+
+template <bool BF, bool C8, int NT>
+__device__ __forceinline__ void cache_step(State<NT>& st, const Raw<C8>& x, const uint32_t (&q)[NT][8][2],
+                                           const float (&f)[NT][2], int left) {
+  constexpr bool kBf = BF && !C8;
+  const int lane = threadIdx.x & 31, g = lane >> 2;
+  float s[NT][4];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[t][e] = 0.f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    uint32_t a[4];
+    if (C8) {
+      const uint32_t w0 = word(x.k[0][k >> 2], k & 3), w1 = word(x.k[1][k >> 2], k & 3);
+      a[0] = e4m3x2_to_half2(w0);
+      a[1] = e4m3x2_to_half2(w1);
+      a[2] = e4m3x2_to_half2(w0 >> 16);
+      a[3] = e4m3x2_to_half2(w1 >> 16);
+    } else {
+      a[0] = word(x.k[0][k >> 1], 2 * (k & 1));
+      a[1] = word(x.k[1][k >> 1], 2 * (k & 1));
+      a[2] = word(x.k[0][k >> 1], 2 * (k & 1) + 1);
+      a[3] = word(x.k[1][k >> 1], 2 * (k & 1) + 1);
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) mma<kBf>(s[t], a[0], a[1], a[2], a[3], q[t][k][0], q[t][k][1]);
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const float y = s[t][2 * h + r] * (C8 ? f[t][r] * x.ks[h] : kScaleLog2);
+        s[t][2 * h + r] = g + 8 * h < left ? y : -CUDART_INF_F;
+      }
+  uint32_t pt[NT][2];
+  softmax_step<kBf, C8, NT>(st, s, x.vs, pt);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    uint32_t h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      h[i] = C8 ? e4m3x2_to_half2(word(x.v[i][0], j >> 1) >> ((j & 1) * 16)) : word(x.v[i][C8 ? 0 : j >> 2], j & 3);
+    const uint32_t a0 = __byte_perm(h[0], h[1], 0x5410), a1 = __byte_perm(h[0], h[1], 0x7632);
+    const uint32_t a2 = __byte_perm(h[2], h[3], 0x5410), a3 = __byte_perm(h[2], h[3], 0x7632);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) mma<kBf>(st.o[j][t], a0, a1, a2, a3, pt[t][0], pt[t][1]);
+  }
+}
+
+// K of the 16 keys from `key` on, of which `left` are in the range: rows past it are not read
+template <bool C8>
+__device__ __forceinline__ void load_k(Raw<C8>& x, const TreeArgs& p, const unsigned char* k, const float* ks, long long key, int left) {
+  const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+  const long long row_bytes = static_cast<long long>(p.n_kv_heads) * kD * (C8 ? 1 : 2);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const unsigned char* row = k + (key + g + 8 * h) * row_bytes + c * 16;
+    const bool there = g + 8 * h < left;
+#pragma unroll
+    for (int u = 0; u < Raw<C8>::kK; ++u) x.k[h][u] = there ? load_once(row + u * 64) : make_uint4(0u, 0u, 0u, 0u);
+    if (C8) x.ks[h] = there ? __ldg(ks + key + g + 8 * h) : 0.f;
+  }
+}
+template <bool C8>
+__device__ __forceinline__ void load_v(Raw<C8>& x, const TreeArgs& p, const unsigned char* v, const float* vs, long long key, int left) {
+  const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+  const long long row_bytes = static_cast<long long>(p.n_kv_heads) * kD * (C8 ? 1 : 2);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int at = 2 * c + (i & 1) + 8 * (i >> 1);
+    const unsigned char* row = v + (key + at) * row_bytes + g * 16;
+#pragma unroll
+    for (int u = 0; u < Raw<C8>::kV; ++u) x.v[i][u] = at < left ? load_once(row + u * 128) : make_uint4(0u, 0u, 0u, 0u);
+  }
+  if (C8) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) x.vs[h] = g + 8 * h < left ? __ldg(vs + key + g + 8 * h) : 0.f;
+  }
+}
+
+// The dim of output (j, e) of lane row group g
+template <bool C8>
+__device__ __forceinline__ int out_dim(int g, int j, int e) {
+  return C8 ? 16 * g + 2 * j + e : (j >> 2) * 64 + 8 * g + 2 * (j & 3) + e;
+}
+
+// New tokens key .. key + 15 of the request: their own type, one mask bit per row and token. A masked
+// weight is 0 but 0 times an infinity or NaN is not: such values go into the product as 0 and are added
+// to the rows that see them.
+template <bool BF, bool C8, int NT>
+__device__ __forceinline__ void new_step(State<NT>& st, const TreeArgs& p, const TreePiece& it, int G, int key) {
+  const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+  const int left = it.r.n - key;
+  const uint16_t* kn = static_cast<const uint16_t*>(p.k_new) + (it.r.t0 + key) * p.new_stride + it.kvh * kD;
+  const uint16_t* vn = static_cast<const uint16_t*>(p.v_new) + (it.r.t0 + key) * p.new_stride + it.kvh * kD;
+  const uint16_t* q = static_cast<const uint16_t*>(p.q);
+  const int rows = it.r.n * G;
+  float s[NT][4];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[t][e] = 0.f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int d = 16 * k + 4 * c;
+    uint2 a[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      a[h] = g + 8 * h < left ? __ldg(reinterpret_cast<const uint2*>(kn + (g + 8 * h) * p.new_stride + d)) : make_uint2(0u, 0u);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int row = it.row0 + 8 * t + g, token = row / G;
+      const uint2 b = row < rows ? __ldg(reinterpret_cast<const uint2*>(q + (it.r.t0 + token) * p.q_stride +
+                                                                         (it.kvh * G + row - token * G) * kD + d))
+                                 : make_uint2(0u, 0u);
+      mma<BF>(s[t], a[0].x, a[1].x, a[0].y, a[1].y, b.x, b.y);
+    }
+  }
+  uint64_t mask[NT][2];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int row = it.row0 + 8 * t + 2 * c + r;
+      mask[t][r] = row < rows ? p.mask[it.r.t0 + row / G] >> key : 0ull;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bool sees = g + 8 * h < left && ((mask[t][r] >> (g + 8 * h)) & 1u);
+        s[t][2 * h + r] = sees ? s[t][2 * h + r] * kScaleLog2 : -CUDART_INF_F;
+      }
+    }
+  const float ones[2] = {1.f, 1.f};
+  uint32_t pt[NT][2];
+  softmax_step<BF, C8, NT>(st, s, ones, pt);
+  uint32_t wild = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    uint32_t h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int at = 2 * c + (i & 1) + 8 * (i >> 1);
+      h[i] = at < left ? __ldg(reinterpret_cast<const uint32_t*>(vn + at * p.new_stride + out_dim<C8>(g, j, 0))) : 0u;
+      const uint32_t bad = not_finite2<BF>(h[i]);
+      wild |= bad;
+      h[i] &= ~((bad >> 15) * 0xffffu);
+    }
+    const uint32_t a0 = __byte_perm(h[0], h[1], 0x5410), a1 = __byte_perm(h[0], h[1], 0x7632);
+    const uint32_t a2 = __byte_perm(h[2], h[3], 0x5410), a3 = __byte_perm(h[2], h[3], 0x7632);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) mma<BF>(st.o[j][t], a0, a1, a2, a3, pt[t][0], pt[t][1]);
+  }
+  if (__any_sync(0xffffffffu, wild != 0)) {
+#pragma unroll 1
+    for (int i = 0; i < min(left, 16); ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t v = __ldg(reinterpret_cast<const uint32_t*>(vn + i * p.new_stride + out_dim<C8>(g, j, 0)));
+        const uint32_t bad = not_finite2<BF>(v);
+        const float2 y = unpack16<BF>(v);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+            if ((mask[t][r] >> i) & 1u) {
+              if (bad & 0x8000u) st.o[j][t][r] += y.x;
+              if (bad & 0x80000000u) st.o[j][t][2 + r] += y.y;
+            }
+      }
+  }
+}
+
+// Queries of the item's rows as B operands; C8: as fp16 times 2^-e, f the factor that undoes it
+template <bool BF, bool C8, int NT>
+__device__ __forceinline__ void load_queries(uint32_t (&qf)[NT][8][2], float (&f)[NT][2], const TreeArgs& p, const TreePiece& it, int G) {
+  const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+  const uint16_t* q = static_cast<const uint16_t*>(p.q);
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int row = it.row0 + 8 * t + g, token = row / G;
+    const bool there = row < it.r.n * G;
+    const uint16_t* src = q + (it.r.t0 + (there ? token : 0)) * p.q_stride + (it.kvh * G + (there ? row - token * G : 0)) * kD;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int d = C8 ? (k >> 2) * 64 + 16 * c + 4 * (k & 3) : 8 * (c + 4 * (k >> 1)) + 4 * (k & 1);
+      const uint2 w = there ? __ldg(reinterpret_cast<const uint2*>(src + d)) : make_uint2(0u, 0u);
+      qf[t][k][0] = w.x;
+      qf[t][k][1] = w.y;
+    }
+    if (C8) {
+      float top = 0.f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float2 x = unpack16<BF>(qf[t][k][i]);
+          top = fmaxf(top, fmaxf(fabsf(x.x), fabsf(x.y)));
+        }
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      // the largest magnitude goes to [2^7, 2^8); a row of zeros, infinities or NaN is taken as it is
+      const int e = static_cast<int>(__float_as_uint(top) >> 23) - 127 - 7;
+      const bool plain = top == 0.f || !(top < CUDART_INF_F);
+      const int ec = plain ? 0 : max(-126, min(e, 126));
+      const float up = __uint_as_float(static_cast<uint32_t>(127 - ec) << 23);
+      const float back = __uint_as_float(static_cast<uint32_t>(127 + ec) << 23);
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float2 x = unpack16<BF>(qf[t][k][i]);
+          qf[t][k][i] = pack_half2(x.x * up, x.y * up);
+        }
+      f[t][0] = __shfl_sync(0xffffffffu, back, 8 * c) * kScaleLog2;
+      f[t][1] = __shfl_sync(0xffffffffu, back, 8 * c + 4) * kScaleLog2;
+    }
+  }
+}
+
+template <int NT>
+struct Shared {
+  long long pre[kMaxSequences + 1];
+  long long scratch[kWarps];
+  float m[kWarps][8 * NT], l[kWarps][8 * NT];
+  float o[kWarps][8 * NT][kD];
+  int last;
+};
+
+__device__ __forceinline__ float weight_of(float m, float top) { return m == -CUDART_INF_F ? 0.f : exp2_fast(m - top); }
+
+// partial results of a slot: [rows][128] sums, then [rows] (maximum, sum of weights)
+template <int NT>
+__device__ __forceinline__ float* slot_of(const TreeArgs& p, int cta, int which) {
+  return reinterpret_cast<float*>(static_cast<unsigned char*>(p.workspace) + kTreeCounterBytes) +
+         static_cast<size_t>(2 * cta + which) * (8 * NT * (kD + 2));
+}
+
+template <bool BF, bool C8, int NT>
+__global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) tree_kernel(const TreeArgs p) {
+  extern __shared__ __align__(16) unsigned char raw_smem[];
+  Shared<NT>& sm = *reinterpret_cast<Shared<NT>*>(raw_smem);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
+  const int G = p.n_heads / p.n_kv_heads;
+  tree_prefix<kThreads>(p, 8 * NT, kChunk, sm.pre, sm.scratch);
+  const long long total = sm.pre[p.B];
+  const long long per = (total + gridDim.x - 1) / gridDim.x;
+  const long long u1 = min(total, (blockIdx.x + 1) * per);
+#pragma unroll 1
+  for (long long u = blockIdx.x * per; u < u1;) {
+    const TreePiece it = tree_piece(p, sm.pre, 8 * NT, kChunk, u, u1, per);
+    u += it.to - it.from;
+    uint32_t qf[NT][8][2];
+    float f[NT][2];
+    // first loads of the cache go out before the queries are waited for
+    const int cache_to = min(it.to, it.n - 1);
+    const unsigned char* kc = static_cast<const unsigned char*>(p.k_cache) + it.kvh * kD * (C8 ? 1 : 2);
+    const unsigned char* vc = static_cast<const unsigned char*>(p.v_cache) + it.kvh * kD * (C8 ? 1 : 2);
+    const float* ks = C8 ? p.k_scale + it.kvh * p.cache_rows + it.r.c0 : nullptr;
+    const float* vs = C8 ? p.v_scale + it.kvh * p.cache_rows + it.r.c0 : nullptr;
+    const long long row_bytes = static_cast<long long>(p.n_kv_heads) * kD * (C8 ? 1 : 2);
+    kc += it.r.c0 * row_bytes;
+    vc += it.r.c0 * row_bytes;
+    Raw<C8> x;
+    int key = it.from * kChunk + 16 * warp;
+    const int end = min(it.r.len, cache_to * kChunk);
+    load_k<C8>(x, p, kc, ks, key, end - key);
+    load_v<C8>(x, p, vc, vs, key, end - key);
+    load_queries<BF, C8, NT>(qf, f, p, it, G);
+    State<NT> st;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      st.m[t][0] = st.m[t][1] = -CUDART_INF_F;
+      st.l[t][0] = st.l[t][1] = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) st.o[j][t][e] = 0.f;
+    }
+    st.vs = 0.f;
+#pragma unroll 1
+    for (; key < end; key += kChunk) {
+      Raw<C8> now = x;
+      load_k<C8>(x, p, kc, ks, key + kChunk, end - key - kChunk);
+      load_v<C8>(x, p, vc, vs, key + kChunk, end - key - kChunk);
+      cache_step<BF, C8, NT>(st, now, qf, f, end - key);
+    }
+    if (it.to == it.n && 16 * warp < it.r.n) new_step<BF, C8, NT>(st, p, it, G, 16 * warp);
+
+    // ---- the four warps' results, then the CTAs'
+    const int rows = min(8 * NT, it.r.n * G - it.row0);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        float l = st.l[t][r];
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        const int row = 8 * t + 2 * c + r;
+        if (g == 0) {
+          sm.m[warp][row] = st.m[t][r];
+          sm.l[warp][row] = l;
+        }
+        if (row < rows) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float a = C8 ? st.o[j][t][r] * st.vs : st.o[j][t][r], b = C8 ? st.o[j][t][2 + r] * st.vs : st.o[j][t][2 + r];
+            *reinterpret_cast<float2*>(&sm.o[warp][row][out_dim<C8>(g, j, 0)]) = make_float2(a, b);
+          }
+        }
+      }
+    __syncthreads();
+    const bool whole = it.from == 0 && it.to == it.n;
+    float* slot = slot_of<NT>(p, blockIdx.x, it.from == 0 ? 1 : 0);
+    auto finish = [&](int row, float m, float l, float o) {
+      const int at = it.row0 + row, token = at / G, head = it.kvh * G + at - token * G;
+      const float y = l == 0.f ? 0.f : o / l;
+      static_cast<uint16_t*>(p.out)[((it.r.t0 + token) * p.n_heads + head) * kD + tid] = static_cast<uint16_t>(pack16<BF>(y, y));
+      if (p.lse != nullptr && tid == 0)
+        p.lse[head * p.new_rows + it.r.t0 + token] = l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * kLn2;
+    };
+#pragma unroll 1
+    for (int row = 0; row < rows; ++row) {  // a thread a dim
+      const float m = fmaxf(fmaxf(sm.m[0][row], sm.m[1][row]), fmaxf(sm.m[2][row], sm.m[3][row]));
+      float l = 0.f, o = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float a = weight_of(sm.m[w][row], m);
+        l += a * sm.l[w][row];
+        o += a * sm.o[w][row][tid];
+      }
+      if (whole) {
+        finish(row, m, l, o);
+      } else {
+        __stcg(slot + row * kD + tid, o);
+        if (tid == 0) __stcg(reinterpret_cast<float2*>(slot + 8 * NT * kD) + row, make_float2(m, l));
+      }
+    }
+    if (!whole) {
+      __threadfence();
+      __syncthreads();
+      int* counter = static_cast<int*>(p.workspace) + it.first_cta;
+      const int pieces = it.last_cta - it.first_cta + 1;
+      if (tid == 0) {
+        sm.last = atomicAdd(counter, 1) == pieces - 1;
+        if (sm.last) *counter = 0;
+      }
+      __syncthreads();
+      if (sm.last) {
+        __threadfence();
+#pragma unroll 1
+        for (int row = 0; row < rows; ++row) {
+          float m = -CUDART_INF_F, l = 0.f, o = 0.f;
+#pragma unroll 4
+          for (int i = 0; i < pieces; ++i) {  // in the order of the ranges
+            const float* other = slot_of<NT>(p, it.first_cta + i, i == 0 ? 1 : 0);
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(other + 8 * NT * kD) + row);
+            const float v = __ldcg(other + row * kD + tid);
+            const float top = fmaxf(m, ml.x);
+            const float a = weight_of(m, top), b = weight_of(ml.x, top);
+            l = l * a + b * ml.y;
+            o = o * a + b * v;
+            m = top;
+          }
+          finish(row, m, l, o);
+        }
+      }
+    }
+    __syncthreads();  // the next piece's results go where these lie
+  }
+}
+
+struct Kernel {
+  const void* fn;
+  size_t smem;
+  int rows;
+};
+template <bool BF, bool C8>
+Kernel kernel_of(int nt) {
+  if (nt == 1) return {reinterpret_cast<const void*>(&tree_kernel<BF, C8, 1>), sizeof(Shared<1>), 8};
+  if (nt == 2) return {reinterpret_cast<const void*>(&tree_kernel<BF, C8, 2>), sizeof(Shared<2>), 16};
+  return {reinterpret_cast<const void*>(&tree_kernel<BF, C8, 4>), sizeof(Shared<4>), 32};
+}
+
+// 8-row tiles of an item, by the rows that a request has on average: a wider tile reads the cache fewer
+// times, a narrower one leaves more warps on an SM
+int tile_count(int B, long long new_rows, int n_heads, int n_kv_heads) {
+  const long long rows = (new_rows * (n_heads / n_kv_heads) + B - 1) / B;
+  return rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
 }
 
 }  // namespace
 
-size_t tree_attention_workspace_bytes(int, long long, int, int) { return 256; }
+size_t tree_attention_workspace_bytes(int B, long long new_rows, int n_heads, int n_kv_heads) {
+  return kTreeCounterBytes +
+         static_cast<size_t>(2 * kTreeMaxGrid) * 8 * tile_count(B, new_rows, n_heads, n_kv_heads) * (kD + 2) * sizeof(float);
+}
 
 cudaError_t launch_tree_attention(const TreeArgs& a, int dtype, bool cache8, cudaStream_t stream) {
+  const int nt = tile_count(a.B, a.new_rows, a.n_heads, a.n_kv_heads);
+  const Kernel k = dtype == FSX_BF16 ? (cache8 ? kernel_of<true, true>(nt) : kernel_of<true, false>(nt))
+                                     : (cache8 ? kernel_of<false, true>(nt) : kernel_of<false, false>(nt));
+  cudaError_t e = cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(k.smem));
+  int dev = 0, sms = 0, per_sm = 0;
+  if (e == cudaSuccess) e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k.fn, kThreads, k.smem);
+  if (e != cudaSuccess) return e;
+  const int grid = sms * per_sm < kTreeMaxGrid ? sms * per_sm : kTreeMaxGrid;
   void* args[] = {const_cast<TreeArgs*>(&a)};
-  const void* fn = dtype == FSX_BF16 ? (cache8 ? reinterpret_cast<const void*>(&tree_rows_kernel<__nv_bfloat16, true>)
-                                               : reinterpret_cast<const void*>(&tree_rows_kernel<__nv_bfloat16, false>))
-                                     : (cache8 ? reinterpret_cast<const void*>(&tree_rows_kernel<__half, true>)
-                                               : reinterpret_cast<const void*>(&tree_rows_kernel<__half, false>));
-  return launch_ex(fn, dim3(kMaxDrafts / 4, a.n_heads, a.B), dim3(128), 0, stream, false, args);
+  return launch_ex(k.fn, dim3(static_cast<unsigned>(grid)), dim3(kThreads), k.smem, stream, false, args);
 }
 
 }  // namespace fsx
