@@ -1,8 +1,9 @@
 // Attention of a few new tokens of each request over its cache and over one another
 // (fsx_tree_attention), for up to 8 NT rows (token, head of the group) an item.
 //
-// Bound by the cache's bytes: each is read once, from global memory straight into the registers that
-// the matrix instructions take it from; no shared memory lies between. A warp takes 16 keys at a time:
+// Bound by the cache's bytes. Each warp copies its own keys into a ring of its own (no barrier between
+// warps), 16 at a time, two and more stages ahead: loads straight into registers, one step ahead, kept only
+// 48 KB a SM on their way and read 128 single tokens' 8-bit caches at 3.6 TB/s. Per 16 keys:
 //   S^T = K Q^T      m16n8k16, keys as M, 8 rows as N: with one row the other form (rows as M) spends twice
 //                    the instructions and registers on rows that are not there
 //   O^T += V^T P^T   dims as M: P^T comes out of S^T by a transposing move of its packed 8 x 8 tiles
@@ -36,12 +37,12 @@ constexpr int kThreads = 32 * kWarps;
 constexpr int kChunk = 16 * kWarps;
 constexpr int kD = kHeadDim;
 
-__device__ __forceinline__ uint4 load_once(const void* p) {  // 16 bytes that no other warp of the SM reads
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "l"(p));
-  return v;
+// 16 or 4 bytes to shared memory, zeros if not `there` (then nothing is read)
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
 }
 __device__ __forceinline__ uint32_t e4m3x2_to_half2(uint32_t two) {
   uint32_t h;
@@ -65,12 +66,14 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
 }
 __device__ __forceinline__ uint32_t word(const uint4& u, int i) { return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w; }
 
-// 16 keys on their way: K of keys g, g + 8 and V of keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9
+// 16 keys of a warp's ring stage: K rows, V rows, then (C8) the 16 scales of each. 16-byte unit u of row r lies
+// at u ^ (r & 1) * 4 (K) or u ^ (r & 6) (V): the 8 lanes that are served together read 8 different units.
 template <bool C8>
-struct Raw {
+struct Stage {
+  static constexpr int kRow = C8 ? kD : 2 * kD;
   static constexpr int kK = C8 ? 2 : 4, kV = C8 ? 1 : 2;  // 16-byte units per row and lane
-  uint4 k[2][kK], v[4][kV];
-  float ks[2], vs[2];
+  static constexpr int kOffV = 16 * kRow, kOffScale = 32 * kRow;
+  static constexpr int kBytes = 32 * kRow + (C8 ? 128 : 0);
 };
 
 template <int NT>
@@ -135,10 +138,17 @@ __device__ __forceinline__ void softmax_step(State<NT>& st, float (&s)[NT][4], c
 }
 
 template <bool BF, bool C8, int NT>
-__device__ __forceinline__ void cache_step(State<NT>& st, const Raw<C8>& x, const uint32_t (&q)[NT][8][2],
+__device__ __forceinline__ void cache_step(State<NT>& st, const unsigned char* x, const uint32_t (&q)[NT][8][2],
                                            const float (&f)[NT][2], int left) {
+  using S = Stage<C8>;
   constexpr bool kBf = BF && !C8;
-  const int lane = threadIdx.x & 31, g = lane >> 2;
+  const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+  uint4 xk[2][S::kK];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int u = 0; u < S::kK; ++u)
+      xk[h][u] = *reinterpret_cast<const uint4*>(x + (g + 8 * h) * S::kRow + (((c + 4 * u) ^ ((g & 1) << 2)) << 4));
   float s[NT][4];
 #pragma unroll
   for (int t = 0; t < NT; ++t)
@@ -148,19 +158,27 @@ __device__ __forceinline__ void cache_step(State<NT>& st, const Raw<C8>& x, cons
   for (int k = 0; k < 8; ++k) {
     uint32_t a[4];
     if (C8) {
-      const uint32_t w0 = word(x.k[0][k >> 2], k & 3), w1 = word(x.k[1][k >> 2], k & 3);
+      const uint32_t w0 = word(xk[0][k >> 2], k & 3), w1 = word(xk[1][k >> 2], k & 3);
       a[0] = e4m3x2_to_half2(w0);
       a[1] = e4m3x2_to_half2(w1);
       a[2] = e4m3x2_to_half2(w0 >> 16);
       a[3] = e4m3x2_to_half2(w1 >> 16);
     } else {
-      a[0] = word(x.k[0][k >> 1], 2 * (k & 1));
-      a[1] = word(x.k[1][k >> 1], 2 * (k & 1));
-      a[2] = word(x.k[0][k >> 1], 2 * (k & 1) + 1);
-      a[3] = word(x.k[1][k >> 1], 2 * (k & 1) + 1);
+      a[0] = word(xk[0][k >> 1], 2 * (k & 1));
+      a[1] = word(xk[1][k >> 1], 2 * (k & 1));
+      a[2] = word(xk[0][k >> 1], 2 * (k & 1) + 1);
+      a[3] = word(xk[1][k >> 1], 2 * (k & 1) + 1);
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) mma<kBf>(s[t], a[0], a[1], a[2], a[3], q[t][k][0], q[t][k][1]);
+  }
+  float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};
+  if (C8) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      ks[h] = reinterpret_cast<const float*>(x + S::kOffScale)[g + 8 * h];
+      vs[h] = reinterpret_cast<const float*>(x + S::kOffScale)[16 + g + 8 * h];
+    }
   }
 #pragma unroll
   for (int t = 0; t < NT; ++t)
@@ -168,17 +186,25 @@ __device__ __forceinline__ void cache_step(State<NT>& st, const Raw<C8>& x, cons
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        const float y = s[t][2 * h + r] * (C8 ? f[t][r] * x.ks[h] : kScaleLog2);
+        const float y = s[t][2 * h + r] * (C8 ? f[t][r] * ks[h] : kScaleLog2);
         s[t][2 * h + r] = g + 8 * h < left ? y : -CUDART_INF_F;
       }
   uint32_t pt[NT][2];
-  softmax_step<kBf, C8, NT>(st, s, x.vs, pt);
+  softmax_step<kBf, C8, NT>(st, s, vs, pt);
+  uint4 xv[4][S::kV];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = 2 * c + (i & 1) + 8 * (i >> 1);
+#pragma unroll
+    for (int u = 0; u < S::kV; ++u)
+      xv[i][u] = *reinterpret_cast<const uint4*>(x + S::kOffV + r * S::kRow + (((g ^ (r & 6)) + 8 * u) << 4));
+  }
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     uint32_t h[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      h[i] = C8 ? e4m3x2_to_half2(word(x.v[i][0], j >> 1) >> ((j & 1) * 16)) : word(x.v[i][C8 ? 0 : j >> 2], j & 3);
+      h[i] = C8 ? e4m3x2_to_half2(word(xv[i][0], j >> 1) >> ((j & 1) * 16)) : word(xv[i][C8 ? 0 : j >> 2], j & 3);
     const uint32_t a0 = __byte_perm(h[0], h[1], 0x5410), a1 = __byte_perm(h[0], h[1], 0x7632);
     const uint32_t a2 = __byte_perm(h[2], h[3], 0x5410), a3 = __byte_perm(h[2], h[3], 0x7632);
 #pragma unroll
@@ -186,34 +212,17 @@ __device__ __forceinline__ void cache_step(State<NT>& st, const Raw<C8>& x, cons
   }
 }
 
-// K of the 16 keys from `key` on, of which `left` are in the range: rows past it are not read
-template <bool C8>
-__device__ __forceinline__ void load_k(Raw<C8>& x, const TreeArgs& p, const unsigned char* k, const float* ks, long long key, int left) {
-  const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-  const long long row_bytes = static_cast<long long>(p.n_kv_heads) * kD * (C8 ? 1 : 2);
+// One tensor's 16 keys into a stage. `src`: this lane's unit of its first row of them; rows past `left` become zeros.
+template <bool C8, bool V>
+__device__ __forceinline__ void copy_rows(uint32_t dst, const unsigned char* src, long long row_bytes, int left) {
+  using S = Stage<C8>;
+  constexpr int kPerRow = S::kRow / 16, kStep = 32 / kPerRow;  // lanes a row, rows a warp copies at once
+  const int lane = threadIdx.x & 31, u = lane % kPerRow, r0 = lane / kPerRow;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const unsigned char* row = k + (key + g + 8 * h) * row_bytes + c * 16;
-    const bool there = g + 8 * h < left;
-#pragma unroll
-    for (int u = 0; u < Raw<C8>::kK; ++u) x.k[h][u] = there ? load_once(row + u * 64) : make_uint4(0u, 0u, 0u, 0u);
-    if (C8) x.ks[h] = there ? __ldg(ks + key + g + 8 * h) : 0.f;
-  }
-}
-template <bool C8>
-__device__ __forceinline__ void load_v(Raw<C8>& x, const TreeArgs& p, const unsigned char* v, const float* vs, long long key, int left) {
-  const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-  const long long row_bytes = static_cast<long long>(p.n_kv_heads) * kD * (C8 ? 1 : 2);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int at = 2 * c + (i & 1) + 8 * (i >> 1);
-    const unsigned char* row = v + (key + at) * row_bytes + g * 16;
-#pragma unroll
-    for (int u = 0; u < Raw<C8>::kV; ++u) x.v[i][u] = at < left ? load_once(row + u * 128) : make_uint4(0u, 0u, 0u, 0u);
-  }
-  if (C8) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) x.vs[h] = g + 8 * h < left ? __ldg(vs + key + g + 8 * h) : 0.f;
+  for (int i = 0; i < 16 / kStep; ++i) {
+    const int r = r0 + i * kStep;
+    const int at = V ? u ^ (r & 6) : u ^ ((r & 1) << 2);
+    copy16(dst + (V ? S::kOffV : 0) + r * S::kRow + at * 16, src + i * kStep * row_bytes, r < left);
   }
 }
 
@@ -355,76 +364,120 @@ __device__ __forceinline__ void load_queries(uint32_t (&qf)[NT][8][2], float (&f
   }
 }
 
-template <int NT>
-struct Shared {
-  long long pre[kMaxSequences + 1];
-  long long scratch[kWarps];
+// CTAs an SM holds, stages of 16 keys in each warp's ring, rows that the warps put together at a time
+template <bool C8, int NT>
+struct Fit {
+  static constexpr int kCtas = NT == 1 ? (C8 ? 4 : 3) : NT == 2 ? 3 : 2;
+  static constexpr int kStages = C8 ? (NT == 4 ? 5 : 3) : (NT < 4 ? 2 : 3);
+  static constexpr int kPass = NT == 1 ? 2 : NT == 2 ? 4 : 8;
+};
+template <bool C8, int NT>
+struct Shared {  // and the plan behind it
+  long long scratch[2 * kWarps];
+  __align__(128) unsigned char ring[kWarps][Fit<C8, NT>::kStages * Stage<C8>::kBytes];
   float m[kWarps][8 * NT], l[kWarps][8 * NT];
-  float o[kWarps][8 * NT][kD];
+  float o[kWarps][Fit<C8, NT>::kPass][kD];
+  long long next;
   int last;
 };
 
 __device__ __forceinline__ float weight_of(float m, float top) { return m == -CUDART_INF_F ? 0.f : exp2_fast(m - top); }
 
-// partial results of a slot: [rows][128] sums, then [rows] (maximum, sum of weights)
+// Workspace behind the header: a counter per slot, then the slots: [rows][128] sums, [rows] (maximum, sum of weights)
+constexpr size_t slot_floats(int nt) { return static_cast<size_t>(8) * nt * (kD + 2); }
+constexpr int slots_of(int nt) { return kTreeCounters / nt; }  // 34 MB
+
 template <int NT>
-__device__ __forceinline__ float* slot_of(const TreeArgs& p, int cta, int which) {
-  return reinterpret_cast<float*>(static_cast<unsigned char*>(p.workspace) + kTreeCounterBytes) +
-         static_cast<size_t>(2 * cta + which) * (8 * NT * (kD + 2));
+__device__ __forceinline__ float* slot_at(const TreeArgs& p, int slot) {
+  return reinterpret_cast<float*>(static_cast<int*>(p.workspace) + kTreeHeader + kTreeCounters) +
+         static_cast<size_t>(slot) * slot_floats(NT);
 }
 
 template <bool BF, bool C8, int NT>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) tree_kernel(const TreeArgs p) {
-  extern __shared__ __align__(16) unsigned char raw_smem[];
-  Shared<NT>& sm = *reinterpret_cast<Shared<NT>*>(raw_smem);
+__global__ void __launch_bounds__(kThreads, Fit<C8, NT>::kCtas) tree_kernel(const TreeArgs p) {
+  using S = Stage<C8>;
+  constexpr int kStages = Fit<C8, NT>::kStages, kPass = Fit<C8, NT>::kPass;
+  constexpr int kPerRow = S::kRow / 16;
+  constexpr TreeShape kShape{8 * NT, kChunk, 8, 16, slots_of(NT)};
+  extern __shared__ __align__(128) unsigned char raw_smem[];
+  Shared<C8, NT>& sm = *reinterpret_cast<Shared<C8, NT>*>(raw_smem);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
   const int G = p.n_heads / p.n_kv_heads;
-  tree_prefix<kThreads>(p, 8 * NT, kChunk, sm.pre, sm.scratch);
-  const long long total = sm.pre[p.B];
-  const long long per = (total + gridDim.x - 1) / gridDim.x;
-  const long long u1 = min(total, (blockIdx.x + 1) * per);
+  int* header = static_cast<int*>(p.workspace);
+  const TreePlan plan = tree_plan<kThreads>(p, kShape, raw_smem + sizeof(sm), sm.scratch);
+  const long long total = plan.pieces[p.B];
+  const long long row_bytes = static_cast<long long>(p.n_kv_heads) * S::kRow;
+  const uint32_t ring = smem_addr(sm.ring[warp]);
+
+  // this warp's copies of a piece: keys staged, staged + 64, ... < end
+  const unsigned char *kc = nullptr, *vc = nullptr;
+  const float* scales = nullptr;
+  int staged = 0, end = 0, slot_in = 0;
+  auto copy_next = [&] {
+    const int left = end - staged;
+    if (left > 0) {
+      const uint32_t dst = ring + slot_in * S::kBytes;
+      copy_rows<C8, false>(dst, kc, row_bytes, left);
+      copy_rows<C8, true>(dst, vc, row_bytes, left);
+      if (C8) copy4(dst + S::kOffScale + lane * 4, scales, (lane & 15) < left);
+    }
+    cp_async_commit();
+    staged += kChunk;
+    kc += kChunk * row_bytes;
+    vc += kChunk * row_bytes;
+    scales += C8 ? kChunk : 0;
+    slot_in = slot_in + 1 == kStages ? 0 : slot_in + 1;
+  };
+  auto begin = [&](const TreePiece& x) {
+    staged = x.from * kChunk + 16 * warp;
+    end = min(x.r.len, min(x.to, x.n - 1) * kChunk);
+    const long long at = (x.r.c0 + staged + lane / kPerRow) * row_bytes + x.kvh * S::kRow + (lane % kPerRow) * 16;
+    kc = static_cast<const unsigned char*>(p.k_cache) + at;
+    vc = static_cast<const unsigned char*>(p.v_cache) + at;
+    if (C8) scales = (lane < 16 ? p.k_scale : p.v_scale) + x.kvh * p.cache_rows + x.r.c0 + staged + (lane & 15);
+    slot_in = 0;
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) copy_next();
+  };
+
+  long long i = blockIdx.x;
+  TreePiece it;
+  if (i < total) {
+    it = tree_piece(p, kShape, plan, i);
+    begin(it);
+  }
 #pragma unroll 1
-  for (long long u = blockIdx.x * per; u < u1;) {
-    const TreePiece it = tree_piece(p, sm.pre, 8 * NT, kChunk, u, u1, per);
-    u += it.to - it.from;
-    uint32_t qf[NT][8][2];
-    float f[NT][2];
-    // first loads of the cache go out before the queries are waited for
-    const int cache_to = min(it.to, it.n - 1);
-    const unsigned char* kc = static_cast<const unsigned char*>(p.k_cache) + it.kvh * kD * (C8 ? 1 : 2);
-    const unsigned char* vc = static_cast<const unsigned char*>(p.v_cache) + it.kvh * kD * (C8 ? 1 : 2);
-    const float* ks = C8 ? p.k_scale + it.kvh * p.cache_rows + it.r.c0 : nullptr;
-    const float* vs = C8 ? p.v_scale + it.kvh * p.cache_rows + it.r.c0 : nullptr;
-    const long long row_bytes = static_cast<long long>(p.n_kv_heads) * kD * (C8 ? 1 : 2);
-    kc += it.r.c0 * row_bytes;
-    vc += it.r.c0 * row_bytes;
-    Raw<C8> x;
-    int key = it.from * kChunk + 16 * warp;
-    const int end = min(it.r.len, cache_to * kChunk);
-    load_k<C8>(x, p, kc, ks, key, end - key);
-    load_v<C8>(x, p, vc, vs, key, end - key);
-    load_queries<BF, C8, NT>(qf, f, p, it, G);
+  while (i < total) {
+    if (tid == 0) sm.next = gridDim.x + static_cast<long long>(atomicAdd(reinterpret_cast<unsigned*>(header), 1u));
     State<NT> st;
+    {
+      uint32_t qf[NT][8][2];
+      float f[NT][2];
+      load_queries<BF, C8, NT>(qf, f, p, it, G);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      st.m[t][0] = st.m[t][1] = -CUDART_INF_F;
-      st.l[t][0] = st.l[t][1] = 0.f;
+      for (int t = 0; t < NT; ++t) {
+        st.m[t][0] = st.m[t][1] = -CUDART_INF_F;
+        st.l[t][0] = st.l[t][1] = 0.f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) st.o[j][t][e] = 0.f;
-    }
-    st.vs = 0.f;
+          for (int e = 0; e < 4; ++e) st.o[j][t][e] = 0.f;
+      }
+      st.vs = 0.f;
+      int slot_out = 0;
 #pragma unroll 1
-    for (; key < end; key += kChunk) {
-      Raw<C8> now = x;
-      load_k<C8>(x, p, kc, ks, key + kChunk, end - key - kChunk);
-      load_v<C8>(x, p, vc, vs, key + kChunk, end - key - kChunk);
-      cache_step<BF, C8, NT>(st, now, qf, f, end - key);
+      for (int key = it.from * kChunk + 16 * warp; key < end; key += kChunk) {
+        cp_async_wait<kStages - 2>();
+        __syncwarp();  // every lane's copies of the stage; and the stage before is read
+        copy_next();
+        cache_step<BF, C8, NT>(st, sm.ring[warp] + slot_out * S::kBytes, qf, f, end - key);
+        slot_out = slot_out + 1 == kStages ? 0 : slot_out + 1;
+      }
     }
+    cp_async_wait<0>();
+    __syncwarp();
     if (it.to == it.n && 16 * warp < it.r.n) new_step<BF, C8, NT>(st, p, it, G, 16 * warp);
 
-    // ---- the four warps' results, then the CTAs'
     const int rows = min(8 * NT, it.r.n * G - it.row0);
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -433,22 +486,20 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) tree_kernel(const T
         float l = st.l[t][r];
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-        const int row = 8 * t + 2 * c + r;
         if (g == 0) {
-          sm.m[warp][row] = st.m[t][r];
-          sm.l[warp][row] = l;
-        }
-        if (row < rows) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float a = C8 ? st.o[j][t][r] * st.vs : st.o[j][t][r], b = C8 ? st.o[j][t][2 + r] * st.vs : st.o[j][t][2 + r];
-            *reinterpret_cast<float2*>(&sm.o[warp][row][out_dim<C8>(g, j, 0)]) = make_float2(a, b);
-          }
+          sm.m[warp][8 * t + 2 * c + r] = st.m[t][r];
+          sm.l[warp][8 * t + 2 * c + r] = l;
         }
       }
     __syncthreads();
-    const bool whole = it.from == 0 && it.to == it.n;
-    float* slot = slot_of<NT>(p, blockIdx.x, it.from == 0 ? 1 : 0);
+    // ---- the next piece's first copies go out before this one's results are put together
+    const long long i_next = sm.next;
+    TreePiece next = it;
+    if (i_next < total) {
+      next = tree_piece(p, kShape, plan, i_next);
+      begin(next);
+    }
+    // ---- the four warps' results, kPass rows at a time; a thread a dim
     auto finish = [&](int row, float m, float l, float o) {
       const int at = it.row0 + row, token = at / G, head = it.kvh * G + at - token * G;
       const float y = l == 0.f ? 0.f : o / l;
@@ -456,30 +507,49 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) tree_kernel(const T
       if (p.lse != nullptr && tid == 0)
         p.lse[head * p.new_rows + it.r.t0 + token] = l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * kLn2;
     };
-#pragma unroll 1
-    for (int row = 0; row < rows; ++row) {  // a thread a dim
-      const float m = fmaxf(fmaxf(sm.m[0][row], sm.m[1][row]), fmaxf(sm.m[2][row], sm.m[3][row]));
-      float l = 0.f, o = 0.f;
+    float* slot = slot_at<NT>(p, it.slot + it.j);
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float a = weight_of(sm.m[w][row], m);
-        l += a * sm.l[w][row];
-        o += a * sm.o[w][row][tid];
+    for (int base = 0; base < 8 * NT; base += kPass) {
+      if (base >= rows) break;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const int row = 8 * t + 2 * c + r;
+          if (row >= base && row < base + kPass && row < rows) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const float a = C8 ? st.o[j][t][r] * st.vs : st.o[j][t][r], b = C8 ? st.o[j][t][2 + r] * st.vs : st.o[j][t][2 + r];
+              *reinterpret_cast<float2*>(&sm.o[warp][row - base][out_dim<C8>(g, j, 0)]) = make_float2(a, b);
+            }
+          }
+        }
+      __syncthreads();
+#pragma unroll 1
+      for (int row = base; row < min(rows, base + kPass); ++row) {
+        const float m = fmaxf(fmaxf(sm.m[0][row], sm.m[1][row]), fmaxf(sm.m[2][row], sm.m[3][row]));
+        float l = 0.f, o = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+          const float a = weight_of(sm.m[w][row], m);
+          l += a * sm.l[w][row];
+          o += a * sm.o[w][row - base][tid];
+        }
+        if (it.of == 1) {
+          finish(row, m, l, o);
+        } else {
+          __stcg(slot + row * kD + tid, o);
+          if (tid == 0) __stcg(reinterpret_cast<float2*>(slot + 8 * NT * kD) + row, make_float2(m, l));
+        }
       }
-      if (whole) {
-        finish(row, m, l, o);
-      } else {
-        __stcg(slot + row * kD + tid, o);
-        if (tid == 0) __stcg(reinterpret_cast<float2*>(slot + 8 * NT * kD) + row, make_float2(m, l));
-      }
+      __syncthreads();
     }
-    if (!whole) {
+    if (it.of > 1) {
       __threadfence();
       __syncthreads();
-      int* counter = static_cast<int*>(p.workspace) + it.first_cta;
-      const int pieces = it.last_cta - it.first_cta + 1;
       if (tid == 0) {
-        sm.last = atomicAdd(counter, 1) == pieces - 1;
+        int* counter = header + kTreeHeader + it.slot;
+        sm.last = atomicAdd(counter, 1) == it.of - 1;
         if (sm.last) *counter = 0;
       }
       __syncthreads();
@@ -489,8 +559,8 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) tree_kernel(const T
         for (int row = 0; row < rows; ++row) {
           float m = -CUDART_INF_F, l = 0.f, o = 0.f;
 #pragma unroll 4
-          for (int i = 0; i < pieces; ++i) {  // in the order of the ranges
-            const float* other = slot_of<NT>(p, it.first_cta + i, i == 0 ? 1 : 0);
+          for (int j = 0; j < it.of; ++j) {  // in the order of the keys
+            const float* other = slot_at<NT>(p, it.slot + j);
             const float2 ml = __ldcg(reinterpret_cast<const float2*>(other + 8 * NT * kD) + row);
             const float v = __ldcg(other + row * kD + tid);
             const float top = fmaxf(m, ml.x);
@@ -503,20 +573,28 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) tree_kernel(const T
         }
       }
     }
-    __syncthreads();  // the next piece's results go where these lie
+    __syncthreads();  // before the next piece writes what was read here
+    it = next;
+    i = i_next;
+  }
+  if (tid == 0 && atomicAdd(reinterpret_cast<unsigned*>(header) + 1, 1u) == gridDim.x - 1) {
+    header[0] = 0;  // every CTA has taken its last piece
+    header[1] = 0;
   }
 }
 
 struct Kernel {
   const void* fn;
   size_t smem;
-  int rows;
+  int ctas;  // per SM
 };
+template <bool BF, bool C8, int NT>
+Kernel kernel_for() {
+  return {reinterpret_cast<const void*>(&tree_kernel<BF, C8, NT>), sizeof(Shared<C8, NT>), Fit<C8, NT>::kCtas};
+}
 template <bool BF, bool C8>
 Kernel kernel_of(int nt) {
-  if (nt == 1) return {reinterpret_cast<const void*>(&tree_kernel<BF, C8, 1>), sizeof(Shared<1>), 8};
-  if (nt == 2) return {reinterpret_cast<const void*>(&tree_kernel<BF, C8, 2>), sizeof(Shared<2>), 16};
-  return {reinterpret_cast<const void*>(&tree_kernel<BF, C8, 4>), sizeof(Shared<4>), 32};
+  return nt == 1 ? kernel_for<BF, C8, 1>() : nt == 2 ? kernel_for<BF, C8, 2>() : kernel_for<BF, C8, 4>();
 }
 
 // 8-row tiles of an item, by the rows that a request has on average: a wider tile reads the cache fewer
@@ -529,23 +607,22 @@ int tile_count(int B, long long new_rows, int n_heads, int n_kv_heads) {
 }  // namespace
 
 size_t tree_attention_workspace_bytes(int B, long long new_rows, int n_heads, int n_kv_heads) {
-  return kTreeCounterBytes +
-         static_cast<size_t>(2 * kTreeMaxGrid) * 8 * tile_count(B, new_rows, n_heads, n_kv_heads) * (kD + 2) * sizeof(float);
+  const int nt = tile_count(B, new_rows, n_heads, n_kv_heads);
+  return (kTreeHeader + kTreeCounters) * sizeof(int) + slots_of(nt) * slot_floats(nt) * sizeof(float);
 }
 
 cudaError_t launch_tree_attention(const TreeArgs& a, int dtype, bool cache8, cudaStream_t stream) {
   const int nt = tile_count(a.B, a.new_rows, a.n_heads, a.n_kv_heads);
   const Kernel k = dtype == FSX_BF16 ? (cache8 ? kernel_of<true, true>(nt) : kernel_of<true, false>(nt))
                                      : (cache8 ? kernel_of<false, true>(nt) : kernel_of<false, false>(nt));
-  cudaError_t e = cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(k.smem));
-  int dev = 0, sms = 0, per_sm = 0;
+  const size_t smem = k.smem + tree_plan_bytes(a.B);
+  cudaError_t e = cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  int dev = 0, sms = 0;
   if (e == cudaSuccess) e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k.fn, kThreads, k.smem);
   if (e != cudaSuccess) return e;
-  const int grid = sms * per_sm < kTreeMaxGrid ? sms * per_sm : kTreeMaxGrid;
   void* args[] = {const_cast<TreeArgs*>(&a)};
-  return launch_ex(k.fn, dim3(static_cast<unsigned>(grid)), dim3(kThreads), k.smem, stream, false, args);
+  return launch_ex(k.fn, dim3(static_cast<unsigned>(sms * k.ctas)), dim3(kThreads), smem, stream, false, args);
 }
 
 }  // namespace fsx

@@ -1,9 +1,13 @@
-// How the attention of drafted tokens shares its work out: every (request, tile of its rows, kv head)
-// is an item of ceil(cache rows / chunk) chunks and one more for the new tokens; the chunks of all items
-// are one line, cut into equal ranges, one per CTA (the host knows no lengths, and one long request must
-// fill the GPU as well as many short ones). An item that ranges cut is put together by whichever of
-// its CTAs comes last, in the order of the ranges, so that results do not depend on the order of arrival.
-// At most one cut item begins in a range and at most one ends in it: two slots of partial results and one counter a CTA.
+// How the attention of drafted tokens shares its work out. Every (request, tile of its rows, kv head)
+// is an item of ceil(cache rows / chunk) chunks and one more for the new tokens. Items of more than
+// `most` chunks are cut into near-equal pieces; `most` follows from the number of all chunks (the host knows no
+// lengths), so that one long request fills the GPU as well as many short ones. CTAs take pieces from
+// one queue: equal shares fixed before left the SMs idle a quarter of the time (some read the caches faster
+// than others, and a short cache costs more per row). The pieces of a cut item are put together by
+// whichever comes last, in the order of its keys, so that results do not depend on the order of arrival.
+//
+// Workspace: the queue, one counter per cut item, one slot of partial results per piece of a cut item.
+// All counters are zero between calls.
 #pragma once
 
 #include "device_util.cuh"
@@ -11,8 +15,8 @@
 
 namespace fsx {
 
-constexpr int kTreeMaxGrid = 1024;
-constexpr size_t kTreeCounterBytes = kTreeMaxGrid * sizeof(int);
+constexpr int kTreeHeader = 64;      // ints: [0] next piece, [1] CTAs that are done
+constexpr int kTreeCounters = 8192;  // as many for every kernel: what follows them may hold anything
 
 struct TreeRequest {
   long long c0;  // first cache row
@@ -35,76 +39,121 @@ __device__ __forceinline__ bool tree_request(const TreeArgs& p, int b, TreeReque
   return true;
 }
 
-__device__ __forceinline__ int tree_chunks(int len, int chunk) { return (len + chunk - 1) / chunk + 1; }
+// Geometry of a kernel's items
+struct TreeShape {
+  int tile_rows, chunk;  // rows of an item, keys of a chunk
+  int few, many;         // an item of `few` chunks or less is not cut; pieces are no longer than `many` for balance alone
+  int slots;             // of the workspace
+};
 
-// pre[b]: chunks of all items of the requests before b, pre[B] of all. THREADS threads of the CTA; `scratch`
-// holds one value per warp.
-template <int THREADS>
-__device__ __forceinline__ void tree_prefix(const TreeArgs& p, int tile_rows, int chunk, long long* pre, long long* scratch) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int G = p.n_heads / p.n_kv_heads;
-  const int per = (p.B + THREADS - 1) / THREADS;
-  auto units = [&](int b) {
-    TreeRequest r;
-    if (!tree_request(p, b, r)) {
-      if (blockIdx.x == 0) set_status(p.status, kStatusDeviceArg);
-      return 0ll;
-    }
-    return static_cast<long long>((r.n * G + tile_rows - 1) / tile_rows) * p.n_kv_heads * tree_chunks(r.len, chunk);
-  };
-  long long mine = 0;
-  for (int i = 0; i < per; ++i) {
-    const int b = tid * per + i;
-    if (b < p.B) {
-      pre[b] = mine;  // within this thread's requests
-      mine += units(b);
-    }
-  }
-  long long sum = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long up = __shfl_up_sync(0xffffffffu, sum, o);
-    if (lane >= o) sum += up;
-  }
-  if (lane == 31) scratch[warp] = sum;
-  __syncthreads();
-  long long before = sum - mine;
-  for (int w = 0; w < warp; ++w) before += scratch[w];
-  for (int i = 0; i < per; ++i) {
-    const int b = tid * per + i;
-    if (b < p.B) pre[b] += before;
-  }
-  if (tid == THREADS - 1) pre[p.B] = before + mine;
-  __syncthreads();
+__device__ __forceinline__ int tree_chunks(const TreeShape& s, int len) { return (len + s.chunk - 1) / s.chunk + 1; }
+__device__ __forceinline__ int tree_pieces(const TreeShape& s, int n, int most) {
+  return n <= s.few ? 1 : (n + most - 1) / most;
 }
 
-// The part of an item that lies in this CTA's range [u, u1).
+struct TreePlan {
+  long long* pieces;  // [B + 1] pieces of the requests before
+  int* slots;         // [B + 1] slots of the requests before
+  int most;           // chunks of a piece
+};
+__host__ __device__ constexpr size_t tree_plan_bytes(int B) { return (B + 1) * (sizeof(long long) + sizeof(int)) + 8; }
+
+// By all THREADS threads of the CTA; `at`: tree_plan_bytes(B) bytes, 8-byte aligned; `scratch`: 2 values per warp.
+template <int THREADS>
+__device__ __forceinline__ TreePlan tree_plan(const TreeArgs& p, const TreeShape& shape, void* at, long long* scratch) {
+  constexpr int kW = THREADS / 32;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int G = p.n_heads / p.n_kv_heads;
+  const int per = (p.B + THREADS - 1) / THREADS, b0 = tid * per, b1 = min(p.B, b0 + per);
+  TreePlan plan;
+  plan.pieces = static_cast<long long*>(at);
+  plan.slots = reinterpret_cast<int*>(plan.pieces + p.B + 1);
+  auto items = [&](const TreeRequest& r) {
+    return static_cast<long long>((r.n * G + shape.tile_rows - 1) / shape.tile_rows) * p.n_kv_heads;
+  };
+  long long total = 0;
+  for (int b = b0; b < b1; ++b) {
+    TreeRequest r;
+    if (!tree_request(p, b, r) && blockIdx.x == 0) set_status(p.status, kStatusDeviceArg);
+    total += items(r) * tree_chunks(shape, r.len);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+  if (lane == 0) scratch[warp] = total;
+  __syncthreads();
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kW; ++w) total += scratch[w];
+  // an even share, but no more than `many`; and cut items of n > most chunks take at most 2 n / most slots
+  const long long share = min((total + gridDim.x - 1) / gridDim.x, static_cast<long long>(shape.many));
+  const long long room = (2 * total + shape.slots - 1) / shape.slots;
+  plan.most = static_cast<int>(min(max(max(share, room), static_cast<long long>((shape.few + 1) / 2)), 0x7fffffffll));
+  long long mine = 0, mine_slots = 0;
+  for (int b = b0; b < b1; ++b) {
+    TreeRequest r;
+    tree_request(p, b, r);
+    const int n = tree_pieces(shape, tree_chunks(shape, r.len), plan.most);
+    plan.pieces[b] = mine;  // within this thread's requests
+    plan.slots[b] = static_cast<int>(mine_slots);
+    mine += items(r) * n;
+    mine_slots += n > 1 ? items(r) * n : 0;
+  }
+  long long sum = mine, sum_slots = mine_slots;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long up = __shfl_up_sync(0xffffffffu, sum, o), up_slots = __shfl_up_sync(0xffffffffu, sum_slots, o);
+    if (lane >= o) {
+      sum += up;
+      sum_slots += up_slots;
+    }
+  }
+  __syncthreads();
+  if (lane == 31) {
+    scratch[warp] = sum;
+    scratch[kW + warp] = sum_slots;
+  }
+  __syncthreads();
+  sum -= mine;
+  sum_slots -= mine_slots;
+  for (int w = 0; w < warp; ++w) {
+    sum += scratch[w];
+    sum_slots += scratch[kW + w];
+  }
+  for (int b = b0; b < b1; ++b) {
+    plan.pieces[b] += sum;
+    plan.slots[b] += static_cast<int>(sum_slots);
+  }
+  if (tid == THREADS - 1) plan.pieces[p.B] = sum + mine;
+  __syncthreads();
+  return plan;
+}
+
 struct TreePiece {
   TreeRequest r;
-  int kvh, row0;        // kv head, first row of the tile (row = token G + head of the group)
-  int from, to, n;      // chunks from .. to - 1 of n; chunk n - 1 holds the new tokens
-  int first_cta, last_cta;
+  int kvh, row0;    // kv head, first row of the tile (row = token G + head of the group)
+  int from, to, n;  // chunks from .. to - 1 of n; chunk n - 1 holds the new tokens
+  int slot, j, of;  // piece j of `of`; `slot` is that of piece 0
 };
-__device__ __forceinline__ TreePiece tree_piece(const TreeArgs& p, const long long* pre, int tile_rows, int chunk, long long u,
-                                                long long u1, long long per) {
-  int lo = 0, hi = p.B;  // pre[lo] <= u < pre[hi]
+__device__ __forceinline__ TreePiece tree_piece(const TreeArgs& p, const TreeShape& shape, const TreePlan& plan, long long i) {
+  int lo = 0, hi = p.B;  // pieces[lo] <= i < pieces[hi]
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (pre[mid] <= u) lo = mid;
+    if (plan.pieces[mid] <= i) lo = mid;
     else hi = mid;
   }
   TreePiece x;
   tree_request(p, lo, x.r);
-  x.n = tree_chunks(x.r.len, chunk);
-  const long long rel = u - pre[lo];
-  const long long item = rel / x.n;
-  x.from = static_cast<int>(rel - item * x.n);
-  x.kvh = static_cast<int>(item % p.n_kv_heads);
-  x.row0 = static_cast<int>(item / p.n_kv_heads) * tile_rows;
-  const long long start = u - x.from, end = start + x.n;
-  x.to = static_cast<int>(min(end, u1) - start);
-  x.first_cta = static_cast<int>(start / per);
-  x.last_cta = static_cast<int>((end - 1) / per);
+  x.n = tree_chunks(shape, x.r.len);
+  x.of = tree_pieces(shape, x.n, plan.most);
+  const uint32_t rel = static_cast<uint32_t>(i - plan.pieces[lo]);  // a request has less than 2^32 pieces
+  const uint32_t item = rel / static_cast<uint32_t>(x.of);
+  x.j = static_cast<int>(rel - item * x.of);
+  x.slot = plan.slots[lo] + static_cast<int>(rel) - x.j;
+  x.from = static_cast<int>(static_cast<long long>(x.n) * x.j / x.of);
+  x.to = static_cast<int>(static_cast<long long>(x.n) * (x.j + 1) / x.of);
+  const uint32_t tile = item / static_cast<uint32_t>(p.n_kv_heads);
+  x.kvh = static_cast<int>(item - tile * p.n_kv_heads);
+  x.row0 = static_cast<int>(tile) * shape.tile_rows;
   return x;
 }
 
