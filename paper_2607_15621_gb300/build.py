@@ -22,7 +22,7 @@ BUILD_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(OUT_DIR, "libfsx.so")
 SOURCES = ["fsx.cu", "launch.cu", "gemm_tc.cu", "gemm_stream.cu", "gemm_res.cu", "attention.cu", "attention_tc.cu", "embed_head.cu",
            "attention_noalloc.cu", "tick_persistent.cu", "append.cu", "paper_tokens.cu", "session.cu",
-           "llm.cu", "cache8.cu", "prompt_attention.cu", "tree_attention.cu"]
+           "llm.cu", "cache8.cu", "prompt_attention.cu", "tree_attention.cu", "tree_tc.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-pthread",
          "--expt-relaxed-constexpr", "-I", os.path.join(ROOT, "include")]

@@ -73,6 +73,9 @@ struct TreeArgs {
   int* status;
 };
 size_t tree_attention_workspace_bytes(int B, long long new_rows, int n_heads, int n_kv_heads);
+// for many rows per request (tree_tc.cu)
+size_t tree_tc_workspace_bytes(long long new_rows, int n_heads, int n_kv_heads);
+cudaError_t launch_tree_tc(const TreeArgs& a, int dtype, bool cache8, cudaStream_t stream);
 cudaError_t launch_tree_attention(const TreeArgs& a, int dtype, bool cache8, cudaStream_t stream);
 
 }  // namespace fsx

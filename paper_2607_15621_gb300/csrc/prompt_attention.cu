@@ -152,6 +152,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
   volatile int* abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* wild = reinterpret_cast<volatile int*>(tmem_slot + 2);  // a guarded value was not finite
   Item* item_slot = reinterpret_cast<Item*>(smem);  // before the queries
+  if ((smem_addr(smem) & 1023u) != 0u) {  // the swizzled operands need a 1024-byte aligned base
+    if (tid == 0) set_status(p.status, kStatusDeviceArg);
+    return;
+  }
 
   // ---- which item
   int2* lens = reinterpret_cast<int2*>(smem + kOffRing);

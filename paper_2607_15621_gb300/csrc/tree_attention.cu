@@ -11,8 +11,8 @@
 // operands agree: a lane takes whole 16-byte units of a row, so a warp's loads cover 64 to 128 bytes a row.
 //   lane (g, c) = (lane / 4, lane % 4): K of keys g, g + 8; V of keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9;
 //   scores and weights of keys g, g + 8 for rows 2 c, 2 c + 1; outputs of rows 2 c, 2 c + 1 for 16 dims.
-// 8-bit caches: codes become fp16 exactly, queries fp16 times a power of two per row (exact for bf16, whose
-// 8 bits fit; components 2^-22 below the row's largest may lose their last bits), a key's scale multiplies its
+// 8-bit caches: codes become fp16 exactly, bf16 queries fp16 times a power of two per row (their 8 bits fit;
+// components 2^-22 below the row's largest may lose their last bits), a key's scale multiplies its
 // score, a value's scale its weight, relative to the largest value scale so far (`vs`). Weights are then fp16,
 // also for bf16 queries. 16-bit caches and the new tokens use their own type, weights rounded to it.
 // The running maximum moves only when a score exceeds it by more than 2^8, seen by one vote a step.
@@ -317,7 +317,7 @@ __device__ __forceinline__ void new_step(State<NT>& st, const TreeArgs& p, const
   }
 }
 
-// Queries of the item's rows as B operands; C8: as fp16 times 2^-e, f the factor that undoes it
+// Queries of the item's rows as B operands; C8: bf16 as fp16 times 2^-e, f the factor that undoes it
 template <bool BF, bool C8, int NT>
 __device__ __forceinline__ void load_queries(uint32_t (&qf)[NT][8][2], float (&f)[NT][2], const TreeArgs& p, const TreePiece& it, int G) {
   const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
@@ -334,7 +334,9 @@ __device__ __forceinline__ void load_queries(uint32_t (&qf)[NT][8][2], float (&f
       qf[t][k][0] = w.x;
       qf[t][k][1] = w.y;
     }
-    if (C8) {
+    if (C8 && !BF) {
+      f[t][0] = f[t][1] = kScaleLog2;  // fp16 as it is
+    } else if (C8) {
       float top = 0.f;
 #pragma unroll
       for (int k = 0; k < 8; ++k)
@@ -367,9 +369,9 @@ __device__ __forceinline__ void load_queries(uint32_t (&qf)[NT][8][2], float (&f
 // CTAs an SM holds, stages of 16 keys in each warp's ring, rows that the warps put together at a time
 template <bool C8, int NT>
 struct Fit {
-  static constexpr int kCtas = NT == 1 ? (C8 ? 4 : 3) : NT == 2 ? 3 : 2;
-  static constexpr int kStages = C8 ? (NT == 4 ? 5 : 3) : (NT < 4 ? 2 : 3);
-  static constexpr int kPass = NT == 1 ? 2 : NT == 2 ? 4 : 8;
+  static constexpr int kCtas = NT == 1 && C8 ? 4 : 3;
+  static constexpr int kStages = C8 ? 3 : 2;
+  static constexpr int kPass = 2 * NT;
 };
 template <bool C8, int NT>
 struct Shared {  // and the plan behind it
@@ -555,21 +557,41 @@ __global__ void __launch_bounds__(kThreads, Fit<C8, NT>::kCtas) tree_kernel(cons
       __syncthreads();
       if (sm.last) {
         __threadfence();
+        const float* first = slot_at<NT>(p, it.slot);
 #pragma unroll 1
-        for (int row = 0; row < rows; ++row) {
-          float m = -CUDART_INF_F, l = 0.f, o = 0.f;
-#pragma unroll 4
-          for (int j = 0; j < it.of; ++j) {  // in the order of the keys
-            const float* other = slot_at<NT>(p, it.slot + j);
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(other + 8 * NT * kD) + row);
-            const float v = __ldcg(other + row * kD + tid);
-            const float top = fmaxf(m, ml.x);
-            const float a = weight_of(m, top), b = weight_of(ml.x, top);
-            l = l * a + b * ml.y;
-            o = o * a + b * v;
-            m = top;
+        for (int row = warp; row < rows; row += kWarps) {  // a warp a row, 4 dims a lane
+          const float* ml = first + 8 * NT * kD + 2 * row;
+          float m = -CUDART_INF_F;
+          for (int j = lane; j < it.of; j += 32) m = fmaxf(m, __ldcg(ml + j * slot_floats(NT)));
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+          float l = 0.f;
+          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int j0 = 0; j0 < it.of; j0 += 32) {  // in the order of the keys
+            const int count = min(32, it.of - j0);
+            float w = 0.f;
+            if (lane < count) {
+              const float2 x = __ldcg(reinterpret_cast<const float2*>(ml + (j0 + lane) * slot_floats(NT)));
+              w = weight_of(x.x, m);
+              l += w * x.y;
+            }
+#pragma unroll 8
+            for (int j = 0; j < count; ++j) {
+              const float a = __shfl_sync(0xffffffffu, w, j);
+              const float4 v = __ldcg(reinterpret_cast<const float4*>(first + (j0 + j) * slot_floats(NT) + row * kD) + lane);
+              o.x += a * v.x;
+              o.y += a * v.y;
+              o.z += a * v.z;
+              o.w += a * v.w;
+            }
           }
-          finish(row, m, l, o);
+          l = warp_sum(l);
+          const int at = it.row0 + row, token = at / G, head = it.kvh * G + at - token * G;
+          const float inv = l == 0.f ? 0.f : 1.f / l;
+          uint16_t* out = static_cast<uint16_t*>(p.out) + ((it.r.t0 + token) * p.n_heads + head) * kD + 4 * lane;
+          *reinterpret_cast<uint2*>(out) = make_uint2(pack16<BF>(o.x * inv, o.y * inv), pack16<BF>(o.z * inv, o.w * inv));
+          if (p.lse != nullptr && lane == 0)
+            p.lse[head * p.new_rows + it.r.t0 + token] = l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * kLn2;
         }
       }
     }
@@ -594,25 +616,26 @@ Kernel kernel_for() {
 }
 template <bool BF, bool C8>
 Kernel kernel_of(int nt) {
-  return nt == 1 ? kernel_for<BF, C8, 1>() : nt == 2 ? kernel_for<BF, C8, 2>() : kernel_for<BF, C8, 4>();
+  return nt == 1 ? kernel_for<BF, C8, 1>() : kernel_for<BF, C8, 2>();
 }
 
-// 8-row tiles of an item, by the rows that a request has on average: a wider tile reads the cache fewer
-// times, a narrower one leaves more warps on an SM
+// 8-row tiles of an item, by the rows that a request has on average; 0: the kernel of tree_tc.cu
 int tile_count(int B, long long new_rows, int n_heads, int n_kv_heads) {
   const long long rows = (new_rows * (n_heads / n_kv_heads) + B - 1) / B;
-  return rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
+  return rows <= 8 ? 1 : rows <= 16 ? 2 : 0;
 }
 
 }  // namespace
 
 size_t tree_attention_workspace_bytes(int B, long long new_rows, int n_heads, int n_kv_heads) {
   const int nt = tile_count(B, new_rows, n_heads, n_kv_heads);
+  if (nt == 0) return tree_tc_workspace_bytes(new_rows, n_heads, n_kv_heads);
   return (kTreeHeader + kTreeCounters) * sizeof(int) + slots_of(nt) * slot_floats(nt) * sizeof(float);
 }
 
 cudaError_t launch_tree_attention(const TreeArgs& a, int dtype, bool cache8, cudaStream_t stream) {
   const int nt = tile_count(a.B, a.new_rows, a.n_heads, a.n_kv_heads);
+  if (nt == 0) return launch_tree_tc(a, dtype, cache8, stream);
   const Kernel k = dtype == FSX_BF16 ? (cache8 ? kernel_of<true, true>(nt) : kernel_of<true, false>(nt))
                                      : (cache8 ? kernel_of<false, true>(nt) : kernel_of<false, false>(nt));
   const size_t smem = k.smem + tree_plan_bytes(a.B);

@@ -52,13 +52,13 @@ __device__ __forceinline__ int tree_pieces(const TreeShape& s, int n, int most) 
 }
 
 struct TreePlan {
-  long long* pieces;  // [B + 1] pieces of the requests before
+  uint32_t* pieces;   // [B + 1] pieces of the requests before: at most 2^31 items and the slots of cut ones
   int* slots;         // [B + 1] slots of the requests before
   int most;           // chunks of a piece
 };
-__host__ __device__ constexpr size_t tree_plan_bytes(int B) { return (B + 1) * (sizeof(long long) + sizeof(int)) + 8; }
+__host__ __device__ constexpr size_t tree_plan_bytes(int B) { return (B + 1) * 2 * sizeof(int); }
 
-// By all THREADS threads of the CTA; `at`: tree_plan_bytes(B) bytes, 8-byte aligned; `scratch`: 2 values per warp.
+// By all THREADS threads of the CTA; `at`: tree_plan_bytes(B) bytes; `scratch`: 2 values per warp.
 template <int THREADS>
 __device__ __forceinline__ TreePlan tree_plan(const TreeArgs& p, const TreeShape& shape, void* at, long long* scratch) {
   constexpr int kW = THREADS / 32;
@@ -66,7 +66,7 @@ __device__ __forceinline__ TreePlan tree_plan(const TreeArgs& p, const TreeShape
   const int G = p.n_heads / p.n_kv_heads;
   const int per = (p.B + THREADS - 1) / THREADS, b0 = tid * per, b1 = min(p.B, b0 + per);
   TreePlan plan;
-  plan.pieces = static_cast<long long*>(at);
+  plan.pieces = static_cast<uint32_t*>(at);
   plan.slots = reinterpret_cast<int*>(plan.pieces + p.B + 1);
   auto items = [&](const TreeRequest& r) {
     return static_cast<long long>((r.n * G + shape.tile_rows - 1) / shape.tile_rows) * p.n_kv_heads;
@@ -93,7 +93,7 @@ __device__ __forceinline__ TreePlan tree_plan(const TreeArgs& p, const TreeShape
     TreeRequest r;
     tree_request(p, b, r);
     const int n = tree_pieces(shape, tree_chunks(shape, r.len), plan.most);
-    plan.pieces[b] = mine;  // within this thread's requests
+    plan.pieces[b] = static_cast<uint32_t>(mine);  // within this thread's requests
     plan.slots[b] = static_cast<int>(mine_slots);
     mine += items(r) * n;
     mine_slots += n > 1 ? items(r) * n : 0;
@@ -120,10 +120,10 @@ __device__ __forceinline__ TreePlan tree_plan(const TreeArgs& p, const TreeShape
     sum_slots += scratch[kW + w];
   }
   for (int b = b0; b < b1; ++b) {
-    plan.pieces[b] += sum;
+    plan.pieces[b] += static_cast<uint32_t>(sum);
     plan.slots[b] += static_cast<int>(sum_slots);
   }
-  if (tid == THREADS - 1) plan.pieces[p.B] = sum + mine;
+  if (tid == THREADS - 1) plan.pieces[p.B] = static_cast<uint32_t>(sum + mine);
   __syncthreads();
   return plan;
 }
