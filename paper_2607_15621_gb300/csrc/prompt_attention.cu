@@ -36,14 +36,14 @@ constexpr int kTile = 128;              // query rows of a tile, keys of a chunk
 constexpr int kItemRows = 2 * kTile;
 constexpr int kStages = 5;
 constexpr int kStageBytes = kTile * kD * 2;  // 32 KB
-constexpr int kMmaWarp = 8, kLoadWarp = 9, kGuardWarp = 10;
-constexpr int kThreads = 384;
+constexpr int kMmaWarp = 8, kLoadWarp = 9;  // the last two guard
+constexpr int kThreads = 384;           // three warpgroups: 168 registers a thread at launch
 constexpr int kMaxGuarded = 3;          // 256 rows are at most 256 tokens: their diagonals and the end
 constexpr uint32_t kColS = 0, kColO = 256;
 constexpr int kOffRing = 2 * kStageBytes;  // the two Q tiles lie in front
 constexpr int kOffBar = kOffRing + kStages * kStageBytes;
-// full[5], empty[5], gfull[3], gdone[3], qfull[2], sfull[2], pfull[2], odone[2], drain
-constexpr int kNumBars = 25;
+// full[5], empty[5], gfull[3], gdone[3], qfull[2], sfull[2], pfull[2][2], odone[2], drain
+constexpr int kNumBars = 27;
 constexpr int kSmem = kOffBar + kNumBars * 8 + 64;
 static_assert(kSmem <= 227 * 1024, "shared memory");
 static_assert(kMaxSequences * 16 <= kStages * kStageBytes, "the lengths lie in the ring before it is used");
@@ -145,9 +145,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
   uint64_t* gdone = bars + 13;   // [3] and is guarded (waited for in place of `full`)
   uint64_t* qfull = bars + 16;   // [2] a tile's queries are there
   uint64_t* sfull = bars + 18;   // [2] S of a chunk in tensor memory
-  uint64_t* pfull = bars + 20;   // [2] P of a chunk written over it
-  uint64_t* odone = bars + 22;   // [2] every P V of the tile done
-  uint64_t* drain = bars + 24;   // every MMA done
+  uint64_t* pfull = bars + 20;   // [2][2] P of half a chunk written over it
+  uint64_t* odone = bars + 24;   // [2] every P V of the tile done
+  uint64_t* drain = bars + 26;   // every MMA done
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kNumBars);
   volatile int* abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* wild = reinterpret_cast<volatile int*>(tmem_slot + 2);  // a guarded value was not finite
@@ -177,7 +177,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
     for (int i = 0; i < 2; ++i) {
       mbar_init(qfull + i, 4);
       mbar_init(sfull + i, 1);
-      mbar_init(pfull + i, 4);
+      mbar_init(pfull + 2 * i, 4);
+      mbar_init(pfull + 2 * i + 1, 4);
       mbar_init(odone + i, 1);
     }
     mbar_init(drain, 1);
@@ -219,53 +220,76 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
 
   if (it.b < 0) {
     // nothing: more blocks than items
-  } else if (warp == kMmaWarp) {
+  } else if (warp >= kMmaWarp) {
+  leave_registers<88>();  // of 3 x 168 a lane at launch; the softmax warpgroups take 2 x 208
+  if (warp == kMmaWarp) {
     // ---------------------------------------------------------------- MMAs
     if (lane == 0) {
       const uint32_t id_s = idesc_16(BF, kTile, kTile, false), id_o = idesc_16(BF, kTile, kD, true);
-      const uint32_t ring = smem_addr(smem + kOffRing);
+      const uint32_t ring = smem_addr(smem + kOffRing), q = smem_addr(smem);
       bool ok = true;
       // the guarded chunks are the last three V chunks at most: no later chunk takes their stages
-      auto wait_stage = [&](int c) {
+      auto stage_bar = [&](int c, uint32_t& parity) {
         const bool guarded = (c & 1) && (c >> 1) >= guard0;
-        ok = ok && (guarded ? wait_or_abort(gdone + ((c >> 1) - guard0), 0, p.status, abort)
-                            : wait_or_abort(full + c % kStages, (c / kStages) & 1, p.status, abort));
+        parity = guarded ? 0 : (c / kStages) & 1;
+        return guarded ? gdone + ((c >> 1) - guard0) : full + c % kStages;
       };
-      auto issue_s = [&](int t, int j) {
-        const uint32_t a = smem_addr(smem + t * kStageBytes), b = ring + ((2 * j) % kStages) * kStageBytes;
-        const uint32_t d = tmem + kColS + t * kTile;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const uint32_t off = (k >> 2) * 16384 + (k & 3) * 32;
-          umma_f16(d, sw128_desc(a + off), sw128_desc(b + off), id_s, k > 0 ? 1u : 0u);
-        }
-        umma_commit(sfull + t);
+      auto test_stage = [&](int c) {
+        uint32_t parity;
+        uint64_t* bar = stage_bar(c, parity);
+        return test_bar(bar, parity);
       };
-      auto issue_o = [&](int t, int j) {
-        const uint32_t b = ring + ((2 * j + 1) % kStages) * kStageBytes;
-        const uint32_t a = tmem + kColS + t * kTile, d = tmem + kColO + t * kTile;
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          umma_f16_ta(d, a + k * 8, sw128_desc_mn(b + k * 2048, 16384, 1024), id_o, j > 0 || k > 0 ? 1u : 0u);
+      auto need_stage = [&](int c, uint32_t there) {
+        uint32_t parity;
+        uint64_t* bar = stage_bar(c, parity);
+        ok = ok && (there || wait_or_abort(bar, parity, p.status, abort));
       };
+      uint32_t k_there = 0, v_there = 0, p_there[2][2] = {{0, 0}, {0, 0}};  // tested already
 #pragma unroll 1
-      for (int j = 0; j <= n_all && ok; ++j) {  // P V of chunk j - 1, then S of chunk j
-        if (j < n_all) wait_stage(2 * j);
-        if (j > 0) wait_stage(2 * j - 1);
+      for (int j = 0; j <= n_all && ok; ++j) {  // per tile: P V of chunk j - 1, then S of chunk j
+        const uint32_t vb = ring + ((2 * j + 2 * kStages - 1) % kStages) * kStageBytes, kb = ring + ((2 * j) % kStages) * kStageBytes;
+        if (j > 0) need_stage(2 * j - 1, v_there);
+        if (j < n_all) need_stage(2 * j, k_there);
+        v_there = k_there = 0;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
+          const uint32_t s_at = tmem + kColS + t * kTile, o_at = tmem + kColO + t * kTile;
+          if (!ok) break;
           if (j > 0 && j <= n[t]) {
-            ok = ok && wait_or_abort(pfull + t, (j - 1) & 1, p.status, abort);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {  // the keys' first 64, whose weights are there first
+              ok = p_there[t][half] || wait_or_abort(pfull + 2 * t + half, (j - 1) & 1, p.status, abort);
+              if (!ok) break;
+              tc_fence_after();
+              if (half == 0 && !p_there[t][1]) p_there[t][1] = test_bar(pfull + 2 * t + 1, (j - 1) & 1);
+#pragma unroll
+              for (int k = 4 * half; k < 4 * half + 4; ++k)
+                umma_f16_ta(o_at, s_at + k * 8, sw128_desc_mn(vb + k * 2048, 16384, 1024), id_o, j > 1 || k > 0 ? 1u : 0u);
+            }
             if (!ok) break;
-            tc_fence_after();
-            issue_o(t, j - 1);
+            p_there[t][0] = p_there[t][1] = 0;
             if (j == n[t]) umma_commit(odone + t);
           }
           if (j < n[t]) {
-            if (j == 0) ok = ok && wait_or_abort(qfull + t, 0, p.status, abort);
+            if (j == 0) ok = wait_or_abort(qfull + t, 0, p.status, abort);
             if (!ok) break;
             tc_fence_after();
-            issue_s(t, j);
+            // the other tile's weights: of chunk j - 1 for tile 1, of chunk j for tile 0 (there after its S)
+            const int pj = t == 0 ? j - 1 : j;
+            if (pj >= 0 && pj < n[t ^ 1]) {
+              p_there[t ^ 1][0] = test_bar(pfull + 2 * (t ^ 1), pj & 1);
+              p_there[t ^ 1][1] = test_bar(pfull + 2 * (t ^ 1) + 1, pj & 1);
+            }
+            if (t == 1 && j < n_all) {
+              v_there = test_stage(2 * j + 1);
+              if (j + 1 < n_all) k_there = test_stage(2 * j + 2);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const uint32_t off = (k >> 2) * 16384 + (k & 3) * 32;
+              umma_f16(s_at, sw128_desc(q + t * kStageBytes + off), sw128_desc(kb + off), id_s, k > 0 ? 1u : 0u);
+            }
+            umma_commit(sfull + t);
           }
         }
         if (!ok) break;
@@ -301,9 +325,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
         }
     }
     __syncwarp();
-  } else if (warp >= kGuardWarp) {
-    // ---------------------------------------------------------------- guards
-    const int w = warp - kGuardWarp;
+  } else {
+    // ---------------------------------------------------------------- guard
 #pragma unroll 1
     for (int j = guard0; j < n_all; ++j) {
       if (!wait_or_abort(gfull + (j - guard0), 0, p.status, abort)) break;
@@ -312,7 +335,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
       const int in_range = it.nk - j * kTile;  // rows of the sequence in this chunk
       uint32_t bad = 0;
 #pragma unroll 4
-      for (int r = w * 2 + (lane >> 4); r < kTile; r += 4) {
+      for (int r = (warp & 1) * 2 + (lane >> 4); r < kTile; r += 4) {
         uint4* u = reinterpret_cast<uint4*>(v + tile_off(r, lane & 15));
         if (r >= in_range) {
           *u = make_uint4(0u, 0u, 0u, 0u);
@@ -333,8 +356,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
       __syncwarp();
       if (lane == 0) mbar_arrive(gdone + (j - guard0));
     }
+  }
   } else {
     // ---------------------------------------------------------------- softmax of tile t
+    take_registers<208>();
     const int t = warp >> 2;
     const int r = tid & (kTile - 1);  // this thread's row: tensor-memory lane r
     const long long first = it.row0 + t * kTile;
@@ -346,15 +371,15 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
     {
       const uint16_t* q = static_cast<const uint16_t*>(p.q);
       const int u = tid & 15;
-#pragma unroll 4
-      for (int i = (tid & (kTile - 1)) >> 4; i < kTile; i += 8) {
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (i < valid) {
-          const uint32_t g = head0 + i, on = g / static_cast<uint32_t>(G);
-          x = __ldg(reinterpret_cast<const uint4*>(q + (it.q0 + token0 + on) * p.q_stride + (kvh * G + g - on * G) * kD) + u);
-        }
-        *reinterpret_cast<uint4*>(qt + tile_off(i, u)) = x;
+#pragma unroll
+      for (int i = 0; i < kTile / 8; ++i) {  // all on their way at once
+        const int at = ((tid & (kTile - 1)) >> 4) + 8 * i;
+        const bool there = at < valid;
+        const uint32_t g = head0 + (there ? at : 0), on = g / static_cast<uint32_t>(G);
+        copy16(smem_addr(qt + tile_off(at, u)), q + (it.q0 + token0 + on) * p.q_stride + (kvh * G + g - on * G) * kD + u * 8, there);
       }
+      cp_async_commit();
+      cp_async_wait<0>();
       fence_proxy_async();
       __syncwarp();
       if (lane == 0) mbar_arrive(qfull + t);
@@ -428,12 +453,12 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
           pk[e] = pack16<BF>(a, b);
         }
         tmem_st32(scol + 32 * i, pk);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(pfull + 2 * t + i);
       }
       l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(pfull + t);
     }
     // ---- output
     if (ok && n[t] > 0) ok = wait_or_abort(odone + t, 0, p.status, abort);

@@ -91,6 +91,22 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// Whether the phase of `parity` is complete, without waiting. The answer of a test takes about 150 cycles:
+// a thread that asks before it issues MMAs has it when they are issued.
+__device__ __forceinline__ uint32_t test_bar(uint64_t* bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+      : "=r"(done)
+      : "r"(smem_addr(bar)), "r"(parity)
+      : "memory");
+  return done;
+}
+// 16 bytes to shared memory, zeros if not `there` (then nothing is read)
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+
 // Waits for phase `parity` of an mbarrier; false once a wait of the CTA has given up (about one second:
 // the status word and `abort` are set). The timer's low word wraps after 4.3 s.
 __device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, int* status, volatile int* abort) {
@@ -114,6 +130,13 @@ __device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, in
     }
   }
 }
+
+// The warpgroup's share of the block's registers from here on (a multiple of 8 per thread). The shares of
+// all warpgroups together stay within what the block was launched with.
+template <int N>
+__device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void leave_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
 // a box of rows of one head: 3-D map [rows, heads, 128]
 __device__ __forceinline__ void tma_load_head(void* dst, const CUtensorMap* map, int x, int head, int row, uint64_t* bar) {

@@ -37,10 +37,7 @@ constexpr int kThreads = 32 * kWarps;
 constexpr int kChunk = 16 * kWarps;
 constexpr int kD = kHeadDim;
 
-// 16 or 4 bytes to shared memory, zeros if not `there` (then nothing is read)
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
+// 4 bytes to shared memory, 0 if not `there` (then nothing is read)
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
 }
