@@ -809,17 +809,16 @@ bool encode_rows_map(CUtensorMap* map, const void* base, int n_vehicles, int row
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-bool encode_kv_map(CUtensorMap* map, const void* base, long long rows, int n_heads, long long row_bytes, int element,
-                   int box_rows) {
+bool encode_kv_map(CUtensorMap* map, const void* base, long long rows, int n_heads, long long row_bytes, int box_rows) {
   const EncodeTiledFn fn = encode_fn();
   if (fn == nullptr || rows < 1) return false;
-  const cuuint64_t dims[3] = {128, static_cast<cuuint64_t>(n_heads), static_cast<cuuint64_t>(rows)};
-  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(128 * element), static_cast<cuuint64_t>(row_bytes)};
-  const cuuint32_t box[3] = {static_cast<cuuint32_t>(128 / element), 1, static_cast<cuuint32_t>(box_rows)};
-  const cuuint32_t estr[3] = {1, 1, 1};
-  return fn(map, element == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void*>(base),
-            dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const cuuint64_t dims[4] = {64, static_cast<cuuint64_t>(rows), 2, static_cast<cuuint64_t>(n_heads)};
+  const cuuint64_t strides[3] = {static_cast<cuuint64_t>(row_bytes), 128, 256};
+  const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(box_rows), 2, 1};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, const_cast<void*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace fsx

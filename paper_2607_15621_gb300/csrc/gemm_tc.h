@@ -81,10 +81,9 @@ bool encode_cache_map(CUtensorMap* map, const void* base, uint64_t rows, uint32_
 // TMA map of n_vehicles x rows fp16 rows of n_heads x 128 values, 64-row boxes of one head and vehicle
 // (rows past a vehicle's are filled with zeros)
 bool encode_rows_map(CUtensorMap* map, const void* base, int n_vehicles, int rows, long long row_stride, int n_heads);
-// 3-D map over rows of n_heads x 128 values of `element` bytes (1 or 2), row_bytes apart: a box is
-// `box_rows` rows of one head and 128 bytes of it, 128-byte swizzle
-bool encode_kv_map(CUtensorMap* map, const void* base, long long rows, int n_heads, long long row_bytes, int element,
-                   int box_rows);
+// 4-D map [64 columns, rows, 2 blocks of them, heads] over rows of n_heads x 128 16-bit values, row_bytes apart:
+// a box is `box_rows` rows of one head, block by block, 128-byte swizzle
+bool encode_kv_map(CUtensorMap* map, const void* base, long long rows, int n_heads, long long row_bytes, int box_rows);
 // 2-D fp16 tensor map over an output y[rows, cols] with row stride `ld` elements, 64-column x
 // 32-row boxes, 128-byte swizzle (the store / SwiGLU epilogues' TMA stores)
 bool encode_out_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t ld);

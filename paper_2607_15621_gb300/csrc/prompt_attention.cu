@@ -19,8 +19,12 @@
 // sequence): a masked weight is 0, but 0 times an infinity or NaN is not, so rows past the sequence become
 // zeros, and values that are not finite too; such a value is added to the rows that do see it at the end.
 //
-// Items are taken longest first: block i works on the i-th item in the order of its number of
-// chunks, found by counting (the host knows no lengths).
+// A CTA works through up to 36 items, one CTA per SM: the next item's first loads and scores run under
+// the last one's outputs (an item of its own CTA spent 13,000 cycles before its first chunk and 4,000 after
+// the last; a chunk takes about 2,600). Items go longest first, mirrored from round to round; the rank of an item
+// in the order of chunks is found by counting (the host knows no lengths).
+//
+// Stages are released by the softmax threads (S of chunk j there: K of j and V of j - 1 are free).
 #include "fsx.h"
 #include "gemm_tc.h"
 #include "kernels.h"
@@ -36,75 +40,82 @@ constexpr int kTile = 128;              // query rows of a tile, keys of a chunk
 constexpr int kItemRows = 2 * kTile;
 constexpr int kStages = 5;
 constexpr int kStageBytes = kTile * kD * 2;  // 32 KB
-constexpr int kMmaWarp = 8, kLoadWarp = 9;  // the last two guard
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kQueryWarp = 10;  // then the guard
 constexpr int kThreads = 384;           // three warpgroups: 168 registers a thread at launch
-constexpr int kMaxGuarded = 3;          // 256 rows are at most 256 tokens: their diagonals and the end
+constexpr int kWarps = kThreads / 32;
+constexpr int kMaxRounds = 36;          // items of a CTA
+constexpr int kGuarded = 4;             // ring of guarded chunks: no more than 3 V chunks lie in the stages
 constexpr uint32_t kColS = 0, kColO = 256;
 constexpr int kOffRing = 2 * kStageBytes;  // the two Q tiles lie in front
 constexpr int kOffBar = kOffRing + kStages * kStageBytes;
-// full[5], empty[5], gfull[3], gdone[3], qfull[2], sfull[2], pfull[2][2], odone[2], drain
-constexpr int kNumBars = 27;
-constexpr int kSmem = kOffBar + kNumBars * 8 + 64;
-static_assert(kSmem <= 227 * 1024, "shared memory");
-static_assert(kMaxSequences * 16 <= kStages * kStageBytes, "the lengths lie in the ring before it is used");
+// full[5], empty[5], gfull[4], qfull[2], qempty[2], sfull[2], pfull[2][2], odone[2], oread[2], drain
+constexpr int kNumBars = 29;
+constexpr int kOffItems = kOffBar + kNumBars * 8 + 32;
 
 struct Maps {
   CUtensorMap k, v;
 };
 
+// Rows (token G + head) are counted in 32 bits: 2^31 rows of queries would be 550 GB. Each 64-bit division is some
+// hundred instructions, and the code of all roles has to stay near.
 struct Item {
-  int b;            // sequence, -1: none
-  long long row0;   // first packed row of the item
-  long long q0, k0; // first query row, first key row
+  long long q0, k0;  // first query row, first key row of the sequence
+  uint32_t row0;     // first packed row of the item
   int nq, nk;
+  int n[2];          // chunks of each tile
+  int guard0;        // chunks from here on are seen in part by some row of the item
+  int kvh;           // -1: none
+  int pad;
 };
+constexpr int kSmem = kOffItems + kMaxRounds * static_cast<int>(sizeof(Item));
+static_assert(kSmem <= 227 * 1024, "shared memory");
+static_assert(kMaxSequences * 16 <= kStages * kStageBytes, "the lengths lie in the ring before it is used");
 
 // keys that query token i of (nq, nk) sees
-__device__ __forceinline__ int sees(int causal, int nq, int nk, long long i) {
-  if (!causal) return nk;
-  const long long n = i + 1 + nk - nq;
-  return static_cast<int>(n < 0 ? 0 : (n > nk ? nk : n));
+__device__ __forceinline__ int sees(int causal, int nq, int nk, int i) {
+  return causal ? max(0, min(nk, i + 1 + nk - nq)) : nk;
 }
 
 // items of a sequence with at least c chunks (c = 0: all of them); they are its last ones
-__device__ __forceinline__ int items_from(int causal, int G, int nq, int nk, int c) {
-  const long long rows = static_cast<long long>(nq) * G;
-  const int n = static_cast<int>((rows + kItemRows - 1) / kItemRows);
+__device__ __forceinline__ int items_from(int causal, uint32_t G, int nq, int nk, int c) {
+  const int n = static_cast<int>((nq * G + kItemRows - 1) / kItemRows);
   if (c == 0) return n;
-  const long long key = static_cast<long long>(c - 1) * kTile;  // the first key of chunk c - 1 must be seen
+  const int key = (c - 1) * kTile;  // the first key of chunk c - 1 must be seen
   if (key >= nk) return 0;
-  if (!causal) return n;
-  const long long token = key - (nk - nq);  // the first token that sees it
-  return token <= 0 ? n : n - static_cast<int>((token * G) / kItemRows);
+  const int token = key - (nk - nq);  // the first token that sees it
+  return !causal || token <= 0 ? n : n - static_cast<int>(token * G / kItemRows);
 }
 
-// The item of rank `rank` in the order of decreasing chunks, by one warp. lens: (nq, nk) per sequence.
-__device__ __forceinline__ Item find_item(const PromptArgs& p, const int2* lens, int G, int rank) {
+// The item of rank `rank` by one warp; in the order of decreasing chunks if `ordered`, else by sequence.
+// lens: (nq, nk) per sequence. False: there are not so many.
+__device__ __forceinline__ bool find_item(const PromptArgs& p, const int2* lens, uint32_t G, int rank, bool ordered, Item& it) {
   const int lane = threadIdx.x & 31;
-  auto count = [&](int c) {
-    int n = 0;
-    for (int b = lane; b < p.B; b += 32) n += items_from(p.causal, G, lens[b].x, lens[b].y, c);
-    return static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(n)));
-  };
-  Item it;
-  it.b = -1;
-  if (rank >= count(0)) return it;
-  int lo = 0, hi = static_cast<int>((p.kv_rows + kTile - 1) / kTile) + 1;  // count(lo) > rank >= count(hi)
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (count(mid) > rank) lo = mid;
-    else hi = mid;
+  int level = 0, left = rank;  // among the items with exactly `level` chunks (all of them if not ordered), by sequence
+  if (ordered) {
+    auto count = [&](int c) {
+      int n = 0;
+      for (int b = lane; b < p.B; b += 32) n += items_from(p.causal, G, lens[b].x, lens[b].y, c);
+      return static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(n)));
+    };
+    if (rank >= count(0)) return false;
+    int hi = static_cast<int>((p.kv_rows + kTile - 1) / kTile) + 1;  // count(level) > rank >= count(hi)
+    while (hi - level > 1) {
+      const int mid = (level + hi) >> 1;
+      if (count(mid) > rank) level = mid;
+      else hi = mid;
+    }
+    left -= count(level + 1);
   }
-  int left = rank - count(lo + 1);  // among the items with exactly lo chunks, by sequence
   for (int b0 = 0; b0 < p.B; b0 += 32) {
     const int b = b0 + lane;
     int from = 0, n = 0;
     if (b < p.B) {
-      const int all = items_from(p.causal, G, lens[b].x, lens[b].y, 0);
-      const int ge = items_from(p.causal, G, lens[b].x, lens[b].y, lo);
-      from = all - ge;
-      n = ge - items_from(p.causal, G, lens[b].x, lens[b].y, lo + 1);
-      if (!p.causal) from = 0;
+      n = items_from(p.causal, G, lens[b].x, lens[b].y, 0);
+      if (ordered) {
+        const int ge = items_from(p.causal, G, lens[b].x, lens[b].y, level);
+        from = p.causal ? n - ge : 0;
+        n = ge - items_from(p.causal, G, lens[b].x, lens[b].y, level + 1);
+      }
     }
     int before = n;
 #pragma unroll
@@ -115,49 +126,53 @@ __device__ __forceinline__ Item find_item(const PromptArgs& p, const int2* lens,
     const int total = __shfl_sync(0xffffffffu, before, 31);
     before -= n;
     if (left < total) {
-      const uint32_t mine = __ballot_sync(0xffffffffu, left >= before && left < before + n);
-      const int src = __ffs(mine) - 1;
+      const int src = __ffs(__ballot_sync(0xffffffffu, left >= before && left < before + n)) - 1;
       const int t = from + left - before;
-      it.b = b0 + src;
-      it.row0 = static_cast<long long>(__shfl_sync(0xffffffffu, t, src)) * kItemRows;
-      it.nq = lens[it.b].x;
-      it.nk = lens[it.b].y;
-      it.q0 = p.q_offsets[it.b];
-      it.k0 = p.kv_offsets[it.b];
-      return it;
+      const int found = b0 + src;
+      it.row0 = static_cast<uint32_t>(__shfl_sync(0xffffffffu, t, src)) * kItemRows;
+      it.nq = lens[found].x;
+      it.nk = lens[found].y;
+      it.q0 = p.q_offsets[found];
+      it.k0 = p.kv_offsets[found];
+      const uint32_t rows = it.nq * G;
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t first = it.row0 + i * kTile;
+        it.n[i] = first < rows ? (sees(p.causal, it.nq, it.nk, (min(first + kTile, rows) - 1) / G) + kTile - 1) / kTile : 0;
+      }
+      it.guard0 = sees(p.causal, it.nq, it.nk, it.row0 / G) / kTile;
+      return true;
     }
     left -= total;
   }
-  return it;
+  return false;
 }
 
 template <bool BF>
-__global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p, const __grid_constant__ Maps maps) {
+__global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p, const int rounds, const __grid_constant__ Maps maps) {
   extern __shared__ __align__(1024) unsigned char smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int G = p.n_heads / p.n_kv_heads;
-  const int kvh = static_cast<int>(blockIdx.x % static_cast<unsigned>(p.n_kv_heads));
-  const int rank = static_cast<int>(blockIdx.x / static_cast<unsigned>(p.n_kv_heads));
+  const uint32_t G = static_cast<uint32_t>(p.n_heads) / static_cast<uint32_t>(p.n_kv_heads);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kOffBar);
-  uint64_t* full = bars;         // [5] a stage's chunk is there
+  uint64_t* full = bars;         // [5] a stage's chunk is there (and guarded)
   uint64_t* empty = bars + 5;    // [5] the MMAs that read it are done
-  uint64_t* gfull = bars + 10;   // [3] a V chunk to be guarded has landed
-  uint64_t* gdone = bars + 13;   // [3] and is guarded (waited for in place of `full`)
-  uint64_t* qfull = bars + 16;   // [2] a tile's queries are there
+  uint64_t* gfull = bars + 10;   // [4] a V chunk to be guarded has landed
+  uint64_t* qfull = bars + 14;   // [2] a tile's queries are there
+  uint64_t* qempty = bars + 16;  // [2] every S of the tile's item is done
   uint64_t* sfull = bars + 18;   // [2] S of a chunk in tensor memory
   uint64_t* pfull = bars + 20;   // [2][2] P of half a chunk written over it
-  uint64_t* odone = bars + 24;   // [2] every P V of the tile done
-  uint64_t* drain = bars + 26;   // every MMA done
+  uint64_t* odone = bars + 24;   // [2] every P V of the tile's item done
+  uint64_t* oread = bars + 26;   // [2] and its O read
+  uint64_t* drain = bars + 28;   // every MMA done
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kNumBars);
   volatile int* abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  volatile int* wild = reinterpret_cast<volatile int*>(tmem_slot + 2);  // a guarded value was not finite
-  Item* item_slot = reinterpret_cast<Item*>(smem);  // before the queries
+  volatile int* wild = reinterpret_cast<volatile int*>(tmem_slot + 2);  // [4]: item + 1 with a guarded value that is not finite
+  Item* items = reinterpret_cast<Item*>(smem + kOffItems);
   if ((smem_addr(smem) & 1023u) != 0u) {  // the swizzled operands need a 1024-byte aligned base
     if (tid == 0) set_status(p.status, kStatusDeviceArg);
     return;
   }
 
-  // ---- which item
+  // ---- the CTA's items
   int2* lens = reinterpret_cast<int2*>(smem + kOffRing);
   for (int b = tid; b < p.B; b += kThreads) {
     const long long q0 = p.q_offsets[b], q1 = p.q_offsets[b + 1], k0 = p.kv_offsets[b], k1 = p.kv_offsets[b + 1];
@@ -170,27 +185,31 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
       mbar_init(full + i, 1);
       mbar_init(empty + i, 1);
     }
-    for (int i = 0; i < kMaxGuarded; ++i) {
-      mbar_init(gfull + i, 1);
-      mbar_init(gdone + i, 2);
-    }
+    for (int i = 0; i < kGuarded; ++i) mbar_init(gfull + i, 1);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(qfull + i, 4);
+      mbar_init(qfull + i, 1);
+      mbar_init(qempty + i, 1);
       mbar_init(sfull + i, 1);
       mbar_init(pfull + 2 * i, 4);
       mbar_init(pfull + 2 * i + 1, 4);
       mbar_init(odone + i, 1);
+      mbar_init(oread + i, 4);
     }
     mbar_init(drain, 1);
     *abort = 0;
-    *wild = 0;
+    for (int i = 0; i < 4; ++i) wild[i] = 0;
   }
   __syncthreads();
-  if (warp == 0) {
-    const Item found = find_item(p, lens, G, rank);
-    if (lane == 0) *item_slot = found;
+#pragma unroll 1
+  for (int k = warp; k < rounds; k += kWarps) {
+    const unsigned slot = k * gridDim.x + ((k & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+    Item it{};
+    const int rank = static_cast<int>(slot / static_cast<unsigned>(p.n_kv_heads));
+    it.kvh = find_item(p, lens, G, rank, rounds > 1, it) ? static_cast<int>(slot - rank * static_cast<unsigned>(p.n_kv_heads)) : -1;
+    if (lane == 0) items[k] = it;
   }
   if (warp == kMmaWarp) {
+    __syncwarp();
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_slot)), "r"(512)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -199,162 +218,195 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const Item it = *item_slot;
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(tmem_slot);
-  __syncthreads();  // the queries go where the item lies
-  const long long rows = static_cast<long long>(it.nq) * G;
-  int n[2] = {0, 0};  // chunks of each tile
-  if (it.b >= 0) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const long long first = it.row0 + t * kTile;
-      if (first < rows) {
-        const long long last = min(first + kTile, rows) - 1;
-        n[t] = (sees(p.causal, it.nq, it.nk, last / G) + kTile - 1) / kTile;
-      }
-    }
-  }
-  const int n_all = max(n[0], n[1]);
-  // chunks from here on are seen in part by some row of the item
-  const int guard0 = it.b >= 0 ? sees(p.causal, it.nq, it.nk, it.row0 / G) / kTile : 0;
+  // Counts that run through the CTA's items: c-th chunk of the ring (K0 V0 K1 ...), g-th guarded chunk, and per
+  // tile the chunks and the items with chunks. A barrier's phase is the count of its uses.
 
-  if (it.b < 0) {
-    // nothing: more blocks than items
-  } else if (warp >= kMmaWarp) {
+  if (warp >= kMmaWarp) {
   leave_registers<88>();  // of 3 x 168 a lane at launch; the softmax warpgroups take 2 x 208
   if (warp == kMmaWarp) {
-    // ---------------------------------------------------------------- MMAs
-    if (lane == 0) {
-      const uint32_t id_s = idesc_16(BF, kTile, kTile, false), id_o = idesc_16(BF, kTile, kD, true);
-      const uint32_t ring = smem_addr(smem + kOffRing), q = smem_addr(smem);
-      bool ok = true;
-      // the guarded chunks are the last three V chunks at most: no later chunk takes their stages
-      auto stage_bar = [&](int c, uint32_t& parity) {
-        const bool guarded = (c & 1) && (c >> 1) >= guard0;
-        parity = guarded ? 0 : (c / kStages) & 1;
-        return guarded ? gdone + ((c >> 1) - guard0) : full + c % kStages;
-      };
-      auto test_stage = [&](int c) {
-        uint32_t parity;
-        uint64_t* bar = stage_bar(c, parity);
-        return test_bar(bar, parity);
-      };
-      auto need_stage = [&](int c, uint32_t there) {
-        uint32_t parity;
-        uint64_t* bar = stage_bar(c, parity);
-        ok = ok && (there || wait_or_abort(bar, parity, p.status, abort));
-      };
-      uint32_t k_there = 0, v_there = 0, p_there[2][2] = {{0, 0}, {0, 0}};  // tested already
+    // ---------------------------------------------------------------- MMAs: the whole warp waits, one lane issues
+    const bool leader = elect_lane();
+    const uint32_t id_s = idesc_16(BF, kTile, kTile, false), id_o = idesc_16(BF, kTile, kD, true);
+    const uint32_t ring = smem_addr(smem + kOffRing);
+    // descriptors change by their addresses alone
+    const uint64_t q_desc = sw128_desc(smem_addr(smem)), k_desc = sw128_desc(ring), v_desc = sw128_desc_mn(ring, 16384, 1024);
+    bool ok = true;
+    int c0 = 0;
+    uint32_t done0 = 0, done1 = 0, uses0 = 0, uses1 = 0;  // chunks and items of the tiles before this item
+#pragma unroll 1
+    for (int i = 0; i < rounds && ok; ++i) {
+      const Item it = items[i];
+      if (it.kvh < 0) continue;
+      const int n_all = max(it.n[0], it.n[1]);
 #pragma unroll 1
       for (int j = 0; j <= n_all && ok; ++j) {  // per tile: P V of chunk j - 1, then S of chunk j
-        const uint32_t vb = ring + ((2 * j + 2 * kStages - 1) % kStages) * kStageBytes, kb = ring + ((2 * j) % kStages) * kStageBytes;
-        if (j > 0) need_stage(2 * j - 1, v_there);
-        if (j < n_all) need_stage(2 * j, k_there);
-        v_there = k_there = 0;
-#pragma unroll
+        const int ck = c0 + 2 * j, cv = ck - 1;
+        const uint32_t sk = ck % kStages, sv = sk == 0 ? kStages - 1 : sk - 1;
+        const uint64_t kd = k_desc + sk * (kStageBytes >> 4), vd = v_desc + sv * (kStageBytes >> 4);
+        if (j > 0) ok = wait_or_abort(full + sv, (cv / kStages) & 1, p.status, abort);
+        if (ok && j < n_all) ok = wait_or_abort(full + sk, (ck / kStages) & 1, p.status, abort);
+        if (!ok) break;
+#pragma unroll 1
         for (int t = 0; t < 2; ++t) {
+          const int n = t ? it.n[1] : it.n[0];
+          const uint32_t done = t ? done1 : done0, uses = t ? uses1 : uses0;
           const uint32_t s_at = tmem + kColS + t * kTile, o_at = tmem + kColO + t * kTile;
-          if (!ok) break;
-          if (j > 0 && j <= n[t]) {
-#pragma unroll
+          if (j > 0 && j <= n) {
+            const uint32_t parity = (done + j - 1) & 1;
+            if (j == 1 && uses > 0) ok = wait_or_abort(oread + t, (uses - 1) & 1, p.status, abort);
+            if (!ok) break;
+#pragma unroll 1
             for (int half = 0; half < 2; ++half) {  // the keys' first 64, whose weights are there first
-              ok = p_there[t][half] || wait_or_abort(pfull + 2 * t + half, (j - 1) & 1, p.status, abort);
+              ok = wait_or_abort(pfull + 2 * t + half, parity, p.status, abort);
               if (!ok) break;
               tc_fence_after();
-              if (half == 0 && !p_there[t][1]) p_there[t][1] = test_bar(pfull + 2 * t + 1, (j - 1) & 1);
+              if (leader) {
 #pragma unroll
-              for (int k = 4 * half; k < 4 * half + 4; ++k)
-                umma_f16_ta(o_at, s_at + k * 8, sw128_desc_mn(vb + k * 2048, 16384, 1024), id_o, j > 1 || k > 0 ? 1u : 0u);
+                for (int k = 0; k < 4; ++k)
+                  umma_f16_ta(o_at, s_at + half * 32 + k * 8, vd + (half * 4 + k) * 128, id_o, j > 1 || half > 0 || k > 0 ? 1u : 0u);
+              }
+              __syncwarp();
             }
             if (!ok) break;
-            p_there[t][0] = p_there[t][1] = 0;
-            if (j == n[t]) umma_commit(odone + t);
+            if (leader && j == n) umma_commit(odone + t);
           }
-          if (j < n[t]) {
-            if (j == 0) ok = wait_or_abort(qfull + t, 0, p.status, abort);
+          if (j < n) {
+            if (j == 0) ok = wait_or_abort(qfull + t, uses & 1, p.status, abort);
             if (!ok) break;
             tc_fence_after();
-            // the other tile's weights: of chunk j - 1 for tile 1, of chunk j for tile 0 (there after its S)
-            const int pj = t == 0 ? j - 1 : j;
-            if (pj >= 0 && pj < n[t ^ 1]) {
-              p_there[t ^ 1][0] = test_bar(pfull + 2 * (t ^ 1), pj & 1);
-              p_there[t ^ 1][1] = test_bar(pfull + 2 * (t ^ 1) + 1, pj & 1);
-            }
-            if (t == 1 && j < n_all) {
-              v_there = test_stage(2 * j + 1);
-              if (j + 1 < n_all) k_there = test_stage(2 * j + 2);
-            }
+            const uint64_t qd = q_desc + t * (kStageBytes >> 4);
+            if (leader) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const uint32_t off = (k >> 2) * 16384 + (k & 3) * 32;
-              umma_f16(s_at, sw128_desc(q + t * kStageBytes + off), sw128_desc(kb + off), id_s, k > 0 ? 1u : 0u);
+              for (int k = 0; k < 8; ++k) {
+                const uint32_t off = (k >> 2) * (16384 >> 4) + (k & 3) * 2;
+                umma_f16(s_at, qd + off, kd + off, id_s, k > 0 ? 1u : 0u);
+              }
+              umma_commit(sfull + t);
             }
-            umma_commit(sfull + t);
+            __syncwarp();
           }
         }
-        if (!ok) break;
-        if (j > 0) umma_commit(empty + (2 * j - 1) % kStages);
-        if (j < n_all) umma_commit(empty + (2 * j) % kStages);
       }
-      umma_commit(drain);
-      mbar_wait(drain, 0, p.status);
+      c0 += 2 * n_all;
+      done0 += it.n[0];
+      done1 += it.n[1];
+      uses0 += it.n[0] > 0 ? 1 : 0;
+      uses1 += it.n[1] > 0 ? 1 : 0;
     }
+    if (leader) umma_commit(drain);
     __syncwarp();
+    mbar_wait(drain, 0, p.status);
   } else if (warp == kLoadWarp) {
-    // ---------------------------------------------------------------- loads
+    // ---------------------------------------------------------------- loads of K and V
     if (lane == 0) {
-      int c = 0;
+      int c = 0, g = 0;
+      uint32_t guarded = 0;  // bit 0: the last chunk, bit 1: the one before, ...
       bool ok = true;
 #pragma unroll 1
-      for (; c < 2 * n_all; ++c) {
-        const int s = c % kStages, j = c >> 1;
-        if (c >= kStages) ok = wait_or_abort(empty + s, (c / kStages - 1) & 1, p.status, abort);
-        if (!ok) break;
-        uint64_t* bar = (c & 1) && j >= guard0 ? gfull + (j - guard0) : full + s;
-        unsigned char* dst = smem + kOffRing + s * kStageBytes;
-        const int row = static_cast<int>(it.k0 + static_cast<long long>(j) * kTile);
-        mbar_arrive_expect_tx(bar, kStageBytes);
-        tma_load_head(dst, (c & 1) ? &maps.v : &maps.k, 0, kvh, row, bar);
-        tma_load_head(dst + kStageBytes / 2, (c & 1) ? &maps.v : &maps.k, 64, kvh, row, bar);
+      for (int i = 0; i < rounds && ok; ++i) {
+        const Item it = items[i];
+        if (it.kvh < 0) continue;
+        const int n_all = max(it.n[0], it.n[1]);
+#pragma unroll 1
+        for (int k = 0; k < 2 * n_all; ++k) {
+          const int s = c % kStages, j = k >> 1;
+          if (c >= kStages) ok = wait_or_abort(empty + s, (c / kStages - 1) & 1, p.status, abort);
+          if (!ok) break;
+          const bool guard = (k & 1) && j >= it.guard0;
+          uint64_t* bar = guard ? gfull + g % kGuarded : full + s;
+          mbar_arrive_expect_tx(bar, kStageBytes);
+          tma_load_chunk(smem + kOffRing + s * kStageBytes, (k & 1) ? &maps.v : &maps.k,
+                         static_cast<int>(it.k0 + static_cast<long long>(j) * kTile), it.kvh, bar);
+          guarded = guarded << 1 | (guard ? 1u : 0u);
+          g += guard ? 1 : 0;
+          ++c;
+        }
       }
       if (!ok)  // what is on its way lands before the CTA leaves
-        for (int d = max(0, c - kStages); d < c; ++d) {
-          const int j = d >> 1;
-          if ((d & 1) && j >= guard0) mbar_wait(gfull + (j - guard0), 0, p.status);
-          else mbar_wait(full + d % kStages, (d / kStages) & 1, p.status);
+        for (int d = c - 1; d >= 0 && d >= c - kStages; --d, guarded >>= 1) {
+          if (guarded & 1u) {
+            --g;
+            mbar_wait(gfull + g % kGuarded, (g / kGuarded) & 1, p.status);
+          } else {
+            mbar_wait(full + d % kStages, (d / kStages) & 1, p.status);
+          }
         }
     }
     __syncwarp();
+  } else if (warp == kQueryWarp) {
+    // ---------------------------------------------------------------- loads of Q
+    uint32_t uses[2] = {0, 0};
+    bool ok = true;
+#pragma unroll 1
+    for (int i = 0; i < rounds && ok; ++i) {
+      const Item it = items[i];
+      if (it.kvh < 0) continue;
+      const uint16_t* q = static_cast<const uint16_t*>(p.q);
+      const int u = lane & 15;
+#pragma unroll 1
+      for (int t = 0; t < 2; ++t) {
+        if (it.n[t] == 0) continue;
+        if (uses[t] > 0) ok = wait_or_abort(qempty + t, (uses[t] - 1) & 1, p.status, abort);
+        if (!ok) break;
+        ++uses[t];
+        const uint32_t first = it.row0 + t * kTile;
+        const int valid = min(kTile, static_cast<int>(it.nq * G - first));
+        const uint16_t* from = q + it.q0 * p.q_stride + it.kvh * G * kD + u * 8;
+        const uint32_t dst = smem_addr(smem + t * kStageBytes);
+#pragma unroll 8
+        for (int r = lane >> 4; r < kTile; r += 2) {
+          const bool there = r < valid;
+          const uint32_t row = first + (there ? r : 0), token = row / G;
+          copy16(dst + tile_off(r, u), from + token * p.q_stride + (row - token * G) * kD, there);
+        }
+        cp_async_commit();
+        cp_async_wait<0>();
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(qfull + t);
+      }
+    }
   } else {
     // ---------------------------------------------------------------- guard
+    int c0 = 0, g = 0;
+    bool ok = true;
 #pragma unroll 1
-    for (int j = guard0; j < n_all; ++j) {
-      if (!wait_or_abort(gfull + (j - guard0), 0, p.status, abort)) break;
-      const int s = (2 * j + 1) % kStages;
-      unsigned char* v = smem + kOffRing + s * kStageBytes;
-      const int in_range = it.nk - j * kTile;  // rows of the sequence in this chunk
-      uint32_t bad = 0;
-#pragma unroll 4
-      for (int r = (warp & 1) * 2 + (lane >> 4); r < kTile; r += 4) {
-        uint4* u = reinterpret_cast<uint4*>(v + tile_off(r, lane & 15));
-        if (r >= in_range) {
-          *u = make_uint4(0u, 0u, 0u, 0u);
-        } else {
-          uint4 x = *u;
-          const uint32_t f[4] = {not_finite2<BF>(x.x), not_finite2<BF>(x.y), not_finite2<BF>(x.z), not_finite2<BF>(x.w)};
-          if ((f[0] | f[1] | f[2] | f[3]) != 0u) {
-            bad = 1u;
-            uint32_t y[4] = {x.x, x.y, x.z, x.w};
+    for (int i = 0; i < rounds && ok; ++i) {
+      const Item it = items[i];
+      if (it.kvh < 0) continue;
+      const int n_all = max(it.n[0], it.n[1]);
+#pragma unroll 1
+      for (int j = it.guard0; j < n_all; ++j, ++g) {
+        ok = wait_or_abort(gfull + g % kGuarded, (g / kGuarded) & 1, p.status, abort);
+        if (!ok) break;
+        const int s = (c0 + 2 * j + 1) % kStages;
+        unsigned char* v = smem + kOffRing + s * kStageBytes;
+        const int in_range = it.nk - j * kTile;  // rows of the sequence in this chunk
+        uint32_t bad = 0;
+#pragma unroll 8
+        for (int r = lane >> 4; r < kTile; r += 2) {
+          uint4* u = reinterpret_cast<uint4*>(v + tile_off(r, lane & 15));
+          if (r >= in_range) {
+            *u = make_uint4(0u, 0u, 0u, 0u);
+          } else {
+            const uint4 x = *u;
+            const uint32_t f[4] = {not_finite2<BF>(x.x), not_finite2<BF>(x.y), not_finite2<BF>(x.z), not_finite2<BF>(x.w)};
+            if ((f[0] | f[1] | f[2] | f[3]) != 0u) {
+              bad = 1u;
+              uint32_t y[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] &= ~((f[i] >> 15) * 0xffffu);  // 16-bit lanes of ones where flagged
-            *u = make_uint4(y[0], y[1], y[2], y[3]);
+              for (int k = 0; k < 4; ++k) y[k] &= ~((f[k] >> 15) * 0xffffu);  // 16-bit lanes of ones where flagged
+              *u = make_uint4(y[0], y[1], y[2], y[3]);
+            }
           }
         }
+        if (bad) wild[i & 3] = i + 1;
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(full + s);
       }
-      if (bad) *wild = 1;
-      fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(gdone + (j - guard0));
+      c0 += 2 * n_all;
     }
   }
   } else {
@@ -362,41 +414,37 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
     take_registers<208>();
     const int t = warp >> 2;
     const int r = tid & (kTile - 1);  // this thread's row: tensor-memory lane r
-    const long long first = it.row0 + t * kTile;
-    const int valid = static_cast<int>(max(0ll, min(static_cast<long long>(kTile), rows - first)));
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    unsigned char* qt = smem + t * kStageBytes;
-    const long long token0 = first / G;
-    const uint32_t head0 = static_cast<uint32_t>(first - token0 * G);  // row i of the tile: (head0 + i) / G tokens on
-    {
-      const uint16_t* q = static_cast<const uint16_t*>(p.q);
-      const int u = tid & 15;
-#pragma unroll
-      for (int i = 0; i < kTile / 8; ++i) {  // all on their way at once
-        const int at = ((tid & (kTile - 1)) >> 4) + 8 * i;
-        const bool there = at < valid;
-        const uint32_t g = head0 + (there ? at : 0), on = g / static_cast<uint32_t>(G);
-        copy16(smem_addr(qt + tile_off(at, u)), q + (it.q0 + token0 + on) * p.q_stride + (kvh * G + g - on * G) * kD + u * 8, there);
-      }
-      cp_async_commit();
-      cp_async_wait<0>();
-      fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(qfull + t);
-    }
-    const bool mine = r < valid;
-    const uint32_t my_g = head0 + (mine ? r : 0), my_on = my_g / static_cast<uint32_t>(G);
-    const long long token = token0 + my_on;
-    const int head = kvh * G + static_cast<int>(my_g - my_on * G);
-    const int see = mine ? sees(p.causal, it.nq, it.nk, token) : 0;
-    const int see_all = valid > 0 ? sees(p.causal, it.nq, it.nk, token0) : 0;  // every row of the tile sees these
     const uint32_t scol = tmem + lanes + kColS + t * kTile, ocol = tmem + lanes + kColO + t * kTile;
-    float m = -CUDART_INF_F, l = 0.f;  // in units of log2; m may lag behind the maximum by up to 8
     bool ok = true;
+    int c0 = 0;
+    uint32_t done = 0, uses = 0;
 #pragma unroll 1
-    for (int j = 0; j < n[t]; ++j) {
-      ok = wait_or_abort(sfull + t, j & 1, p.status, abort);
+    for (int i = 0; i < rounds && ok; ++i) {
+    const Item it = items[i];
+    if (it.kvh < 0) continue;
+    const int n_all = max(it.n[0], it.n[1]);
+    const int n = t == 0 ? it.n[0] : it.n[1];
+    // the tile whose S of a chunk, and whose P V of the last one, is issued last frees the stages
+    const bool last_of_all = t == 1 ? n == n_all : it.n[1] < n_all;
+    const uint32_t first = it.row0 + t * kTile;
+    const bool mine = first + r < it.nq * G;
+    const uint32_t row = first + (mine ? r : 0), token = row / G;
+    const int head = it.kvh * G + (row - token * G);
+    const int see = mine ? sees(p.causal, it.nq, it.nk, token) : 0;
+    const int see_all = sees(p.causal, it.nq, it.nk, first / G);  // every row of the tile sees these
+    float m = -CUDART_INF_F, l = 0.f;  // in units of log2; m may lag behind the maximum by up to 8
+#pragma unroll 1
+    for (int j = 0; j < n; ++j) {
+      ok = wait_or_abort(sfull + t, (done + j) & 1, p.status, abort);
       if (!ok) break;
+      if (r == 0) {
+        if (t == 1 || j >= it.n[1]) {
+          if (j > 0) mbar_arrive(empty + (c0 + 2 * j - 1) % kStages);
+          mbar_arrive(empty + (c0 + 2 * j) % kStages);
+        }
+        if (j == n - 1) mbar_arrive(qempty + t);
+      }
       tc_fence_after();
       uint32_t raw[4][32];
 #pragma unroll
@@ -461,17 +509,23 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
       l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     }
     // ---- output
-    if (ok && n[t] > 0) ok = wait_or_abort(odone + t, 0, p.status, abort);
+    if (ok && n > 0) ok = wait_or_abort(odone + t, uses & 1, p.status, abort);
     if (ok) {
+      if (r == 0 && n > 0 && last_of_all) mbar_arrive(empty + (c0 + 2 * n_all - 1) % kStages);
       tc_fence_after();
       const float inv = l == 0.f ? 0.f : 1.f / l;
       uint16_t* out = static_cast<uint16_t*>(p.out) + ((it.q0 + token) * p.n_heads + head) * kD;
 #pragma unroll 1
       for (int c = 0; c < kD; c += 32) {
         uint32_t o[32];
-        if (n[t] > 0) {
+        if (n > 0) {
           tmem_ld32_issue(ocol + c, o);
           tmem_wait_ld32(o);
+          if (c + 32 == kD) {  // O is read
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(oread + t);
+          }
         } else {
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = 0u;
@@ -480,9 +534,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
           float x[32];
 #pragma unroll
           for (int e = 0; e < 32; ++e) x[e] = l == 0.f ? 0.f : __uint_as_float(o[e]) * inv;
-          if (*wild) {  // values that the guards took out, for the rows that see them
-            for (int k = guard0 * kTile; k < see; ++k) {
-              const uint32_t* v = reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(p.v) + (it.k0 + k) * p.kv_stride + kvh * kD + c);
+          if (wild[i & 3] == i + 1) {  // values that the guard took out, for the rows that see them
+            for (int k = it.guard0 * kTile; k < see; ++k) {
+              const uint32_t* v = reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(p.v) + (it.k0 + k) * p.kv_stride + it.kvh * kD + c);
 #pragma unroll
               for (int e = 0; e < 16; ++e) {
                 const uint32_t f = not_finite2<BF>(v[e]);
@@ -502,6 +556,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
       if (mine && p.lse != nullptr)
         p.lse[head * p.q_rows + it.q0 + token] = l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * kLn2;
     }
+    c0 += 2 * n_all;
+    done += n;
+    uses += n > 0 ? 1 : 0;
+    }
   }
 
   tc_fence_before();
@@ -517,18 +575,26 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
 cudaError_t launch_prompt_attention(const PromptArgs& a, int dtype, cudaStream_t stream) {
   const long long G = a.n_heads / a.n_kv_heads;
   // at most this many items: every sequence rounds up once
-  const long long blocks = (a.q_rows * G / kItemRows + a.B) * a.n_kv_heads;
-  if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+  const long long items = (a.q_rows * G / kItemRows + a.B) * a.n_kv_heads;
+  if (items > 0x7fffffffll - 65536 || a.q_rows * G >= 0x7fffffffll - kItemRows) return cudaErrorInvalidConfiguration;
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return e;
+  // one CTA per SM; beyond kMaxRounds items each, further waves of CTAs
+  const long long waves = (items + static_cast<long long>(sms) * kMaxRounds - 1) / (static_cast<long long>(sms) * kMaxRounds);
+  const long long grid = items < waves * sms ? items : waves * sms;
+  int rounds = static_cast<int>((items + grid - 1) / grid);
   Maps maps{};
-  if (a.kv_rows > 0 && (!encode_kv_map(&maps.k, a.k, a.kv_rows, a.n_kv_heads, a.kv_stride * 2, 2, kTile) ||
-                        !encode_kv_map(&maps.v, a.v, a.kv_rows, a.n_kv_heads, a.kv_stride * 2, 2, kTile)))
+  if (a.kv_rows > 0 && (!encode_kv_map(&maps.k, a.k, a.kv_rows, a.n_kv_heads, a.kv_stride * 2, kTile) ||
+                        !encode_kv_map(&maps.v, a.v, a.kv_rows, a.n_kv_heads, a.kv_stride * 2, kTile)))
     return cudaErrorInvalidValue;
   const void* fn = dtype == FSX_BF16 ? reinterpret_cast<const void*>(&prompt_kernel<true>)
                                      : reinterpret_cast<const void*>(&prompt_kernel<false>);
-  const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   if (e != cudaSuccess) return e;
-  void* args[] = {const_cast<PromptArgs*>(&a), &maps};
-  return launch_ex(fn, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), kSmem, stream, false, args);
+  void* args[] = {const_cast<PromptArgs*>(&a), &rounds, &maps};
+  return launch_ex(fn, dim3(static_cast<unsigned>(grid)), dim3(kThreads), kSmem, stream, false, args);
 }
 
 }  // namespace fsx

@@ -149,8 +149,9 @@ __device__ __forceinline__ TreePiece tree_piece(const TreeArgs& p, const TreeSha
   const uint32_t item = rel / static_cast<uint32_t>(x.of);
   x.j = static_cast<int>(rel - item * x.of);
   x.slot = plan.slots[lo] + static_cast<int>(rel) - x.j;
-  x.from = static_cast<int>(static_cast<long long>(x.n) * x.j / x.of);
-  x.to = static_cast<int>(static_cast<long long>(x.n) * (x.j + 1) / x.of);
+  const uint32_t least = static_cast<uint32_t>(x.n) / static_cast<uint32_t>(x.of), more = x.n - least * x.of;
+  x.from = static_cast<int>(x.j * least + min(static_cast<uint32_t>(x.j), more));
+  x.to = static_cast<int>(x.from + least + (static_cast<uint32_t>(x.j) < more ? 1 : 0));
   const uint32_t tile = item / static_cast<uint32_t>(p.n_kv_heads);
   x.kvh = static_cast<int>(item - tile * p.n_kv_heads);
   x.row0 = static_cast<int>(tile) * shape.tile_rows;

@@ -207,68 +207,82 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
   // the c-th K or V chunk of the CTA (K0 V0 K1 ... through all its pieces) lies in slot c mod kSlots
 
   if (warp == kMmaWarp) {
-    // ---------------------------------------------------------------- MMAs
-    if (lane == 0) {
-      const uint32_t id_s = idesc_16(kBf, kTile, kTile, false), id_o = idesc_16(kBf, kTile, kD, true);
-      const uint32_t slots = smem_addr(smem + L::kOffSlots), q = smem_addr(smem);
-      bool ok = true;
-      int c0 = 0, ord = 0;
-      uint32_t p_count[2] = {0, 0};
-      for (long long i = blockIdx.x; i < total && ok; i += step, ++ord) {
-        const Work w = work_of<L::kRows>(p, kShape, plan, i, G);
-        const int lag = w.pair ? 1 : 2;
-        bool fresh = true;
-        for (int j = 0; j < w.chunks + lag && ok; ++j) {
-          for (int t = 0; t < 2 && ok; ++t) {
-            if (!w.pair && t != (j & 1)) continue;
-            const int jp = j - lag;  // P V of chunk jp, then S of chunk j
-            if (jp >= 0) {
-              const int c = c0 + 2 * jp + 1;
-              ok = ok && wait_or_abort(pfull + t, p_count[t] & 1, p.status, abort);
-              ok = ok && wait_or_abort(full + c % kSlots, (c / kSlots) & 1, p.status, abort);
-              if (fresh && ord > 0) ok = ok && wait_or_abort(oread, (ord - 1) & 1, p.status, abort);
-              if (!ok) break;
-              fresh = false;
-              ++p_count[t];
-              tc_fence_after();
-              const uint32_t b = slots + (c % kSlots) * kSlotBytes;
-              const uint32_t a = tmem + kColS + t * kTile, d = tmem + kColO + t * kTile;
-              const int steps = w.has_new && jp == w.chunks - 1 ? kMaxDrafts / 16 : kTile / 16;
-              const bool more = jp >= (w.pair ? 1 : 2);  // not the group's first chunk
-              for (int k = 0; k < steps; ++k)
-                umma_f16_ta(d, a + k * 8, sw128_desc_mn(b + k * 2048, 16384, 1024), id_o, more || k > 0 ? 1u : 0u);
-              if (!w.pair || t == 1) {
+    // ---------------------------------------------------------------- MMAs: the whole warp waits, one lane issues
+    const bool leader = elect_lane();
+    const uint32_t id_s = idesc_16(kBf, kTile, kTile, false), id_o = idesc_16(kBf, kTile, kD, true);
+    const uint32_t slots = smem_addr(smem + L::kOffSlots);
+    const uint64_t q_desc = sw128_desc(smem_addr(smem)), k_desc = sw128_desc(slots), v_desc = sw128_desc_mn(slots, 16384, 1024);
+    bool ok = true;
+    int c0 = 0, ord = 0;
+    uint32_t p_count0 = 0, p_count1 = 0;
+#pragma unroll 1
+    for (long long i = blockIdx.x; i < total && ok; i += step, ++ord) {
+      const Work w = work_of<L::kRows>(p, kShape, plan, i, G);
+      const int lag = w.pair ? 1 : 2;
+      bool fresh = ord > 0;
+#pragma unroll 1
+      for (int j = 0; j < w.chunks + lag && ok; ++j) {
+#pragma unroll 1
+        for (int t = 0; t < 2; ++t) {
+          if (!w.pair && t != (j & 1)) continue;
+          const bool last_tile = !w.pair || t == 1;
+          const uint32_t s_at = tmem + kColS + t * kTile, o_at = tmem + kColO + t * kTile;
+          const int jp = j - lag;  // P V of chunk jp, then S of chunk j
+          if (jp >= 0) {
+            const int c = c0 + 2 * jp + 1;
+            ok = wait_or_abort(pfull + t, (t ? p_count1 : p_count0) & 1, p.status, abort) &&
+                 wait_or_abort(full + c % kSlots, (c / kSlots) & 1, p.status, abort) &&
+                 (!fresh || wait_or_abort(oread, (ord - 1) & 1, p.status, abort));
+            if (!ok) break;
+            fresh = false;
+            if (t) ++p_count1;
+            else ++p_count0;
+            tc_fence_after();
+            const uint64_t vd = v_desc + (c % kSlots) * (kSlotBytes >> 4);
+            const bool more = jp >= lag;  // not the group's first chunk
+            const int steps = w.has_new && jp == w.chunks - 1 ? kMaxDrafts / 64 : kTile / 64;
+            if (leader) {
+#pragma unroll 1
+              for (int h = 0; h < steps; ++h) {  // 64 keys
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                  umma_f16_ta(o_at, s_at + h * 32 + k * 8, vd + (h * 4 + k) * 128, id_o, more || h > 0 || k > 0 ? 1u : 0u);
+              }
+              if (last_tile) {
                 umma_commit(empty + c % kSlots);
                 if (jp == w.chunks - 1) umma_commit(odone);
               }
             }
-            if (j < w.chunks) {
-              const int c = c0 + 2 * j;
-              if (j == 0) ok = ok && wait_or_abort(qfull, ord & 1, p.status, abort);
-              ok = ok && wait_or_abort(full + c % kSlots, (c / kSlots) & 1, p.status, abort);
-              if (!ok) break;
-              tc_fence_after();
-              const uint32_t a = q + (w.pair && t == 1 ? kSlotBytes : 0), b = slots + (c % kSlots) * kSlotBytes;
-              const uint32_t d = tmem + kColS + t * kTile;
+            __syncwarp();
+          }
+          if (j < w.chunks) {
+            const int c = c0 + 2 * j;
+            ok = (j > 0 || wait_or_abort(qfull, ord & 1, p.status, abort)) &&
+                 wait_or_abort(full + c % kSlots, (c / kSlots) & 1, p.status, abort);
+            if (!ok) break;
+            tc_fence_after();
+            const uint64_t qd = q_desc + (w.pair && t == 1 ? kSlotBytes >> 4 : 0), kd = k_desc + (c % kSlots) * (kSlotBytes >> 4);
+            if (leader) {
 #pragma unroll
               for (int k = 0; k < 8; ++k) {
-                const uint32_t off = (k >> 2) * 16384 + (k & 3) * 32;
-                umma_f16(d, sw128_desc(a + off), sw128_desc(b + off), id_s, k > 0 ? 1u : 0u);
+                const uint32_t off = (k >> 2) * (16384 >> 4) + (k & 3) * 2;
+                umma_f16(s_at, qd + off, kd + off, id_s, k > 0 ? 1u : 0u);
               }
               umma_commit(sfull + t);
-              if (!w.pair || t == 1) {
+              if (last_tile) {
                 umma_commit(empty + c % kSlots);
                 if (j == w.chunks - 1) umma_commit(qempty);
               }
             }
+            __syncwarp();
           }
         }
-        c0 += 2 * w.chunks;
       }
-      umma_commit(drain);
-      mbar_wait(drain, 0, p.status);
+      c0 += 2 * w.chunks;
     }
+    if (leader) umma_commit(drain);
     __syncwarp();
+    mbar_wait(drain, 0, p.status);
   } else if (warp >= kProdWarp) {
     // ---------------------------------------------------------------- producers
     const int pt = tid - kProdWarp * 32;
