@@ -13,9 +13,9 @@
 // being there means that P V of chunk j - 1 is done: the running maximum may then be moved and O
 // rescaled (by the softmax threads, only when a maximum grew by more than 2^8) without another wait.
 //
-// Warps 0-3, 4-7: softmax of tile 0, 1 (they also load the queries and write the outputs); warp 8 issues
+// Warps 0-3, 4-7: softmax of tile 0, 1 (they also write the outputs); warp 8 issues
 // MMAs; warp 9 loads K and V chunks by TMA into a ring of five 32 KB stages (K0 V0 K1 V1 ...); warps
-// 10-11 guard the V chunks that some row of the item sees only in part (the diagonal, the end of the
+// 10-11 load the queries and guard the V chunks that some row of the item sees only in part (the diagonal, the end of the
 // sequence): a masked weight is 0, but 0 times an infinity or NaN is not, so rows past the sequence become
 // zeros, and values that are not finite too; such a value is added to the rows that do see it at the end.
 //
@@ -40,7 +40,7 @@ constexpr int kTile = 128;              // query rows of a tile, keys of a chunk
 constexpr int kItemRows = 2 * kTile;
 constexpr int kStages = 5;
 constexpr int kStageBytes = kTile * kD * 2;  // 32 KB
-constexpr int kMmaWarp = 8, kLoadWarp = 9, kQueryWarp = 10;  // then the guard
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kAuxWarp = 10;  // two of them
 constexpr int kThreads = 384;           // three warpgroups: 168 registers a thread at launch
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxRounds = 36;          // items of a CTA
@@ -90,6 +90,12 @@ __device__ __forceinline__ int items_from(int causal, uint32_t G, int nq, int nk
 // lens: (nq, nk) per sequence. False: there are not so many.
 __device__ __forceinline__ bool find_item(const PromptArgs& p, const int2* lens, uint32_t G, int rank, bool ordered, Item& it) {
   const int lane = threadIdx.x & 31;
+  if (p.B == 1 && ordered) {  // the last items have the most chunks
+    const int n = items_from(p.causal, G, lens[0].x, lens[0].y, 0);
+    if (rank >= n) return false;
+    rank = n - 1 - rank;
+    ordered = false;
+  }
   int level = 0, left = rank;  // among the items with exactly `level` chunks (all of them if not ordered), by sequence
   if (ordered) {
     auto count = [&](int c) {
@@ -98,7 +104,9 @@ __device__ __forceinline__ bool find_item(const PromptArgs& p, const int2* lens,
       return static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(n)));
     };
     if (rank >= count(0)) return false;
-    int hi = static_cast<int>((p.kv_rows + kTile - 1) / kTile) + 1;  // count(level) > rank >= count(hi)
+    int most = 0;
+    for (int b = lane; b < p.B; b += 32) most = max(most, lens[b].y);
+    int hi = (__reduce_max_sync(0xffffffffu, most) + kTile - 1) / kTile + 1;  // count(level) > rank >= count(hi)
     while (hi - level > 1) {
       const int mid = (level + hi) >> 1;
       if (count(mid) > rank) level = mid;
@@ -182,12 +190,12 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
   }
   if (tid == 0) {
     for (int i = 0; i < kStages; ++i) {
-      mbar_init(full + i, 1);
-      mbar_init(empty + i, 1);
+      mbar_init(full + i, 2);
+      mbar_init(empty + i, 4);
     }
     for (int i = 0; i < kGuarded; ++i) mbar_init(gfull + i, 1);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(qfull + i, 1);
+      mbar_init(qfull + i, 2);
       mbar_init(qempty + i, 1);
       mbar_init(sfull + i, 1);
       mbar_init(pfull + 2 * i, 4);
@@ -316,6 +324,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
           const bool guard = (k & 1) && j >= it.guard0;
           uint64_t* bar = guard ? gfull + g % kGuarded : full + s;
           mbar_arrive_expect_tx(bar, kStageBytes);
+          if (!guard) mbar_arrive(bar);  // for the two guard warps
           tma_load_chunk(smem + kOffRing + s * kStageBytes, (k & 1) ? &maps.v : &maps.k,
                          static_cast<int>(it.k0 + static_cast<long long>(j) * kTile), it.kvh, bar);
           guarded = guarded << 1 | (guard ? 1u : 0u);
@@ -334,41 +343,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
         }
     }
     __syncwarp();
-  } else if (warp == kQueryWarp) {
-    // ---------------------------------------------------------------- loads of Q
-    uint32_t uses[2] = {0, 0};
-    bool ok = true;
-#pragma unroll 1
-    for (int i = 0; i < rounds && ok; ++i) {
-      const Item it = items[i];
-      if (it.kvh < 0) continue;
-      const uint16_t* q = static_cast<const uint16_t*>(p.q);
-      const int u = lane & 15;
-#pragma unroll 1
-      for (int t = 0; t < 2; ++t) {
-        if (it.n[t] == 0) continue;
-        if (uses[t] > 0) ok = wait_or_abort(qempty + t, (uses[t] - 1) & 1, p.status, abort);
-        if (!ok) break;
-        ++uses[t];
-        const uint32_t first = it.row0 + t * kTile;
-        const int valid = min(kTile, static_cast<int>(it.nq * G - first));
-        const uint16_t* from = q + it.q0 * p.q_stride + it.kvh * G * kD + u * 8;
-        const uint32_t dst = smem_addr(smem + t * kStageBytes);
-#pragma unroll 8
-        for (int r = lane >> 4; r < kTile; r += 2) {
-          const bool there = r < valid;
-          const uint32_t row = first + (there ? r : 0), token = row / G;
-          copy16(dst + tile_off(r, u), from + token * p.q_stride + (row - token * G) * kD, there);
-        }
-        cp_async_commit();
-        cp_async_wait<0>();
-        fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(qfull + t);
-      }
-    }
   } else {
-    // ---------------------------------------------------------------- guard
+    // ---------------------------------------------------------------- queries and guarded chunks, half of the rows a warp
+    const int half = (warp - kAuxWarp) * (kTile / 2), u = lane & 15;
+    uint32_t uses[2] = {0, 0};
     int c0 = 0, g = 0;
     bool ok = true;
 #pragma unroll 1
@@ -376,8 +354,35 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
       const Item it = items[i];
       if (it.kvh < 0) continue;
       const int n_all = max(it.n[0], it.n[1]);
+      const uint16_t* q = static_cast<const uint16_t*>(p.q) + it.q0 * p.q_stride + it.kvh * G * kD + u * 8;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (it.n[t] > 0 && uses[t] > 0) ok = ok && wait_or_abort(qempty + t, (uses[t] - 1) & 1, p.status, abort);
+        if (it.n[t] > 0 && ok) {
+          const uint32_t first = it.row0 + t * kTile, rows = it.nq * G;
+          const uint32_t dst = smem_addr(smem + t * kStageBytes);
+#pragma unroll 8
+          for (int r = half + (lane >> 4); r < half + kTile / 2; r += 2) {
+            const bool there = first + r < rows;
+            const uint32_t row = there ? first + r : first, token = row / G;
+            copy16(dst + tile_off(r, u), q + token * p.q_stride + (row - token * G) * kD, there);
+          }
+        }
+        cp_async_commit();
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (t == 0) cp_async_wait<1>();
+        else cp_async_wait<0>();
+        if (it.n[t] > 0 && ok) {
+          ++uses[t];
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(qfull + t);
+        }
+      }
 #pragma unroll 1
-      for (int j = it.guard0; j < n_all; ++j, ++g) {
+      for (int j = it.guard0; j < n_all && ok; ++j, ++g) {
         ok = wait_or_abort(gfull + g % kGuarded, (g / kGuarded) & 1, p.status, abort);
         if (!ok) break;
         const int s = (c0 + 2 * j + 1) % kStages;
@@ -385,20 +390,16 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
         const int in_range = it.nk - j * kTile;  // rows of the sequence in this chunk
         uint32_t bad = 0;
 #pragma unroll 8
-        for (int r = lane >> 4; r < kTile; r += 2) {
-          uint4* u = reinterpret_cast<uint4*>(v + tile_off(r, lane & 15));
+        for (int r = half + (lane >> 4); r < half + kTile / 2; r += 2) {
+          uint4* at = reinterpret_cast<uint4*>(v + tile_off(r, u));
+          const uint4 x = *at;
+          const uint32_t f[4] = {not_finite2<BF>(x.x), not_finite2<BF>(x.y), not_finite2<BF>(x.z), not_finite2<BF>(x.w)};
           if (r >= in_range) {
-            *u = make_uint4(0u, 0u, 0u, 0u);
-          } else {
-            const uint4 x = *u;
-            const uint32_t f[4] = {not_finite2<BF>(x.x), not_finite2<BF>(x.y), not_finite2<BF>(x.z), not_finite2<BF>(x.w)};
-            if ((f[0] | f[1] | f[2] | f[3]) != 0u) {
-              bad = 1u;
-              uint32_t y[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-              for (int k = 0; k < 4; ++k) y[k] &= ~((f[k] >> 15) * 0xffffu);  // 16-bit lanes of ones where flagged
-              *u = make_uint4(y[0], y[1], y[2], y[3]);
-            }
+            *at = make_uint4(0u, 0u, 0u, 0u);
+          } else if ((f[0] | f[1] | f[2] | f[3]) != 0u) {
+            bad = 1u;  // 16-bit lanes of ones where flagged
+            *at = make_uint4(x.x & ~((f[0] >> 15) * 0xffffu), x.y & ~((f[1] >> 15) * 0xffffu), x.z & ~((f[2] >> 15) * 0xffffu),
+                             x.w & ~((f[3] >> 15) * 0xffffu));
           }
         }
         if (bad) wild[i & 3] = i + 1;
@@ -408,6 +409,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
       }
       c0 += 2 * n_all;
     }
+    cp_async_wait<0>();
   }
   } else {
     // ---------------------------------------------------------------- softmax of tile t
@@ -425,8 +427,6 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
     if (it.kvh < 0) continue;
     const int n_all = max(it.n[0], it.n[1]);
     const int n = t == 0 ? it.n[0] : it.n[1];
-    // the tile whose S of a chunk, and whose P V of the last one, is issued last frees the stages
-    const bool last_of_all = t == 1 ? n == n_all : it.n[1] < n_all;
     const uint32_t first = it.row0 + t * kTile;
     const bool mine = first + r < it.nq * G;
     const uint32_t row = first + (mine ? r : 0), token = row / G;
@@ -438,12 +438,12 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
     for (int j = 0; j < n; ++j) {
       ok = wait_or_abort(sfull + t, (done + j) & 1, p.status, abort);
       if (!ok) break;
-      if (r == 0) {
-        if (t == 1 || j >= it.n[1]) {
+      if (lane == 0) {
+        if (t == 1 || j >= it.n[1]) {  // S of both tiles: K of chunk j and V of j - 1 are free
           if (j > 0) mbar_arrive(empty + (c0 + 2 * j - 1) % kStages);
-          mbar_arrive(empty + (c0 + 2 * j) % kStages);
+          if (j + 1 != it.n[0]) mbar_arrive(empty + (c0 + 2 * j) % kStages);  // tile 0 writes its output through its last one
         }
-        if (j == n - 1) mbar_arrive(qempty + t);
+        if (warp == 4 * t && j == n - 1) mbar_arrive(qempty + t);
       }
       tc_fence_after();
       uint32_t raw[4][32];
@@ -508,33 +508,26 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
       }
       l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     }
-    // ---- output
+    // ---- output: through the stage of the tile's last K (tile 0) or V (tile 1) chunk, so that rows are written whole
     if (ok && n > 0) ok = wait_or_abort(odone + t, uses & 1, p.status, abort);
     if (ok) {
-      if (r == 0 && n > 0 && last_of_all) mbar_arrive(empty + (c0 + 2 * n_all - 1) % kStages);
       tc_fence_after();
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      uint16_t* out = static_cast<uint16_t*>(p.out) + ((it.q0 + token) * p.n_heads + head) * kD;
+      const int stage = (c0 + (t == 0 ? 2 * n - 2 : 2 * n - 1)) % kStages;
+      unsigned char* staged = smem + kOffRing + (n > 0 ? stage : 0) * kStageBytes;
+      const bool found = wild[i & 3] == i + 1;
+      uint16_t* out = static_cast<uint16_t*>(p.out) + (it.q0 * p.n_heads + it.kvh * G) * kD + (lane & 15) * 8;
+      if (n > 0) {
 #pragma unroll 1
-      for (int c = 0; c < kD; c += 32) {
-        uint32_t o[32];
-        if (n > 0) {
+        for (int c = 0; c < kD; c += 32) {
+          uint32_t o[32];
           tmem_ld32_issue(ocol + c, o);
           tmem_wait_ld32(o);
-          if (c + 32 == kD) {  // O is read
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(oread + t);
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = 0u;
-        }
-        if (mine) {
           float x[32];
 #pragma unroll
           for (int e = 0; e < 32; ++e) x[e] = l == 0.f ? 0.f : __uint_as_float(o[e]) * inv;
-          if (wild[i & 3] == i + 1) {  // values that the guard took out, for the rows that see them
+          if (found) {  // values that the guard took out, for the rows that see them
+#pragma unroll 1
             for (int k = it.guard0 * kTile; k < see; ++k) {
               const uint32_t* v = reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(p.v) + (it.k0 + k) * p.kv_stride + it.kvh * kD + c);
 #pragma unroll
@@ -548,9 +541,30 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            *reinterpret_cast<uint4*>(out + c + 8 * e) =
+            *reinterpret_cast<uint4*>(staged + tile_off(r, c / 8 + e)) =
                 make_uint4(pack16<BF>(x[8 * e], x[8 * e + 1]), pack16<BF>(x[8 * e + 2], x[8 * e + 3]),
                            pack16<BF>(x[8 * e + 4], x[8 * e + 5]), pack16<BF>(x[8 * e + 6], x[8 * e + 7]));
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(oread + t);
+      }
+      const uint32_t rows = it.nq * G;
+#pragma unroll 8
+      for (int k = 0; k < 16; ++k) {  // this warp's 32 rows, two at a time
+        const int at = (r & ~31) + 2 * k + (lane >> 4);
+        if (first + at < rows) {
+          const uint32_t to = (first + at) / G;
+          *reinterpret_cast<uint4*>(out + (static_cast<long long>(to) * p.n_heads + (first + at - to * G)) * kD) =
+              n > 0 ? *reinterpret_cast<const uint4*>(staged + tile_off(at, lane & 15)) : make_uint4(0u, 0u, 0u, 0u);
+        }
+      }
+      if (n > 0) {
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(empty + stage);
+          if (t == 0 && it.n[1] < n_all) mbar_arrive(empty + (c0 + 2 * n_all - 1) % kStages);  // there is no tile 1
         }
       }
       if (mine && p.lse != nullptr)
