@@ -155,11 +155,26 @@ __device__ __forceinline__ bool find_item(const PromptArgs& p, const int2* lens,
   return false;
 }
 
+// token and head of the group of a packed row, two rows on at a time; `two`: 2 / G and 2 % G
+struct RowWalk {
+  uint32_t token, head;
+  __device__ __forceinline__ RowWalk(uint32_t row, uint32_t G, uint2) : token(row / G), head(row - token * G) {}
+  __device__ __forceinline__ void next(uint32_t G, uint2 two) {
+    token += two.x;
+    head += two.y;
+    if (head >= G) {
+      head -= G;
+      ++token;
+    }
+  }
+};
+
 template <bool BF>
 __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p, const int rounds, const __grid_constant__ Maps maps) {
   extern __shared__ __align__(1024) unsigned char smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t G = static_cast<uint32_t>(p.n_heads) / static_cast<uint32_t>(p.n_kv_heads);
+  const uint2 two = make_uint2(2 / G, 2 % G);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kOffBar);
   uint64_t* full = bars;         // [5] a stage's chunk is there (and guarded)
   uint64_t* empty = bars + 5;    // [5] the MMAs that read it are done
@@ -359,13 +374,14 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
       for (int t = 0; t < 2; ++t) {
         if (it.n[t] > 0 && uses[t] > 0) ok = ok && wait_or_abort(qempty + t, (uses[t] - 1) & 1, p.status, abort);
         if (it.n[t] > 0 && ok) {
-          const uint32_t first = it.row0 + t * kTile, rows = it.nq * G;
+          const uint32_t rows = it.nq * G;
+          uint32_t row = it.row0 + t * kTile + half + (lane >> 4);
+          RowWalk at(row, G, two);
           const uint32_t dst = smem_addr(smem + t * kStageBytes);
-#pragma unroll 8
-          for (int r = half + (lane >> 4); r < half + kTile / 2; r += 2) {
-            const bool there = first + r < rows;
-            const uint32_t row = there ? first + r : first, token = row / G;
-            copy16(dst + tile_off(r, u), q + token * p.q_stride + (row - token * G) * kD, there);
+#pragma unroll 4
+          for (int r = half + (lane >> 4); r < half + kTile / 2; r += 2, row += 2, at.next(G, two)) {
+            const bool there = row < rows;
+            copy16(dst + tile_off(r, u), q + (there ? at.token * p.q_stride + at.head * kD : 0ll), there);
           }
         }
         cp_async_commit();
@@ -389,7 +405,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
         unsigned char* v = smem + kOffRing + s * kStageBytes;
         const int in_range = it.nk - j * kTile;  // rows of the sequence in this chunk
         uint32_t bad = 0;
-#pragma unroll 8
+#pragma unroll 2
         for (int r = half + (lane >> 4); r < half + kTile / 2; r += 2) {
           uint4* at = reinterpret_cast<uint4*>(v + tile_off(r, u));
           const uint4 x = *at;
@@ -550,14 +566,13 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
         if (lane == 0) mbar_arrive(oread + t);
       }
       const uint32_t rows = it.nq * G;
-#pragma unroll 8
-      for (int k = 0; k < 16; ++k) {  // this warp's 32 rows, two at a time
-        const int at = (r & ~31) + 2 * k + (lane >> 4);
-        if (first + at < rows) {
-          const uint32_t to = (first + at) / G;
-          *reinterpret_cast<uint4*>(out + (static_cast<long long>(to) * p.n_heads + (first + at - to * G)) * kD) =
-              n > 0 ? *reinterpret_cast<const uint4*>(staged + tile_off(at, lane & 15)) : make_uint4(0u, 0u, 0u, 0u);
-        }
+      int r2 = (r & ~31) + (lane >> 4);  // this warp's 32 rows, two at a time
+      RowWalk at(first + r2, G, two);
+#pragma unroll 2
+      for (int k = 0; k < 16; ++k, r2 += 2, at.next(G, two)) {
+        if (first + r2 < rows)
+          *reinterpret_cast<uint4*>(out + (static_cast<long long>(at.token) * p.n_heads + at.head) * kD) =
+              n > 0 ? *reinterpret_cast<const uint4*>(staged + tile_off(r2, lane & 15)) : make_uint4(0u, 0u, 0u, 0u);
       }
       if (n > 0) {
         fence_proxy_async();
