@@ -821,4 +821,16 @@ bool encode_kv_map(CUtensorMap* map, const void* base, long long rows, int n_hea
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool encode_q_map(CUtensorMap* map, const void* base, long long rows, int n_heads, long long row_bytes, int group, int tile) {
+  const EncodeTiledFn fn = encode_fn();
+  if (fn == nullptr || rows < 1) return false;
+  const cuuint64_t dims[4] = {64, static_cast<cuuint64_t>(n_heads), static_cast<cuuint64_t>(rows), 2};
+  const cuuint64_t strides[3] = {256, static_cast<cuuint64_t>(row_bytes), 128};
+  const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(group), static_cast<cuuint32_t>(tile / group), 2};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, const_cast<void*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace fsx

@@ -84,6 +84,9 @@ bool encode_rows_map(CUtensorMap* map, const void* base, int n_vehicles, int row
 // 4-D map [64 columns, rows, 2 blocks of them, heads] over rows of n_heads x 128 16-bit values, row_bytes apart:
 // a box is `box_rows` rows of one head, block by block, 128-byte swizzle
 bool encode_kv_map(CUtensorMap* map, const void* base, long long rows, int n_heads, long long row_bytes, int box_rows);
+// 4-D map [64 columns, heads, rows, 2 blocks] over the same rows: a box is `tile` (row, head) pairs of `group` heads,
+// heads inside, block by block, 128-byte swizzle
+bool encode_q_map(CUtensorMap* map, const void* base, long long rows, int n_heads, long long row_bytes, int group, int tile);
 // 2-D fp16 tensor map over an output y[rows, cols] with row stride `ld` elements, 64-column x
 // 32-row boxes, 128-byte swizzle (the store / SwiGLU epilogues' TMA stores)
 bool encode_out_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t ld);

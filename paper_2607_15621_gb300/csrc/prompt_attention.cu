@@ -54,6 +54,7 @@ constexpr int kOffItems = kOffBar + kNumBars * 8 + 32;
 
 struct Maps {
   CUtensorMap k, v;
+  CUtensorMap q;  // if G divides a tile: [64 columns, heads, rows, 2 blocks], a box is a tile
 };
 
 // Rows (token G + head) are counted in 32 bits: 2^31 rows of queries would be 550 GB. Each 64-bit division is some
@@ -69,7 +70,11 @@ struct Item {
 };
 constexpr int kSmem = kOffItems + kMaxRounds * static_cast<int>(sizeof(Item));
 static_assert(kSmem <= 227 * 1024, "shared memory");
-static_assert(kMaxSequences * 16 <= kStages * kStageBytes, "the lengths lie in the ring before it is used");
+struct Sequence {
+  long long q0, k0;
+  int nq, nk;
+};
+static_assert(kMaxSequences * sizeof(Sequence) <= kStages * kStageBytes, "the sequences lie in the ring before it is used");
 
 // keys that query token i of (nq, nk) sees
 __device__ __forceinline__ int sees(int causal, int nq, int nk, int i) {
@@ -87,11 +92,11 @@ __device__ __forceinline__ int items_from(int causal, uint32_t G, int nq, int nk
 }
 
 // The item of rank `rank` by one warp; in the order of decreasing chunks if `ordered`, else by sequence.
-// lens: (nq, nk) per sequence. False: there are not so many.
-__device__ __forceinline__ bool find_item(const PromptArgs& p, const int2* lens, uint32_t G, int rank, bool ordered, Item& it) {
+// False: there are not so many.
+__device__ __forceinline__ bool find_item(const PromptArgs& p, const Sequence* seqs, uint32_t G, int rank, bool ordered, Item& it) {
   const int lane = threadIdx.x & 31;
   if (p.B == 1 && ordered) {  // the last items have the most chunks
-    const int n = items_from(p.causal, G, lens[0].x, lens[0].y, 0);
+    const int n = items_from(p.causal, G, seqs[0].nq, seqs[0].nk, 0);
     if (rank >= n) return false;
     rank = n - 1 - rank;
     ordered = false;
@@ -100,12 +105,12 @@ __device__ __forceinline__ bool find_item(const PromptArgs& p, const int2* lens,
   if (ordered) {
     auto count = [&](int c) {
       int n = 0;
-      for (int b = lane; b < p.B; b += 32) n += items_from(p.causal, G, lens[b].x, lens[b].y, c);
+      for (int b = lane; b < p.B; b += 32) n += items_from(p.causal, G, seqs[b].nq, seqs[b].nk, c);
       return static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(n)));
     };
     if (rank >= count(0)) return false;
     int most = 0;
-    for (int b = lane; b < p.B; b += 32) most = max(most, lens[b].y);
+    for (int b = lane; b < p.B; b += 32) most = max(most, seqs[b].nk);
     int hi = (__reduce_max_sync(0xffffffffu, most) + kTile - 1) / kTile + 1;  // count(level) > rank >= count(hi)
     while (hi - level > 1) {
       const int mid = (level + hi) >> 1;
@@ -118,11 +123,11 @@ __device__ __forceinline__ bool find_item(const PromptArgs& p, const int2* lens,
     const int b = b0 + lane;
     int from = 0, n = 0;
     if (b < p.B) {
-      n = items_from(p.causal, G, lens[b].x, lens[b].y, 0);
+      n = items_from(p.causal, G, seqs[b].nq, seqs[b].nk, 0);
       if (ordered) {
-        const int ge = items_from(p.causal, G, lens[b].x, lens[b].y, level);
+        const int ge = items_from(p.causal, G, seqs[b].nq, seqs[b].nk, level);
         from = p.causal ? n - ge : 0;
-        n = ge - items_from(p.causal, G, lens[b].x, lens[b].y, level + 1);
+        n = ge - items_from(p.causal, G, seqs[b].nq, seqs[b].nk, level + 1);
       }
     }
     int before = n;
@@ -138,10 +143,10 @@ __device__ __forceinline__ bool find_item(const PromptArgs& p, const int2* lens,
       const int t = from + left - before;
       const int found = b0 + src;
       it.row0 = static_cast<uint32_t>(__shfl_sync(0xffffffffu, t, src)) * kItemRows;
-      it.nq = lens[found].x;
-      it.nk = lens[found].y;
-      it.q0 = p.q_offsets[found];
-      it.k0 = p.kv_offsets[found];
+      it.nq = seqs[found].nq;
+      it.nk = seqs[found].nk;
+      it.q0 = seqs[found].q0;
+      it.k0 = seqs[found].k0;
       const uint32_t rows = it.nq * G;
       for (int i = 0; i < 2; ++i) {
         const uint32_t first = it.row0 + i * kTile;
@@ -196,12 +201,12 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
   }
 
   // ---- the CTA's items
-  int2* lens = reinterpret_cast<int2*>(smem + kOffRing);
+  Sequence* seqs = reinterpret_cast<Sequence*>(smem + kOffRing);
   for (int b = tid; b < p.B; b += kThreads) {
     const long long q0 = p.q_offsets[b], q1 = p.q_offsets[b + 1], k0 = p.kv_offsets[b], k1 = p.kv_offsets[b + 1];
     const bool good = q0 >= 0 && q1 >= q0 && q1 <= p.q_rows && k0 >= 0 && k1 >= k0 && k1 <= p.kv_rows;
     if (!good && blockIdx.x == 0) set_status(p.status, kStatusDeviceArg);
-    lens[b] = good ? make_int2(static_cast<int>(q1 - q0), static_cast<int>(k1 - k0)) : make_int2(0, 0);
+    seqs[b] = good ? Sequence{q0, k0, static_cast<int>(q1 - q0), static_cast<int>(k1 - k0)} : Sequence{0, 0, 0, 0};
   }
   if (tid == 0) {
     for (int i = 0; i < kStages; ++i) {
@@ -228,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
     const unsigned slot = k * gridDim.x + ((k & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
     Item it{};
     const int rank = static_cast<int>(slot / static_cast<unsigned>(p.n_kv_heads));
-    it.kvh = find_item(p, lens, G, rank, rounds > 1, it) ? static_cast<int>(slot - rank * static_cast<unsigned>(p.n_kv_heads)) : -1;
+    it.kvh = find_item(p, seqs, G, rank, rounds > 1, it) ? static_cast<int>(slot - rank * static_cast<unsigned>(p.n_kv_heads)) : -1;
     if (lane == 0) items[k] = it;
   }
   if (warp == kMmaWarp) {
@@ -341,7 +346,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
           mbar_arrive_expect_tx(bar, kStageBytes);
           if (!guard) mbar_arrive(bar);  // for the two guard warps
           tma_load_chunk(smem + kOffRing + s * kStageBytes, (k & 1) ? &maps.v : &maps.k,
-                         static_cast<int>(it.k0 + static_cast<long long>(j) * kTile), it.kvh, bar);
+                         static_cast<int>(it.k0 + static_cast<long long>(j) * kTile), 0, it.kvh, bar);
           guarded = guarded << 1 | (guard ? 1u : 0u);
           g += guard ? 1 : 0;
           ++c;
@@ -360,7 +365,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
     __syncwarp();
   } else {
     // ---------------------------------------------------------------- queries and guarded chunks, half of the rows a warp
-    const int half = (warp - kAuxWarp) * (kTile / 2), u = lane & 15;
+    const int side = warp - kAuxWarp;
+    const bool by_tma = kTile % G == 0;
     uint32_t uses[2] = {0, 0};
     int c0 = 0, g = 0;
     bool ok = true;
@@ -369,32 +375,47 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
       const Item it = items[i];
       if (it.kvh < 0) continue;
       const int n_all = max(it.n[0], it.n[1]);
-      const uint16_t* q = static_cast<const uint16_t*>(p.q) + it.q0 * p.q_stride + it.kvh * G * kD + u * 8;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        if (it.n[t] > 0 && uses[t] > 0) ok = ok && wait_or_abort(qempty + t, (uses[t] - 1) & 1, p.status, abort);
         if (it.n[t] > 0 && ok) {
-          const uint32_t rows = it.nq * G;
-          uint32_t row = it.row0 + t * kTile + half + (lane >> 4);
-          RowWalk at(row, G, two);
-          const uint32_t dst = smem_addr(smem + t * kStageBytes);
-#pragma unroll 4
-          for (int r = half + (lane >> 4); r < half + kTile / 2; r += 2, row += 2, at.next(G, two)) {
-            const bool there = row < rows;
-            copy16(dst + tile_off(r, u), q + (there ? at.token * p.q_stride + at.head * kD : 0ll), there);
+          if (uses[t] > 0) ok = wait_or_abort(qempty + t, (uses[t] - 1) & 1, p.status, abort);
+          if (ok && by_tma) {
+            ++uses[t];
+            if (lane == 0) {
+              if (side == 0) {
+                mbar_arrive_expect_tx(qfull + t, kStageBytes);
+                tma_load_chunk(smem + t * kStageBytes, &maps.q, it.kvh * G, static_cast<int>(it.q0) + (it.row0 + t * kTile) / G, 0, qfull + t);
+              } else {
+                mbar_arrive(qfull + t);
+              }
+            }
+          } else if (ok) {
+            const int half = side * (kTile / 2), u = lane & 15;
+            const uint16_t* q = static_cast<const uint16_t*>(p.q) + it.q0 * p.q_stride + it.kvh * G * kD + u * 8;
+            const uint32_t rows = it.nq * G;
+            uint32_t row = it.row0 + t * kTile + half + (lane >> 4);
+            RowWalk at(row, G, two);
+            const uint32_t dst = smem_addr(smem + t * kStageBytes);
+#pragma unroll 2
+            for (int r = half + (lane >> 4); r < half + kTile / 2; r += 2, row += 2, at.next(G, two)) {
+              const bool there = row < rows;
+              copy16(dst + tile_off(r, u), q + (there ? at.token * p.q_stride + at.head * kD : 0ll), there);
+            }
           }
         }
         cp_async_commit();
       }
+      if (!by_tma) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        if (t == 0) cp_async_wait<1>();
-        else cp_async_wait<0>();
-        if (it.n[t] > 0 && ok) {
-          ++uses[t];
-          fence_proxy_async();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(qfull + t);
+        for (int t = 0; t < 2; ++t) {
+          if (t == 0) cp_async_wait<1>();
+          else cp_async_wait<0>();
+          if (it.n[t] > 0 && ok) {
+            ++uses[t];
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(qfull + t);
+          }
         }
       }
 #pragma unroll 1
@@ -404,21 +425,32 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
         const int s = (c0 + 2 * j + 1) % kStages;
         unsigned char* v = smem + kOffRing + s * kStageBytes;
         const int in_range = it.nk - j * kTile;  // rows of the sequence in this chunk
-        uint32_t bad = 0;
-#pragma unroll 2
-        for (int r = half + (lane >> 4); r < half + kTile / 2; r += 2) {
-          uint4* at = reinterpret_cast<uint4*>(v + tile_off(r, u));
-          const uint4 x = *at;
-          const uint32_t f[4] = {not_finite2<BF>(x.x), not_finite2<BF>(x.y), not_finite2<BF>(x.z), not_finite2<BF>(x.w)};
-          if (r >= in_range) {
-            *at = make_uint4(0u, 0u, 0u, 0u);
-          } else if ((f[0] | f[1] | f[2] | f[3]) != 0u) {
-            bad = 1u;  // 16-bit lanes of ones where flagged
-            *at = make_uint4(x.x & ~((f[0] >> 15) * 0xffffu), x.y & ~((f[1] >> 15) * 0xffffu), x.z & ~((f[2] >> 15) * 0xffffu),
-                             x.w & ~((f[3] >> 15) * 0xffffu));
+        // rows r, r + 8, ... lie 1024 bytes apart; a lane takes unit u of two such columns of rows
+#pragma unroll 1
+        for (int c = 0; c < 2; ++c) {
+          const int r = side * 4 + c * 2 + (lane >> 4);
+          uint4* at = reinterpret_cast<uint4*>(v + tile_off(r, lane & 15));
+          if (in_range < kTile) {  // the end of the sequence
+#pragma unroll 1
+            for (int k = 0; k < kTile / 8; ++k)
+              if (r + 8 * k >= in_range) at[k * 64] = make_uint4(0u, 0u, 0u, 0u);
+          }
+          uint32_t bad = 0;
+#pragma unroll 8
+          for (int k = 0; k < kTile / 8; ++k) {
+            const uint4 x = at[k * 64];
+            bad |= not_finite2<BF>(x.x) | not_finite2<BF>(x.y) | not_finite2<BF>(x.z) | not_finite2<BF>(x.w);
+          }
+          if (bad != 0u) {
+            wild[i & 3] = i + 1;
+#pragma unroll 1
+            for (int k = 0; k < kTile / 8; ++k) {
+              uint32_t* w = reinterpret_cast<uint32_t*>(at + k * 64);
+#pragma unroll 1
+              for (int e = 0; e < 4; ++e) w[e] &= ~((not_finite2<BF>(w[e]) >> 15) * 0xffffu);  // 16-bit lanes of ones where flagged
+            }
           }
         }
-        if (bad) wild[i & 3] = i + 1;
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(full + s);
@@ -426,6 +458,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
       c0 += 2 * n_all;
     }
     cp_async_wait<0>();
+    if (!ok && by_tma && lane == 0)  // queries on their way land before the CTA leaves
+      for (int t = 0; t < 2; ++t)
+        if (uses[t] > 0) mbar_wait(qfull + t, (uses[t] - 1) & 1, p.status);
   }
   } else {
     // ---------------------------------------------------------------- softmax of tile t
@@ -541,7 +576,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
           tmem_wait_ld32(o);
           float x[32];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) x[e] = l == 0.f ? 0.f : __uint_as_float(o[e]) * inv;
+          for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(o[e]) * inv;  // zeros where no weight is
           if (found) {  // values that the guard took out, for the rows that see them
 #pragma unroll 1
             for (int k = it.guard0 * kTile; k < see; ++k) {
@@ -565,14 +600,22 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
         __syncwarp();
         if (lane == 0) mbar_arrive(oread + t);
       }
-      const uint32_t rows = it.nq * G;
+      const int rows = static_cast<int>(it.nq * G - first);
       int r2 = (r & ~31) + (lane >> 4);  // this warp's 32 rows, two at a time
       RowWalk at(first + r2, G, two);
+      out += (static_cast<long long>(at.token) * p.n_heads + at.head) * kD;
+      const int step = (two.x * p.n_heads + two.y) * kD, wrap = (p.n_heads - static_cast<int>(G)) * kD;
 #pragma unroll 2
-      for (int k = 0; k < 16; ++k, r2 += 2, at.next(G, two)) {
-        if (first + r2 < rows)
-          *reinterpret_cast<uint4*>(out + (static_cast<long long>(at.token) * p.n_heads + at.head) * kD) =
+      for (int k = 0; k < 16; ++k, r2 += 2) {
+        if (r2 < rows)
+          *reinterpret_cast<uint4*>(out) =
               n > 0 ? *reinterpret_cast<const uint4*>(staged + tile_off(r2, lane & 15)) : make_uint4(0u, 0u, 0u, 0u);
+        out += step;
+        at.head += two.y;
+        if (at.head >= G) {
+          at.head -= G;
+          out += wrap;
+        }
       }
       if (n > 0) {
         fence_proxy_async();
@@ -615,6 +658,8 @@ cudaError_t launch_prompt_attention(const PromptArgs& a, int dtype, cudaStream_t
   const long long grid = items < waves * sms ? items : waves * sms;
   int rounds = static_cast<int>((items + grid - 1) / grid);
   Maps maps{};
+  if (kTile % G == 0 && !encode_q_map(&maps.q, a.q, a.q_rows, a.n_heads, a.q_stride * 2, static_cast<int>(G), kTile))
+    return cudaErrorInvalidValue;
   if (a.kv_rows > 0 && (!encode_kv_map(&maps.k, a.k, a.kv_rows, a.n_kv_heads, a.kv_stride * 2, kTile) ||
                         !encode_kv_map(&maps.v, a.v, a.kv_rows, a.n_kv_heads, a.kv_stride * 2, kTile)))
     return cudaErrorInvalidValue;

@@ -142,12 +142,13 @@ __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.
 template <int N>
 __device__ __forceinline__ void leave_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
-// rows of one head through a map of encode_kv_map: a tile of two swizzled blocks of 64 columns
-__device__ __forceinline__ void tma_load_chunk(void* dst, const CUtensorMap* map, int row, int head, uint64_t* bar) {
+// a tile of two swizzled blocks of 64 columns through a map of encode_kv_map (row, block 0, head) or encode_q_map
+// (head, row, block 0)
+__device__ __forceinline__ void tma_load_chunk(void* dst, const CUtensorMap* map, int y, int z, int w, uint64_t* bar) {
   asm volatile(
       "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], "
       "[%6];" ::"r"(smem_addr(dst)),
-      "l"(map), "r"(0), "r"(row), "r"(0), "r"(head), "r"(smem_addr(bar))
+      "l"(map), "r"(0), "r"(y), "r"(z), "r"(w), "r"(smem_addr(bar))
       : "memory");
 }
 
