@@ -13,6 +13,10 @@ constexpr int kMaxSequences = 1024;  // B of prompt and tree attention
 constexpr int kMaxGroup = 64;        // query heads per kv head
 constexpr int kMaxDrafts = 64;       // new tokens of a request (one mask word)
 
+// SMs of the current device (0: none); the most dynamic shared memory that launches of `fn` may ask for (launch.cu)
+int sm_count();
+cudaError_t allow_shared_memory(const void* fn, size_t bytes);
+
 struct Cache8Args {
   const void* k;  // rows in or out, kv_stride elements apart
   const void* v;
@@ -74,7 +78,7 @@ struct TreeArgs {
 };
 size_t tree_attention_workspace_bytes(int B, long long new_rows, int n_heads, int n_kv_heads);
 // for many rows per request (tree_tc.cu)
-size_t tree_tc_workspace_bytes(long long new_rows, int n_heads, int n_kv_heads);
+size_t tree_tc_workspace_bytes(int B, long long new_rows, int n_heads, int n_kv_heads);
 cudaError_t launch_tree_tc(const TreeArgs& a, int dtype, bool cache8, cudaStream_t stream);
 cudaError_t launch_tree_attention(const TreeArgs& a, int dtype, bool cache8, cudaStream_t stream);
 

@@ -649,10 +649,8 @@ cudaError_t launch_prompt_attention(const PromptArgs& a, int dtype, cudaStream_t
   // at most this many items: every sequence rounds up once
   const long long items = (a.q_rows * G / kItemRows + a.B) * a.n_kv_heads;
   if (items > 0x7fffffffll - 65536 || a.q_rows * G >= 0x7fffffffll - kItemRows) return cudaErrorInvalidConfiguration;
-  int dev = 0, sms = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  if (e != cudaSuccess) return e;
+  const int sms = sm_count();
+  if (sms == 0) return cudaErrorNoDevice;
   // one CTA per SM; beyond kMaxRounds items each, further waves of CTAs
   const long long waves = (items + static_cast<long long>(sms) * kMaxRounds - 1) / (static_cast<long long>(sms) * kMaxRounds);
   const long long grid = items < waves * sms ? items : waves * sms;
@@ -665,7 +663,7 @@ cudaError_t launch_prompt_attention(const PromptArgs& a, int dtype, cudaStream_t
     return cudaErrorInvalidValue;
   const void* fn = dtype == FSX_BF16 ? reinterpret_cast<const void*>(&prompt_kernel<true>)
                                      : reinterpret_cast<const void*>(&prompt_kernel<false>);
-  e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  const cudaError_t e = allow_shared_memory(fn, kSmem);
   if (e != cudaSuccess) return e;
   void* args[] = {const_cast<PromptArgs*>(&a), &rounds, &maps};
   return launch_ex(fn, dim3(static_cast<unsigned>(grid)), dim3(kThreads), kSmem, stream, false, args);

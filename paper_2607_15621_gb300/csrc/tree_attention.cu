@@ -626,7 +626,7 @@ int tile_count(int B, long long new_rows, int n_heads, int n_kv_heads) {
 
 size_t tree_attention_workspace_bytes(int B, long long new_rows, int n_heads, int n_kv_heads) {
   const int nt = tile_count(B, new_rows, n_heads, n_kv_heads);
-  if (nt == 0) return tree_tc_workspace_bytes(new_rows, n_heads, n_kv_heads);
+  if (nt == 0) return tree_tc_workspace_bytes(B, new_rows, n_heads, n_kv_heads);
   return (kTreeHeader + kTreeCounters) * sizeof(int) + slots_of(nt) * slot_floats(nt) * sizeof(float);
 }
 
@@ -636,10 +636,9 @@ cudaError_t launch_tree_attention(const TreeArgs& a, int dtype, bool cache8, cud
   const Kernel k = dtype == FSX_BF16 ? (cache8 ? kernel_of<true, true>(nt) : kernel_of<true, false>(nt))
                                      : (cache8 ? kernel_of<false, true>(nt) : kernel_of<false, false>(nt));
   const size_t smem = k.smem + tree_plan_bytes(a.B);
-  cudaError_t e = cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-  int dev = 0, sms = 0;
-  if (e == cudaSuccess) e = cudaGetDevice(&dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  const int sms = sm_count();
+  if (sms == 0) return cudaErrorNoDevice;
+  const cudaError_t e = allow_shared_memory(k.fn, smem);
   if (e != cudaSuccess) return e;
   void* args[] = {const_cast<TreeArgs*>(&a)};
   return launch_ex(k.fn, dim3(static_cast<unsigned>(sms * k.ctas)), dim3(kThreads), smem, stream, false, args);

@@ -8,7 +8,7 @@
 // own 128 rows and every chunk; else both on the same rows, one on the even and one on the odd chunks, so that
 // the tensor core always has the other's work while one is at its exponentials; their two results meet at the end.
 //
-// Four producer warps copy the rows of a chunk by 16-byte asynchronous copies, each thread its own units, and wait
+// Eight producer warps, four for K and four for V, copy the rows of a chunk by 16-byte asynchronous copies, each thread its own units, and wait
 // for nobody: 16-bit rows straight into their slot, 8-bit rows into a private stage, from where the thread that copied
 // them turns them into fp16 in the slot. A chunk whose scales are powers of two between 2^-15 and 2^7 (a cache as it is
 // written, unless its values are extreme) becomes its values, exactly; any other keeps its codes, and the softmax
@@ -18,11 +18,14 @@
 // The values of new tokens are looked over on the way: a masked weight is 0, but 0 times an infinity or NaN is not,
 // so these become 0 in the product and are added to the rows that see them at the end.
 //
-// Work is shared out as in tree_schedule.cuh: one warp takes pieces from the queue and describes them in a
-// ring for the other roles; cut items are put together by a second kernel, a warp a row: 256 rows
-// are too many for the one CTA that comes last.
+// Work: items are whole, or cut into pieces of at most `most` chunks that CTAs take from a queue, or the chunks of all
+// items are one line, cut into equal ranges, one per CTA; whichever ends first by the count of rounds, chunks and
+// of starts (a piece's queries and results take about as long as 5 chunks). Pieces keep items apart, which pays where they
+// fill the GPU evenly; ranges leave no SM without work but may hold the end of one item and the start of the next. One
+// warp finds the pieces and describes them in a ring for the other roles. Cut items are put together by a
+// second kernel, a warp a row: 256 rows are too many for the one CTA that comes last.
 //
-// Registers: 512 threads at 128 from launch; softmax warpgroups take 2 x 184, MMA and scheduler 56, producers 88.
+// Registers: 640 threads at 96 from launch; softmax warpgroups take 2 x 104, MMA and scheduler leave 16.
 #include "fsx.h"
 #include "kernels.h"
 #include "llm.h"
@@ -38,11 +41,15 @@ constexpr int kTile = 128;                   // rows of a tile, keys of a chunk
 constexpr int kSlotBytes = kTile * kD * 2;   // 32 KB
 constexpr int kRawBytes = kTile * kD;        // 16 KB of codes
 constexpr int kMmaWarp = 8, kSchedWarp = 9, kProdWarp = 12;
-constexpr int kThreads = 512;
+constexpr int kProds = 256;                  // producer threads
+constexpr int kThreads = 384 + kProds;
 constexpr int kWorkRing = 4;
-constexpr int kWorkUsers = 13;               // warps that read a piece's description: MMA, producers, softmax
+constexpr int kWorkUsers = 17;               // warps that read a piece's description: MMA, producers, softmax
 constexpr uint32_t kColS = 0, kColO = 256;
-constexpr int kPartials = 512;               // slots of the workspace
+constexpr int kMaxGrid = 256;
+constexpr int kPartials = 2 * kMaxGrid;      // slots of the workspace
+constexpr int kLeast = 4;                    // chunks of a range or of a piece of a cut item
+constexpr int kStart = 5;                    // chunks that a piece's start and end cost
 
 // A piece as every role sees it
 struct Work {
@@ -53,7 +60,7 @@ struct Work {
   int from, chunks;  // of this piece
   int pair;          // more than 128 rows: a softmax group per tile; else a group per chunk parity
   int has_new;       // its last chunk holds the new tokens
-  int slot, j, of;
+  int slot, first, j, of;  // piece j of `of`, its slot, and `first` for the join: ~slot of piece 0, or the CTA of its range
 };
 
 template <bool C8, bool WIDE>
@@ -70,11 +77,11 @@ struct Layout {
   static constexpr int kOffFactor = kOffScale + kScaleRing * 2 * kTile * 4;  // C8: [piece parity][row]
   static constexpr int kOffMl = kOffFactor + (C8 ? 2 * kRows * 4 : 0);       // [group][128] (m, l)
   static constexpr int kOffScratch = kOffMl + 2 * kTile * 8;
-  static constexpr int kOffWork = kOffScratch + 32 * 8;
+  static constexpr int kOffWork = kOffScratch + 2 * (kThreads / 32) * 8;
   static constexpr int kOffBar = kOffWork + kWorkRing * static_cast<int>(sizeof(Work));
-  static constexpr int kMisc = kOffBar + 29 * 8;  // tmem, abort, wild[4], vs of the groups [2], plain[4]
-  static constexpr int kPlan = kMisc + 12 * 4;
-  static constexpr int kSmem = kPlan + static_cast<int>(tree_plan_bytes(kMaxSequences));
+  static constexpr int kMisc = kOffBar + 33 * 8;  // tmem, abort, wild[4], vs of the groups [2], plain [4][2]
+  static constexpr int kPlan = (kMisc + 16 * 4 + 7) / 8 * 8;
+  static constexpr int kSmem = kPlan + (kMaxSequences + 1) * 8;
 };
 static_assert(Layout<true, true>::kSmem <= 227 * 1024 && Layout<true, false>::kSmem <= 227 * 1024, "shared memory");
 static_assert(Layout<false, true>::kSmem <= 227 * 1024 && Layout<false, false>::kSmem <= 227 * 1024, "shared memory");
@@ -129,7 +136,141 @@ __device__ __forceinline__ float row_max16(float t) {  // over the 16 lanes that
   return t;
 }
 
-// Workspace behind the header and counters: (first slot, pieces) per (head, new token), then the slots:
+// The line of work: pre[b] pieces (most > 0) or chunks (ranges) of the requests before b, pre[B] of all.
+struct Line {
+  long long* pre;
+  int most;       // chunks of a piece; 0: ranges
+  long long per;  // chunks of a range
+};
+constexpr int kPlans = 5;
+__device__ __forceinline__ int chunks_of(int len) { return (len + kTile - 1) / kTile + 1; }  // the last one: new tokens
+template <int ROWS>
+__device__ __forceinline__ Line line_of(const TreeArgs& p, long long* pre, long long* scratch) {
+  constexpr int kW = kThreads / 32;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int G = p.n_heads / p.n_kv_heads;
+  const int each = (p.B + kThreads - 1) / kThreads, b0 = tid * each, b1 = min(p.B, b0 + each);
+  auto items = [&](const TreeRequest& r) { return static_cast<long long>((r.n * G + ROWS - 1) / ROWS) * p.n_kv_heads; };
+  // sums over the block; `scratch` has room for one value per warp
+  auto block_sum = [&](long long x) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    __syncthreads();
+    if (lane == 0) scratch[warp] = x;
+    __syncthreads();
+    x = 0;
+    for (int w = 0; w < kW; ++w) x += scratch[w];
+    return x;
+  };
+  long long mine = 0, longest = 0;
+  for (int b = b0; b < b1; ++b) {
+    TreeRequest r;
+    if (!tree_request(p, b, r) && blockIdx.x == 0) set_status(p.status, kStatusDeviceArg);
+    mine += items(r) * chunks_of(r.len);
+    if (r.n > 0) longest = max(longest, static_cast<long long>(chunks_of(r.len)));
+  }
+  const long long total = block_sum(mine);
+  __syncthreads();
+  if (lane == 0) scratch[warp] = 0;
+  __syncthreads();
+  atomicMax(reinterpret_cast<unsigned long long*>(scratch), static_cast<unsigned long long>(longest));
+  __syncthreads();
+  longest = scratch[0];
+  const long long grid = gridDim.x;
+  Line line{pre, 0, total < 0x7fffffffll ? (static_cast<uint32_t>(total) + gridDim.x - 1) / gridDim.x : (total + grid - 1) / grid};
+  line.per = max(line.per, static_cast<long long>(kLeast));
+  float best = static_cast<float>(line.per + 2 * kStart);
+  for (int i = 0; i < kPlans; ++i) {  // whole items, then pieces of 1, 1.25, 1.5 and 2 ranges
+    const long long most = i == 0 ? longest : line.per * (i < 4 ? 3 + i : 8) / 4;
+    if (most < 1 || (i > 0 && most >= longest)) continue;
+    long long pieces = 0;
+    for (int b = b0; b < b1; ++b) {
+      TreeRequest r;
+      tree_request(p, b, r);
+      pieces += items(r) * ((chunks_of(r.len) + static_cast<uint32_t>(most) - 1) / static_cast<uint32_t>(most));
+    }
+    pieces = block_sum(pieces);
+    if (pieces == 0 || (i > 0 && pieces > kPartials)) continue;
+    const float rounds = ceilf(static_cast<float>(pieces) / static_cast<float>(grid));
+    const float cost = (rounds - 1.f) * (static_cast<float>(total) / static_cast<float>(pieces) + kStart) + most + kStart;
+    if (cost < best) {
+      best = cost;
+      line.most = static_cast<int>(most);
+    }
+  }
+  mine = 0;
+  for (int b = b0; b < b1; ++b) {
+    TreeRequest r;
+    tree_request(p, b, r);
+    pre[b] = mine;  // within this thread's requests
+    mine += items(r) * (line.most > 0 ? (chunks_of(r.len) + line.most - 1u) / static_cast<uint32_t>(line.most) : chunks_of(r.len));
+  }
+  long long sum = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long up = __shfl_up_sync(0xffffffffu, sum, o);
+    if (lane >= o) sum += up;
+  }
+  __syncthreads();
+  if (lane == 31) scratch[warp] = sum;
+  __syncthreads();
+  sum -= mine;
+  for (int w = 0; w < warp; ++w) sum += scratch[w];
+  for (int b = b0; b < b1; ++b) pre[b] += sum;
+  if (tid == kThreads - 1) pre[p.B] = sum + mine;
+  __syncthreads();
+  return line;
+}
+
+// The piece at `u` of the line; of a range that ends at u1
+template <int ROWS>
+__device__ __forceinline__ Work work_at(const TreeArgs& p, const Line& line, long long u, long long u1, int G) {
+  int lo = 0, hi = p.B;  // pre[lo] <= u < pre[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (line.pre[mid] <= u) lo = mid;
+    else hi = mid;
+  }
+  TreeRequest r;
+  tree_request(p, lo, r);
+  Work w{};
+  w.c0 = r.c0;
+  w.t0 = r.t0;
+  w.len = r.len;
+  w.n = r.n;
+  const int n = chunks_of(r.len);
+  const long long rel = u - line.pre[lo];
+  long long item;
+  if (line.most > 0) {
+    w.of = (n + line.most - 1) / line.most;
+    item = rel / w.of;
+    w.j = static_cast<int>(rel - item * w.of);
+    const int least = n / w.of, more = n - least * w.of;
+    w.from = w.j * least + min(w.j, more);
+    w.chunks = least + (w.j < more ? 1 : 0);
+    w.slot = static_cast<int>(min(u, static_cast<long long>(kPartials - 1)));  // used if the item is cut: then u < kPartials
+    w.first = ~(w.slot - w.j);
+  } else {
+    item = rel / n;
+    w.from = static_cast<int>(rel - item * n);
+    const long long start = u - w.from, end = start + n;
+    w.chunks = static_cast<int>(min(end, u1) - u);
+    w.first = static_cast<int>(start / line.per);
+    w.j = static_cast<int>(u / line.per) - w.first;
+    w.of = static_cast<int>((end - 1) / line.per) - w.first + 1;
+    w.slot = 2 * (w.first + w.j) + (w.j == 0 ? 1 : 0);
+  }
+  w.kvh = static_cast<int>(item % p.n_kv_heads);
+  w.row0 = static_cast<int>(item / p.n_kv_heads) * ROWS;
+  w.rows = min(ROWS, r.n * G - w.row0);
+  w.pair = w.rows > kTile;
+  w.has_new = w.from + w.chunks == n;
+  return w;
+}
+// slot of piece j of an item: at most one cut item begins in a range (slot 2 cta + 1) and one ends there (2 cta)
+__device__ __forceinline__ int slot_of(int first, int j) { return first < 0 ? ~first + j : 2 * (first + j) + (j == 0 ? 1 : 0); }
+
+// Workspace behind the header and counters: (Work::first, pieces) per (head, new token), then the slots:
 // [rows][128] sums, [rows] (maximum, sum of weights)
 __host__ __device__ constexpr size_t slot_floats(int rows) { return static_cast<size_t>(rows) * (kD + 2); }
 __device__ __forceinline__ int2* table_of(const TreeArgs& p) {
@@ -147,13 +288,16 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
   using L = Layout<C8, WIDE>;
   constexpr bool kBf = BF && !C8;  // type of the operands
   constexpr int kSlots = L::kSlots;
-  constexpr TreeShape kShape{L::kRows, kTile, 8, 64, kPartials};
   extern __shared__ __align__(1024) unsigned char smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t G = static_cast<uint32_t>(p.n_heads) / static_cast<uint32_t>(p.n_kv_heads);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kOffBar);
-  uint64_t* full = bars;          // [6] a slot's rows are there
-  uint64_t* empty = bars + 6;     // [6] the MMAs that read it are done
+  // Per chunk, in rings of 4 (chunk n of the CTA: entry n mod 4, phase n / 4): every barrier is filled by one role and
+  // waited for by each role that waits chunk after chunk, which is never 4 chunks behind.
+  uint64_t* kfull = bars;         // K is there
+  uint64_t* vfull = bars + 4;     // V is there
+  uint64_t* sdone = bars + 8;     // S of both tiles done with K
+  uint64_t* pdone = bars + 29;    // P V of both tiles done with V
   uint64_t* qfull = bars + 12;    // an item's queries are there
   uint64_t* qempty = bars + 13;   // the softmax warps are done with the piece and with their place
   uint64_t* sfull = bars + 14;    // [2] S of a chunk in tensor memory
@@ -167,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
   volatile int* abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* wild = reinterpret_cast<volatile int*>(tmem_slot + 2);  // [4]: piece ordinal + 1 with values taken out
   volatile float* group_vs = reinterpret_cast<volatile float*>(tmem_slot + 6);  // [2]
-  volatile int* plain_of = reinterpret_cast<volatile int*>(tmem_slot + 8);      // [4]: no scales left in the chunk
+  volatile int* plain_of = reinterpret_cast<volatile int*>(tmem_slot + 8);      // [4][k, v]: no scales left in the chunk
   Work* works = reinterpret_cast<Work*>(smem + L::kOffWork);
   float* scales = reinterpret_cast<float*>(smem + L::kOffScale);
   float* row_factor = reinterpret_cast<float*>(smem + L::kOffFactor);
@@ -179,11 +323,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
     return;
   }
   if (tid == 0) {
-    for (int i = 0; i < 6; ++i) {
-      mbar_init(full + i, 128);
-      mbar_init(empty + i, 1);
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(kfull + i, kProds / 2);
+      mbar_init(vfull + i, kProds / 2);
+      mbar_init(sdone + i, 1);
+      mbar_init(pdone + i, 1);
     }
-    mbar_init(qfull, 128);
+    mbar_init(qfull, kProds);
     mbar_init(qempty, 8);
     for (int i = 0; i < 2; ++i) {
       mbar_init(sfull + i, 1);
@@ -204,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  const TreePlan plan = tree_plan<kThreads>(p, kShape, smem + L::kPlan, scratch);
+  const Line line = line_of<L::kRows>(p, reinterpret_cast<long long*>(smem + L::kPlan), scratch);
   fence_proxy_async();
   tc_fence_before();
   __syncthreads();
@@ -218,44 +364,32 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
     __syncwarp();
     if (lane == 0) mbar_arrive(wempty + ord % kWorkRing);
   };
-  // the c-th K or V chunk of the CTA (K0 V0 K1 ... through all its pieces) lies in slot c mod kSlots
+  // K of the CTA's chunk n lies in slot 2 n mod kSlots, V in slot 2 n + 1 mod kSlots
+  auto wait_chunk = [&](uint64_t* ring, int n) { return wait_or_abort(ring + (n & 3), (n >> 2) & 1, p.status, abort); };
 
   if (warp >= kMmaWarp && warp < kProdWarp) {
-  leave_registers<56>();
+  leave_registers<80>();
   if (warp == kSchedWarp) {
     // ---------------------------------------------------------------- pieces
     int* header = static_cast<int*>(p.workspace);
-    const long long total = plan.pieces[p.B];
-    long long i = blockIdx.x;
+    const long long total = line.pre[p.B];
+    const bool queue = line.most > 0;
+    long long u = queue ? blockIdx.x : blockIdx.x * line.per;
+    const long long u1 = queue ? total : min(total, u + line.per);
 #pragma unroll 1
     for (int ord = 0;; ++ord) {
       if (ord >= kWorkRing && !wait_or_abort(wempty + ord % kWorkRing, (ord / kWorkRing - 1) & 1, p.status, abort)) break;
       if (lane == 0) {
         Work w{};
         w.kvh = -1;
-        if (i < total) {
-          const TreePiece x = tree_piece(p, kShape, plan, i);
-          w.c0 = x.r.c0;
-          w.t0 = x.r.t0;
-          w.len = x.r.len;
-          w.n = x.r.n;
-          w.kvh = x.kvh;
-          w.row0 = x.row0;
-          w.rows = min(L::kRows, x.r.n * static_cast<int>(G) - x.row0);
-          w.from = x.from;
-          w.chunks = x.to - x.from;
-          w.pair = w.rows > kTile;
-          w.has_new = x.to == x.n;
-          w.slot = x.slot;
-          w.j = x.j;
-          w.of = x.of;
-        }
+        if (u < u1) w = work_at<L::kRows>(p, line, u, u1, static_cast<int>(G));
         works[ord % kWorkRing] = w;
         mbar_arrive(wfull + ord % kWorkRing);
+        if (u < u1) u = queue ? gridDim.x + static_cast<long long>(atomicAdd(reinterpret_cast<unsigned*>(header), 1u)) : u + w.chunks;
+        else u = -1;
       }
-      if (i >= total) break;
-      if (lane == 0) i = gridDim.x + static_cast<long long>(atomicAdd(reinterpret_cast<unsigned*>(header), 1u));
-      i = __shfl_sync(0xffffffffu, i, 0);
+      u = __shfl_sync(0xffffffffu, u, 0);
+      if (u < 0) break;
     }
     if (lane == 0 && atomicAdd(reinterpret_cast<unsigned*>(header) + 1, 1u) == gridDim.x - 1) {
       header[0] = 0;  // every CTA has taken its last piece
@@ -269,7 +403,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
     const uint32_t slots = smem_addr(smem + L::kOffSlots);
     const uint64_t q_desc = sw128_desc(smem_addr(smem)), k_desc = sw128_desc(slots), v_desc = sw128_desc_mn(slots, 16384, 1024);
     bool ok = true;
-    int c0 = 0, ord = 0;
+    int n0 = 0, ord = 0;
     uint32_t p_count0 = 0, p_count1 = 0;
 #pragma unroll 1
     for (; ok; ++ord) {
@@ -286,16 +420,15 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
           const uint32_t s_at = tmem + kColS + t * kTile, o_at = tmem + kColO + t * kTile;
           const int jp = j - lag;  // P V of chunk jp, then S of chunk j
           if (jp >= 0) {
-            const int c = c0 + 2 * jp + 1;
-            ok = wait_or_abort(pfull + t, (t ? p_count1 : p_count0) & 1, p.status, abort) &&
-                 wait_or_abort(full + c % kSlots, (c / kSlots) & 1, p.status, abort) &&
+            const int n = n0 + jp;
+            ok = wait_or_abort(pfull + t, (t ? p_count1 : p_count0) & 1, p.status, abort) && wait_chunk(vfull, n) &&
                  (!fresh || wait_or_abort(oread, (ord - 1) & 1, p.status, abort));
             if (!ok) break;
             fresh = false;
             if (t) ++p_count1;
             else ++p_count0;
             tc_fence_after();
-            const uint64_t vd = v_desc + (c % kSlots) * (kSlotBytes >> 4);
+            const uint64_t vd = v_desc + ((2 * n + 1) % kSlots) * (kSlotBytes >> 4);
             const bool more = jp >= lag;  // not the group's first chunk
             const int steps = w.has_new && jp == w.chunks - 1 ? kMaxDrafts / 64 : kTile / 64;
             if (leader) {
@@ -306,19 +439,18 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
                   umma_f16_ta(o_at, s_at + h * 32 + k * 8, vd + (h * 4 + k) * 128, id_o, more || h > 0 || k > 0 ? 1u : 0u);
               }
               if (last_tile) {
-                umma_commit(empty + c % kSlots);
+                umma_commit(pdone + (n & 3));
                 if (jp == w.chunks - 1) umma_commit(odone);
               }
             }
             __syncwarp();
           }
           if (j < w.chunks) {
-            const int c = c0 + 2 * j;
-            ok = (j > 0 || wait_or_abort(qfull, ord & 1, p.status, abort)) &&
-                 wait_or_abort(full + c % kSlots, (c / kSlots) & 1, p.status, abort);
+            const int n = n0 + j;
+            ok = (j > 0 || wait_or_abort(qfull, ord & 1, p.status, abort)) && wait_chunk(kfull, n);
             if (!ok) break;
             tc_fence_after();
-            const uint64_t qd = q_desc + (w.pair && t == 1 ? kSlotBytes >> 4 : 0), kd = k_desc + (c % kSlots) * (kSlotBytes >> 4);
+            const uint64_t qd = q_desc + (w.pair && t == 1 ? kSlotBytes >> 4 : 0), kd = k_desc + ((2 * n) % kSlots) * (kSlotBytes >> 4);
             if (leader) {
 #pragma unroll
               for (int k = 0; k < 8; ++k) {
@@ -326,13 +458,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
                 umma_f16(s_at, qd + off, kd + off, id_s, k > 0 ? 1u : 0u);
               }
               umma_commit(sfull + t);
-              if (last_tile) umma_commit(empty + c % kSlots);
+              if (last_tile) umma_commit(sdone + (n & 3));
             }
             __syncwarp();
           }
         }
       }
-      c0 += 2 * w.chunks;
+      n0 += w.chunks;
       give_back(ord);
     }
     if (leader) umma_commit(drain);
@@ -341,23 +473,32 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
   }
   } else if (warp >= kProdWarp) {
     // ---------------------------------------------------------------- producers
-    leave_registers<88>();
-    // A thread's units of a K or V chunk: 16-bit rows, unit u of rows r0, r0 + 8, ...; codes, units q and q + 4 of rows
-    // r0, r0 + 32, ...: four lanes a row, so that the 8 lanes whose fp16 units are stored together have rows of both
-    // parities and meet no bank twice.
-    const int pt = tid - kProdWarp * 32;
+    // Four warps make the K chunks ready, four the V chunks. A thread's units: of 16-bit rows, unit u of rows r0, r0 + 8,
+    // ...; of codes, which are copied and converted 64 rows at a time, units u and u + 4 of rows r0 and r0 + 32: four
+    // lanes a row, so that the 8 lanes whose fp16 units are stored together have rows of both parities and meet no
+    // bank twice.
+    const int is_v = (warp - kProdWarp) >> 2;
+    const int pt = tid & 127;
     const int u = C8 ? pt & 3 : pt & 15, r0 = C8 ? pt >> 2 : pt >> 4;
-    constexpr int kRowStep = C8 ? 32 : 8;
-    constexpr int kAhead = C8 ? L::kRaw - 1 : kSlots - 2;  // K or V chunks copied ahead of the one that is made ready
-    constexpr int kRaws = L::kRaw > 0 ? L::kRaw : 1;
+    constexpr int kCopyRows = C8 ? 64 : kTile;  // rows of one copy
+    constexpr int kAhead = C8 ? 2 : 1;          // copies under way beside the one that is made ready
+    constexpr int kSteps = kTile / kCopyRows;
     const long long row_bytes = static_cast<long long>(p.n_kv_heads) * kD * (C8 ? 1 : 2);
-    const long long row_step = kRowStep * row_bytes;
     unsigned char* slots = smem + L::kOffSlots;
-    unsigned char* raw = smem + L::kOffRaw;
+    unsigned char* raw = smem + L::kOffRaw + is_v * (3 * kRawBytes / 2) + pt * 16;  // three copies of 8 KB each
+    const unsigned char* cache = static_cast<const unsigned char*>(is_v ? p.v_cache : p.k_cache) + u * 16;
+    const float* scale_of = is_v ? p.v_scale : p.k_scale;
+    const uint16_t* fresh = static_cast<const uint16_t*>(is_v ? p.v_new : p.k_new);
     bool ok = true;
-    // the next K or V chunk to copy: `ci` of piece `iord`, which is up to two pieces ahead of the one made ready
-    int iord = 0, ci = 0, issued = 0, left = 0;  // left: rows from this thread's first row of the chunk to the end
-    const unsigned char *src_k = nullptr, *src_v = nullptr;
+    // Chunk n of this tensor takes the slot of the other tensor's or its own chunk kSlots before in the order K0 V0 K1 ...
+    auto wait_slot = [&](int n) {
+      const int before = 2 * n + is_v - kSlots;
+      return before < 0 || wait_chunk(before & 1 ? pdone : sdone, before >> 1);
+    };
+    // the next copy: step `ci` of piece `iord`, which is up to two pieces ahead of the one made ready
+    int iord = 0, ci = 0, cn = 0, left = 0;  // cn: steps of the cache rows; left: rows from this thread's first row on
+    int in = 0, raw_in = 0;                  // chunks and raw stages copied
+    const unsigned char* src = nullptr;
     bool more = false;
     auto begin_copies = [&] {
       more = find_work(iord);
@@ -365,104 +506,95 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
         const Work& x = works[iord % kWorkRing];
         const int key0 = x.from * kTile + r0;
         left = x.len - key0;
-        const long long at = (x.c0 + key0) * row_bytes + (x.kvh * kD * (C8 ? 1 : 2) + u * 16);
-        src_k = static_cast<const unsigned char*>(p.k_cache) + at;
-        src_v = static_cast<const unsigned char*>(p.v_cache) + at;
-      }
-    };
-    begin_copies();
-    // C8: this lane's scales of keys lane, lane + 32, ... of the next chunk that is made ready
-    float ks_now[4], vs_now[4], ks_next[4], vs_next[4];
-    auto load_scales = [&](const Work& x, int j) {
-      const int first = (x.from + j) * kTile + lane;
-      const long long at = x.kvh * p.cache_rows + x.c0 + first;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const bool there = first + 32 * e < x.len;
-        ks_next[e] = there ? __ldg(p.k_scale + at + 32 * e) : 0.f;
-        vs_next[e] = there ? __ldg(p.v_scale + at + 32 * e) : 0.f;
+        src = cache + (x.c0 + key0) * row_bytes + x.kvh * (kD * (C8 ? 1 : 2));
+        cn = (x.chunks - x.has_new) * kSteps;
       }
     };
     auto issue = [&] {
       if (more) {
-        const bool is_v = ci & 1;
-        const Work& x = works[iord % kWorkRing];
-        const bool is_new = x.has_new && (ci >> 1) == x.chunks - 1;
-        const unsigned char* src = is_v ? src_v : src_k;
         if (!C8) {
-          ok = ok && (issued < kSlots || wait_or_abort(empty + issued % kSlots, (issued / kSlots - 1) & 1, p.status, abort));
+          const int c = 2 * in + is_v;
+          ok = ok && wait_slot(in);
           if (ok) {
-            long long step = row_step;
+            const unsigned char* from = src;
+            long long step = 8 * row_bytes;
             int rows = left;
-            if (is_new) {
-              step = kRowStep * p.new_stride * 2;
+            if (ci >= cn) {  // the new tokens
+              const Work& x = works[iord % kWorkRing];
+              step = 8 * p.new_stride * 2;
               rows = x.n - r0;
-              src = static_cast<const unsigned char*>(is_v ? p.v_new : p.k_new) + ((x.t0 + r0) * p.new_stride + x.kvh * kD) * 2 + u * 16;
+              from = reinterpret_cast<const unsigned char*>(fresh + (x.t0 + r0) * p.new_stride + x.kvh * kD + u * 8);
             }
-            const uint32_t dst = smem_addr(slots + (issued % kSlots) * kSlotBytes + tile_off(r0, u));  // rows 8 on lie 1024 bytes on
+            const uint32_t dst = smem_addr(slots + (c % kSlots) * kSlotBytes + tile_off(r0, u));  // rows 8 on lie 1024 bytes on
 #pragma unroll 4
-            for (int m = 0; m < 16; ++m, src += step) copy16(dst + m * 1024, src, kRowStep * m < rows);
+            for (int m = 0; m < 16; ++m, from += step) copy16(dst + m * 1024, from, 8 * m < rows);
           }
-        } else if (!is_new) {
-          const uint32_t dst = smem_addr(raw + (issued % kRaws) * kRawBytes + pt * 16);
-#pragma unroll
-          for (int m = 0; m < 4; ++m, src += row_step) {
-            copy16(dst + m * 4096, src, kRowStep * m < left);
-            copy16(dst + m * 4096 + 2048, src + 64, kRowStep * m < left);
-          }
+          ++in;
+        } else if (ci < cn) {
+          const uint32_t dst = smem_addr(raw) + raw_in * (kRawBytes / 2);
+          const unsigned char* next = src + 32 * row_bytes;
+          copy16(dst, src, left > 0);
+          copy16(dst + 2048, src + 64, left > 0);
+          copy16(dst + 4096, next, left > 32);
+          copy16(dst + 6144, next + 64, left > 32);
         }
-        ++issued;
-        ++ci;
-        if (is_v) {
-          left -= kTile;
-          src_k += kTile * row_bytes;
-          src_v += kTile * row_bytes;
-          if (ci == 2 * x.chunks) {
-            ci = 0;
-            ++iord;
-            begin_copies();
-          }
+        raw_in = raw_in == 2 ? 0 : raw_in + 1;
+        left -= kCopyRows;
+        src += kCopyRows * row_bytes;
+        if (++ci == works[iord % kWorkRing].chunks * kSteps) {
+          ci = 0;
+          ++iord;
+          begin_copies();
         }
       }
       cp_async_commit();
     };
+    // C8: this lane's scales of keys lane, lane + 32, ... of the next chunk that is made ready
+    float sc_next[4];
+    auto load_scales = [&](const Work& x, int j) {
+      const int first = (x.from + j) * kTile + lane;
+      const float* at = scale_of + x.kvh * p.cache_rows + x.c0 + first;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sc_next[e] = first + 32 * e < x.len ? __ldg(at + 32 * e) : 0.f;
+    };
+    begin_copies();
     if (C8 && more) load_scales(works[0], 0);
 #pragma unroll 1
     for (int k = 0; k < kAhead; ++k) issue();
-    bool plain = true;
-    int c = 0, chunk_no = 0;
+    int c = is_v, chunk_no = 0, raw_out = 0;
 #pragma unroll 1
     for (int ord = 0; ok; ++ord) {
       if (!find_work(ord)) break;
       const Work& w = works[ord % kWorkRing];
-      // ---- queries
+      // ---- queries, by both groups
       if (ord > 0) ok = wait_or_abort(qempty, (ord - 1) & 1, p.status, abort);
       if (!ok) break;
       if (C8 && ord > 0) load_scales(w, 0);
       {
-        const int qu = pt & 15;
+        const int qt = tid - kProdWarp * 32, qu = qt & 15;
         const uint16_t* q = static_cast<const uint16_t*>(p.q) + w.t0 * p.q_stride + w.kvh * G * kD + qu * 8;
         const int to = w.pair ? 2 * kTile : kTile;
         if (!C8) {  // all on their way at once
 #pragma unroll 2
-          for (int r = pt >> 4; r < to; r += 8) {
+          for (int r = qt >> 4; r < to; r += 16) {
             const bool there = r < w.rows;
             const uint32_t row = w.row0 + (there ? r : 0), token = row / G;
             copy16(smem_addr(smem + (r >> 7) * kSlotBytes + tile_off(r & 127, qu)), q + token * p.q_stride + (row - token * G) * kD, there);
           }
+          cp_async_commit();  // waited for with the piece's first chunk
         } else {
 #pragma unroll 1
-          for (int r1 = pt >> 4; r1 < to; r1 += 32) {  // four rows at a time
+          for (int r1 = qt >> 4; r1 < to; r1 += 64) {  // four rows at a time
             uint4 x[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const int r = r1 + 8 * e;
+              const int r = r1 + 16 * e;
               const uint32_t row = w.row0 + r, token = row / G;
               x[e] = r < w.rows ? __ldg(reinterpret_cast<const uint4*>(q + token * p.q_stride + (row - token * G) * kD)) : make_uint4(0u, 0u, 0u, 0u);
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const int r = r1 + 8 * e;
+              const int r = r1 + 16 * e;
               float power = 1.f;
               if (BF) {
                 power = row_power(row_max16(top_of(x[e])));
@@ -472,62 +604,53 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
               *reinterpret_cast<uint4*>(smem + (r >> 7) * kSlotBytes + tile_off(r & 127, qu)) = x[e];
             }
           }
-        }
-        if (C8) {
           fence_proxy_async();
           mbar_arrive(qfull);
-        } else {
-          // counted with the chunk copies behind them: ready when the piece's first chunk is
-          cp_async_commit();
         }
       }
       // ---- chunks
+      const int chunks = w.chunks;
 #pragma unroll 1
-      for (int tc = 0; tc < 2 * w.chunks && ok; ++tc, ++c) {
-        const int j = tc >> 1;
-        const bool is_v = tc & 1, is_new = w.has_new && j == w.chunks - 1;
+      for (int j = 0; j < chunks && ok; ++j, ++chunk_no, c += 2) {
+        const bool is_new = w.has_new && j == chunks - 1;
         unsigned char* slot = slots + (c % kSlots) * kSlotBytes;
         if (C8) {
-          issue();  // chunk c + kAhead, into the stage that chunk c - 1 was made ready from
-          ok = c < kSlots || wait_or_abort(empty + c % kSlots, (c / kSlots - 1) & 1, p.status, abort);
+          ok = wait_slot(chunk_no);
           if (!ok) break;
-          float* ks = scales + (chunk_no % kScaleRing) * 2 * kTile;
-          if (!is_v) {
+          float* to_scales = scales + ((chunk_no % kScaleRing) * 2 + is_v) * kTile;
+          if (!is_new) {
             // scales that leave every code exact in fp16: powers of two, 2^-15 <= s <= 2^7 (rows that are not there: 0)
-            plain = true;
+            float sc[4];
+            bool plain = true;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              ks_now[e] = ks_next[e];
-              vs_now[e] = vs_next[e];
-              const uint32_t x = __float_as_uint(ks_now[e]), y = __float_as_uint(vs_now[e]);
-              plain = plain && ((x | y) & 0x7fffffu) == 0u && (x == 0u || x - (112u << 23) <= 22u << 23) &&
-                      (y == 0u || y - (112u << 23) <= 22u << 23);
+              sc[e] = sc_next[e];
+              const uint32_t x = __float_as_uint(sc[e]);
+              plain = plain && (x & 0x7fffffu) == 0u && (x == 0u || x - (112u << 23) <= 22u << 23);
             }
             plain = __all_sync(0xffffffffu, plain);
-          } else if (j + 1 < w.chunks) {
-            load_scales(w, j + 1);
-          }
-          if (!is_new) {
-            if (!is_v && pt < 32) {
-              if (lane == 0) plain_of[chunk_no & 3] = plain ? 1 : 0;
+            if (j + 1 < chunks) load_scales(w, j + 1);
+            if (pt < 32) {
+              if (lane == 0) plain_of[(chunk_no & 3) * 2 + is_v] = plain ? 1 : 0;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                ks[lane + 32 * e] = plain ? 1.f : ks_now[e];
-                ks[kTile + lane + 32 * e] = plain ? 1.f : vs_now[e];
-              }
+              for (int e = 0; e < 4; ++e) to_scales[lane + 32 * e] = plain ? 1.f : sc[e];
             }
-            cp_async_wait<kAhead>();
-            const unsigned char* mine = raw + (c % kRaws) * kRawBytes + pt * 16;
             unsigned char* to = slot + tile_off(r0, 2 * u);  // unit 2 u + 1 at the other place of its pair
             const int other = (r0 & 1) ? -16 : 16;
 #pragma unroll
-            for (int m = 0; m < 4; ++m) {  // rows r0 + 32 m lie 4096 bytes apart; the row's scale is the lane's r0 mod 32
-              const float sc = __shfl_sync(0xffffffffu, is_v ? vs_now[m] : ks_now[m], r0 & 31);
-              const __half2 f = __float2half2_rn(plain ? sc : 1.f);
+            for (int h = 0; h < 2; ++h) {  // 64 rows; the copy issued here goes where those before were made ready from
+              issue();
+              cp_async_wait<kAhead>();
+              const unsigned char* mine = raw + raw_out * (kRawBytes / 2);
+              raw_out = raw_out == 2 ? 0 : raw_out + 1;
+              uint4 x[4];
 #pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const uint4 x = *reinterpret_cast<const uint4*>(mine + m * 4096 + h * 2048);
-                const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+              for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const uint4*>(mine + i * 2048);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {  // unit u + 4 (i & 1) of row r0 + 64 h + 32 (i >> 1): the scale is lane r0's
+                const float s1 = __shfl_sync(0xffffffffu, sc[2 * h + (i >> 1)], r0);
+                const __half2 f = __float2half2_rn(plain ? s1 : 1.f);
+                const uint32_t y[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
                 uint32_t z[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -535,52 +658,42 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
                   const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&code), f);
                   z[e] = *reinterpret_cast<const uint32_t*>(&v);
                 }
-                *reinterpret_cast<uint4*>(to + m * 4096 + h * 16384) = make_uint4(z[0], z[1], z[2], z[3]);
-                *reinterpret_cast<uint4*>(to + m * 4096 + h * 16384 + other) = make_uint4(z[4], z[5], z[6], z[7]);
+                unsigned char* at = to + h * 8192 + (i >> 1) * 4096 + (i & 1) * 16384;
+                *reinterpret_cast<uint4*>(at) = make_uint4(z[0], z[1], z[2], z[3]);
+                *reinterpret_cast<uint4*>(at + other) = make_uint4(z[4], z[5], z[6], z[7]);
               }
             }
           } else {
-            if (!is_v && pt == 0) plain_of[chunk_no & 3] = 0;
+            issue();
+            issue();
+            raw_out = raw_out == 0 ? 2 : raw_out - 1;  // two stages on
+            if (pt == 0) plain_of[(chunk_no & 3) * 2 + is_v] = 0;
             bool found = false;
             const int nu = pt & 15;
+            const uint16_t* from = fresh + w.t0 * p.new_stride + w.kvh * kD + nu * 8;
 #pragma unroll 1
             for (int r = pt >> 4; r < kMaxDrafts; r += 8) {
               const bool there = r < w.n;
-              auto row_of = [&](const void* base) {
-                return there ? __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + (w.t0 + r) * p.new_stride + w.kvh * kD) + nu)
-                             : make_uint4(0u, 0u, 0u, 0u);
-              };
-              uint4 y = row_of(p.v_new);
-              bool wild_here = false;
-              y = take_out_wild<BF>(y, wild_here);
-              float yp = 1.f;
-              if (BF) yp = row_power(row_max16(top_of(y)));
-              if (!is_v) {
-                uint4 x = row_of(p.k_new);
-                float xp = 1.f;
-                if (BF) {
-                  xp = row_power(row_max16(top_of(x)));
-                  x = bf16_to_half(x, inverse_power(xp));
-                }
-                if (nu == 0) {
-                  ks[r] = xp;
-                  ks[kTile + r] = there ? yp : 0.f;
-                  ks[kMaxDrafts + r] = 0.f;
-                  ks[kTile + kMaxDrafts + r] = 0.f;
-                }
-                *reinterpret_cast<uint4*>(slot + tile_off(r, nu)) = x;
-              } else {
-                found = found || wild_here;
-                if (BF) y = bf16_to_half(y, inverse_power(yp));
-                *reinterpret_cast<uint4*>(slot + tile_off(r, nu)) = y;
+              uint4 x = there ? __ldg(reinterpret_cast<const uint4*>(from + r * p.new_stride)) : make_uint4(0u, 0u, 0u, 0u);
+              if (is_v) x = take_out_wild<BF>(x, found);
+              float power = 1.f;
+              if (BF) {
+                power = row_power(row_max16(top_of(x)));
+                x = bf16_to_half(x, inverse_power(power));
               }
+              if (nu == 0) {
+                to_scales[r] = there ? power : 0.f;
+                to_scales[kMaxDrafts + r] = 0.f;
+              }
+              *reinterpret_cast<uint4*>(slot + tile_off(r, nu)) = x;
             }
             if (found) wild[ord & 3] = ord + 1;
           }
         } else {
-          // the piece's queries were committed behind the copies of the first kAhead chunks
-          if (tc < kAhead) cp_async_wait<0>();
-          else cp_async_wait<kAhead - 1>();
+          // the piece's queries were committed behind the copies of its first kAhead chunks
+          issue();
+          if (j < kAhead) cp_async_wait<0>();
+          else cp_async_wait<kAhead>();
           if (is_new && is_v) {
             bool found = false;
 #pragma unroll 1
@@ -595,23 +708,21 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
           }
         }
         fence_proxy_async();
-        if (!C8 && tc == 0) mbar_arrive(qfull);
-        mbar_arrive(full + c % kSlots);
-        if (!C8) issue();
-        if (is_v) ++chunk_no;
+        if (!C8 && j == 0) mbar_arrive(qfull);
+        mbar_arrive((is_v ? vfull : kfull) + (chunk_no & 3));
       }
       give_back(ord);
     }
     cp_async_wait<0>();
   } else {
     // ---------------------------------------------------------------- softmax of group t
-    take_registers<184>();
+    take_registers<104>();
     const int t = warp >> 2;
     const int r = tid & (kTile - 1);
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t scol = tmem + lanes + kColS + t * kTile, ocol = tmem + lanes + kColO;
     bool ok = true;
-    int c0 = 0, chunk0 = 0;
+    int chunk0 = 0;
     uint32_t s_count = 0;
 #pragma unroll 1
     for (int ord = 0; ok; ++ord) {
@@ -639,29 +750,30 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
       for (int j = w.pair ? 0 : t; j < w.chunks && ok; j += w.pair ? 1 : 2) {
         ok = wait_or_abort(sfull + t, s_count & 1, p.status, abort);
         ++s_count;
-        const int cv = c0 + 2 * j + 1;
-        if (C8) ok = ok && wait_or_abort(full + cv % kSlots, (cv / kSlots) & 1, p.status, abort);  // the scales, too
+        // S is there, so K and its scales were; V's scales come with V
+        if (C8) ok = ok && wait_chunk(vfull, chunk0 + j);
         if (!ok) break;
         tc_fence_after();
         const bool is_new = w.has_new && j == w.chunks - 1;
         const int left = w.len - (w.from + j) * kTile;  // cache rows of this chunk
         if (C8) f = row_factor[(ord & 1) * L::kRows + my_row];
-        if (!is_new && left >= kTile && (!C8 || (plain_of[(chunk0 + j) & 3] != 0 && vs <= 1.f))) {
-          // ---- a whole chunk without scales: scores in registers
-          uint32_t raw[4][32];
+        if (!is_new && left >= kTile && (!C8 || ((plain_of[((chunk0 + j) & 3) * 2] & plain_of[((chunk0 + j) & 3) * 2 + 1]) != 0 && vs <= 1.f))) {
+          // ---- a whole chunk without scales
+          float mx[2] = {-CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) tmem_ld32_issue(scol + 32 * i, raw[i]);
+          for (int i = 0; i < 4; i += 2) {
+            uint32_t a[32], b[32];
+            tmem_ld32_issue(scol + 32 * i, a);
+            tmem_ld32_issue(scol + 32 * i + 32, b);
+            tmem_wait_ld32(a);
+            tmem_wait_ld32(b);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) tmem_wait_ld32(raw[i]);
-          float mx[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            mx[i] = __uint_as_float(raw[i][0]);
-#pragma unroll
-            for (int e = 1; e < 31; e += 2) mx[i] = max3(mx[i], __uint_as_float(raw[i][e]), __uint_as_float(raw[i][e + 1]));
-            mx[i] = fmaxf(mx[i], __uint_as_float(raw[i][31]));
+            for (int e = 0; e < 32; e += 2) {
+              mx[0] = max3(mx[0], __uint_as_float(a[e]), __uint_as_float(a[e + 1]));
+              mx[1] = max3(mx[1], __uint_as_float(b[e]), __uint_as_float(b[e + 1]));
+            }
           }
-          const float top = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * f;
+          const float top = fmaxf(mx[0], mx[1]) * f;
           if (__any_sync(0xffffffffu, top > m + 8.f || vs < 1.f)) {
             const float m_new = top > m + 8.f ? top : m;
             const float alpha = m_new == m ? 1.f : exp2_fast(m - m_new);
@@ -672,12 +784,16 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
           }
           const float nm = m == -CUDART_INF_F ? 0.f : -m;
           float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {  // 64 keys: 32 columns of P
-            uint32_t pk[32];
+#pragma unroll 1
+          for (int i = 0; i < 2; ++i) {  // 64 keys: 32 columns of P over S columns that have been read
+            uint32_t raw[2][32], pk[32];
+            tmem_ld32_issue(scol + 64 * i, raw[0]);
+            tmem_ld32_issue(scol + 64 * i + 32, raw[1]);
+            tmem_wait_ld32(raw[0]);
+            tmem_wait_ld32(raw[1]);
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
-              float a = __uint_as_float(raw[2 * i + (e >> 4)][2 * (e & 15)]), b = __uint_as_float(raw[2 * i + (e >> 4)][2 * (e & 15) + 1]);
+              float a = __uint_as_float(raw[e >> 4][2 * (e & 15)]), b = __uint_as_float(raw[e >> 4][2 * (e & 15) + 1]);
               fma2(a, b, f, nm);
               a = exp2_fast(a);
               b = exp2_fast(b);
@@ -810,7 +926,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
       // 32 columns at a time through this warp's 4 KB of the queries' place (all S are done), so that rows are
       // written in 128-byte or, as sums, 64-byte pieces by neighbouring lanes; unit u of row r lies at u ^ (r mod 8)
       float* place = reinterpret_cast<float*>(smem + warp * 4096);
-      float* slot = slots_of(p) + static_cast<size_t>(w.slot + w.j) * slot_floats(L::kRows);
+      float* slot = slots_of(p) + static_cast<size_t>(w.slot) * slot_floats(L::kRows);
       uint16_t* out = static_cast<uint16_t*>(p.out);
       const int d_from = w.pair ? 0 : t * (kD / 2), d_to = w.pair ? kD : d_from + kD / 2;
       const uint32_t own = ocol + (w.pair ? t * kTile : 0);
@@ -876,9 +992,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
         } else {
           __stcg(reinterpret_cast<float2*>(slot + L::kRows * kD) + my_row, make_float2(m, l));
         }
-        if (w.j == 0) table_of(p)[head * p.new_rows + w.t0 + token] = make_int2(w.slot, w.of);
+        if (w.j == 0) table_of(p)[head * p.new_rows + w.t0 + token] = make_int2(w.first, w.of);
       }
-      c0 += 2 * w.chunks;
       chunk0 += w.chunks;
       give_back(ord);
       fence_proxy_async();  // the queries' place goes back to the tensor core
@@ -914,13 +1029,13 @@ __global__ void __launch_bounds__(128) tree_join_kernel(const TreeArgs p) {
   if (t0 < 0) return;
   const int2 entry = table_of(p)[at];
   const int of = entry.y;
-  if (of <= 1 || entry.x < 0 || of > kPartials || entry.x + of > kPartials) return;
+  if (of <= 1 || of > kPartials || slot_of(entry.x, 0) < 0 || slot_of(entry.x, of - 1) >= kPartials) return;
   const int G = p.n_heads / p.n_kv_heads;
   const int row = static_cast<int>((token - t0) * G + head % G) % ROWS;
-  const float* first = slots_of(p) + entry.x * slot_floats(ROWS);
-  const float* ml = first + ROWS * kD + 2 * row;
+  const float* slots = slots_of(p);
+  auto slot = [&](int j) { return slots + slot_of(entry.x, j) * slot_floats(ROWS); };
   float m = -CUDART_INF_F;
-  for (int j = lane; j < of; j += 32) m = fmaxf(m, __ldcg(ml + j * slot_floats(ROWS)));
+  for (int j = lane; j < of; j += 32) m = fmaxf(m, __ldcg(slot(j) + ROWS * kD + 2 * row));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   float l = 0.f;
@@ -929,14 +1044,14 @@ __global__ void __launch_bounds__(128) tree_join_kernel(const TreeArgs p) {
     const int count = min(32, of - j0);
     float w = 0.f;
     if (lane < count) {
-      const float2 x = __ldcg(reinterpret_cast<const float2*>(ml + (j0 + lane) * slot_floats(ROWS)));
+      const float2 x = __ldcg(reinterpret_cast<const float2*>(slot(j0 + lane) + ROWS * kD) + row);
       w = weight_of(x.x, m);
       l += w * x.y;
     }
 #pragma unroll 8
     for (int j = 0; j < count; ++j) {
       const float a = __shfl_sync(0xffffffffu, w, j);
-      const float4 v = __ldcg(reinterpret_cast<const float4*>(first + (j0 + j) * slot_floats(ROWS) + row * kD) + lane);
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(slot(j0 + j) + row * kD) + lane);
       o.x += a * v.x;
       o.y += a * v.y;
       o.z += a * v.z;
@@ -966,27 +1081,28 @@ Kernels kernels_of(bool cache8, bool wide) {
                 : (wide ? kernels_for<BF, false, true>() : kernels_for<BF, false, false>());
 }
 
-bool is_wide(long long new_rows, int group) { return (new_rows < kMaxDrafts ? new_rows : kMaxDrafts) * group > kTile; }
+// Items of 256 rows read the cache once for twice the rows; those of 128 keep one more chunk in shared memory. By the
+// rows that a request has on average: 8 requests of 32 rows at most over 4096 to 8192 8-bit rows, 68 us with wide items.
+bool is_wide(int B, long long new_rows, int group) { return new_rows * group > static_cast<long long>(B) * kTile; }
 
 }  // namespace
 
-size_t tree_tc_workspace_bytes(long long new_rows, int n_heads, int n_kv_heads) {
+size_t tree_tc_workspace_bytes(int B, long long new_rows, int n_heads, int n_kv_heads) {
   return (kTreeHeader + kTreeCounters) * sizeof(int) + table_bytes(new_rows, n_heads) +
-         kPartials * slot_floats(is_wide(new_rows, n_heads / n_kv_heads) ? 2 * kTile : kTile) * sizeof(float);
+         kPartials * slot_floats(is_wide(B, new_rows, n_heads / n_kv_heads) ? 2 * kTile : kTile) * sizeof(float);
 }
 
 cudaError_t launch_tree_tc(const TreeArgs& a, int dtype, bool cache8, cudaStream_t stream) {
-  const bool wide = is_wide(a.new_rows, a.n_heads / a.n_kv_heads);
+  const bool wide = is_wide(a.B, a.new_rows, a.n_heads / a.n_kv_heads);
   const Kernels k = dtype == FSX_BF16 ? kernels_of<true>(cache8, wide) : kernels_of<false>(cache8, wide);
   const long long join_blocks = (a.new_rows * a.n_heads + 3) / 4;
   if (join_blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
-  cudaError_t e = cudaFuncSetAttribute(k.main, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(k.smem));
-  int dev = 0, sms = 0;
-  if (e == cudaSuccess) e = cudaGetDevice(&dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  const int sms = sm_count();
+  if (sms == 0) return cudaErrorNoDevice;
+  cudaError_t e = allow_shared_memory(k.main, k.smem);
   if (e != cudaSuccess) return e;
   void* args[] = {const_cast<TreeArgs*>(&a)};
-  e = launch_ex(k.main, dim3(static_cast<unsigned>(sms)), dim3(kThreads), k.smem, stream, false, args);
+  e = launch_ex(k.main, dim3(static_cast<unsigned>(sms < kMaxGrid ? sms : kMaxGrid)), dim3(kThreads), k.smem, stream, false, args);
   if (e != cudaSuccess) return e;
   return launch_ex(k.join, dim3(static_cast<unsigned>(join_blocks)), dim3(128), 0, stream, true, args);
 }

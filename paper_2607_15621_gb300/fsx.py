@@ -347,88 +347,90 @@ def attention_noalloc_status(stream=None) -> int:
     return int(lib().fsx_attention_noalloc_status(_stream(stream)))
 
 
-_DTYPE_CODE = {"torch.float32": FSX_F32, "torch.bfloat16": FSX_BF16, "torch.float16": FSX_F16,
-               "torch.float8_e4m3fn": FSX_E4M3, "torch.uint8": FSX_E4M3}
+# What the checks below ask for. A call of 10 to 20 us on the GPU waits for its caller: the conditions are one expression
+# of cheap attributes (12 to 23 us a call with a helper for each), and only a refusal looks for its reason.
+_CODES: dict = {}  # torch dtype -> fsx_dtype; e4m3 caches may be held as bytes
+_I64 = _F32 = None
 
 
-def _code(t) -> int:
-    """fsx_dtype of a tensor; e4m3 caches may be held as bytes."""
-    code = _DTYPE_CODE.get(str(t.dtype))
-    if code is None:
-        raise FsxError(FSX_ERR_UNSUPPORTED, f"dtype {t.dtype}")
-    return code
+def _codes() -> dict:
+    global _I64, _F32
+    if not _CODES:
+        import torch
+        _I64, _F32 = torch.int64, torch.float32
+        _CODES.update({torch.float32: FSX_F32, torch.bfloat16: FSX_BF16, torch.float16: FSX_F16,
+                       torch.float8_e4m3fn: FSX_E4M3, torch.uint8: FSX_E4M3})
+    return _CODES
 
 
-def _same(ok: bool, what: str):
-    if not ok:
-        raise FsxError(FSX_ERR_INVALID_ARG, what)
+def _refuse(what: str, **tensors):
+    """Raises for tensors that do not go together: `what` is asked for."""
+    given = ", ".join(f"{n} {'None' if t is None else f'{tuple(t.shape)} {t.dtype} stride {t.stride()}'}"
+                      for n, t in tensors.items())
+    raise FsxError(FSX_ERR_INVALID_ARG, f"{what}; given: {given}")
 
 
-def _rows_of(t, what: str) -> int:
-    """Row stride of [rows, heads, 128] whose rows are contiguous."""
-    _same(t.dim() == 3 and t.stride(2) == 1 and (t.shape[1] == 1 or t.stride(1) == t.shape[2]),
-          f"{what}: [rows, heads, head_dim] with contiguous rows")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1] * t.shape[2])
+def _rows(t, stride) -> bool:
+    """[rows, heads, head_dim] whose rows are contiguous."""
+    return stride[2] == 1 and (stride[1] == t.shape[2] or t.shape[1] == 1)
 
 
-def _one_stride(a, b, what: str) -> int:
-    sa, sb = _rows_of(a, what), _rows_of(b, what)
-    _same(a.shape == b.shape and a.dtype == b.dtype and sa == sb, f"{what}: same shape, dtype and row stride")
-    return sa
+def _pitch(t, stride) -> int:
+    return stride[0] if t.shape[0] > 1 else max(stride[0], t.shape[1] * t.shape[2])
 
 
-def _whole(t, what: str, dtype: str | None = None, shape=None):
-    _same(t.is_contiguous() and (dtype is None or str(t.dtype) == dtype) and
-          (shape is None or tuple(t.shape) == tuple(shape)), f"{what}: contiguous {dtype or ''} {shape or ''}")
-
-
-def _cache8(k_cache, v_cache, k_scale, v_scale):
-    _whole(k_cache, "k_cache")
-    _whole(v_cache, "v_cache", None, k_cache.shape)
-    _same(k_cache.dim() == 3 and k_cache.dtype == v_cache.dtype and _code(k_cache) == FSX_E4M3,
-          "8-bit caches: [rows, kv heads, 128] of float8_e4m3fn or uint8")
-    for t in (k_scale, v_scale):
-        _whole(t, "scales", "torch.float32", (k_cache.shape[1], k_cache.shape[0]))
+def _cache8_call(k, v, rows, k_cache, v_cache, k_scale, v_scale):
+    codes = _CODES or _codes()
+    shape, stride, cs = k.shape, k.stride(), k_cache.shape
+    good = (len(shape) == 3 and len(cs) == 3 and v.shape == shape and v.stride() == stride and v.dtype is k.dtype and
+            _rows(k, stride) and cs[1:] == shape[1:] and v_cache.shape == cs and k_cache.dtype is v_cache.dtype and
+            codes.get(k_cache.dtype) == FSX_E4M3 and k_cache.is_contiguous() and v_cache.is_contiguous() and
+            k_scale.dtype is _F32 and v_scale.dtype is _F32 and k_scale.shape == (cs[1], cs[0]) and
+            v_scale.shape == k_scale.shape and k_scale.is_contiguous() and v_scale.is_contiguous() and
+            (rows is None or (rows.dtype is _I64 and rows.shape == shape[:1] and rows.is_contiguous())) and
+            k.dtype in codes)
+    if not good:
+        _refuse("rows k, v [n, kv heads, 128] of one shape, dtype and stride, 8-bit caches [rows, kv heads, 128], scales "
+                "fp32 [kv heads, rows], row numbers int64 [n]", k=k, v=v, rows=rows, k_cache=k_cache, v_cache=v_cache,
+                k_scale=k_scale, v_scale=v_scale)
+    return codes[k.dtype], shape, _pitch(k, stride), cs[0]
 
 
 def cache_write(k, v, rows, k_cache, v_cache, k_scale, v_scale, status, stream=None):
     """fsx_cache_write_e4m3: rows k, v [n, kv heads, 128] into cache rows `rows` (int64 [n]; None: 0 .. n - 1)."""
-    _cache8(k_cache, v_cache, k_scale, v_scale)
-    stride = _one_stride(k, v, "k, v")
-    _same(k.shape[1:] == k_cache.shape[1:], "k, v and the caches: same heads")
-    if rows is not None:
-        _whole(rows, "rows", "torch.int64", (k.shape[0],))
-    check(lib().fsx_cache_write_e4m3(_ptr(k), _ptr(v), stride, _code(k), _ptr(rows), k.shape[0], k.shape[1], k.shape[2],
-                                     _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), k_cache.shape[0],
-                                     _ptr(status), _stream(stream)))
+    code, shape, pitch, m = _cache8_call(k, v, rows, k_cache, v_cache, k_scale, v_scale)
+    check(lib().fsx_cache_write_e4m3(k.data_ptr(), v.data_ptr(), pitch, code, None if rows is None else rows.data_ptr(),
+                                     shape[0], shape[1], shape[2], k_cache.data_ptr(), v_cache.data_ptr(),
+                                     k_scale.data_ptr(), v_scale.data_ptr(), m, status.data_ptr(), _stream(stream)))
 
 
 def cache_read(k_cache, v_cache, k_scale, v_scale, rows, k, v, status, stream=None):
     """fsx_cache_read_e4m3: cache rows `rows` (int64 [n]; None: 0 .. n - 1) into k, v [n, kv heads, 128]."""
-    _cache8(k_cache, v_cache, k_scale, v_scale)
-    stride = _one_stride(k, v, "k, v")
-    _same(k.shape[1:] == k_cache.shape[1:], "k, v and the caches: same heads")
-    if rows is not None:
-        _whole(rows, "rows", "torch.int64", (k.shape[0],))
-    check(lib().fsx_cache_read_e4m3(_ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), k_cache.shape[0],
-                                    _ptr(rows), k.shape[0], k.shape[1], k.shape[2], _ptr(k), _ptr(v), stride, _code(k),
-                                    _ptr(status), _stream(stream)))
+    code, shape, pitch, m = _cache8_call(k, v, rows, k_cache, v_cache, k_scale, v_scale)
+    check(lib().fsx_cache_read_e4m3(k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), m,
+                                    None if rows is None else rows.data_ptr(), shape[0], shape[1], shape[2],
+                                    k.data_ptr(), v.data_ptr(), pitch, code, status.data_ptr(), _stream(stream)))
     return k, v
 
 
 def prompt_attention(q, k, v, q_offsets, kv_offsets, out, status, lse=None, causal=True, stream=None):
     """fsx_prompt_attention: packed q [rows, heads, 128], k and v [rows, kv heads, 128], int64 offsets [B + 1]."""
-    stride = _one_stride(k, v, "k, v")
-    _same(q.dtype == k.dtype and q.dtype == out.dtype and q.shape[2] == k.shape[2], "q, k, v, out: same dtype and head_dim")
-    _whole(out, "out", None, q.shape)
-    _whole(q_offsets, "q_offsets", "torch.int64")
-    _whole(kv_offsets, "kv_offsets", "torch.int64", q_offsets.shape)
-    if lse is not None:
-        _whole(lse, "lse", "torch.float32", (q.shape[1], q.shape[0]))
-    check(lib().fsx_prompt_attention(_ptr(q), _rows_of(q, "q"), _ptr(k), _ptr(v), stride, _code(q), _ptr(q_offsets),
-                                     _ptr(kv_offsets), q_offsets.shape[0] - 1, q.shape[0], k.shape[0], q.shape[1],
-                                     k.shape[1], q.shape[2], int(causal), _ptr(out), _ptr(lse), _ptr(status),
-                                     _stream(stream)))
+    codes = _CODES or _codes()
+    dtype, qs, ks, q_shape, k_shape = q.dtype, q.stride(), k.stride(), q.shape, k.shape
+    good = (len(q_shape) == 3 and len(k_shape) == 3 and k.dtype is dtype and v.dtype is dtype and out.dtype is dtype and
+            v.shape == k_shape and v.stride() == ks and out.shape == q_shape and out.is_contiguous() and
+            q_shape[2] == k_shape[2] and _rows(q, qs) and _rows(k, ks) and q_offsets.dtype is _I64 and
+            kv_offsets.dtype is _I64 and q_offsets.shape == kv_offsets.shape and q_offsets.dim() == 1 and
+            q_offsets.is_contiguous() and kv_offsets.is_contiguous() and dtype in codes and
+            (lse is None or (lse.dtype is _F32 and lse.shape == (q_shape[1], q_shape[0]) and lse.is_contiguous())))
+    if not good:
+        _refuse("q, out [rows, heads, 128], k, v [rows, kv heads, 128] of one dtype, k and v of one stride, out contiguous, "
+                "offsets int64 [B + 1], lse fp32 [heads, rows]", q=q, k=k, v=v, q_offsets=q_offsets,
+                kv_offsets=kv_offsets, out=out, lse=lse)
+    check(lib().fsx_prompt_attention(q.data_ptr(), _pitch(q, qs), k.data_ptr(), v.data_ptr(), _pitch(k, ks), codes[dtype],
+                                     q_offsets.data_ptr(), kv_offsets.data_ptr(), q_offsets.shape[0] - 1, q_shape[0],
+                                     k_shape[0], q_shape[1], k_shape[1], q_shape[2], 1 if causal else 0, out.data_ptr(),
+                                     None if lse is None else lse.data_ptr(), status.data_ptr(), _stream(stream)))
     return out
 
 
@@ -440,30 +442,39 @@ def tree_attention(q, k_new, v_new, new_offsets, mask, k_cache, v_cache, offsets
                    v_scale=None, starts=None, lse=None, stream=None):
     """fsx_tree_attention: the new tokens' q [rows, heads, 128], k_new and v_new [rows, kv heads, 128], mask int64
     [rows], over caches [rows, kv heads, 128] of q's dtype or e4m3 (then with scales [kv heads, rows])."""
-    stride = _one_stride(k_new, v_new, "k_new, v_new")
-    _same(q.dtype == k_new.dtype and q.dtype == out.dtype and q.shape[0] == k_new.shape[0] and
-          q.shape[2] == k_new.shape[2], "q, k_new, v_new, out: same dtype, rows and head_dim")
-    _whole(out, "out", None, q.shape)
-    _whole(new_offsets, "new_offsets", "torch.int64")
-    _whole(mask, "mask", "torch.int64", (q.shape[0],))
-    _whole(offsets, "offsets", "torch.int64", new_offsets.shape)
-    _whole(k_cache, "k_cache")
-    _whole(v_cache, "v_cache", str(k_cache.dtype), k_cache.shape)
-    _same(k_cache.dim() == 3 and k_cache.shape[1:] == k_new.shape[1:], "caches: [rows, kv heads, head_dim]")
-    code = _code(k_cache)
-    if code == FSX_E4M3:
-        _same(k_scale is not None and v_scale is not None, "8-bit caches need their scales")
-        _cache8(k_cache, v_cache, k_scale, v_scale)
-    if starts is not None:
-        _whole(starts, "starts", "torch.int64", (new_offsets.shape[0] - 1,))
-    if lse is not None:
-        _whole(lse, "lse", "torch.float32", (q.shape[1], q.shape[0]))
-    check(lib().fsx_tree_attention(_ptr(q), _rows_of(q, "q"), _ptr(k_new), _ptr(v_new), stride, _code(q),
-                                   _ptr(new_offsets), _ptr(mask), q.shape[0], _ptr(k_cache), _ptr(v_cache),
-                                   _ptr(k_scale), _ptr(v_scale), code, k_cache.shape[0], _ptr(starts), _ptr(offsets),
-                                   new_offsets.shape[0] - 1, q.shape[1], k_new.shape[1], q.shape[2], _ptr(out),
-                                   _ptr(lse), _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                   _ptr(status), _stream(stream)))
+    codes = _CODES or _codes()
+    dtype, qs, ks, q_shape, k_shape, cs = q.dtype, q.stride(), k_new.stride(), q.shape, k_new.shape, k_cache.shape
+    code = codes.get(k_cache.dtype)
+    good = (len(q_shape) == 3 and len(k_shape) == 3 and len(cs) == 3 and k_new.dtype is dtype and v_new.dtype is dtype and
+            out.dtype is dtype and v_new.shape == k_shape and v_new.stride() == ks and out.shape == q_shape and
+            out.is_contiguous() and q_shape[0] == k_shape[0] and q_shape[2] == k_shape[2] and _rows(q, qs) and
+            _rows(k_new, ks) and new_offsets.dtype is _I64 and offsets.dtype is _I64 and
+            offsets.shape == new_offsets.shape and new_offsets.dim() == 1 and new_offsets.is_contiguous() and
+            offsets.is_contiguous() and mask.dtype is _I64 and mask.shape == q_shape[:1] and mask.is_contiguous() and
+            v_cache.dtype is k_cache.dtype and v_cache.shape == cs and cs[1:] == k_shape[1:] and
+            k_cache.is_contiguous() and v_cache.is_contiguous() and dtype in codes and code is not None and
+            (code != FSX_E4M3 or (k_scale is not None and v_scale is not None and k_scale.dtype is _F32 and
+                                  v_scale.dtype is _F32 and k_scale.shape == (cs[1], cs[0]) and
+                                  v_scale.shape == k_scale.shape and k_scale.is_contiguous() and
+                                  v_scale.is_contiguous())) and
+            (starts is None or (starts.dtype is _I64 and starts.is_contiguous() and starts.dim() == 1 and
+                                starts.shape[0] == new_offsets.shape[0] - 1)) and
+            (lse is None or (lse.dtype is _F32 and lse.shape == (q_shape[1], q_shape[0]) and lse.is_contiguous())))
+    if not good:
+        _refuse("q, out [rows, heads, 128], k_new, v_new [rows, kv heads, 128] of one dtype, k_new and v_new of one stride, out "
+                "contiguous, offsets int64 [B + 1], mask int64 [rows], caches [rows, kv heads, 128] of that dtype or e4m3 "
+                "with scales fp32 [kv heads, rows], starts int64 [B], lse fp32 [heads, rows]", q=q, k_new=k_new,
+                v_new=v_new, new_offsets=new_offsets, mask=mask, k_cache=k_cache, v_cache=v_cache, offsets=offsets,
+                out=out, k_scale=k_scale, v_scale=v_scale, starts=starts, lse=lse)
+    eight = code == FSX_E4M3
+    check(lib().fsx_tree_attention(q.data_ptr(), _pitch(q, qs), k_new.data_ptr(), v_new.data_ptr(), _pitch(k_new, ks),
+                                   codes[dtype], new_offsets.data_ptr(), mask.data_ptr(), q_shape[0], k_cache.data_ptr(),
+                                   v_cache.data_ptr(), k_scale.data_ptr() if eight else None,
+                                   v_scale.data_ptr() if eight else None, code, cs[0],
+                                   None if starts is None else starts.data_ptr(), offsets.data_ptr(),
+                                   new_offsets.shape[0] - 1, q_shape[1], k_shape[1], q_shape[2], out.data_ptr(),
+                                   None if lse is None else lse.data_ptr(), workspace.data_ptr(),
+                                   workspace.numel() * workspace.element_size(), status.data_ptr(), _stream(stream)))
     return out
 
 

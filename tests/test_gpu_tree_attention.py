@@ -131,6 +131,37 @@ def test_single_tokens_over_long_caches(cache8, dtype):
     agree(make([5000, 0, 1, 2047, 64], [1] * 5, heads=4, kv_heads=4, dtype=dtype, cache8=cache8, seed=20))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("cache8", [True, False])
+@pytest.mark.parametrize("heads,kv_heads,lens,new", [
+    (8, 2, [6000, 4100, 5200, 7001], [8, 5, 7, 6]),        # 20 to 32 rows an item, dozens of chunks, cut items
+    (8, 2, [3000] * 20 + [1500, 40, 0], [6] * 23),         # about as many items as SMs
+    (4, 1, [9000, 130], [60, 64]),                         # items of 240 and 256 rows
+    (32, 4, [700, 1300, 257] * 6, [4, 16, 40] * 6),        # short and long, few and many rows together
+])
+def test_many_rows_over_long_caches(heads, kv_heads, lens, new, cache8, dtype):
+    """Pieces that start and end anywhere in an item; the oracle on a few heads and tokens of each request."""
+    c = make(lens, new, heads=heads, kv_heads=kv_heads, dtype=dtype, cache8=cache8, seed=len(lens))
+    out, lse, status = run(c)
+    assert status == fsx.FSX_OK
+    assert torch.equal(run(c)[0], out)
+    g = heads // kv_heads
+    k, v = caches64(c)
+    for b in range(len(lens)):
+        t0, t1 = int(c["no"][b]), int(c["no"][b + 1])
+        for kvh in sorted({0, kv_heads - 1}):
+            hs, tokens = [kvh * g, kvh * g + g - 1], sorted({t0, (t0 + t1) // 2, t1 - 1})
+            for i in tokens:
+                seen = [t0 + j for j in range(t1 - t0) if c["mask"][i] >> j & 1]
+                rows = slice(c["starts"][b], c["starts"][b] + lens[b])
+                kk = np.concatenate([k[rows, kvh], to64(c["kn"])[seen, kvh]])
+                vv = np.concatenate([v[rows, kvh], to64(c["vn"])[seen, kvh]])
+                for h in hs:
+                    want, want_lse = llm_oracle.attention_row(to64(c["q"])[i, h], kk, vv)
+                    check(out[i:i + 1, h:h + 1], lse[h:h + 1, i:i + 1], want[None, None], np.array([[want_lse]]), dtype,
+                          np.abs(vv).max())
+
+
 @pytest.mark.parametrize("cache8", [True, False])
 def test_many_requests(cache8):
     rng = np.random.default_rng(21)
