@@ -36,6 +36,7 @@ constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kChunk = 16 * kWarps;
 constexpr int kD = kHeadDim;
+constexpr int kJoin = 12;  // pieces whose partial results are loaded at once
 
 // 4 bytes to shared memory, 0 if not `there` (then nothing is read)
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool there) {
@@ -233,13 +234,13 @@ __device__ __forceinline__ int out_dim(int g, int j, int e) {
 // weight is 0 but 0 times an infinity or NaN is not: such values go into the product as 0 and are added
 // to the rows that see them.
 template <bool BF, bool C8, int NT>
-__device__ __forceinline__ void new_step(State<NT>& st, const TreeArgs& p, const TreePiece& it, int G, int key) {
+__device__ __forceinline__ void new_step(State<NT>& st, const TreeArgs& p, const TreePiece& it, uint32_t G, int key) {
   const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
   const int left = it.r.n - key;
   const uint16_t* kn = static_cast<const uint16_t*>(p.k_new) + (it.r.t0 + key) * p.new_stride + it.kvh * kD;
   const uint16_t* vn = static_cast<const uint16_t*>(p.v_new) + (it.r.t0 + key) * p.new_stride + it.kvh * kD;
   const uint16_t* q = static_cast<const uint16_t*>(p.q);
-  const int rows = it.r.n * G;
+  const uint32_t rows = it.r.n * G;
   float s[NT][4];
 #pragma unroll
   for (int t = 0; t < NT; ++t)
@@ -254,7 +255,7 @@ __device__ __forceinline__ void new_step(State<NT>& st, const TreeArgs& p, const
       a[h] = g + 8 * h < left ? __ldg(reinterpret_cast<const uint2*>(kn + (g + 8 * h) * p.new_stride + d)) : make_uint2(0u, 0u);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const int row = it.row0 + 8 * t + g, token = row / G;
+      const uint32_t row = it.row0 + 8 * t + g, token = row / G;
       const uint2 b = row < rows ? __ldg(reinterpret_cast<const uint2*>(q + (it.r.t0 + token) * p.q_stride +
                                                                          (it.kvh * G + row - token * G) * kD + d))
                                  : make_uint2(0u, 0u);
@@ -266,7 +267,7 @@ __device__ __forceinline__ void new_step(State<NT>& st, const TreeArgs& p, const
   for (int t = 0; t < NT; ++t)
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      const int row = it.row0 + 8 * t + 2 * c + r;
+      const uint32_t row = it.row0 + 8 * t + 2 * c + r;
       mask[t][r] = row < rows ? p.mask[it.r.t0 + row / G] >> key : 0ull;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -314,16 +315,16 @@ __device__ __forceinline__ void new_step(State<NT>& st, const TreeArgs& p, const
   }
 }
 
-// Queries of the item's rows as B operands; C8: bf16 as fp16 times 2^-e, f the factor that undoes it
-template <bool BF, bool C8, int NT>
-__device__ __forceinline__ void load_queries(uint32_t (&qf)[NT][8][2], float (&f)[NT][2], const TreeArgs& p, const TreePiece& it, int G) {
+// Queries of the item's rows, as they lie
+template <bool C8, int NT>
+__device__ __forceinline__ void load_queries(uint32_t (&qf)[NT][8][2], const TreeArgs& p, const TreePiece& it, uint32_t G) {
   const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-  const uint16_t* q = static_cast<const uint16_t*>(p.q);
+  const uint16_t* q = static_cast<const uint16_t*>(p.q) + it.r.t0 * p.q_stride + it.kvh * G * kD;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const int row = it.row0 + 8 * t + g, token = row / G;
+    const uint32_t row = it.row0 + 8 * t + g, token = row / G;
     const bool there = row < it.r.n * G;
-    const uint16_t* src = q + (it.r.t0 + (there ? token : 0)) * p.q_stride + (it.kvh * G + (there ? row - token * G : 0)) * kD;
+    const uint16_t* src = q + (there ? token * p.q_stride + (row - token * G) * kD : 0ll);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const int d = C8 ? (k >> 2) * 64 + 16 * c + 4 * (k & 3) : 8 * (c + 4 * (k >> 1)) + 4 * (k & 1);
@@ -331,6 +332,14 @@ __device__ __forceinline__ void load_queries(uint32_t (&qf)[NT][8][2], float (&f
       qf[t][k][0] = w.x;
       qf[t][k][1] = w.y;
     }
+  }
+}
+// The same as B operands; C8: bf16 as fp16 times 2^-e, f the factor that undoes it
+template <bool BF, bool C8, int NT>
+__device__ __forceinline__ void make_queries(uint32_t (&qf)[NT][8][2], float (&f)[NT][2]) {
+  const int c = threadIdx.x & 3;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
     if (C8 && !BF) {
       f[t][0] = f[t][1] = kScaleLog2;  // fp16 as it is
     } else if (C8) {
@@ -397,11 +406,11 @@ __global__ void __launch_bounds__(kThreads, Fit<C8, NT>::kCtas) tree_kernel(cons
   using S = Stage<C8>;
   constexpr int kStages = Fit<C8, NT>::kStages, kPass = Fit<C8, NT>::kPass;
   constexpr int kPerRow = S::kRow / 16;
-  constexpr TreeShape kShape{8 * NT, kChunk, 8, 16, slots_of(NT)};
+  constexpr TreeShape kShape{8 * NT, kChunk, 8, 28, slots_of(NT)};
   extern __shared__ __align__(128) unsigned char raw_smem[];
   Shared<C8, NT>& sm = *reinterpret_cast<Shared<C8, NT>*>(raw_smem);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
-  const int G = p.n_heads / p.n_kv_heads;
+  const uint32_t G = static_cast<uint32_t>(p.n_heads) / static_cast<uint32_t>(p.n_kv_heads);
   int* header = static_cast<int*>(p.workspace);
   const TreePlan plan = tree_plan<kThreads>(p, kShape, raw_smem + sizeof(sm), sm.scratch);
   const long long total = plan.pieces[p.B];
@@ -441,43 +450,43 @@ __global__ void __launch_bounds__(kThreads, Fit<C8, NT>::kCtas) tree_kernel(cons
 
   long long i = blockIdx.x;
   TreePiece it;
+  uint32_t qf[NT][8][2];
   if (i < total) {
     it = tree_piece(p, kShape, plan, i);
+    load_queries<C8, NT>(qf, p, it, G);  // in front of the cache's copies
     begin(it);
   }
 #pragma unroll 1
   while (i < total) {
     if (tid == 0) sm.next = gridDim.x + static_cast<long long>(atomicAdd(reinterpret_cast<unsigned*>(header), 1u));
     State<NT> st;
-    {
-      uint32_t qf[NT][8][2];
-      float f[NT][2];
-      load_queries<BF, C8, NT>(qf, f, p, it, G);
+    float f[NT][2];
+    make_queries<BF, C8, NT>(qf, f);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        st.m[t][0] = st.m[t][1] = -CUDART_INF_F;
-        st.l[t][0] = st.l[t][1] = 0.f;
+    for (int t = 0; t < NT; ++t) {
+      st.m[t][0] = st.m[t][1] = -CUDART_INF_F;
+      st.l[t][0] = st.l[t][1] = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+      for (int j = 0; j < 8; ++j)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) st.o[j][t][e] = 0.f;
-      }
-      st.vs = 0.f;
-      int slot_out = 0;
+        for (int e = 0; e < 4; ++e) st.o[j][t][e] = 0.f;
+    }
+    st.vs = 0.f;
+    // the new tokens first, while the cache's first rows are on their way
+    if (it.to == it.n && 16 * warp < it.r.n) new_step<BF, C8, NT>(st, p, it, G, 16 * warp);
+    int slot_out = 0;
 #pragma unroll 1
-      for (int key = it.from * kChunk + 16 * warp; key < end; key += kChunk) {
-        cp_async_wait<kStages - 2>();
-        __syncwarp();  // every lane's copies of the stage; and the stage before is read
-        copy_next();
-        cache_step<BF, C8, NT>(st, sm.ring[warp] + slot_out * S::kBytes, qf, f, end - key);
-        slot_out = slot_out + 1 == kStages ? 0 : slot_out + 1;
-      }
+    for (int key = it.from * kChunk + 16 * warp; key < end; key += kChunk) {
+      cp_async_wait<kStages - 2>();
+      __syncwarp();  // every lane's copies of the stage; and the stage before is read
+      copy_next();
+      cache_step<BF, C8, NT>(st, sm.ring[warp] + slot_out * S::kBytes, qf, f, end - key);
+      slot_out = slot_out + 1 == kStages ? 0 : slot_out + 1;
     }
     cp_async_wait<0>();
     __syncwarp();
-    if (it.to == it.n && 16 * warp < it.r.n) new_step<BF, C8, NT>(st, p, it, G, 16 * warp);
 
-    const int rows = min(8 * NT, it.r.n * G - it.row0);
+    const int rows = min(8 * NT, static_cast<int>(it.r.n * G - it.row0));
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -496,11 +505,12 @@ __global__ void __launch_bounds__(kThreads, Fit<C8, NT>::kCtas) tree_kernel(cons
     TreePiece next = it;
     if (i_next < total) {
       next = tree_piece(p, kShape, plan, i_next);
+      load_queries<C8, NT>(qf, p, next, G);
       begin(next);
     }
     // ---- the four warps' results, kPass rows at a time; a thread a dim
     auto finish = [&](int row, float m, float l, float o) {
-      const int at = it.row0 + row, token = at / G, head = it.kvh * G + at - token * G;
+      const uint32_t at = it.row0 + row, token = at / G, head = it.kvh * G + at - token * G;
       const float y = l == 0.f ? 0.f : o / l;
       static_cast<uint16_t*>(p.out)[((it.r.t0 + token) * p.n_heads + head) * kD + tid] = static_cast<uint16_t>(pack16<BF>(y, y));
       if (p.lse != nullptr && tid == 0)
@@ -557,33 +567,38 @@ __global__ void __launch_bounds__(kThreads, Fit<C8, NT>::kCtas) tree_kernel(cons
         const float* first = slot_at<NT>(p, it.slot);
 #pragma unroll 1
         for (int row = warp; row < rows; row += kWarps) {  // a warp a row, 4 dims a lane
-          const float* ml = first + 8 * NT * kD + 2 * row;
-          float m = -CUDART_INF_F;
-          for (int j = lane; j < it.of; j += 32) m = fmaxf(m, __ldcg(ml + j * slot_floats(NT)));
-#pragma unroll
-          for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-          float l = 0.f;
+          float m = -CUDART_INF_F, l = 0.f;
           float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (int j0 = 0; j0 < it.of; j0 += 32) {  // in the order of the keys
-            const int count = min(32, it.of - j0);
-            float w = 0.f;
-            if (lane < count) {
-              const float2 x = __ldcg(reinterpret_cast<const float2*>(ml + (j0 + lane) * slot_floats(NT)));
-              w = weight_of(x.x, m);
-              l += w * x.y;
+#pragma unroll 1
+          for (int j0 = 0; j0 < it.of; j0 += kJoin) {  // in the order of the keys; the loads of kJoin pieces at once
+            float2 x[kJoin];
+            float4 v[kJoin];
+#pragma unroll
+            for (int j = 0; j < kJoin; ++j) {
+              const float* other = first + min(j0 + j, it.of - 1) * slot_floats(NT);
+              x[j] = __ldcg(reinterpret_cast<const float2*>(other + 8 * NT * kD) + row);
+              v[j] = __ldcg(reinterpret_cast<const float4*>(other + row * kD) + lane);
             }
-#pragma unroll 8
-            for (int j = 0; j < count; ++j) {
-              const float a = __shfl_sync(0xffffffffu, w, j);
-              const float4 v = __ldcg(reinterpret_cast<const float4*>(first + (j0 + j) * slot_floats(NT) + row * kD) + lane);
-              o.x += a * v.x;
-              o.y += a * v.y;
-              o.z += a * v.z;
-              o.w += a * v.w;
+            float top = m;
+#pragma unroll
+            for (int j = 0; j < kJoin; ++j) top = fmaxf(top, x[j].x);
+            const float old = weight_of(m, top);
+            m = top;
+            l *= old;
+            o = make_float4(o.x * old, o.y * old, o.z * old, o.w * old);
+#pragma unroll
+            for (int j = 0; j < kJoin; ++j) {
+              const float a = weight_of(x[j].x, top);
+              if (j0 + j < it.of) {
+                l += a * x[j].y;
+                o.x += a * v[j].x;
+                o.y += a * v[j].y;
+                o.z += a * v[j].z;
+                o.w += a * v[j].w;
+              }
             }
           }
-          l = warp_sum(l);
-          const int at = it.row0 + row, token = at / G, head = it.kvh * G + at - token * G;
+          const uint32_t at = it.row0 + row, token = at / G, head = it.kvh * G + at - token * G;
           const float inv = l == 0.f ? 0.f : 1.f / l;
           uint16_t* out = static_cast<uint16_t*>(p.out) + ((it.r.t0 + token) * p.n_heads + head) * kD + 4 * lane;
           *reinterpret_cast<uint2*>(out) = make_uint2(pack16<BF>(o.x * inv, o.y * inv), pack16<BF>(o.z * inv, o.w * inv));

@@ -42,7 +42,7 @@ __device__ __forceinline__ bool tree_request(const TreeArgs& p, int b, TreeReque
 // Geometry of a kernel's items
 struct TreeShape {
   int tile_rows, chunk;  // rows of an item, keys of a chunk
-  int few, many;         // an item of `few` chunks or less is not cut; pieces are no longer than `many` for balance alone
+  int few, many;         // an item of `few` chunks or less is not cut; a piece has `many` at most
   int slots;             // of the workspace
 };
 
@@ -71,6 +71,49 @@ __device__ __forceinline__ TreePlan tree_plan(const TreeArgs& p, const TreeShape
   auto items = [&](const TreeRequest& r) {
     return static_cast<long long>((r.n * G + shape.tile_rows - 1) / shape.tile_rows) * p.n_kv_heads;
   };
+  // an even share, or a part of it; and cut items of n > most chunks take at most 2 n / most slots (in 32 bits where
+  // it fits: a 64-bit division is a hundred instructions that every CTA waits for)
+  auto most_of = [&](long long total) {
+    const bool small = total < 0x3fffffff;
+    const uint32_t even = small ? (static_cast<uint32_t>(total) + gridDim.x - 1) / gridDim.x : 0x7fffffffu;
+    const uint32_t turns = (even + shape.many - 1) / shape.many;  // pieces that a CTA takes, if they were all alike
+    const long long share = turns > 0 ? (even + turns - 1) / turns : 1;
+    const long long room = small ? (2 * static_cast<uint32_t>(total) + shape.slots - 1) / shape.slots : (2 * total + shape.slots - 1) / shape.slots;
+    return static_cast<int>(min(max(max(share, room), static_cast<long long>((shape.few + 1) / 2)), 0x7fffffffll));
+  };
+  if (p.B <= 32) {  // a lane a request, one barrier
+    if (warp == 0) {
+      TreeRequest r{};
+      const bool mine = lane < p.B;
+      if (mine && !tree_request(p, lane, r) && blockIdx.x == 0) set_status(p.status, kStatusDeviceArg);
+      const long long n_items = mine ? items(r) : 0;
+      const int n = mine ? tree_chunks(shape, r.len) : 0;
+      long long total = n_items * n;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+      const int most = most_of(total);
+      const int of = tree_pieces(shape, n, most);
+      const uint32_t pieces = static_cast<uint32_t>(n_items) * of, slots = of > 1 ? pieces : 0;
+      uint32_t sum = pieces, sum_slots = slots;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t up = __shfl_up_sync(0xffffffffu, sum, o), up_slots = __shfl_up_sync(0xffffffffu, sum_slots, o);
+        if (lane >= o) {
+          sum += up;
+          sum_slots += up_slots;
+        }
+      }
+      if (mine) {
+        plan.pieces[lane] = sum - pieces;
+        plan.slots[lane] = static_cast<int>(sum_slots - slots);
+        if (lane == p.B - 1) plan.pieces[p.B] = sum;
+      }
+      if (lane == 0) scratch[0] = most;
+    }
+    __syncthreads();
+    plan.most = static_cast<int>(scratch[0]);
+    return plan;
+  }
   long long total = 0;
   for (int b = b0; b < b1; ++b) {
     TreeRequest r;
@@ -84,10 +127,7 @@ __device__ __forceinline__ TreePlan tree_plan(const TreeArgs& p, const TreeShape
   total = 0;
 #pragma unroll
   for (int w = 0; w < kW; ++w) total += scratch[w];
-  // an even share, but no more than `many`; and cut items of n > most chunks take at most 2 n / most slots
-  const long long share = min((total + gridDim.x - 1) / gridDim.x, static_cast<long long>(shape.many));
-  const long long room = (2 * total + shape.slots - 1) / shape.slots;
-  plan.most = static_cast<int>(min(max(max(share, room), static_cast<long long>((shape.few + 1) / 2)), 0x7fffffffll));
+  plan.most = most_of(total);
   long long mine = 0, mine_slots = 0;
   for (int b = b0; b < b1; ++b) {
     TreeRequest r;
