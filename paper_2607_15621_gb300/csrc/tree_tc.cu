@@ -43,6 +43,7 @@ constexpr int kRawBytes = kTile * kD;        // 16 KB of codes
 constexpr int kMmaWarp = 8, kSchedWarp = 9, kProdWarp = 12;
 constexpr int kProds = 256;                  // producer threads
 constexpr int kThreads = 384 + kProds;
+constexpr int kPlans = 5;  // whole items; pieces of 1, 1.25, 1.5 and 2 ranges
 constexpr int kWorkRing = 4;
 constexpr int kWorkUsers = 17;               // warps that read a piece's description: MMA, producers, softmax
 constexpr uint32_t kColS = 0, kColO = 256;
@@ -77,11 +78,11 @@ struct Layout {
   static constexpr int kOffFactor = kOffScale + kScaleRing * 2 * kTile * 4;  // C8: [piece parity][row]
   static constexpr int kOffMl = kOffFactor + (C8 ? 2 * kRows * 4 : 0);       // [group][128] (m, l)
   static constexpr int kOffScratch = kOffMl + 2 * kTile * 8;
-  static constexpr int kOffWork = kOffScratch + 2 * (kThreads / 32) * 8;
+  static constexpr int kOffWork = kOffScratch + (2 * kPlans + 1 + kThreads / 32 + 1) / 2 * 8;
   static constexpr int kOffBar = kOffWork + kWorkRing * static_cast<int>(sizeof(Work));
   static constexpr int kMisc = kOffBar + 33 * 8;  // tmem, abort, wild[4], vs of the groups [2], plain [4][2]
   static constexpr int kPlan = (kMisc + 16 * 4 + 7) / 8 * 8;
-  static constexpr int kSmem = kPlan + (kMaxSequences + 1) * 8;
+  static constexpr int kSmem = kPlan + (2 * kMaxSequences + 1) * 4;
 };
 static_assert(Layout<true, true>::kSmem <= 227 * 1024 && Layout<true, false>::kSmem <= 227 * 1024, "shared memory");
 static_assert(Layout<false, true>::kSmem <= 227 * 1024 && Layout<false, false>::kSmem <= 227 * 1024, "shared memory");
@@ -136,95 +137,100 @@ __device__ __forceinline__ float row_max16(float t) {  // over the 16 lanes that
   return t;
 }
 
-// The line of work: pre[b] pieces (most > 0) or chunks (ranges) of the requests before b, pre[B] of all.
+// The line of work: pre[b] pieces (most > 0) or chunks (ranges) of the requests before b, pre[B] of all. Counted in 32 bits:
+// 2^32 chunks would take hours, and each 64-bit division is a hundred instructions that every CTA waits for.
 struct Line {
-  long long* pre;
-  int most;       // chunks of a piece; 0: ranges
-  long long per;  // chunks of a range
+  uint32_t* pre;
+  uint32_t most;  // chunks of a piece; 0: ranges
+  uint32_t per;   // chunks of a range
 };
-constexpr int kPlans = 5;
-__device__ __forceinline__ int chunks_of(int len) { return (len + kTile - 1) / kTile + 1; }  // the last one: new tokens
+__device__ __forceinline__ uint32_t chunks_of(int len) { return (len + kTile - 1) / kTile + 1; }  // the last one: new tokens
+__device__ __forceinline__ uint32_t above(uint32_t a, uint32_t b) { return (a + b - 1) / b; }
+// By the whole CTA: a warp weighs a plan. `costs`: kPlans (cost, most), then the range and a value per warp
 template <int ROWS>
-__device__ __forceinline__ Line line_of(const TreeArgs& p, long long* pre, long long* scratch) {
-  constexpr int kW = kThreads / 32;
+__device__ __forceinline__ Line line_of(const TreeArgs& p, uint32_t* pre, uint32_t* chunks, uint32_t* costs) {
+  constexpr int kW = kThreads / 32, kEach = (kMaxSequences + kThreads - 1) / kThreads;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int G = p.n_heads / p.n_kv_heads;
-  const int each = (p.B + kThreads - 1) / kThreads, b0 = tid * each, b1 = min(p.B, b0 + each);
-  auto items = [&](const TreeRequest& r) { return static_cast<long long>((r.n * G + ROWS - 1) / ROWS) * p.n_kv_heads; };
-  // sums over the block; `scratch` has room for one value per warp
-  auto block_sum = [&](long long x) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    __syncthreads();
-    if (lane == 0) scratch[warp] = x;
-    __syncthreads();
-    x = 0;
-    for (int w = 0; w < kW; ++w) x += scratch[w];
-    return x;
-  };
-  long long mine = 0, longest = 0;
-  for (int b = b0; b < b1; ++b) {
+  const uint32_t G = static_cast<uint32_t>(p.n_heads) / static_cast<uint32_t>(p.n_kv_heads);
+#pragma unroll 1
+  for (int b = tid; b < p.B; b += kThreads) {
     TreeRequest r;
     if (!tree_request(p, b, r) && blockIdx.x == 0) set_status(p.status, kStatusDeviceArg);
-    mine += items(r) * chunks_of(r.len);
-    if (r.n > 0) longest = max(longest, static_cast<long long>(chunks_of(r.len)));
+    pre[b] = above(r.n * G, ROWS) * p.n_kv_heads;  // items
+    chunks[b] = r.n > 0 ? chunks_of(r.len) : 0;
   }
-  const long long total = block_sum(mine);
   __syncthreads();
-  if (lane == 0) scratch[warp] = 0;
-  __syncthreads();
-  atomicMax(reinterpret_cast<unsigned long long*>(scratch), static_cast<unsigned long long>(longest));
-  __syncthreads();
-  longest = scratch[0];
-  const long long grid = gridDim.x;
-  Line line{pre, 0, total < 0x7fffffffll ? (static_cast<uint32_t>(total) + gridDim.x - 1) / gridDim.x : (total + grid - 1) / grid};
-  line.per = max(line.per, static_cast<long long>(kLeast));
-  float best = static_cast<float>(line.per + 2 * kStart);
-  for (int i = 0; i < kPlans; ++i) {  // whole items, then pieces of 1, 1.25, 1.5 and 2 ranges
-    const long long most = i == 0 ? longest : line.per * (i < 4 ? 3 + i : 8) / 4;
-    if (most < 1 || (i > 0 && most >= longest)) continue;
-    long long pieces = 0;
-    for (int b = b0; b < b1; ++b) {
-      TreeRequest r;
-      tree_request(p, b, r);
-      pieces += items(r) * ((chunks_of(r.len) + static_cast<uint32_t>(most) - 1) / static_cast<uint32_t>(most));
+  if (warp < kPlans) {
+    uint32_t total = 0, longest = 0;
+#pragma unroll 1
+    for (int b = lane; b < p.B; b += 32) {
+      total += pre[b] * chunks[b];
+      longest = max(longest, chunks[b]);
     }
-    pieces = block_sum(pieces);
-    if (pieces == 0 || (i > 0 && pieces > kPartials)) continue;
-    const float rounds = ceilf(static_cast<float>(pieces) / static_cast<float>(grid));
-    const float cost = (rounds - 1.f) * (static_cast<float>(total) / static_cast<float>(pieces) + kStart) + most + kStart;
+    total = __reduce_add_sync(0xffffffffu, total);
+    longest = __reduce_max_sync(0xffffffffu, longest);
+    const uint32_t per = max(above(total, gridDim.x), static_cast<uint32_t>(kLeast));
+    // whole items, then pieces of 1, 1.25, 1.5 and 2 ranges
+    const uint32_t most = warp == 0 ? longest : per * (warp < 4 ? 3 + warp : 8) / 4;
+    float cost = CUDART_INF_F;
+    if (most > 0 && (warp == 0 || most < longest)) {
+      uint32_t pieces = 0;
+#pragma unroll 1
+      for (int b = lane; b < p.B; b += 32) pieces += pre[b] * above(chunks[b], most);
+      pieces = __reduce_add_sync(0xffffffffu, pieces);
+      const float rounds = ceilf(static_cast<float>(pieces) / static_cast<float>(gridDim.x));
+      if (warp == 0 || pieces <= kPartials)
+        cost = (rounds - 1.f) * (static_cast<float>(total) / static_cast<float>(pieces) + kStart) + most + kStart;
+    }
+    if (lane == 0) {
+      costs[2 * warp] = __float_as_uint(cost);
+      costs[2 * warp + 1] = most;
+      if (warp == 0) costs[2 * kPlans] = per;
+    }
+  }
+  __syncthreads();
+  Line line{pre, 0, costs[2 * kPlans]};
+  float best = static_cast<float>(line.per + 2 * kStart);
+#pragma unroll
+  for (int i = 0; i < kPlans; ++i) {
+    const float cost = __uint_as_float(costs[2 * i]);
     if (cost < best) {
       best = cost;
-      line.most = static_cast<int>(most);
+      line.most = costs[2 * i + 1];
     }
   }
-  mine = 0;
-  for (int b = b0; b < b1; ++b) {
-    TreeRequest r;
-    tree_request(p, b, r);
-    pre[b] = mine;  // within this thread's requests
-    mine += items(r) * (line.most > 0 ? (chunks_of(r.len) + line.most - 1u) / static_cast<uint32_t>(line.most) : chunks_of(r.len));
+  // each thread's requests, then those of the threads before
+  const int each = above(p.B, kThreads), b0 = min(p.B, tid * each);
+  uint32_t mine[kEach], sum = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int b = b0 + i;
+    mine[i] = sum;
+    if (i < each && b < p.B) sum += pre[b] * (line.most > 0 ? above(chunks[b], line.most) : chunks[b]);
   }
-  long long sum = mine;
+  uint32_t upto = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long up = __shfl_up_sync(0xffffffffu, sum, o);
-    if (lane >= o) sum += up;
+    const uint32_t up = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += up;
   }
+  uint32_t* ends = costs + 2 * kPlans + 1;
+  if (lane == 31) ends[warp] = upto;
   __syncthreads();
-  if (lane == 31) scratch[warp] = sum;
-  __syncthreads();
-  sum -= mine;
-  for (int w = 0; w < warp; ++w) sum += scratch[w];
-  for (int b = b0; b < b1; ++b) pre[b] += sum;
-  if (tid == kThreads - 1) pre[p.B] = sum + mine;
+  const uint32_t before = __reduce_add_sync(0xffffffffu, lane < warp ? ends[lane] : 0u) + upto - sum;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    if (i < each && b0 + i < p.B) pre[b0 + i] = before + mine[i];
+  }
+  if (tid == kThreads - 1) pre[p.B] = before + sum;
   __syncthreads();
   return line;
 }
+static_assert(kThreads / 32 <= 32, "a lane a warp");
 
 // The piece at `u` of the line; of a range that ends at u1
 template <int ROWS>
-__device__ __forceinline__ Work work_at(const TreeArgs& p, const Line& line, long long u, long long u1, int G) {
+__device__ __forceinline__ Work work_at(const TreeArgs& p, const Line& line, uint32_t u, uint32_t u1, uint32_t G) {
   int lo = 0, hi = p.B;  // pre[lo] <= u < pre[hi]
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
@@ -238,33 +244,34 @@ __device__ __forceinline__ Work work_at(const TreeArgs& p, const Line& line, lon
   w.t0 = r.t0;
   w.len = r.len;
   w.n = r.n;
-  const int n = chunks_of(r.len);
-  const long long rel = u - line.pre[lo];
-  long long item;
+  const uint32_t n = chunks_of(r.len), rel = u - line.pre[lo];
+  uint32_t item;
   if (line.most > 0) {
-    w.of = (n + line.most - 1) / line.most;
-    item = rel / w.of;
-    w.j = static_cast<int>(rel - item * w.of);
-    const int least = n / w.of, more = n - least * w.of;
-    w.from = w.j * least + min(w.j, more);
-    w.chunks = least + (w.j < more ? 1 : 0);
-    w.slot = static_cast<int>(min(u, static_cast<long long>(kPartials - 1)));  // used if the item is cut: then u < kPartials
+    const uint32_t of = above(n, line.most);
+    item = rel / of;
+    const uint32_t j = rel - item * of, least = n / of, more = n - least * of;
+    w.of = static_cast<int>(of);
+    w.j = static_cast<int>(j);
+    w.from = static_cast<int>(j * least + min(j, more));
+    w.chunks = static_cast<int>(least + (j < more ? 1 : 0));
+    w.slot = static_cast<int>(min(u, static_cast<uint32_t>(kPartials - 1)));  // used if the item is cut: then u < kPartials
     w.first = ~(w.slot - w.j);
   } else {
     item = rel / n;
     w.from = static_cast<int>(rel - item * n);
-    const long long start = u - w.from, end = start + n;
+    const uint32_t start = u - w.from, end = start + n;
     w.chunks = static_cast<int>(min(end, u1) - u);
     w.first = static_cast<int>(start / line.per);
     w.j = static_cast<int>(u / line.per) - w.first;
     w.of = static_cast<int>((end - 1) / line.per) - w.first + 1;
     w.slot = 2 * (w.first + w.j) + (w.j == 0 ? 1 : 0);
   }
-  w.kvh = static_cast<int>(item % p.n_kv_heads);
-  w.row0 = static_cast<int>(item / p.n_kv_heads) * ROWS;
-  w.rows = min(ROWS, r.n * G - w.row0);
+  const uint32_t tile = item / static_cast<uint32_t>(p.n_kv_heads);
+  w.kvh = static_cast<int>(item - tile * p.n_kv_heads);
+  w.row0 = static_cast<int>(tile * ROWS);
+  w.rows = min(ROWS, static_cast<int>(r.n * G) - w.row0);
   w.pair = w.rows > kTile;
-  w.has_new = w.from + w.chunks == n;
+  w.has_new = w.from + w.chunks == static_cast<int>(n);
   return w;
 }
 // slot of piece j of an item: at most one cut item begins in a range (slot 2 cta + 1) and one ends there (2 cta)
@@ -316,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
   float* scales = reinterpret_cast<float*>(smem + L::kOffScale);
   float* row_factor = reinterpret_cast<float*>(smem + L::kOffFactor);
   float2* ml_of = reinterpret_cast<float2*>(smem + L::kOffMl);
-  long long* scratch = reinterpret_cast<long long*>(smem + L::kOffScratch);
+  uint32_t* scratch = reinterpret_cast<uint32_t*>(smem + L::kOffScratch);
   constexpr int kScaleRing = L::kScaleRing > 0 ? L::kScaleRing : 1;
   if ((smem_addr(smem) & 1023u) != 0u) {  // the swizzled operands need a 1024-byte aligned base
     if (tid == 0) set_status(p.status, kStatusDeviceArg);
@@ -350,7 +357,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  const Line line = line_of<L::kRows>(p, reinterpret_cast<long long*>(smem + L::kPlan), scratch);
+  const Line line = line_of<L::kRows>(p, reinterpret_cast<uint32_t*>(smem + L::kPlan), reinterpret_cast<uint32_t*>(smem + L::kPlan) + kMaxSequences + 1, scratch);
   fence_proxy_async();
   tc_fence_before();
   __syncthreads();
@@ -372,24 +379,24 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
   if (warp == kSchedWarp) {
     // ---------------------------------------------------------------- pieces
     int* header = static_cast<int*>(p.workspace);
-    const long long total = line.pre[p.B];
+    const uint32_t total = line.pre[p.B];
     const bool queue = line.most > 0;
-    long long u = queue ? blockIdx.x : blockIdx.x * line.per;
-    const long long u1 = queue ? total : min(total, u + line.per);
+    uint32_t u = queue ? blockIdx.x : blockIdx.x * line.per;
+    const uint32_t u1 = queue ? total : min(total, u + line.per);
 #pragma unroll 1
     for (int ord = 0;; ++ord) {
       if (ord >= kWorkRing && !wait_or_abort(wempty + ord % kWorkRing, (ord / kWorkRing - 1) & 1, p.status, abort)) break;
       if (lane == 0) {
         Work w{};
         w.kvh = -1;
-        if (u < u1) w = work_at<L::kRows>(p, line, u, u1, static_cast<int>(G));
+        if (u < u1) w = work_at<L::kRows>(p, line, u, u1, G);
         works[ord % kWorkRing] = w;
         mbar_arrive(wfull + ord % kWorkRing);
-        if (u < u1) u = queue ? gridDim.x + static_cast<long long>(atomicAdd(reinterpret_cast<unsigned*>(header), 1u)) : u + w.chunks;
-        else u = -1;
+        if (w.kvh >= 0) u = queue ? gridDim.x + atomicAdd(reinterpret_cast<unsigned*>(header), 1u) : u + w.chunks;
+        else u = 0xffffffffu;
       }
       u = __shfl_sync(0xffffffffu, u, 0);
-      if (u < 0) break;
+      if (u == 0xffffffffu) break;
     }
     if (lane == 0 && atomicAdd(reinterpret_cast<unsigned*>(header) + 1, 1u) == gridDim.x - 1) {
       header[0] = 0;  // every CTA has taken its last piece
@@ -584,16 +591,16 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
           cp_async_commit();  // waited for with the piece's first chunk
         } else {
 #pragma unroll 1
-          for (int r1 = qt >> 4; r1 < to; r1 += 64) {  // four rows at a time
-            uint4 x[4];
+          for (int r1 = qt >> 4; r1 < to; r1 += 128) {  // eight rows at a time
+            uint4 x[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int e = 0; e < 8; ++e) {
               const int r = r1 + 16 * e;
               const uint32_t row = w.row0 + r, token = row / G;
               x[e] = r < w.rows ? __ldg(reinterpret_cast<const uint4*>(q + token * p.q_stride + (row - token * G) * kD)) : make_uint4(0u, 0u, 0u, 0u);
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int e = 0; e < 8; ++e) {
               const int r = r1 + 16 * e;
               float power = 1.f;
               if (BF) {
@@ -672,20 +679,26 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
             const int nu = pt & 15;
             const uint16_t* from = fresh + w.t0 * p.new_stride + w.kvh * kD + nu * 8;
 #pragma unroll 1
-            for (int r = pt >> 4; r < kMaxDrafts; r += 8) {
-              const bool there = r < w.n;
-              uint4 x = there ? __ldg(reinterpret_cast<const uint4*>(from + r * p.new_stride)) : make_uint4(0u, 0u, 0u, 0u);
-              if (is_v) x = take_out_wild<BF>(x, found);
-              float power = 1.f;
-              if (BF) {
-                power = row_power(row_max16(top_of(x)));
-                x = bf16_to_half(x, inverse_power(power));
+            for (int r1 = pt >> 4; r1 < kMaxDrafts; r1 += 32) {  // four rows at a time
+              uint4 x[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                x[e] = r1 + 8 * e < w.n ? __ldg(reinterpret_cast<const uint4*>(from + (r1 + 8 * e) * p.new_stride)) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int r = r1 + 8 * e;
+                if (is_v) x[e] = take_out_wild<BF>(x[e], found);
+                float power = 1.f;
+                if (BF) {
+                  power = row_power(row_max16(top_of(x[e])));
+                  x[e] = bf16_to_half(x[e], inverse_power(power));
+                }
+                if (nu == 0) {
+                  to_scales[r] = r < w.n ? power : 0.f;
+                  to_scales[kMaxDrafts + r] = 0.f;
+                }
+                *reinterpret_cast<uint4*>(slot + tile_off(r, nu)) = x[e];
               }
-              if (nu == 0) {
-                to_scales[r] = there ? power : 0.f;
-                to_scales[kMaxDrafts + r] = 0.f;
-              }
-              *reinterpret_cast<uint4*>(slot + tile_off(r, nu)) = x;
             }
             if (found) wild[ord & 3] = ord + 1;
           }
