@@ -592,12 +592,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
         } else {
 #pragma unroll 1
           for (int r1 = qt >> 4; r1 < to; r1 += 128) {  // eight rows at a time
+            // (token, head of the group) of row r1 + 16 qu by lane qu: a division for eight rows
+            const uint32_t row = w.row0 + r1 + 16 * (qu & 7), of = row / G, place = of << 16 | (row - of * G);
             uint4 x[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              const int r = r1 + 16 * e;
-              const uint32_t row = w.row0 + r, token = row / G;
-              x[e] = r < w.rows ? __ldg(reinterpret_cast<const uint4*>(q + token * p.q_stride + (row - token * G) * kD)) : make_uint4(0u, 0u, 0u, 0u);
+              const uint32_t at = __shfl_sync(0xffffffffu, place, e, 16);
+              x[e] = r1 + 16 * e < w.rows ? __ldg(reinterpret_cast<const uint4*>(q + (at >> 16) * p.q_stride + (at & 0xffffu) * kD))
+                                          : make_uint4(0u, 0u, 0u, 0u);
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -940,10 +942,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
       // written in 128-byte or, as sums, 64-byte pieces by neighbouring lanes; unit u of row r lies at u ^ (r mod 8)
       float* place = reinterpret_cast<float*>(smem + warp * 4096);
       float* slot = slots_of(p) + static_cast<size_t>(w.slot) * slot_floats(L::kRows);
-      uint16_t* out = static_cast<uint16_t*>(p.out);
+      uint16_t* out = static_cast<uint16_t*>(p.out) + w.t0 * p.n_heads * kD;
       const int d_from = w.pair ? 0 : t * (kD / 2), d_to = w.pair ? kD : d_from + kD / 2;
       const uint32_t own = ocol + (w.pair ? t * kTile : 0);
       const int row_base = (w.pair ? t * kTile : 0) + (warp & 3) * 32;
+      const uint32_t line_at = token * p.n_heads + head;  // of this lane's row, from the request's first on
       if (row_base < w.rows) {
 #pragma unroll 1
         for (int d = d_from; d < d_to; d += 32) {
@@ -980,14 +983,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
             *reinterpret_cast<float4*>(place + lane * 32 + ((e ^ (lane & 7)) << 2)) = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
           __syncwarp();
           const int e = lane & 7;
-#pragma unroll 2
+#pragma unroll 4
           for (int k = lane >> 3; k < 32; k += 4) {
             const int row = row_base + k;
+            const uint32_t row_line = __shfl_sync(0xffffffffu, line_at, k);
             if (row < w.rows) {
               const float4 y = *reinterpret_cast<const float4*>(place + k * 32 + ((e ^ (k & 7)) << 2));
               if (whole) {
-                const uint32_t a = w.row0 + row, to = a / G;
-                *reinterpret_cast<uint2*>(out + ((w.t0 + to) * p.n_heads + w.kvh * G + (a - to * G)) * kD + d + 4 * e) =
+                *reinterpret_cast<uint2*>(out + row_line * kD + d + 4 * e) =
                     make_uint2(pack16<BF>(y.x, y.y), pack16<BF>(y.z, y.w));
               } else {
                 __stcg(reinterpret_cast<float4*>(slot + row * kD + d) + e, y);
