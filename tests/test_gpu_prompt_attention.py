@@ -145,6 +145,23 @@ def test_many_sequences():
     agree(make(lens.tolist(), heads=2, kv_heads=1, seed=11))
 
 
+@pytest.mark.parametrize("causal", [True, False])
+def test_items_of_one_and_two_tiles_of_uneven_length(causal):
+    lens = [100, 300, 129, 128, 500, 20, 0, 257]
+    past = [700, 0, 260, 900, 5, 130, 40, 128]
+    agree(make(lens, [a + b for a, b in zip(lens, past)], heads=32, kv_heads=32, seed=14), causal)
+
+
+@pytest.mark.parametrize("lens,heads", [([3, 200, 40], 16), ([130, 1, 300], 8)])
+def test_sequences_with_more_queries_than_keys(lens, heads):
+    agree(make(lens, [n // 2 for n in lens], heads=heads, kv_heads=2, seed=15))
+
+
+def test_more_items_than_one_wave_of_blocks_takes():
+    rng = np.random.default_rng(16)
+    agree(make(rng.integers(0, 7, 1000).tolist(), heads=16, kv_heads=16, seed=16))
+
+
 def test_a_bad_sequence_is_reported_and_passed_over():
     c = make([40, 30, 50], seed=12)
     want, want_lse = oracle(c)
