@@ -492,8 +492,10 @@ void fsx_session_destroy(fsx_session s);
  *     16 bytes); outputs and caches are contiguous. Offsets may exceed 32 bits in elements.
  *   - d_status: DEVICE int, not NULL, that the caller zeroes once and reads when it likes. A
  *     call that finds an error writes its code there unless one is there already; no call clears it.
- *   - Softmax statistics and sums are fp32. Weights of the values are rounded to the type of the
- *     values, or for e4m3 caches to a sum of e4m3 parts that carries as many bits as the type.
+ *   - Scores, softmax statistics and sums are fp32. Weights of the values are rounded to `dtype`. Over
+ *     an 8-bit cache the products are in fp16: weights are rounded to fp16, codes are exact in it, and
+ *     rows of bf16 that meet codes become fp16 times a power of two a row, exact for values of at
+ *     least 2^-22 of the row's largest; smaller ones may lose their last bits.
  *   - A key that a row does not see has no effect on it, whatever the key and value hold (NaN and
  *     infinities too). A row that sees no key gets zeros and a log-sum-exp of -infinity.
  *   - Asynchronous on `stream`; nothing is allocated. */
@@ -529,11 +531,12 @@ fsx_status fsx_cache_read_e4m3(const void* d_k_cache, const void* d_v_cache, con
  *   d_q        : DEVICE [q_rows] rows of `dtype` (FSX_BF16 or FSX_F16), q_stride apart.
  *   d_k, d_v   : DEVICE [kv_rows] rows of the same type, kv_stride apart.
  *   d_q_offsets, d_kv_offsets : DEVICE int64 [B+1], non-decreasing, within 0 .. q_rows / kv_rows.
- *                B is 1 .. 1024; q_rows and kv_rows are below 2^31.
+ *                B is 1 .. 1024; kv_rows and q_rows times the heads per kv head are below 2^31 - 257.
  *   d_out      : DEVICE [q_rows, n_heads, 128] of `dtype`; rows of no sequence stay unwritten.
  *   d_lse      : DEVICE fp32 [n_heads, q_rows], natural log-sum-exp of the scaled scores, or NULL.
  * A sequence whose offsets are negative, decrease or pass the rows sets FSX_ERR_DEVICE_ARG and
- * gets no output row; the others are written. */
+ * gets no output row; the others are written. (Where offsets go back, sequences may overlap: if they
+ * name more than q_rows rows together, some of these may stay unwritten too.) */
 fsx_status fsx_prompt_attention(const void* d_q, long long q_stride, const void* d_k, const void* d_v,
                                 long long kv_stride, int dtype, const int64_t* d_q_offsets,
                                 const int64_t* d_kv_offsets, int B, long long q_rows, long long kv_rows,

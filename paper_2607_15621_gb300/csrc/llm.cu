@@ -122,6 +122,9 @@ fsx_status fsx_prompt_attention(const void* d_q, long long q_stride, const void*
   if (kv_rows > 0 && (s = check_stride("d_k", d_k, kv_stride, n_kv_heads, 2)) != FSX_OK) return s;
   if (kv_rows > 0 && (s = check_stride("d_v", d_v, kv_stride, n_kv_heads, 2)) != FSX_OK) return s;
   if (!aligned16(d_out)) return fail(FSX_ERR_INVALID_ARG, "d_out must be 16-byte aligned");
+  const long long group_rows = q_rows * (n_heads / n_kv_heads);
+  if (group_rows >= kMaxRows - 256 || (group_rows / 256 + B) * n_kv_heads >= kMaxRows - 65536)
+    return fail(FSX_ERR_UNSUPPORTED, "q_rows times the heads per kv head must be below 2^31 - 257, and 256-row items below 2^31 - 65537");
   const fsx::PromptArgs a{d_q,    q_stride, d_k,     d_v,     kv_stride,  d_q_offsets, d_kv_offsets, B,
                           q_rows, kv_rows,  n_heads, n_kv_heads, causal, d_out,       d_lse,        d_status};
   return launched(fsx::launch_prompt_attention(a, dtype, static_cast<cudaStream_t>(stream)), "prompt attention");

@@ -71,6 +71,12 @@ def test_cache_write_and_read_refuse(lib, over, code):
     assert fsx.last_error()
 
 
+def test_prompt_attention_refuses_more_rows_than_it_counts(lib):
+    for over in (dict(qr=(1 << 30) - 100), dict(qr=(1 << 31) - 1, H=4096, Hk=4096, qs=4096 * 128, kvs=4096 * 128)):
+        assert lib.fsx_prompt_attention(*dict(PROMPT, **over).values()) == UNS
+        assert fsx.last_error()
+
+
 def test_nothing_to_do_is_no_error(lib):
     assert lib.fsx_prompt_attention(*dict(PROMPT, qr=0, q=None, out=None).values()) == fsx.FSX_OK
     assert lib.fsx_tree_attention(*dict(TREE, nr=0, q=None, out=None).values()) == fsx.FSX_OK
