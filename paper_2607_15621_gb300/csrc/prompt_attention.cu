@@ -597,6 +597,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
                            pack16<BF>(x[8 * e + 4], x[8 * e + 5]), pack16<BF>(x[8 * e + 6], x[8 * e + 7]));
         }
         tc_fence_before();
+        fence_proxy_async();  // the next copy into the stage comes behind these writes
         __syncwarp();
         if (lane == 0) mbar_arrive(oread + t);
       }
@@ -605,20 +606,24 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
       RowWalk at(first + r2, G, two);
       out += (static_cast<long long>(at.token) * p.n_heads + at.head) * kD;
       const int step = (two.x * p.n_heads + two.y) * kD, wrap = (p.n_heads - static_cast<int>(G)) * kD;
-#pragma unroll 2
-      for (int k = 0; k < 16; ++k, r2 += 2) {
-        if (r2 < rows)
-          *reinterpret_cast<uint4*>(out) =
-              n > 0 ? *reinterpret_cast<const uint4*>(staged + tile_off(r2, lane & 15)) : make_uint4(0u, 0u, 0u, 0u);
-        out += step;
-        at.head += two.y;
-        if (at.head >= G) {
-          at.head -= G;
-          out += wrap;
+#pragma unroll 1
+      for (int k = 0; k < 16; k += 8) {  // eight rows are read, then written: a store may not be passed by a read
+        uint4 x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          x[e] = n > 0 ? *reinterpret_cast<const uint4*>(staged + tile_off(r2 + 2 * e, lane & 15)) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int e = 0; e < 8; ++e, r2 += 2) {
+          if (r2 < rows) *reinterpret_cast<uint4*>(out) = x[e];
+          out += step;
+          at.head += two.y;
+          if (at.head >= G) {
+            at.head -= G;
+            out += wrap;
+          }
         }
       }
       if (n > 0) {
-        fence_proxy_async();
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(empty + stage);
@@ -646,9 +651,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
 
 cudaError_t launch_prompt_attention(const PromptArgs& a, int dtype, cudaStream_t stream) {
   const long long G = a.n_heads / a.n_kv_heads;
-  // at most this many items: every sequence rounds up once
+  // at most this many items, which the caller keeps below 2^31: every sequence rounds up once
   const long long items = (a.q_rows * G / kItemRows + a.B) * a.n_kv_heads;
-  if (items > 0x7fffffffll - 65536 || a.q_rows * G >= 0x7fffffffll - kItemRows) return cudaErrorInvalidConfiguration;
   const int sms = sm_count();
   if (sms == 0) return cudaErrorNoDevice;
   // one CTA per SM; beyond kMaxRounds items each, further waves of CTAs
