@@ -54,7 +54,8 @@ constexpr int kOffItems = kOffBar + kNumBars * 8 + 32;
 
 struct Maps {
   CUtensorMap k, v;
-  CUtensorMap q;  // if G divides a tile: [64 columns, heads, rows, 2 blocks], a box is a tile
+  CUtensorMap q;    // if G divides a tile: [64 columns, heads, rows, 2 blocks], a box is a tile
+  CUtensorMap out;  // if G divides a warp's 32 rows: the same, a box is 32 rows
 };
 
 // Rows (token G + head) are counted in 32 bits: 2^31 rows of queries would be 550 GB. Each 64-bit division is some
@@ -79,6 +80,11 @@ static_assert(kMaxSequences * sizeof(Sequence) <= kStages * kStageBytes, "the se
 // keys that query token i of (nq, nk) sees
 __device__ __forceinline__ int sees(int causal, int nq, int nk, int i) {
   return causal ? max(0, min(nk, i + 1 + nk - nq)) : nk;
+}
+
+// Byte offset of 16-byte unit u of row r of a warp's 32 output rows: two swizzled blocks of 64 columns, 4 KB apart
+__device__ __forceinline__ uint32_t out_off(int r, int u) {
+  return static_cast<uint32_t>((u >> 3) * 4096 + r * 128 + (((u & 7) ^ (r & 7)) << 4));
 }
 
 // items of a sequence with at least c chunks (c = 0: all of them); they are its last ones
@@ -565,7 +571,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
       tc_fence_after();
       const float inv = l == 0.f ? 0.f : 1.f / l;
       const int stage = (c0 + (t == 0 ? 2 * n - 2 : 2 * n - 1)) % kStages;
-      unsigned char* staged = smem + kOffRing + (n > 0 ? stage : 0) * kStageBytes;
+      unsigned char* staged = smem + kOffRing + (n > 0 ? stage : 0) * kStageBytes + (warp & 3) * 8192;  // this warp's 32 rows
       const bool found = wild[i & 3] == i + 1;
       uint16_t* out = static_cast<uint16_t*>(p.out) + (it.q0 * p.n_heads + it.kvh * G) * kD + (lane & 15) * 8;
       if (n > 0) {
@@ -592,7 +598,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            *reinterpret_cast<uint4*>(staged + tile_off(r, c / 8 + e)) =
+            *reinterpret_cast<uint4*>(staged + out_off(lane, c / 8 + e)) =
                 make_uint4(pack16<BF>(x[8 * e], x[8 * e + 1]), pack16<BF>(x[8 * e + 2], x[8 * e + 3]),
                            pack16<BF>(x[8 * e + 4], x[8 * e + 5]), pack16<BF>(x[8 * e + 6], x[8 * e + 7]));
         }
@@ -603,35 +609,45 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
       }
       const int rows = static_cast<int>(it.nq * G - first);
       int r2 = (r & ~31) + (lane >> 4);  // this warp's 32 rows, two at a time
-      RowWalk at(first + r2, G, two);
-      out += (static_cast<long long>(at.token) * p.n_heads + at.head) * kD;
-      const int step = (two.x * p.n_heads + two.y) * kD, wrap = (p.n_heads - static_cast<int>(G)) * kD;
-#pragma unroll 1
-      for (int k = 0; k < 16; k += 8) {  // eight rows are read, then written: a store may not be passed by a read
-        uint4 x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          x[e] = n > 0 ? *reinterpret_cast<const uint4*>(staged + tile_off(r2 + 2 * e, lane & 15)) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-        for (int e = 0; e < 8; ++e, r2 += 2) {
-          if (r2 < rows) *reinterpret_cast<uint4*>(out) = x[e];
-          out += step;
-          at.head += two.y;
-          if (at.head >= G) {
-            at.head -= G;
-            out += wrap;
-          }
-        }
-      }
-      if (n > 0) {
-        __syncwarp();
+      const bool by_tma = n > 0 && 32 % G == 0 && (r & ~31) + 32 <= rows;
+      if (by_tma) {
         if (lane == 0) {
-          mbar_arrive(empty + stage);
-          if (t == 0 && it.n[1] < n_all) mbar_arrive(empty + (c0 + 2 * n_all - 1) % kStages);  // there is no tile 1
+          tma_store_chunk(&maps.out, staged, it.kvh * G, static_cast<int>(it.q0) + (first + (r & ~31)) / G, 0);
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+      } else {
+        RowWalk at(first + r2, G, two);
+        out += (static_cast<long long>(at.token) * p.n_heads + at.head) * kD;
+        const int step = (two.x * p.n_heads + two.y) * kD, wrap = (p.n_heads - static_cast<int>(G)) * kD;
+#pragma unroll 1
+        for (int k = 0; k < 16; k += 8) {  // eight rows are read, then written: a store may not be passed by a read
+          uint4 x[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            x[e] = n > 0 ? *reinterpret_cast<const uint4*>(staged + out_off((r2 + 2 * e) & 31, lane & 15)) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+          for (int e = 0; e < 8; ++e, r2 += 2) {
+            if (r2 < rows) *reinterpret_cast<uint4*>(out) = x[e];
+            out += step;
+            at.head += two.y;
+            if (at.head >= G) {
+              at.head -= G;
+              out += wrap;
+            }
+          }
         }
       }
       if (mine && p.lse != nullptr)
         p.lse[head * p.q_rows + it.q0 + token] = l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * kLn2;
+      if (n > 0) {
+        __syncwarp();
+        if (lane == 0) {
+          if (by_tma) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+          mbar_arrive(empty + stage);
+          if (t == 0 && it.n[1] < n_all) mbar_arrive(empty + (c0 + 2 * n_all - 1) % kStages);  // there is no tile 1
+        }
+        __syncwarp();
+      }
     }
     c0 += 2 * n_all;
     done += n;
@@ -661,6 +677,8 @@ cudaError_t launch_prompt_attention(const PromptArgs& a, int dtype, cudaStream_t
   int rounds = static_cast<int>((items + grid - 1) / grid);
   Maps maps{};
   if (kTile % G == 0 && !encode_q_map(&maps.q, a.q, a.q_rows, a.n_heads, a.q_stride * 2, static_cast<int>(G), kTile))
+    return cudaErrorInvalidValue;
+  if (32 % G == 0 && !encode_q_map(&maps.out, a.out, a.q_rows, a.n_heads, static_cast<long long>(a.n_heads) * kD * 2, static_cast<int>(G), 32))
     return cudaErrorInvalidValue;
   if (a.kv_rows > 0 && (!encode_kv_map(&maps.k, a.k, a.kv_rows, a.n_kv_heads, a.kv_stride * 2, kTile) ||
                         !encode_kv_map(&maps.v, a.v, a.kv_rows, a.n_kv_heads, a.kv_stride * 2, kTile)))

@@ -152,6 +152,13 @@ __device__ __forceinline__ void tma_load_chunk(void* dst, const CUtensorMap* map
       : "memory");
 }
 
+// The other way, in the caller's bulk group
+__device__ __forceinline__ void tma_store_chunk(const CUtensorMap* map, const void* src, int y, int z, int w) {
+  asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3, %4}], [%5];" ::"l"(map), "r"(0),
+               "r"(y), "r"(z), "r"(w), "r"(smem_addr(src))
+               : "memory");
+}
+
 // Byte offset of 16-byte unit u (0..15) of row r in a [128][128] tile of 16-bit values: two swizzled
 // blocks of 64 columns, 16 KB apart.
 __device__ __forceinline__ uint32_t tile_off(int r, int u) {
