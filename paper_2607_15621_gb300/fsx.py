@@ -379,10 +379,15 @@ def _pitch(t, stride) -> int:
     return stride[0] if t.shape[0] > 1 else max(stride[0], t.shape[1] * t.shape[2])
 
 
+def _alike(v, k) -> bool:
+    """Rows as far apart in both, where the strides of an axis of one entry say nothing."""
+    return _rows(v, v.stride()) and (v.shape[0] < 2 or v.stride(0) == k.stride(0))
+
+
 def _cache8_call(k, v, rows, k_cache, v_cache, k_scale, v_scale):
     codes = _CODES or _codes()
     shape, stride, cs = k.shape, k.stride(), k_cache.shape
-    good = (len(shape) == 3 and len(cs) == 3 and v.shape == shape and v.stride() == stride and v.dtype is k.dtype and
+    good = (len(shape) == 3 and len(cs) == 3 and v.shape == shape and (v.stride() == stride or _alike(v, k)) and v.dtype is k.dtype and
             _rows(k, stride) and cs[1:] == shape[1:] and v_cache.shape == cs and k_cache.dtype is v_cache.dtype and
             codes.get(k_cache.dtype) == FSX_E4M3 and k_cache.is_contiguous() and v_cache.is_contiguous() and
             k_scale.dtype is _F32 and v_scale.dtype is _F32 and k_scale.shape == (cs[1], cs[0]) and
@@ -418,7 +423,7 @@ def prompt_attention(q, k, v, q_offsets, kv_offsets, out, status, lse=None, caus
     codes = _CODES or _codes()
     dtype, qs, ks, q_shape, k_shape = q.dtype, q.stride(), k.stride(), q.shape, k.shape
     good = (len(q_shape) == 3 and len(k_shape) == 3 and k.dtype is dtype and v.dtype is dtype and out.dtype is dtype and
-            v.shape == k_shape and v.stride() == ks and out.shape == q_shape and out.is_contiguous() and
+            v.shape == k_shape and (v.stride() == ks or _alike(v, k)) and out.shape == q_shape and out.is_contiguous() and
             q_shape[2] == k_shape[2] and _rows(q, qs) and _rows(k, ks) and q_offsets.dtype is _I64 and
             kv_offsets.dtype is _I64 and q_offsets.shape == kv_offsets.shape and q_offsets.dim() == 1 and
             q_offsets.is_contiguous() and kv_offsets.is_contiguous() and dtype in codes and
@@ -446,7 +451,7 @@ def tree_attention(q, k_new, v_new, new_offsets, mask, k_cache, v_cache, offsets
     dtype, qs, ks, q_shape, k_shape, cs = q.dtype, q.stride(), k_new.stride(), q.shape, k_new.shape, k_cache.shape
     code = codes.get(k_cache.dtype)
     good = (len(q_shape) == 3 and len(k_shape) == 3 and len(cs) == 3 and k_new.dtype is dtype and v_new.dtype is dtype and
-            out.dtype is dtype and v_new.shape == k_shape and v_new.stride() == ks and out.shape == q_shape and
+            out.dtype is dtype and v_new.shape == k_shape and (v_new.stride() == ks or _alike(v_new, k_new)) and out.shape == q_shape and
             out.is_contiguous() and q_shape[0] == k_shape[0] and q_shape[2] == k_shape[2] and _rows(q, qs) and
             _rows(k_new, ks) and new_offsets.dtype is _I64 and offsets.dtype is _I64 and
             offsets.shape == new_offsets.shape and new_offsets.dim() == 1 and new_offsets.is_contiguous() and

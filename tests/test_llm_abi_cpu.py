@@ -111,3 +111,11 @@ def test_binding_refuses_tensors_that_do_not_fit():
                       offsets=off, out=out, status=st, workspace=z(256, dtype=torch.uint8), k_scale=scale, v_scale=scale), **over)
         with pytest.raises(fsx.FsxError):
             fsx.tree_attention(**a)
+
+
+def test_binding_asks_for_one_stride_only_where_it_means_something():
+    k = torch.zeros(5, 128)[:, None, :]  # one kv head: its stride may be anything
+    assert fsx._alike(k.clone(), k.expand(5, 1, 128).as_strided((5, 1, 128), (128, 0, 1)))
+    assert fsx._alike(torch.zeros(1, 2, 128), torch.zeros(1, 6, 128)[:, :2])
+    assert not fsx._alike(torch.zeros(5, 2, 128), torch.zeros(5, 6, 128)[:, :2])
+    assert not fsx._alike(torch.zeros(5, 128, 2).transpose(1, 2), torch.zeros(5, 2, 128))
