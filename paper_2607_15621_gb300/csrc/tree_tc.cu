@@ -474,6 +474,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
       n0 += w.chunks;
       give_back(ord);
     }
+    pdl_launch_dependents();  // the join's CTAs find their requests under the last results
     if (leader) umma_commit(drain);
     __syncwarp();
     mbar_wait(drain, 0, p.status);
@@ -1026,59 +1027,70 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
   }
 }
 
-// The rows of cut items: a warp a row, 4 dims a lane, the pieces in the order of their keys. ROWS: rows of a slot.
+// The rows of cut items: a warp a row, 4 dims a lane, the pieces in the order of their keys, kJoin of them loaded at
+// once. ROWS: rows of a slot. What does not hang on the pieces is done before they are waited for.
+constexpr int kJoin = 10;
 template <bool BF, int ROWS>
 __global__ void __launch_bounds__(128) tree_join_kernel(const TreeArgs p) {
-  pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const long long at = static_cast<long long>(blockIdx.x) * 4 + warp;  // head * new_rows + token
-  if (at >= p.new_rows * p.n_heads) return;
-  const int head = static_cast<int>(at / p.new_rows);
-  const long long token = at - head * p.new_rows;
+  const long long at = static_cast<long long>(blockIdx.x) * 4 + warp;  // token * n_heads + head
+  const long long token = at / p.n_heads;
+  const int head = static_cast<int>(at - token * p.n_heads);
   long long t0 = -1;  // first token of its request
-  for (int b0 = 0; b0 < p.B && t0 < 0; b0 += 32) {
-    TreeRequest r;
-    const bool mine = b0 + lane < p.B && tree_request(p, b0 + lane, r) && token >= r.t0 && token < r.t0 + r.n;
-    const uint32_t found = __ballot_sync(0xffffffffu, mine);
-    if (found != 0u) t0 = __shfl_sync(0xffffffffu, r.t0, __ffs(found) - 1);
+  if (token < p.new_rows) {
+    for (int b0 = 0; b0 < p.B && t0 < 0; b0 += 32) {
+      TreeRequest r;
+      const bool mine = b0 + lane < p.B && tree_request(p, b0 + lane, r) && token >= r.t0 && token < r.t0 + r.n;
+      const uint32_t found = __ballot_sync(0xffffffffu, mine);
+      if (found != 0u) t0 = __shfl_sync(0xffffffffu, r.t0, __ffs(found) - 1);
+    }
   }
+  const int G = p.n_heads / p.n_kv_heads;
+  const int row = static_cast<int>(token - t0) * G % ROWS;
+  pdl_wait();
   if (t0 < 0) return;
-  const int2 entry = table_of(p)[at];
+  const int2 entry = table_of(p)[head * p.new_rows + token];
   const int of = entry.y;
   if (of <= 1 || of > kPartials || slot_of(entry.x, 0) < 0 || slot_of(entry.x, of - 1) >= kPartials) return;
-  const int G = p.n_heads / p.n_kv_heads;
-  const int row = static_cast<int>((token - t0) * G + head % G) % ROWS;
+  const int my_row = (row + head % G) % ROWS;
   const float* slots = slots_of(p);
   auto slot = [&](int j) { return slots + slot_of(entry.x, j) * slot_floats(ROWS); };
+  float4 v[kJoin];
+  auto load = [&](int j0) {
+#pragma unroll
+    for (int e = 0; e < kJoin; ++e)
+      v[e] = j0 + e < of ? __ldcg(reinterpret_cast<const float4*>(slot(j0 + e) + my_row * kD) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+  };
+  load(0);
   float m = -CUDART_INF_F;
-  for (int j = lane; j < of; j += 32) m = fmaxf(m, __ldcg(slot(j) + ROWS * kD + 2 * row));
+  for (int j = lane; j < of; j += 32) m = fmaxf(m, __ldcg(slot(j) + ROWS * kD + 2 * my_row));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   float l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int j0 = 0; j0 < of; j0 += 32) {
-    const int count = min(32, of - j0);
+#pragma unroll 1
+  for (int j0 = 0; j0 < of; j0 += kJoin) {
+    if (j0 > 0) load(j0);
     float w = 0.f;
-    if (lane < count) {
-      const float2 x = __ldcg(reinterpret_cast<const float2*>(slot(j0 + lane) + ROWS * kD) + row);
+    if (lane < min(kJoin, of - j0)) {
+      const float2 x = __ldcg(reinterpret_cast<const float2*>(slot(j0 + lane) + ROWS * kD) + my_row);
       w = weight_of(x.x, m);
       l += w * x.y;
     }
-#pragma unroll 8
-    for (int j = 0; j < count; ++j) {
-      const float a = __shfl_sync(0xffffffffu, w, j);
-      const float4 v = __ldcg(reinterpret_cast<const float4*>(slot(j0 + j) + row * kD) + lane);
-      o.x += a * v.x;
-      o.y += a * v.y;
-      o.z += a * v.z;
-      o.w += a * v.w;
+#pragma unroll
+    for (int e = 0; e < kJoin; ++e) {
+      const float a = __shfl_sync(0xffffffffu, w, e);
+      o.x += a * v[e].x;
+      o.y += a * v[e].y;
+      o.z += a * v[e].z;
+      o.w += a * v[e].w;
     }
   }
   l = warp_sum(l);
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + (token * p.n_heads + head) * kD + 4 * lane) =
+  *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at * kD + 4 * lane) =
       make_uint2(pack16<BF>(o.x * inv, o.y * inv), pack16<BF>(o.z * inv, o.w * inv));
-  if (p.lse != nullptr && lane == 0) p.lse[at] = l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * kLn2;
+  if (p.lse != nullptr && lane == 0) p.lse[head * p.new_rows + token] = l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * kLn2;
 }
 
 struct Kernels {
