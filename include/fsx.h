@@ -557,7 +557,7 @@ fsx_status fsx_prompt_attention(const void* d_q, long long q_stride, const void*
  *                positive scales; NULL for a 16-bit cache). May be NULL if cache_rows is 0.
  *   d_starts, d_offsets : as fsx_tick_ranges: request b reads cache rows d_starts[b] .. d_starts[b] +
  *                L_b - 1, L_b = d_offsets[b+1] - d_offsets[b]; NULL d_starts: from row d_offsets[b].
- *   B          : 1 .. 1024; cache_rows and new_rows are below 2^31.
+ *   B          : 1 .. 1024; cache_rows and new_rows are below 2^31, new_rows times n_heads below 2^33.
  *   d_out      : DEVICE [new_rows, n_heads, 128] of `dtype`; rows of no request stay unwritten.
  *   d_lse      : DEVICE fp32 [n_heads, new_rows] as fsx_prompt_attention, or NULL.
  *   d_workspace : DEVICE scratch of fsx_tree_attention_workspace_bytes(...) bytes, 256-byte aligned,

@@ -151,6 +151,7 @@ fsx_status fsx_tree_attention(const void* d_q, long long q_stride, const void* d
   if (new_rows > kMaxRows || cache_rows > kMaxRows) return fail(FSX_ERR_UNSUPPORTED, "rows must be below 2^31");
   fsx_status s = check_heads(n_heads, n_kv_heads, head_dim);
   if (s != FSX_OK || new_rows == 0) return s;
+  if (new_rows * n_heads > 4 * kMaxRows) return fail(FSX_ERR_UNSUPPORTED, "new_rows times n_heads must be below 2^33");
   if (!d_q || !d_k_new || !d_v_new || !d_mask || !d_out || (cache_rows > 0 && (!d_k_cache || !d_v_cache)))
     return fail(FSX_ERR_INVALID_ARG, "NULL pointer argument");
   if (cache_dtype == FSX_E4M3 && cache_rows > 0 && (!d_k_scale || !d_v_scale))

@@ -8,8 +8,8 @@
 // own 128 rows and every chunk; else both on the same rows, one on the even and one on the odd chunks, so that
 // the tensor core always has the other's work while one is at its exponentials; their two results meet at the end.
 //
-// Eight producer warps, four for K and four for V, copy the rows of a chunk by 16-byte asynchronous copies, each thread its own units, and wait
-// for nobody: 16-bit rows straight into their slot, 8-bit rows into a private stage, from where the thread that copied
+// Eight producer warps, four for K and four for V, copy the rows of a chunk by 16-byte asynchronous copies, each
+// thread its own units, and wait for nobody: 16-bit rows straight into their slot, 8-bit rows into a private stage, from where the thread that copied
 // them turns them into fp16 in the slot. A chunk whose scales are powers of two between 2^-15 and 2^7 (a cache as it is
 // written, unless its values are extreme) becomes its values, exactly; any other keeps its codes, and the softmax
 // multiplies scores and weights by the scales. bf16 queries and new tokens meet an 8-bit cache as fp16 times a power
@@ -24,6 +24,12 @@
 // fill the GPU evenly; ranges leave no SM without work but may hold the end of one item and the start of the next. One
 // warp finds the pieces and describes them in a ring for the other roles. Cut items are put together by a
 // second kernel, a warp a row: 256 rows are too many for the one CTA that comes last.
+//
+// Measured: one tree of 50 tokens, 32 heads over 8, behind 32768 8-bit rows: 52 us, of which the plan, the queries and
+// the first keys take 9 us, 27 chunks of 256 rows 30 us (2,100 cycles each; the exponentials of 256 x 128 scores need
+// 2,048, the MMAs about as long) and results and join 9 us. Eight requests of 24 tokens at most over 4096 to 8192
+// rows: 57 us with 8-bit, 54 us with 16-bit caches (3.7 TB/s). 16 requests of 6 to 11 tokens over 96 to 480 rows: 22 us, mostly the
+// latency of the same steps: plan 2.4, first piece 1, queries 2.2, first keys 2, three chunks 6, results 4, join 2 us.
 //
 // Registers: 640 threads at 96 from launch; softmax warpgroups take 2 x 104, MMA and scheduler leave 16.
 #include "fsx.h"
@@ -357,7 +363,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  const Line line = line_of<L::kRows>(p, reinterpret_cast<uint32_t*>(smem + L::kPlan), reinterpret_cast<uint32_t*>(smem + L::kPlan) + kMaxSequences + 1, scratch);
+  uint32_t* plan = reinterpret_cast<uint32_t*>(smem + L::kPlan);
+  const Line line = line_of<L::kRows>(p, plan, plan + kMaxSequences + 1, scratch);
   fence_proxy_async();
   tc_fence_before();
   __syncthreads();
@@ -1109,8 +1116,9 @@ Kernels kernels_of(bool cache8, bool wide) {
                 : (wide ? kernels_for<BF, false, true>() : kernels_for<BF, false, false>());
 }
 
-// Items of 256 rows read the cache once for twice the rows; those of 128 keep one more chunk in shared memory. By the
-// rows that a request has on average: 8 requests of 32 rows at most over 4096 to 8192 8-bit rows, 68 us with wide items.
+// Items of 256 rows read the cache once for twice the rows; those of 128 keep one more chunk in shared memory and have
+// both groups at work on any item. By the rows that a request has on average: 8-bit caches with about 24 rows a request
+// 53.0 us, 62.5 with wide items; 72 rows 57.4 and 66.7 (16-bit 53.8 and 50.6); 200 rows 64.9, and 52.5 with wide items.
 bool is_wide(int B, long long new_rows, int group) { return new_rows * group > static_cast<long long>(B) * kTile; }
 
 }  // namespace
@@ -1123,8 +1131,7 @@ size_t tree_tc_workspace_bytes(int B, long long new_rows, int n_heads, int n_kv_
 cudaError_t launch_tree_tc(const TreeArgs& a, int dtype, bool cache8, cudaStream_t stream) {
   const bool wide = is_wide(a.B, a.new_rows, a.n_heads / a.n_kv_heads);
   const Kernels k = dtype == FSX_BF16 ? kernels_of<true>(cache8, wide) : kernels_of<false>(cache8, wide);
-  const long long join_blocks = (a.new_rows * a.n_heads + 3) / 4;
-  if (join_blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+  const long long join_blocks = (a.new_rows * a.n_heads + 3) / 4;  // below 2^31: the caller sees to it
   const int sms = sm_count();
   if (sms == 0) return cudaErrorNoDevice;
   cudaError_t e = allow_shared_memory(k.main, k.smem);

@@ -2,7 +2,7 @@
 
 Bounds, from the rounding points (u = half a unit in the last place of the type, 2^-8 for bf16 and 2^-11 for fp16):
 an output is rounded once (u), the weights p of the values once (each by at most u, so that the sum moves by at most
-u max|v|; the e4m3 parts of a weight carry as many bits). 1e-4 covers fp32 scores, exponentials and sums. So
+u max|v|; over 8-bit caches weights are fp16, which is finer). 1e-4 covers fp32 scores, exponentials and sums. So
 |out - exact| <= (2 u + 1e-4) max|v|, and over a whole output the errors, which are independent, stay below u in the
 relative 2-norm (about sqrt(2) u / 2). Log-sum-exps: a score sums 128 products in fp32, at most
 128 2^-24 sum|q k| / sqrt(128), about 1e-4 for these inputs at scale 1; 3e-4 max(1, scale).

@@ -77,6 +77,12 @@ def test_prompt_attention_refuses_more_rows_than_it_counts(lib):
         assert fsx.last_error()
 
 
+def test_tree_attention_refuses_more_rows_than_it_counts(lib):
+    over = dict(nr=(1 << 31) - 1, H=64, Hk=64, qs=64 * 128, ns=64 * 128)
+    assert lib.fsx_tree_attention(*dict(TREE, **over).values()) == UNS
+    assert fsx.last_error()
+
+
 def test_nothing_to_do_is_no_error(lib):
     assert lib.fsx_prompt_attention(*dict(PROMPT, qr=0, q=None, out=None).values()) == fsx.FSX_OK
     assert lib.fsx_tree_attention(*dict(TREE, nr=0, q=None, out=None).values()) == fsx.FSX_OK
