@@ -31,7 +31,8 @@
 // rows: 57 us with 8-bit, 54 us with 16-bit caches (3.7 TB/s). 16 requests of 6 to 11 tokens over 96 to 480 rows: 22 us, mostly the
 // latency of the same steps: plan 2.4, first piece 1, queries 2.2, first keys 2, three chunks 6, results 4, join 2 us.
 //
-// Registers: 640 threads at 96 from launch; softmax warpgroups take 2 x 104, MMA and scheduler leave 16.
+// Registers: 640 threads at 96 from launch; softmax warpgroups take 2 x 128, producers keep 2 x 88, MMA and scheduler 48
+// (with 104, 96 and 80 the softmax spilled into its loop: the wide tree 52.4 for 49.8 us).
 #include "fsx.h"
 #include "kernels.h"
 #include "llm.h"
@@ -382,7 +383,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
   auto wait_chunk = [&](uint64_t* ring, int n) { return wait_or_abort(ring + (n & 3), (n >> 2) & 1, p.status, abort); };
 
   if (warp >= kMmaWarp && warp < kProdWarp) {
-  leave_registers<80>();
+  leave_registers<48>();
   if (warp == kSchedWarp) {
     // ---------------------------------------------------------------- pieces
     int* header = static_cast<int*>(p.workspace);
@@ -487,6 +488,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
     mbar_wait(drain, 0, p.status);
   }
   } else if (warp >= kProdWarp) {
+    leave_registers<88>();
     // ---------------------------------------------------------------- producers
     // Four warps make the K chunks ready, four the V chunks. A thread's units: of 16-bit rows, unit u of rows r0, r0 + 8,
     // ...; of codes, which are copied and converted 64 rows at a time, units u and u + 4 of rows r0 and r0 + 32: four
@@ -599,18 +601,18 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
           cp_async_commit();  // waited for with the piece's first chunk
         } else {
 #pragma unroll 1
-          for (int r1 = qt >> 4; r1 < to; r1 += 128) {  // eight rows at a time
-            // (token, head of the group) of row r1 + 16 qu by lane qu: a division for eight rows
-            const uint32_t row = w.row0 + r1 + 16 * (qu & 7), of = row / G, place = of << 16 | (row - of * G);
-            uint4 x[8];
+          for (int r1 = qt >> 4; r1 < to; r1 += 64) {  // four rows at a time
+            // (token, head of the group) of row r1 + 16 qu by lane qu: a division for four rows
+            const uint32_t row = w.row0 + r1 + 16 * (qu & 3), of = row / G, place = of << 16 | (row - of * G);
+            uint4 x[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < 4; ++e) {
               const uint32_t at = __shfl_sync(0xffffffffu, place, e, 16);
               x[e] = r1 + 16 * e < w.rows ? __ldg(reinterpret_cast<const uint4*>(q + (at >> 16) * p.q_stride + (at & 0xffffu) * kD))
                                           : make_uint4(0u, 0u, 0u, 0u);
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < 4; ++e) {
               const int r = r1 + 16 * e;
               float power = 1.f;
               if (BF) {
@@ -739,7 +741,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
     cp_async_wait<0>();
   } else {
     // ---------------------------------------------------------------- softmax of group t
-    take_registers<104>();
+    take_registers<128>();
     const int t = warp >> 2;
     const int r = tid & (kTile - 1);
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
