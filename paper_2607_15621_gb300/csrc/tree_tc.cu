@@ -31,8 +31,9 @@
 // rows: 57 us with 8-bit, 54 us with 16-bit caches (3.7 TB/s). 16 requests of 6 to 11 tokens over 96 to 480 rows: 22 us, mostly the
 // latency of the same steps: plan 2.4, first piece 1, queries 2.2, first keys 2, three chunks 6, results 4, join 2 us.
 //
-// Registers: 640 threads at 96 from launch; softmax warpgroups take 2 x 128, producers keep 2 x 88, MMA and scheduler 48
-// (with 104, 96 and 80 the softmax spilled into its loop: the wide tree 52.4 for 49.8 us).
+// Registers: 640 threads at 96 from launch; softmax warpgroups take 2 x 128, producers keep 2 x 80, MMA and scheduler 64
+// (with 104, 96 and 80 the softmax spilled into its loop, with 128, 88 and 48 the MMA warp into its own: the wide
+// tree 52.4 and 50.2 for 48.9 us).
 #include "fsx.h"
 #include "kernels.h"
 #include "llm.h"
@@ -383,7 +384,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
   auto wait_chunk = [&](uint64_t* ring, int n) { return wait_or_abort(ring + (n & 3), (n >> 2) & 1, p.status, abort); };
 
   if (warp >= kMmaWarp && warp < kProdWarp) {
-  leave_registers<48>();
+  leave_registers<64>();
   if (warp == kSchedWarp) {
     // ---------------------------------------------------------------- pieces
     int* header = static_cast<int*>(p.workspace);
@@ -417,55 +418,59 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
     const uint32_t id_s = idesc_16(kBf, kTile, kTile, false), id_o = idesc_16(kBf, kTile, kD, true);
     const uint32_t slots = smem_addr(smem + L::kOffSlots);
     const uint64_t q_desc = sw128_desc(smem_addr(smem)), k_desc = sw128_desc(slots), v_desc = sw128_desc_mn(slots, 16384, 1024);
+    // What the loop needs of a piece stays in registers and slots are counted on: with a read of shared memory, a
+    // division or a wait more per tile, this warp and not the tensor core was what a chunk took its time for.
     bool ok = true;
-    int n0 = 0, ord = 0;
-    uint32_t p_count0 = 0, p_count1 = 0;
+    int nk = 0, nv = 0;            // chunks whose S, whose P V has been issued
+    uint32_t ks = 0, vs = 1;       // their slots
+    uint32_t counts = 0;           // bits 0, 16: parity of the tiles' next P
 #pragma unroll 1
-    for (; ok; ++ord) {
+    for (int ord = 0; ok; ++ord) {
       if (!find_work(ord)) break;
       const Work& w = works[ord % kWorkRing];
-      const int lag = w.pair ? 1 : 2;
-      bool fresh = ord > 0;
+      const int chunks = w.chunks, has_new = w.has_new;
+      const int lag = w.pair ? 1 : 2, tiles = w.pair ? 2 : 1;
+      ok = wait_or_abort(qfull, ord & 1, p.status, abort);
 #pragma unroll 1
-      for (int j = 0; j < w.chunks + lag && ok; ++j) {
+      for (int j = 0; j < chunks + lag && ok; ++j) {
+        const int jp = j - lag;  // per tile: P V of chunk jp, then S of chunk j
+        if (jp >= 0) {
+          ok = wait_chunk(vfull, nv);
+          if (jp == 0 && ord > 0) ok = ok && wait_or_abort(oread, (ord - 1) & 1, p.status, abort);
+        }
+        if (!ok) break;
+        const uint64_t vd = v_desc + vs * (kSlotBytes >> 4), kd = k_desc + ks * (kSlotBytes >> 4);
+        uint32_t t = tiles == 2 ? 0u : j & 1;  // chunk by chunk, or both tiles
 #pragma unroll 1
-        for (int t = 0; t < 2; ++t) {
-          if (!w.pair && t != (j & 1)) continue;
-          const bool last_tile = !w.pair || t == 1;
+        for (int i = 0; i < tiles; ++i, ++t) {
           const uint32_t s_at = tmem + kColS + t * kTile, o_at = tmem + kColO + t * kTile;
-          const int jp = j - lag;  // P V of chunk jp, then S of chunk j
+          const bool last_tile = i + 1 == tiles;
           if (jp >= 0) {
-            const int n = n0 + jp;
-            ok = wait_or_abort(pfull + t, (t ? p_count1 : p_count0) & 1, p.status, abort) && wait_chunk(vfull, n) &&
-                 (!fresh || wait_or_abort(oread, (ord - 1) & 1, p.status, abort));
+            ok = wait_or_abort(pfull + t, (counts >> (16 * t)) & 1u, p.status, abort);
             if (!ok) break;
-            fresh = false;
-            if (t) ++p_count1;
-            else ++p_count0;
+            counts ^= 1u << (16 * t);
             tc_fence_after();
-            const uint64_t vd = v_desc + ((2 * n + 1) % kSlots) * (kSlotBytes >> 4);
-            const bool more = jp >= lag;  // not the group's first chunk
-            const int steps = w.has_new && jp == w.chunks - 1 ? kMaxDrafts / 64 : kTile / 64;
             if (leader) {
-#pragma unroll 1
-              for (int h = 0; h < steps; ++h) {  // 64 keys
+              const uint32_t more = jp >= lag ? 1u : 0u;  // not the group's first chunk
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                  umma_f16_ta(o_at, s_at + h * 32 + k * 8, vd + (h * 4 + k) * 128, id_o, more || h > 0 || k > 0 ? 1u : 0u);
+              for (int k = 0; k < 4; ++k) umma_f16_ta(o_at, s_at + k * 8, vd + k * 128, id_o, k > 0 ? 1u : more);
+              if (!(has_new && jp == chunks - 1)) {  // 64 keys more
+#pragma unroll
+                for (int k = 4; k < 8; ++k) umma_f16_ta(o_at, s_at + k * 8, vd + k * 128, id_o, 1u);
               }
               if (last_tile) {
-                umma_commit(pdone + (n & 3));
-                if (jp == w.chunks - 1) umma_commit(odone);
+                umma_commit(pdone + (nv & 3));
+                if (jp == chunks - 1) umma_commit(odone);
               }
             }
             __syncwarp();
           }
-          if (j < w.chunks) {
-            const int n = n0 + j;
-            ok = (j > 0 || wait_or_abort(qfull, ord & 1, p.status, abort)) && wait_chunk(kfull, n);
+          if (j < chunks) {
+            // behind P V, which may be what the chunk's slot waits for
+            if (i == 0) ok = wait_chunk(kfull, nk);
             if (!ok) break;
             tc_fence_after();
-            const uint64_t qd = q_desc + (w.pair && t == 1 ? kSlotBytes >> 4 : 0), kd = k_desc + ((2 * n) % kSlots) * (kSlotBytes >> 4);
+            const uint64_t qd = q_desc + (tiles == 2 && t == 1 ? kSlotBytes >> 4 : 0);
             if (leader) {
 #pragma unroll
               for (int k = 0; k < 8; ++k) {
@@ -473,13 +478,20 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
                 umma_f16(s_at, qd + off, kd + off, id_s, k > 0 ? 1u : 0u);
               }
               umma_commit(sfull + t);
-              if (last_tile) umma_commit(sdone + (n & 3));
+              if (last_tile) umma_commit(sdone + (nk & 3));
             }
             __syncwarp();
           }
         }
+        if (jp >= 0) {
+          ++nv;
+          vs = vs + 2 >= kSlots ? vs + 2 - kSlots : vs + 2;
+        }
+        if (j < chunks) {
+          ++nk;
+          ks = ks + 2 >= kSlots ? ks + 2 - kSlots : ks + 2;
+        }
       }
-      n0 += w.chunks;
       give_back(ord);
     }
     pdl_launch_dependents();  // the join's CTAs find their requests under the last results
@@ -488,7 +500,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
     mbar_wait(drain, 0, p.status);
   }
   } else if (warp >= kProdWarp) {
-    leave_registers<88>();
+    leave_registers<80>();
     // ---------------------------------------------------------------- producers
     // Four warps make the K chunks ready, four the V chunks. A thread's units: of 16-bit rows, unit u of rows r0, r0 + 8,
     // ...; of codes, which are copied and converted 64 rows at a time, units u and u + 4 of rows r0 and r0 + 32: four
