@@ -172,6 +172,15 @@ __device__ __forceinline__ bool find_item(const PromptArgs& p, const Sequence* s
   return false;
 }
 
+// two stages on in the ring
+__device__ __forceinline__ void two_on(uint32_t& stage, uint32_t& phase) {
+  stage += 2;
+  if (stage >= kStages) {
+    stage -= kStages;
+    phase ^= 1u;
+  }
+}
+
 // token and head of the group of a packed row, two rows on at a time; `two`: 2 / G and 2 % G
 struct RowWalk {
   uint32_t token, head;
@@ -272,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
     // descriptors change by their addresses alone
     const uint64_t q_desc = sw128_desc(smem_addr(smem)), k_desc = sw128_desc(ring), v_desc = sw128_desc_mn(ring, 16384, 1024);
     bool ok = true;
-    int c0 = 0;
+    uint32_t sk = 0, pk = 0, sv = 1, pv = 0;              // stage and phase of the next K and V
     uint32_t done0 = 0, done1 = 0, uses0 = 0, uses1 = 0;  // chunks and items of the tiles before this item
 #pragma unroll 1
     for (int i = 0; i < rounds && ok; ++i) {
@@ -281,11 +290,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
       const int n_all = max(it.n[0], it.n[1]);
 #pragma unroll 1
       for (int j = 0; j <= n_all && ok; ++j) {  // per tile: P V of chunk j - 1, then S of chunk j
-        const int ck = c0 + 2 * j, cv = ck - 1;
-        const uint32_t sk = ck % kStages, sv = sk == 0 ? kStages - 1 : sk - 1;
         const uint64_t kd = k_desc + sk * (kStageBytes >> 4), vd = v_desc + sv * (kStageBytes >> 4);
-        if (j > 0) ok = wait_or_abort(full + sv, (cv / kStages) & 1, p.status, abort);
-        if (ok && j < n_all) ok = wait_or_abort(full + sk, (ck / kStages) & 1, p.status, abort);
+        if (j > 0) ok = wait_or_abort(full + sv, pv, p.status, abort);
+        if (ok && j < n_all) ok = wait_or_abort(full + sk, pk, p.status, abort);
         if (!ok) break;
 #pragma unroll 1
         for (int t = 0; t < 2; ++t) {
@@ -327,8 +334,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
             __syncwarp();
           }
         }
+        if (j > 0) two_on(sv, pv);
+        if (j < n_all) two_on(sk, pk);
       }
-      c0 += 2 * n_all;
       done0 += it.n[0];
       done1 += it.n[1];
       uses0 += it.n[0] > 0 ? 1 : 0;
@@ -497,21 +505,23 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
     const int see = mine ? sees(p.causal, it.nq, it.nk, token) : 0;
     const int see_all = sees(p.causal, it.nq, it.nk, first / G);  // every row of the tile sees these
     float m = -CUDART_INF_F, l = 0.f;  // in units of log2; m may lag behind the maximum by up to 8
+    uint32_t at_k = c0 % kStages;      // stage of the chunk's K
 #pragma unroll 1
     for (int j = 0; j < n; ++j) {
       ok = wait_or_abort(sfull + t, (done + j) & 1, p.status, abort);
       if (!ok) break;
-      if (lane == 0) {
-        if (t == 1 || j >= it.n[1]) {  // S of both tiles: K of chunk j and V of j - 1 are free
-          if (j > 0) mbar_arrive(empty + (c0 + 2 * j - 1) % kStages);
-          if (j + 1 != it.n[0]) mbar_arrive(empty + (c0 + 2 * j) % kStages);  // tile 0 writes its output through its last one
-        }
-        if (warp == 4 * t && j == n - 1) mbar_arrive(qempty + t);
-      }
       tc_fence_after();
       uint32_t raw[4][32];
 #pragma unroll
       for (int i = 0; i < 4; ++i) tmem_ld32_issue(scol + 32 * i, raw[i]);
+      if (lane == 0) {
+        if (t == 1 || j >= it.n[1]) {  // S of both tiles: K of chunk j and V of j - 1 are free
+          if (j > 0) mbar_arrive(empty + (at_k == 0 ? kStages - 1 : at_k - 1));
+          if (j + 1 != it.n[0]) mbar_arrive(empty + at_k);  // tile 0 writes its output through its last one
+        }
+        if (warp == 4 * t && j == n - 1) mbar_arrive(qempty + t);
+      }
+      at_k = at_k + 2 >= kStages ? at_k + 2 - kStages : at_k + 2;
 #pragma unroll
       for (int i = 0; i < 4; ++i) tmem_wait_ld32(raw[i]);
       if ((j + 1) * kTile > see_all) {
