@@ -417,7 +417,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
     const bool leader = elect_lane();
     const uint32_t id_s = idesc_16(kBf, kTile, kTile, false), id_o = idesc_16(kBf, kTile, kD, true);
     const uint32_t slots = smem_addr(smem + L::kOffSlots);
-    const uint64_t q_desc = sw128_desc(smem_addr(smem)), k_desc = sw128_desc(slots), v_desc = sw128_desc_mn(slots, 16384, 1024);
+    // descriptors: the low words change, the high ones are constants
+    const uint32_t q_lo = static_cast<uint32_t>(sw128_desc(smem_addr(smem))), k_lo = static_cast<uint32_t>(sw128_desc(slots));
+    const uint32_t v_lo = static_cast<uint32_t>(sw128_desc_mn(slots, 16384, 1024));
+    auto k_desc = [](uint32_t lo) { return sw128_desc(0) >> 32 << 32 | lo; };
+    auto v_desc = [](uint32_t lo) { return sw128_desc_mn(0, 16384, 1024) >> 32 << 32 | lo; };
     // What the loop needs of a piece stays in registers and slots are counted on: with a read of shared memory, a
     // division or a wait more per tile, this warp and not the tensor core was what a chunk took its time for.
     bool ok = true;
@@ -439,7 +443,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
           if (jp == 0 && ord > 0) ok = ok && wait_or_abort(oread, (ord - 1) & 1, p.status, abort);
         }
         if (!ok) break;
-        const uint64_t vd = v_desc + vs * (kSlotBytes >> 4), kd = k_desc + ks * (kSlotBytes >> 4);
+        const uint32_t vd = v_lo + vs * (kSlotBytes >> 4), kd = k_lo + ks * (kSlotBytes >> 4);
         uint32_t t = tiles == 2 ? 0u : j & 1;  // chunk by chunk, or both tiles
 #pragma unroll 1
         for (int i = 0; i < tiles; ++i, ++t) {
@@ -453,10 +457,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
             if (leader) {
               const uint32_t more = jp >= lag ? 1u : 0u;  // not the group's first chunk
 #pragma unroll
-              for (int k = 0; k < 4; ++k) umma_f16_ta(o_at, s_at + k * 8, vd + k * 128, id_o, k > 0 ? 1u : more);
+              for (int k = 0; k < 4; ++k) umma_f16_ta(o_at, s_at + k * 8, v_desc(vd + k * 128), id_o, k > 0 ? 1u : more);
               if (!(has_new && jp == chunks - 1)) {  // 64 keys more
 #pragma unroll
-                for (int k = 4; k < 8; ++k) umma_f16_ta(o_at, s_at + k * 8, vd + k * 128, id_o, 1u);
+                for (int k = 4; k < 8; ++k) umma_f16_ta(o_at, s_at + k * 8, v_desc(vd + k * 128), id_o, 1u);
               }
               if (last_tile) {
                 umma_commit(pdone + (nv & 3));
@@ -470,12 +474,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
             if (i == 0) ok = wait_chunk(kfull, nk);
             if (!ok) break;
             tc_fence_after();
-            const uint64_t qd = q_desc + (tiles == 2 && t == 1 ? kSlotBytes >> 4 : 0);
+            const uint32_t qd = q_lo + (tiles == 2 && t == 1 ? kSlotBytes >> 4 : 0);
             if (leader) {
 #pragma unroll
               for (int k = 0; k < 8; ++k) {
                 const uint32_t off = (k >> 2) * (16384 >> 4) + (k & 3) * 2;
-                umma_f16(s_at, qd + off, kd + off, id_s, k > 0 ? 1u : 0u);
+                umma_f16(s_at, k_desc(qd + off), k_desc(kd + off), id_s, k > 0 ? 1u : 0u);
               }
               umma_commit(sfull + t);
               if (last_tile) umma_commit(sdone + (nk & 3));
