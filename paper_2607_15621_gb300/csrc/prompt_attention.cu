@@ -24,10 +24,11 @@
 // the last; a chunk takes about 2,600). Items go longest first, mirrored from round to round; the rank of an item
 // in the order of chunks is found by counting (the host knows no lengths).
 //
-// Measured: 8192 tokens, 32 heads over 8, causal: 327 us, 1680 TFLOP/s (0.88 of the library's matrix product; tensor
-// pipe 74 % active): a chunk of two tiles takes 2,600 cycles, of which its exponentials need 2,048 and its MMAs
-// 2,048. 16 prompts of 139 to 452 tokens: 32 us, where items of one to four chunks pay 5,000 cycles each for their start and
-// outputs. Four chunks of 123 to 511 tokens behind 2048 rows: 47 us; 160 items for 152 SMs, so eight CTAs do two.
+// Measured: 8192 tokens, 32 heads over 8, causal: 322 to 328 us, 1680 TFLOP/s (0.88 of the library's matrix product).
+// A chunk of two tiles takes 2,600 cycles, of which its MMAs need 2,048 (tensor pipe 74 % active over the kernel) and its
+// exponentials 1,024. 16 prompts of 139 to 452 tokens: 32 us, where items of one to four chunks pay 5,000 cycles each for
+// their start and outputs. Four chunks of 123 to 511 tokens behind 1277 to 1936 rows: 48 us; 160 items for 152 SMs, so
+// eight CTAs do two.
 // Outputs leave by bulk copies, a warp's 32 rows each: 16-byte stores of the same rows held a warp for 1,900 cycles.
 //
 // Stages are released by the softmax threads (S of chunk j there: K of j and V of j - 1 are free).

@@ -25,11 +25,12 @@
 // warp finds the pieces and describes them in a ring for the other roles. Cut items are put together by a
 // second kernel, a warp a row: 256 rows are too many for the one CTA that comes last.
 //
-// Measured: one tree of 50 tokens, 32 heads over 8, behind 32768 8-bit rows: 52 us, of which the plan, the queries and
-// the first keys take 9 us, 27 chunks of 256 rows 30 us (2,100 cycles each; the exponentials of 256 x 128 scores need
-// 2,048, the MMAs about as long) and results and join 9 us. Eight requests of 24 tokens at most over 4096 to 8192
-// rows: 57 us with 8-bit, 54 us with 16-bit caches (3.7 TB/s). 16 requests of 6 to 11 tokens over 96 to 480 rows: 22 us, mostly the
-// latency of the same steps: plan 2.4, first piece 1, queries 2.2, first keys 2, three chunks 6, results 4, join 2 us.
+// Measured: one tree of 50 tokens, 32 heads over 8, behind 32768 8-bit rows: 49 us, of which the plan, the queries and
+// the first keys take 10 us, 13.5 chunks of 256 rows 28 us (about 3,900 cycles each, of which MMAs 2,048 and
+// exponentials 1,024: a tile's S, softmax and P V follow each other, and their instructions share the schedulers with
+// the producers') and results and join 10 us. Eight requests of 24 tokens at most over 4096 to 8192 rows: 54 us with
+// 8-bit, 53 us with 16-bit caches (3.8 TB/s). 16 requests of 6 to 11 tokens over 96 to 480 rows: 21 us, mostly the latency
+// of the same steps: plan 2.5, first piece 1, queries 2.4, first keys 1, three chunks 6, results 4, join 2 us.
 //
 // Registers: 640 threads at 96 from launch; softmax warpgroups take 2 x 128, producers keep 2 x 80, MMA and scheduler 64
 // (with 104, 96 and 80 the softmax spilled into its loop, with 128, 88 and 48 the MMA warp into its own: the wide
@@ -1136,7 +1137,8 @@ Kernels kernels_of(bool cache8, bool wide) {
 
 // Items of 256 rows read the cache once for twice the rows; those of 128 keep one more chunk in shared memory and have
 // both groups at work on any item. By the rows that a request has on average: 8-bit caches with about 24 rows a request
-// 53.0 us, 62.5 with wide items; 72 rows 57.4 and 66.7 (16-bit 53.8 and 50.6); 200 rows 64.9, and 52.5 with wide items.
+// 53.0 us, 62.5 with wide items; 72 rows 57.4 and 66.7 (16-bit 53.8 and 50.6); 200 rows 64.9, and 52.5 with wide items (all
+// before the softmax had more registers).
 bool is_wide(int B, long long new_rows, int group) { return new_rows * group > static_cast<long long>(B) * kTile; }
 
 }  // namespace
