@@ -498,7 +498,7 @@ void fsx_session_destroy(fsx_session s);
  *     least 2^-22 of the row's largest; smaller ones may lose their last bits.
  *   - A key that a row does not see has no effect on it, whatever the key and value hold (NaN and
  *     infinities too). A row that sees no key gets zeros and a log-sum-exp of -infinity.
- *   - Asynchronous on `stream`; nothing is allocated. */
+ *   - Outputs overlap no input. Asynchronous on `stream`; nothing is allocated. */
 
 /* Write n_rows rows of keys and values into an 8-bit cache: per row and kv head the scale is
  * the smallest power of two s (at least 2^-126) with max|x| / s <= 448, and the code is x / s

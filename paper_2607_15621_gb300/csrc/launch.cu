@@ -49,19 +49,23 @@ int sm_count() {
   return n;
 }
 
-// An attribute of the kernel on a device, so it is set once.
+// An attribute of the kernel on a device, so it is set once. Nothing is thrown: callers are C entry points.
 cudaError_t allow_shared_memory(const void* fn, size_t bytes) {
   static std::mutex mu;
   static std::map<std::pair<int, const void*>, size_t> known;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  std::lock_guard<std::mutex> lock(mu);
-  size_t& have = known[std::make_pair(dev, fn)];
-  if (have >= bytes) return cudaSuccess;
-  e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
-  if (e == cudaSuccess) have = bytes;
-  return e;
+  try {
+    std::lock_guard<std::mutex> lock(mu);
+    size_t& have = known[std::make_pair(dev, fn)];
+    if (have >= bytes) return cudaSuccess;
+    e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+    if (e == cudaSuccess) have = bytes;
+    return e;
+  } catch (...) {
+    return cudaErrorMemoryAllocation;
+  }
 }
 
 cudaError_t launch_ex(const void* fn, dim3 grid, dim3 block, size_t smem, cudaStream_t stream, bool pdl,

@@ -386,19 +386,20 @@ def _alike(v, k) -> bool:
 
 def _cache8_call(k, v, rows, k_cache, v_cache, k_scale, v_scale):
     codes = _CODES or _codes()
-    shape, stride, cs = k.shape, k.stride(), k_cache.shape
-    good = (len(shape) == 3 and len(cs) == 3 and v.shape == shape and (v.stride() == stride or _alike(v, k)) and v.dtype is k.dtype and
-            _rows(k, stride) and cs[1:] == shape[1:] and v_cache.shape == cs and k_cache.dtype is v_cache.dtype and
-            codes.get(k_cache.dtype) == FSX_E4M3 and k_cache.is_contiguous() and v_cache.is_contiguous() and
-            k_scale.dtype is _F32 and v_scale.dtype is _F32 and k_scale.shape == (cs[1], cs[0]) and
-            v_scale.shape == k_scale.shape and k_scale.is_contiguous() and v_scale.is_contiguous() and
-            (rows is None or (rows.dtype is _I64 and rows.shape == shape[:1] and rows.is_contiguous())) and
-            k.dtype in codes)
+    shape, stride, cs, ss, dtype, held = k.shape, k.stride(), k_cache.shape, k_scale.shape, k.dtype, k_cache.dtype
+    good = (len(shape) == 3 and len(cs) == 3 and len(ss) == 2 and v.shape == shape and
+            (v.stride() == stride or _alike(v, k)) and v.dtype is dtype and dtype in codes and
+            stride[2] == 1 and (stride[1] == shape[2] or shape[1] == 1) and cs[1] == shape[1] and cs[2] == shape[2] and
+            v_cache.shape == cs and v_cache.dtype is held and codes.get(held) == FSX_E4M3 and
+            k_cache.is_contiguous() and v_cache.is_contiguous() and
+            k_scale.dtype is _F32 and v_scale.dtype is _F32 and ss[0] == cs[1] and ss[1] == cs[0] and
+            v_scale.shape == ss and k_scale.is_contiguous() and v_scale.is_contiguous() and
+            (rows is None or (rows.dtype is _I64 and rows.shape == shape[:1] and rows.is_contiguous())))
     if not good:
         _refuse("rows k, v [n, kv heads, 128] of one shape, dtype and stride, 8-bit caches [rows, kv heads, 128], scales "
                 "fp32 [kv heads, rows], row numbers int64 [n]", k=k, v=v, rows=rows, k_cache=k_cache, v_cache=v_cache,
                 k_scale=k_scale, v_scale=v_scale)
-    return codes[k.dtype], shape, _pitch(k, stride), cs[0]
+    return codes[dtype], shape, _pitch(k, stride), cs[0]
 
 
 def cache_write(k, v, rows, k_cache, v_cache, k_scale, v_scale, status, stream=None):
@@ -448,22 +449,25 @@ def tree_attention(q, k_new, v_new, new_offsets, mask, k_cache, v_cache, offsets
     """fsx_tree_attention: the new tokens' q [rows, heads, 128], k_new and v_new [rows, kv heads, 128], mask int64
     [rows], over caches [rows, kv heads, 128] of q's dtype or e4m3 (then with scales [kv heads, rows])."""
     codes = _CODES or _codes()
-    dtype, qs, ks, q_shape, k_shape, cs = q.dtype, q.stride(), k_new.stride(), q.shape, k_new.shape, k_cache.shape
-    code = codes.get(k_cache.dtype)
-    good = (len(q_shape) == 3 and len(k_shape) == 3 and len(cs) == 3 and k_new.dtype is dtype and v_new.dtype is dtype and
-            out.dtype is dtype and v_new.shape == k_shape and (v_new.stride() == ks or _alike(v_new, k_new)) and out.shape == q_shape and
-            out.is_contiguous() and q_shape[0] == k_shape[0] and q_shape[2] == k_shape[2] and _rows(q, qs) and
-            _rows(k_new, ks) and new_offsets.dtype is _I64 and offsets.dtype is _I64 and
-            offsets.shape == new_offsets.shape and new_offsets.dim() == 1 and new_offsets.is_contiguous() and
-            offsets.is_contiguous() and mask.dtype is _I64 and mask.shape == q_shape[:1] and mask.is_contiguous() and
-            v_cache.dtype is k_cache.dtype and v_cache.shape == cs and cs[1:] == k_shape[1:] and
-            k_cache.is_contiguous() and v_cache.is_contiguous() and dtype in codes and code is not None and
+    dtype, held, qs, ks, q_shape, k_shape, cs = (q.dtype, k_cache.dtype, q.stride(), k_new.stride(), q.shape, k_new.shape,
+                                                 k_cache.shape)
+    code, n_shape = codes.get(held), new_offsets.shape
+    good = (len(q_shape) == 3 and len(k_shape) == 3 and len(cs) == 3 and len(n_shape) == 1 and dtype in codes and
+            k_new.dtype is dtype and v_new.dtype is dtype and out.dtype is dtype and v_new.shape == k_shape and
+            (v_new.stride() == ks or _alike(v_new, k_new)) and out.shape == q_shape and out.is_contiguous() and
+            q_shape[0] == k_shape[0] and q_shape[2] == k_shape[2] and qs[2] == 1 and
+            (qs[1] == q_shape[2] or q_shape[1] == 1) and ks[2] == 1 and (ks[1] == k_shape[2] or k_shape[1] == 1) and
+            new_offsets.dtype is _I64 and offsets.dtype is _I64 and offsets.shape == n_shape and
+            new_offsets.is_contiguous() and offsets.is_contiguous() and mask.dtype is _I64 and
+            mask.shape == q_shape[:1] and mask.is_contiguous() and code is not None and v_cache.dtype is held and
+            v_cache.shape == cs and cs[1] == k_shape[1] and cs[2] == k_shape[2] and k_cache.is_contiguous() and
+            v_cache.is_contiguous() and
             (code != FSX_E4M3 or (k_scale is not None and v_scale is not None and k_scale.dtype is _F32 and
                                   v_scale.dtype is _F32 and k_scale.shape == (cs[1], cs[0]) and
-                                  v_scale.shape == k_scale.shape and k_scale.is_contiguous() and
+                                  v_scale.shape == (cs[1], cs[0]) and k_scale.is_contiguous() and
                                   v_scale.is_contiguous())) and
             (starts is None or (starts.dtype is _I64 and starts.is_contiguous() and starts.dim() == 1 and
-                                starts.shape[0] == new_offsets.shape[0] - 1)) and
+                                starts.shape[0] == n_shape[0] - 1)) and
             (lse is None or (lse.dtype is _F32 and lse.shape == (q_shape[1], q_shape[0]) and lse.is_contiguous())))
     if not good:
         _refuse("q, out [rows, heads, 128], k_new, v_new [rows, kv heads, 128] of one dtype, k_new and v_new of one stride, out "
@@ -477,7 +481,7 @@ def tree_attention(q, k_new, v_new, new_offsets, mask, k_cache, v_cache, offsets
                                    v_cache.data_ptr(), k_scale.data_ptr() if eight else None,
                                    v_scale.data_ptr() if eight else None, code, cs[0],
                                    None if starts is None else starts.data_ptr(), offsets.data_ptr(),
-                                   new_offsets.shape[0] - 1, q_shape[1], k_shape[1], q_shape[2], out.data_ptr(),
+                                   n_shape[0] - 1, q_shape[1], k_shape[1], q_shape[2], out.data_ptr(),
                                    None if lse is None else lse.data_ptr(), workspace.data_ptr(),
                                    workspace.numel() * workspace.element_size(), status.data_ptr(), _stream(stream)))
     return out
