@@ -563,6 +563,8 @@ fsx_status fsx_prompt_attention(const void* d_q, long long q_stride, const void*
  *   d_workspace : DEVICE scratch of fsx_tree_attention_workspace_bytes(...) bytes, 256-byte aligned,
  *                zeroed by the caller once before its first use; a call leaves it ready for the next. Calls
  *                that overlap on the GPU must not share it. Zero it again after FSX_ERR_TIMEOUT.
+ * The workspace for some B and new_rows also serves calls with that B and fewer new rows; for calls of
+ * several B take the largest.
  * A request whose offsets are negative, decrease, pass the rows or name more than 64 new tokens
  * sets FSX_ERR_DEVICE_ARG and gets no output row; the others are written. */
 size_t fsx_tree_attention_workspace_bytes(int B, long long new_rows, int n_heads, int n_kv_heads);

@@ -95,6 +95,12 @@ def test_workspace_size(lib):
     assert fsx.tree_attention_workspace_bytes(1, 1, 1, 2) == 0
 
 
+@pytest.mark.parametrize("B,heads,kv_heads", [(1, 32, 32), (1, 64, 1), (3, 8, 2), (16, 32, 8), (128, 4, 1), (1024, 32, 32)])
+def test_workspace_serves_fewer_new_rows(lib, B, heads, kv_heads):
+    sizes = [fsx.tree_attention_workspace_bytes(B, r, heads, kv_heads) for r in [*range(0, min(64 * B, 600)), 64 * B]]
+    assert sizes == sorted(sizes)
+
+
 def test_binding_refuses_tensors_that_do_not_fit():
     z = lambda *s, dtype=torch.bfloat16: torch.zeros(*s, dtype=dtype)
     off, st = z(3, dtype=torch.int64), z(1, dtype=torch.int32)
