@@ -350,14 +350,16 @@ def attention_noalloc_status(stream=None) -> int:
 # What the checks below ask for. A call of 10 to 20 us on the GPU waits for its caller: the conditions are one expression
 # of cheap attributes (12 to 23 us a call with a helper for each), and only a refusal looks for its reason.
 _CODES: dict = {}  # torch dtype -> fsx_dtype; e4m3 caches may be held as bytes
-_I64 = _F32 = None
+_I64 = _F32 = _raw_stream = _device = None
 
 
 def _codes() -> dict:
-    global _I64, _F32
+    global _I64, _F32, _raw_stream, _device
     if not _CODES:
         import torch
         _I64, _F32 = torch.int64, torch.float32
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # of tensors on the GPU: CUDA is at work
+        _device = getattr(torch._C, "_cuda_getDevice", None)
         _CODES.update({torch.float32: FSX_F32, torch.bfloat16: FSX_BF16, torch.float16: FSX_F16,
                        torch.float8_e4m3fn: FSX_E4M3, torch.uint8: FSX_E4M3})
     return _CODES
@@ -399,23 +401,30 @@ def _cache8_call(k, v, rows, k_cache, v_cache, k_scale, v_scale):
         _refuse("rows k, v [n, kv heads, 128] of one shape, dtype and stride, 8-bit caches [rows, kv heads, 128], scales "
                 "fp32 [kv heads, rows], row numbers int64 [n]", k=k, v=v, rows=rows, k_cache=k_cache, v_cache=v_cache,
                 k_scale=k_scale, v_scale=v_scale)
-    return codes[dtype], shape, _pitch(k, stride), cs[0]
+    return codes[dtype], shape, stride[0] if shape[0] > 1 else _pitch(k, stride), cs[0]
 
 
 def cache_write(k, v, rows, k_cache, v_cache, k_scale, v_scale, status, stream=None):
     """fsx_cache_write_e4m3: rows k, v [n, kv heads, 128] into cache rows `rows` (int64 [n]; None: 0 .. n - 1)."""
     code, shape, pitch, m = _cache8_call(k, v, rows, k_cache, v_cache, k_scale, v_scale)
-    check(lib().fsx_cache_write_e4m3(k.data_ptr(), v.data_ptr(), pitch, code, None if rows is None else rows.data_ptr(),
-                                     shape[0], shape[1], shape[2], k_cache.data_ptr(), v_cache.data_ptr(),
-                                     k_scale.data_ptr(), v_scale.data_ptr(), m, status.data_ptr(), _stream(stream)))
+    on = _raw_stream(_device()) if stream is None else _stream(stream)
+    error = (_lib or lib()).fsx_cache_write_e4m3(
+        k.data_ptr(), v.data_ptr(), pitch, code, None if rows is None else rows.data_ptr(), shape[0], shape[1], shape[2],
+        k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), m, status.data_ptr(), on)
+    if error:
+        check(error)
 
 
 def cache_read(k_cache, v_cache, k_scale, v_scale, rows, k, v, status, stream=None):
     """fsx_cache_read_e4m3: cache rows `rows` (int64 [n]; None: 0 .. n - 1) into k, v [n, kv heads, 128]."""
     code, shape, pitch, m = _cache8_call(k, v, rows, k_cache, v_cache, k_scale, v_scale)
-    check(lib().fsx_cache_read_e4m3(k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), m,
-                                    None if rows is None else rows.data_ptr(), shape[0], shape[1], shape[2],
-                                    k.data_ptr(), v.data_ptr(), pitch, code, status.data_ptr(), _stream(stream)))
+    on = _raw_stream(_device()) if stream is None else _stream(stream)
+    error = (_lib or lib()).fsx_cache_read_e4m3(
+        k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), m,
+        None if rows is None else rows.data_ptr(), shape[0], shape[1], shape[2], k.data_ptr(), v.data_ptr(), pitch, code,
+        status.data_ptr(), on)
+    if error:
+        check(error)
     return k, v
 
 
@@ -433,10 +442,13 @@ def prompt_attention(q, k, v, q_offsets, kv_offsets, out, status, lse=None, caus
         _refuse("q, out [rows, heads, 128], k, v [rows, kv heads, 128] of one dtype, k and v of one stride, out contiguous, "
                 "offsets int64 [B + 1], lse fp32 [heads, rows]", q=q, k=k, v=v, q_offsets=q_offsets,
                 kv_offsets=kv_offsets, out=out, lse=lse)
-    check(lib().fsx_prompt_attention(q.data_ptr(), _pitch(q, qs), k.data_ptr(), v.data_ptr(), _pitch(k, ks), codes[dtype],
-                                     q_offsets.data_ptr(), kv_offsets.data_ptr(), q_offsets.shape[0] - 1, q_shape[0],
-                                     k_shape[0], q_shape[1], k_shape[1], q_shape[2], 1 if causal else 0, out.data_ptr(),
-                                     None if lse is None else lse.data_ptr(), status.data_ptr(), _stream(stream)))
+    on = _raw_stream(_device()) if stream is None else _stream(stream)
+    error = (_lib or lib()).fsx_prompt_attention(
+        q.data_ptr(), _pitch(q, qs), k.data_ptr(), v.data_ptr(), _pitch(k, ks), codes[dtype], q_offsets.data_ptr(),
+        kv_offsets.data_ptr(), q_offsets.shape[0] - 1, q_shape[0], k_shape[0], q_shape[1], k_shape[1], q_shape[2],
+        1 if causal else 0, out.data_ptr(), None if lse is None else lse.data_ptr(), status.data_ptr(), on)
+    if error:
+        check(error)
     return out
 
 
@@ -476,14 +488,16 @@ def tree_attention(q, k_new, v_new, new_offsets, mask, k_cache, v_cache, offsets
                 v_new=v_new, new_offsets=new_offsets, mask=mask, k_cache=k_cache, v_cache=v_cache, offsets=offsets,
                 out=out, k_scale=k_scale, v_scale=v_scale, starts=starts, lse=lse)
     eight = code == FSX_E4M3
-    check(lib().fsx_tree_attention(q.data_ptr(), _pitch(q, qs), k_new.data_ptr(), v_new.data_ptr(), _pitch(k_new, ks),
-                                   codes[dtype], new_offsets.data_ptr(), mask.data_ptr(), q_shape[0], k_cache.data_ptr(),
-                                   v_cache.data_ptr(), k_scale.data_ptr() if eight else None,
-                                   v_scale.data_ptr() if eight else None, code, cs[0],
-                                   None if starts is None else starts.data_ptr(), offsets.data_ptr(),
-                                   n_shape[0] - 1, q_shape[1], k_shape[1], q_shape[2], out.data_ptr(),
-                                   None if lse is None else lse.data_ptr(), workspace.data_ptr(),
-                                   workspace.numel() * workspace.element_size(), status.data_ptr(), _stream(stream)))
+    on = _raw_stream(_device()) if stream is None else _stream(stream)
+    error = (_lib or lib()).fsx_tree_attention(
+        q.data_ptr(), _pitch(q, qs), k_new.data_ptr(), v_new.data_ptr(), _pitch(k_new, ks), codes[dtype],
+        new_offsets.data_ptr(), mask.data_ptr(), q_shape[0], k_cache.data_ptr(), v_cache.data_ptr(),
+        k_scale.data_ptr() if eight else None, v_scale.data_ptr() if eight else None, code, cs[0],
+        None if starts is None else starts.data_ptr(), offsets.data_ptr(), n_shape[0] - 1, q_shape[1], k_shape[1],
+        q_shape[2], out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), status.data_ptr(), on)
+    if error:
+        check(error)
     return out
 
 
