@@ -13,9 +13,14 @@
 //   scores and weights of keys g, g + 8 for rows 2 c, 2 c + 1; outputs of rows 2 c, 2 c + 1 for 16 dims.
 // 8-bit caches: codes become fp16 exactly, bf16 queries fp16 times a power of two per row (their 8 bits fit;
 // components 2^-22 below the row's largest may lose their last bits), a key's scale multiplies its
-// score, a value's scale its weight, relative to the largest value scale so far (`vs`). Weights are then fp16,
-// also for bf16 queries. 16-bit caches and the new tokens use their own type, weights rounded to it.
-// The running maximum moves only when a score exceeds it by more than 2^8, seen by one vote a step.
+// score, a value's scale its weight. Weights are then fp16, also for bf16 queries; fp16 has a narrow range, and value scales
+// may have any size, so the product's weights are taken times a power of two `k` of each row's own, which brings the
+// largest (weight times scale) so far, for codes the largest contribution to the output up to a factor of two, to
+// 2^7 .. 2^15. So neither a large value of little weight nor the new tokens decide what is lost: k of what the
+// new tokens leave follows from their sums, and rows of zeros, whose scale says nothing, are left out of it.
+// 16-bit caches and the new tokens use their own type, weights rounded to it.
+// The running maximum moves only when a score exceeds it by more than 2^8, and k only when a weight exceeds 2^15, both
+// seen by one vote a step.
 //
 // The 4 warps of a CTA take every fourth 16 keys of a chunk of 64 and are put together in shared memory. Items are cut
 // into pieces that CTAs take from a queue (tree_schedule.cuh); the last one to end joins the pieces of its item.
@@ -79,64 +84,106 @@ struct Stage {
   static constexpr int kBytes = 32 * kRow + (C8 ? 128 : 0);
 };
 
+constexpr int kMostPower = 118;  // k is 2^118 at most, also where the sums are zero: k times a weight of 2^8 is finite
+constexpr int kTopPower = 7;     // where the largest product goes when k moves
+
 template <int NT>
 struct State {
   float o[8][NT][4];  // [dim pair][8 rows]: (dim 0; row 2 c, 2 c + 1), (dim 1; the same)
   float m[NT][2], l[NT][2];
-  float vs;           // C8: o is in units of it
+  float k[NT][2];     // C8: o is the sums times k, a power of two
 };
+__device__ __forceinline__ float power_of(int e) { return __uint_as_float(static_cast<uint32_t>(127 + e) << 23); }
+__device__ __forceinline__ int exponent_of(float x) { return static_cast<int>(__float_as_uint(x) >> 23) - 127; }  // x >= 0
 
-// Scores s[nt][key half * 2 + row] of 16 keys -> weights into the state, P^T packed for O^T. vs_of: the
-// scales of values of keys g, g + 8. BF: type of the weights.
+// largest over the 8 lanes that hold a row pair's other keys or dims
+__device__ __forceinline__ float max_over_g(float x) {
+#pragma unroll
+  for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  return x;
+}
+
+// Bits g and g + 8 of the warp's 16 value rows: all codes are zeros. A lane looks at half a row; `v`: the stage's V rows.
+__device__ __forceinline__ uint2 zero_rows(const unsigned char* v) {
+  const int lane = threadIdx.x & 31, g = lane >> 2;
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint4 x = reinterpret_cast<const uint4*>(v + (lane >> 1) * kD + (lane & 1) * (kD / 2))[i];
+    any |= x.x | x.y | x.z | x.w;
+  }
+  const uint32_t none = __ballot_sync(0xffffffffu, (any & 0x7f7f7f7fu) == 0u), rows = none & none >> 1;
+  return make_uint2((rows >> (2 * g)) & 1u, (rows >> (2 * g + 16)) & 1u);
+}
+
+// Scores s[nt][key half * 2 + row] of 16 keys -> weights into the state, P^T packed for O^T. BF: type of the weights.
+// C8: vs are the scales of values of keys g, g + 8, `v` their rows.
 template <bool BF, bool C8, int NT>
-__device__ __forceinline__ void softmax_step(State<NT>& st, float (&s)[NT][4], const float (&vs_of)[2], uint32_t (&pt)[NT][2]) {
-  bool move = C8 && fmaxf(vs_of[0], vs_of[1]) > st.vs;
+__device__ __forceinline__ void softmax_step(State<NT>& st, float (&s)[NT][4], float (&vs)[2], const unsigned char* v, uint32_t (&pt)[NT][2]) {
+  float w[NT][4], p[NT][4];
+  auto weigh = [&](int t, int e) {
+    const int r = e & 1;
+    w[t][e] = exp2_fast(s[t][e] - (st.m[t][r] == -CUDART_INF_F ? 0.f : st.m[t][r]));
+    p[t][e] = C8 ? w[t][e] * st.k[t][r] * vs[e >> 1] : w[t][e];
+  };
+  bool move = false;
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int r = 0; r < 2; ++r) move = move || fmaxf(s[t][r], s[t][2 + r]) > st.m[t][r] + 8.f;
+    for (int r = 0; r < 2; ++r) {
+      move = move || fmaxf(s[t][r], s[t][2 + r]) > st.m[t][r] + 8.f;
+      if (C8) {
+        weigh(t, r);
+        weigh(t, 2 + r);
+        move = move || fmaxf(p[t][r], p[t][2 + r]) > 32768.f;
+      }
+    }
   if (__any_sync(0xffffffffu, move)) {
-    float ratio = 1.f;
     if (C8) {
-      float v = fmaxf(vs_of[0], vs_of[1]);
-#pragma unroll
-      for (int o = 4; o < 32; o <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-      v = fmaxf(v, st.vs);
-      ratio = v > 0.f ? st.vs / v : 1.f;
-      st.vs = v;
+      const uint2 zero = zero_rows(v);
+      if (zero.x) vs[0] = 0.f;
+      if (zero.y) vs[1] = 0.f;
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        float top = fmaxf(s[t][r], s[t][2 + r]);
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const float m = fmaxf(st.m[t][r], top);
-        const float alpha = m == st.m[t][r] ? 1.f : exp2_fast(st.m[t][r] - m);
+        const float m = fmaxf(st.m[t][r], max_over_g(fmaxf(s[t][r], s[t][2 + r])));
+        const float up = m == st.m[t][r] ? 0.f : m - st.m[t][r];
+        float alpha = exp2_fast(-up);
         st.m[t][r] = m;
         st.l[t][r] *= alpha;
+        if (C8) {  // the sums do not grow, and no product leaves its range
+          weigh(t, r);
+          weigh(t, 2 + r);
+          const float top = max_over_g(fmaxf(w[t][r] * vs[0], w[t][2 + r] * vs[1]));
+          const float is = static_cast<float>(exponent_of(st.k[t][r]));
+          const float will = fminf(fminf(floorf(is + up), static_cast<float>(kTopPower - exponent_of(top))), static_cast<float>(kMostPower));
+          st.k[t][r] = power_of(static_cast<int>(will));
+          alpha = exp2_fast(will - is - up);
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          st.o[j][t][r] *= alpha * ratio;
-          st.o[j][t][2 + r] *= alpha * ratio;
+          st.o[j][t][r] *= alpha;
+          st.o[j][t][2 + r] *= alpha;
         }
       }
+    if (C8) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) weigh(t, e);
+    }
   }
-  const float inv = C8 ? (st.vs > 0.f ? 1.f / st.vs : 0.f) : 1.f;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float w[2];
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        w[r] = exp2_fast(s[t][2 * h + r] - (st.m[t][r] == -CUDART_INF_F ? 0.f : st.m[t][r]));
-        st.l[t][r] += w[r];
-        if (C8) w[r] *= vs_of[h] * inv;
-      }
-      pt[t][h] = transpose8x8(pack16<BF>(w[0], w[1]));
+    for (int e = 0; e < 4; ++e) {
+      if (!C8) weigh(t, e);
+      st.l[t][e & 1] += w[t][e];
     }
+    pt[t][0] = transpose8x8(pack16<BF>(p[t][0], p[t][1]));
+    pt[t][1] = transpose8x8(pack16<BF>(p[t][2], p[t][3]));
   }
 }
 
@@ -193,7 +240,7 @@ __device__ __forceinline__ void cache_step(State<NT>& st, const unsigned char* x
         s[t][2 * h + r] = g + 8 * h < left ? y : -CUDART_INF_F;
       }
   uint32_t pt[NT][2];
-  softmax_step<kBf, C8, NT>(st, s, vs, pt);
+  softmax_step<kBf, C8, NT>(st, s, vs, x + S::kOffV, pt);
   uint4 xv[4][S::kV];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -236,10 +283,10 @@ __device__ __forceinline__ int out_dim(int g, int j, int e) {
 }
 
 // New tokens key .. key + 15 of the request: their own type, one mask bit per row and token. A masked
-// weight is 0 but 0 times an infinity or NaN is not: such values go into the product as 0 and are added
-// to the rows that see them.
+// weight is 0 but 0 times an infinity or NaN is not: such values go into the product as 0. True: there are some, for
+// add_wild. Comes before the cache's steps.
 template <bool BF, bool C8, int NT>
-__device__ __forceinline__ void new_step(State<NT>& st, const TreeArgs& p, const TreePiece& it, uint32_t G, int key) {
+__device__ __forceinline__ bool new_step(State<NT>& st, const TreeArgs& p, const TreePiece& it, uint32_t G, int key) {
   const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
   const int left = it.r.n - key;
   const uint16_t* kn = static_cast<const uint16_t*>(p.k_new) + (it.r.t0 + key) * p.new_stride + it.kvh * kD;
@@ -267,22 +314,21 @@ __device__ __forceinline__ void new_step(State<NT>& st, const TreeArgs& p, const
       mma<BF>(s[t], a[0].x, a[1].x, a[0].y, a[1].y, b.x, b.y);
     }
   }
-  uint64_t mask[NT][2];
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
       const uint32_t row = it.row0 + 8 * t + 2 * c + r;
-      mask[t][r] = row < rows ? p.mask[it.r.t0 + row / G] >> key : 0ull;
+      const uint64_t mask = row < rows ? p.mask[it.r.t0 + row / G] >> key : 0ull;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const bool sees = g + 8 * h < left && ((mask[t][r] >> (g + 8 * h)) & 1u);
+        const bool sees = g + 8 * h < left && ((mask >> (g + 8 * h)) & 1u);
         s[t][2 * h + r] = sees ? s[t][2 * h + r] * kScaleLog2 : -CUDART_INF_F;
       }
     }
-  const float ones[2] = {1.f, 1.f};
+  float ones[2] = {1.f, 1.f};
   uint32_t pt[NT][2];
-  softmax_step<BF, C8, NT>(st, s, ones, pt);
+  softmax_step<BF, false, NT>(st, s, ones, nullptr, pt);
   uint32_t wild = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
@@ -300,24 +346,51 @@ __device__ __forceinline__ void new_step(State<NT>& st, const TreeArgs& p, const
 #pragma unroll
     for (int t = 0; t < NT; ++t) mma<BF>(st.o[j][t], a0, a1, a2, a3, pt[t][0], pt[t][1]);
   }
-  if (__any_sync(0xffffffffu, wild != 0)) {
-#pragma unroll 1
-    for (int i = 0; i < min(left, 16); ++i)
+  if (C8) {  // the sums' largest magnitude goes to [2^15, 2^16)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint32_t v = __ldg(reinterpret_cast<const uint32_t*>(vn + i * p.new_stride + out_dim<C8>(g, j, 0)));
-        const uint32_t bad = not_finite2<BF>(v);
-        const float2 y = unpack16<BF>(v);
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+      for (int r = 0; r < 2; ++r) {
+        float top = 0.f;
 #pragma unroll
-          for (int r = 0; r < 2; ++r)
-            if ((mask[t][r] >> i) & 1u) {
-              if (bad & 0x8000u) st.o[j][t][r] += y.x;
-              if (bad & 0x80000000u) st.o[j][t][2 + r] += y.y;
-            }
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, fmaxf(fabsf(st.o[j][t][r]), fabsf(st.o[j][t][2 + r])));
+        top = max_over_g(top);
+        st.k[t][r] = top < CUDART_INF_F ? power_of(min(15 - exponent_of(top), kMostPower)) : 1.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          st.o[j][t][r] *= st.k[t][r];
+          st.o[j][t][2 + r] *= st.k[t][r];
+        }
       }
   }
+  return __any_sync(0xffffffffu, wild != 0);
+}
+
+// The values that new_step took out, for the rows that see them; k is 1
+template <bool BF, bool C8, int NT>
+__device__ __forceinline__ void add_wild(State<NT>& st, const TreeArgs& p, const TreePiece& it, uint32_t G, int key) {
+  const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+  const uint16_t* vn = static_cast<const uint16_t*>(p.v_new) + (it.r.t0 + key) * p.new_stride + it.kvh * kD;
+  const uint32_t rows = it.r.n * G;
+#pragma unroll 1
+  for (int i = 0; i < min(it.r.n - key, 16); ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t v = __ldg(reinterpret_cast<const uint32_t*>(vn + i * p.new_stride + out_dim<C8>(g, j, 0)));
+      const uint32_t bad = not_finite2<BF>(v);
+      if (bad == 0u) continue;
+      const float2 y = unpack16<BF>(v);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const uint32_t row = it.row0 + 8 * t + 2 * c + r;
+          if (row < rows && (p.mask[it.r.t0 + row / G] >> (key + i)) & 1u) {
+            if (bad & 0x8000u) st.o[j][t][r] += y.x;
+            if (bad & 0x80000000u) st.o[j][t][2 + r] += y.y;
+          }
+        }
+    }
 }
 
 // Queries of the item's rows, as they lie
@@ -471,14 +544,15 @@ __global__ void __launch_bounds__(kThreads, Fit<C8, NT>::kCtas) tree_kernel(cons
     for (int t = 0; t < NT; ++t) {
       st.m[t][0] = st.m[t][1] = -CUDART_INF_F;
       st.l[t][0] = st.l[t][1] = 0.f;
+      st.k[t][0] = st.k[t][1] = power_of(kMostPower);
 #pragma unroll
       for (int j = 0; j < 8; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) st.o[j][t][e] = 0.f;
     }
-    st.vs = 0.f;
     // the new tokens first, while the cache's first rows are on their way
-    if (it.to == it.n && 16 * warp < it.r.n) new_step<BF, C8, NT>(st, p, it, G, 16 * warp);
+    bool wild = false;
+    if (it.to == it.n && 16 * warp < it.r.n) wild = new_step<BF, C8, NT>(st, p, it, G, 16 * warp);
     int slot_out = 0;
 #pragma unroll 1
     for (int key = it.from * kChunk + 16 * warp; key < end; key += kChunk) {
@@ -490,6 +564,20 @@ __global__ void __launch_bounds__(kThreads, Fit<C8, NT>::kCtas) tree_kernel(cons
     }
     cp_async_wait<0>();
     __syncwarp();
+    if (C8) {  // the sums without k
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const float factor = power_of(-exponent_of(st.k[t][r]));
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            st.o[j][t][r] *= factor;
+            st.o[j][t][2 + r] *= factor;
+          }
+        }
+    }
+    if (wild) add_wild<BF, C8, NT>(st, p, it, G, 16 * warp);
 
     const int rows = min(8 * NT, static_cast<int>(it.r.n * G - it.row0));
 #pragma unroll
@@ -533,8 +621,7 @@ __global__ void __launch_bounds__(kThreads, Fit<C8, NT>::kCtas) tree_kernel(cons
           if (row >= base && row < base + kPass && row < rows) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-              const float a = C8 ? st.o[j][t][r] * st.vs : st.o[j][t][r], b = C8 ? st.o[j][t][2 + r] * st.vs : st.o[j][t][2 + r];
-              *reinterpret_cast<float2*>(&sm.o[warp][row - base][out_dim<C8>(g, j, 0)]) = make_float2(a, b);
+              *reinterpret_cast<float2*>(&sm.o[warp][row - base][out_dim<C8>(g, j, 0)]) = make_float2(st.o[j][t][r], st.o[j][t][2 + r]);
             }
           }
         }
