@@ -2,7 +2,7 @@
 // cores: up to 128 rows (token, head of the group) an item, or 256 (WIDE).
 //
 //   S = Q K^T     128 rows x 128 keys, A and B in shared memory, S in tensor memory
-//   P = 2^(f S k_scale - m) v_scale / vs, rounded to the type of V, over its S; a thread holds a row
+//   P = 2^(f S k_scale - m) v_scale k, rounded to the type of V, over its S; a thread holds a row; k: a power of two
 //   O += P V      A in tensor memory, V read N-contiguous, O in tensor memory
 // Two S / P / O sets and two groups of softmax warps: in an item of more than 128 rows each works on its
 // own 128 rows and every chunk; else both on the same rows, one on the even and one on the odd chunks, so that
@@ -15,6 +15,11 @@
 // multiplies scores and weights by the scales. bf16 queries and new tokens meet an 8-bit cache as fp16 times a power
 // of two per row (their 8 bits fit; components 2^-22 below the row's largest may lose their last bits); the
 // new tokens' powers stand where the cache rows' scales do. Rows past the range become zeros and are never read.
+// Weights are fp16, whose range is narrow, and scales may have any size: where a chunk has scales, the weights are taken
+// times a power of two `k` of each row's own, which brings the largest (weight times scale) that the row sees to 2^7 or, as
+// long as k need not move, 2^15. What a row does not see, or sees with little weight, does not decide what is lost. Rows
+// of zeros, whose scale says nothing, count as none. Where all of a chunk lies far below what k was chosen for, the sums
+// themselves tell how far k may grow. Chunks without scales want k = 1.
 // The values of new tokens are looked over on the way: a masked weight is 0, but 0 times an infinity or NaN is not,
 // so these become 0 in the product and are added to the rows that see them at the end.
 //
@@ -86,11 +91,12 @@ struct Layout {
   static constexpr int kScaleRing = C8 ? 4 : 0;
   static constexpr int kOffFactor = kOffScale + kScaleRing * 2 * kTile * 4;  // C8: [piece parity][row]
   static constexpr int kOffMl = kOffFactor + (C8 ? 2 * kRows * 4 : 0);       // [group][128] (m, l)
-  static constexpr int kOffScratch = kOffMl + 2 * kTile * 8;
+  static constexpr int kOffPower = kOffMl + 2 * kTile * 8;                   // C8: [group][128] log2 k
+  static constexpr int kOffScratch = kOffPower + (C8 ? 2 * kTile * 4 : 0);
   static constexpr int kOffWork = kOffScratch + (2 * kPlans + 1 + kThreads / 32 + 1) / 2 * 8;
   static constexpr int kOffBar = kOffWork + kWorkRing * static_cast<int>(sizeof(Work));
-  static constexpr int kMisc = kOffBar + 33 * 8;  // tmem, abort, wild[4], vs of the groups [2], plain [4][2]
-  static constexpr int kPlan = (kMisc + 16 * 4 + 7) / 8 * 8;
+  static constexpr int kMisc = kOffBar + 33 * 8;  // tmem, abort, wild[4], plain [4][2]
+  static constexpr int kPlan = (kMisc + 14 * 4 + 7) / 8 * 8;
   static constexpr int kSmem = kPlan + (2 * kMaxSequences + 1) * 4;
 };
 static_assert(Layout<true, true>::kSmem <= 227 * 1024 && Layout<true, false>::kSmem <= 227 * 1024, "shared memory");
@@ -116,17 +122,25 @@ __device__ __forceinline__ float row_power(float top) {
 __device__ __forceinline__ float inverse_power(float p) {
   return __uint_as_float((254u << 23) - __float_as_uint(p));
 }
-__device__ __forceinline__ float top_of(uint4 x) {  // largest magnitude of 8 bf16 values
+template <bool BF>
+__device__ __forceinline__ float top_of(uint4 x) {  // largest magnitude of 8 values
   float t = 0.f;
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) t = fmaxf(t, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xffff0000u))));
+  for (int i = 0; i < 4; ++i) {
+    const float2 y = unpack16<BF>(w[i]);
+    t = fmaxf(t, fmaxf(fabsf(y.x), fabsf(y.y)));
+  }
   return t;
 }
-__device__ __forceinline__ uint4 bf16_to_half(uint4 x, float factor) {
+template <bool BF>
+__device__ __forceinline__ uint4 times_to_half(uint4 x, float factor) {
   uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = pack_half2(__uint_as_float(w[i] << 16) * factor, __uint_as_float(w[i] & 0xffff0000u) * factor);
+  for (int i = 0; i < 4; ++i) {
+    const float2 y = unpack16<BF>(w[i]);
+    w[i] = pack_half2(y.x * factor, y.y * factor);
+  }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 template <bool BF>
@@ -303,6 +317,10 @@ template <bool BF, bool C8, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) {
   using L = Layout<C8, WIDE>;
   constexpr bool kBf = BF && !C8;  // type of the operands
+  // The largest weight is 2^kTopPower when the maximum moves, and 2^8 times that before it moves again: fp16 has room above,
+  // and what lies far below the maximum keeps more of its bits
+  constexpr float kTopPower = kBf ? 0.f : 7.f, kLag = 8.f + kTopPower;
+  constexpr float kMostPower = 118.f;  // of log2 k
   constexpr int kSlots = L::kSlots;
   extern __shared__ __align__(1024) unsigned char smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -326,12 +344,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::kMisc);
   volatile int* abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* wild = reinterpret_cast<volatile int*>(tmem_slot + 2);  // [4]: piece ordinal + 1 with values taken out
-  volatile float* group_vs = reinterpret_cast<volatile float*>(tmem_slot + 6);  // [2]
-  volatile int* plain_of = reinterpret_cast<volatile int*>(tmem_slot + 8);      // [4][k, v]: no scales left in the chunk
+  volatile int* plain_of = reinterpret_cast<volatile int*>(tmem_slot + 6);  // [4][k, v]: no scales left in the chunk
   Work* works = reinterpret_cast<Work*>(smem + L::kOffWork);
-  float* scales = reinterpret_cast<float*>(smem + L::kOffScale);
+  float* scales = reinterpret_cast<float*>(smem + L::kOffScale);  // of keys; of values their logarithms, -infinity for a row of zeros
   float* row_factor = reinterpret_cast<float*>(smem + L::kOffFactor);
   float2* ml_of = reinterpret_cast<float2*>(smem + L::kOffMl);
+  float* power_of = reinterpret_cast<float*>(smem + L::kOffPower);
   uint32_t* scratch = reinterpret_cast<uint32_t*>(smem + L::kOffScratch);
   constexpr int kScaleRing = L::kScaleRing > 0 ? L::kScaleRing : 1;
   if ((smem_addr(smem) & 1023u) != 0u) {  // the swizzled operands need a 1024-byte aligned base
@@ -633,8 +651,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
               const int r = r1 + 16 * e;
               float power = 1.f;
               if (BF) {
-                power = row_power(row_max16(top_of(x[e])));
-                x[e] = bf16_to_half(x[e], inverse_power(power));
+                power = row_power(row_max16(top_of<BF>(x[e])));
+                x[e] = times_to_half<BF>(x[e], inverse_power(power));
               }
               if (qu == 0) row_factor[(ord & 1) * L::kRows + r] = power * kScaleLog2;
               *reinterpret_cast<uint4*>(smem + (r >> 7) * kSlotBytes + tile_off(r & 127, qu)) = x[e];
@@ -668,35 +686,71 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
             if (j + 1 < chunks) load_scales(w, j + 1);
             if (pt < 32) {
               if (lane == 0) plain_of[(chunk_no & 3) * 2 + is_v] = plain ? 1 : 0;
+              if (plain || !is_v) {
 #pragma unroll
-              for (int e = 0; e < 4; ++e) to_scales[lane + 32 * e] = plain ? 1.f : sc[e];
+                for (int e = 0; e < 4; ++e) to_scales[lane + 32 * e] = plain ? (is_v ? 0.f : 1.f) : sc[e];
+              }
             }
             unsigned char* to = slot + tile_off(r0, 2 * u);  // unit 2 u + 1 at the other place of its pair
             const int other = (r0 & 1) ? -16 : 16;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {  // 64 rows; the copy issued here goes where those before were made ready from
+            // 64 rows; the copy issued first goes where those before were made ready from
+            auto next_rows = [&](uint4 (&x)[4]) {
               issue();
               cp_async_wait<kAhead>();
               const unsigned char* mine = raw + raw_out * (kRawBytes / 2);
               raw_out = raw_out == 2 ? 0 : raw_out + 1;
-              uint4 x[4];
 #pragma unroll
               for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const uint4*>(mine + i * 2048);
+            };
+            // unit u + 4 (i & 1) of row r0 + 64 h + 32 (i >> 1)
+            auto put_unit = [&](int h, int i, const uint32_t (&z)[8]) {
+              unsigned char* at = to + h * 8192 + (i >> 1) * 4096 + (i & 1) * 16384;
+              *reinterpret_cast<uint4*>(at) = make_uint4(z[0], z[1], z[2], z[3]);
+              *reinterpret_cast<uint4*>(at + other) = make_uint4(z[4], z[5], z[6], z[7]);
+            };
+            if (plain) {
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {  // unit u + 4 (i & 1) of row r0 + 64 h + 32 (i >> 1): the scale is lane r0's
-                const float s1 = __shfl_sync(0xffffffffu, sc[2 * h + (i >> 1)], r0);
-                const __half2 f = __float2half2_rn(plain ? s1 : 1.f);
-                const uint32_t y[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-                uint32_t z[8];
+              for (int h = 0; h < 2; ++h) {
+                uint4 x[4];
+                next_rows(x);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                  const uint32_t code = e4m3x2_to_half2(y[e >> 1] >> (16 * (e & 1)));
-                  const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&code), f);
-                  z[e] = *reinterpret_cast<const uint32_t*>(&v);
+                for (int i = 0; i < 4; ++i) {  // lane r0 has the scale
+                  const __half2 f = __float2half2_rn(__shfl_sync(0xffffffffu, sc[2 * h + (i >> 1)], r0));
+                  const uint32_t y[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+                  uint32_t z[8];
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) {
+                    const uint32_t code = e4m3x2_to_half2(y[e >> 1] >> (16 * (e & 1)));
+                    const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&code), f);
+                    z[e] = *reinterpret_cast<const uint32_t*>(&v);
+                  }
+                  put_unit(h, i, z);
                 }
-                unsigned char* at = to + h * 8192 + (i >> 1) * 4096 + (i & 1) * 16384;
-                *reinterpret_cast<uint4*>(at) = make_uint4(z[0], z[1], z[2], z[3]);
-                *reinterpret_cast<uint4*>(at + other) = make_uint4(z[4], z[5], z[6], z[7]);
+              }
+            } else {  // a loop of its own: with both in one, plain chunks took 2 % longer
+#pragma unroll 1
+              for (int h = 0; h < 2; ++h) {
+                uint4 x[4];
+                next_rows(x);
+                if (is_v) {  // the four lanes of a row look whether it is zeros
+#pragma unroll
+                  for (int i = 0; i < 2; ++i) {
+                    uint32_t any = x[2 * i].x | x[2 * i].y | x[2 * i].z | x[2 * i].w | x[2 * i + 1].x | x[2 * i + 1].y |
+                                   x[2 * i + 1].z | x[2 * i + 1].w;
+                    any |= __shfl_xor_sync(0xffffffffu, any, 1);
+                    any |= __shfl_xor_sync(0xffffffffu, any, 2);
+                    const float s1 = __shfl_sync(0xffffffffu, h == 0 ? sc[i] : sc[2 + i], r0);
+                    if (u == 0) to_scales[r0 + 64 * h + 32 * i] = (any & 0x7f7f7f7fu) == 0u ? -CUDART_INF_F : __log2f(s1);
+                  }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const uint32_t y[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+                  uint32_t z[8];
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) z[e] = e4m3x2_to_half2(y[e >> 1] >> (16 * (e & 1)));
+                  put_unit(h, i, z);
+                }
               }
             }
           } else {
@@ -718,14 +772,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
                 const int r = r1 + 8 * e;
                 if (is_v) x[e] = take_out_wild<BF>(x[e], found);
                 float power = 1.f;
-                if (BF) {
-                  power = row_power(row_max16(top_of(x[e])));
-                  x[e] = bf16_to_half(x[e], inverse_power(power));
+                float top = 1.f;
+                if (BF || is_v) {  // fp16 values only grow, which is exact
+                  top = row_max16(top_of<BF>(x[e]));
+                  power = BF ? row_power(top) : fminf(row_power(top), 1.f);
+                  x[e] = times_to_half<BF>(x[e], inverse_power(power));
                 }
-                if (nu == 0) {
-                  to_scales[r] = r < w.n ? power : 0.f;
-                  to_scales[kMaxDrafts + r] = 0.f;
-                }
+                if (nu == 0) to_scales[r] = !is_v ? power : top == 0.f ? -CUDART_INF_F : __log2f(power);  // no row: zeros
                 *reinterpret_cast<uint4*>(slot + tile_off(r, nu)) = x[e];
               }
             }
@@ -774,7 +827,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
       const bool mine = my_row < w.rows;
       const uint32_t at = w.row0 + (mine ? my_row : 0), token = at / G;
       const int head = w.kvh * G + (at - token * G);
-      float m = -CUDART_INF_F, l = 0.f, vs = C8 ? 0.f : 1.f, f = kScaleLog2;
+      float m = -CUDART_INF_F, l = 0.f, f = kScaleLog2;
+      float power = 0.f;  // C8: log2 k
       bool first = true;
       // O of this group times `alpha`
       auto rescale = [&](float alpha) {
@@ -799,7 +853,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
         const bool is_new = w.has_new && j == w.chunks - 1;
         const int left = w.len - (w.from + j) * kTile;  // cache rows of this chunk
         if (C8) f = row_factor[(ord & 1) * L::kRows + my_row];
-        if (!is_new && left >= kTile && (!C8 || ((plain_of[((chunk0 + j) & 3) * 2] & plain_of[((chunk0 + j) & 3) * 2 + 1]) != 0 && vs <= 1.f))) {
+        const bool plain = !C8 || (plain_of[((chunk0 + j) & 3) * 2] & plain_of[((chunk0 + j) & 3) * 2 + 1]) != 0;
+        // (sums that k has made smaller by 2^40 or more might leave fp32 without it)
+        if (!is_new && left >= kTile && plain && (!C8 || !__any_sync(0xffffffffu, power < -40.f))) {
           // ---- a whole chunk without scales
           float mx[2] = {-CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
@@ -816,13 +872,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
             }
           }
           const float top = fmaxf(mx[0], mx[1]) * f;
-          if (__any_sync(0xffffffffu, top > m + 8.f || vs < 1.f)) {
-            const float m_new = top > m + 8.f ? top : m;
-            const float alpha = m_new == m ? 1.f : exp2_fast(m - m_new);
+          if (__any_sync(0xffffffffu, top > m + kLag || (C8 && power != 0.f))) {
+            const float m_new = top > m + kLag ? top - kTopPower : m;
+            const float up = m_new == m ? 0.f : m_new - m;
             m = m_new;
-            l *= alpha;
-            if (!first) rescale(alpha * vs);
-            vs = 1.f;
+            l *= exp2_fast(-up);
+            if (!first) rescale(exp2_fast(-up - power));
+            power = 0.f;
           }
           const float nm = m == -CUDART_INF_F ? 0.f : -m;
           float sum[4] = {0.f, 0.f, 0.f, 0.f};
@@ -849,7 +905,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
         } else {
           // ---- scales, the end of the cache or the new tokens: 32 keys at a time, twice
           const float4* ks = reinterpret_cast<const float4*>(scales + ((chunk0 + j) % kScaleRing) * 2 * kTile);
-          const float4* vv = ks + kTile / 4;
+          const float4* lv = ks + kTile / 4;
           const uint64_t seen = is_new && mine ? p.mask[w.t0 + token] & (w.n < 64 ? (1ull << w.n) - 1 : ~0ull) : 0ull;
           auto scores = [&](int b, float (&s)[32]) {  // times the keys' scales; -infinity where the row does not see
             uint32_t raw[32];
@@ -868,35 +924,57 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
             }
           };
           const int blocks = is_new ? 2 : 4;
-          float top = -CUDART_INF_F, vtop = vs;
+          float top = -CUDART_INF_F, top_v = -CUDART_INF_F;  // of the scores, and of them with the values' scales
 #pragma unroll 1
           for (int b = 0; b < blocks; ++b) {
             float s[32];
             scores(b, s);
 #pragma unroll
             for (int e = 0; e < 32; e += 2) top = max3(top, s[e], s[e + 1]);
+            if (C8) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const float4 v = lv[8 * b + e];
+                top_v = max3(top_v, fmaf(s[4 * e], f, v.x), fmaf(s[4 * e + 1], f, v.y));
+                top_v = max3(top_v, fmaf(s[4 * e + 2], f, v.z), fmaf(s[4 * e + 3], f, v.w));
+              }
+            }
           }
           top *= f;
-          if (C8) {
-            const float4 x = vv[lane];  // largest value scale of the chunk, the same for every row
-            vtop = fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w));
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) vtop = fmaxf(vtop, __shfl_xor_sync(0xffffffffu, vtop, o));
-            vtop = fmaxf(vtop, vs);
-          }
-          if (__any_sync(0xffffffffu, top > m + 8.f || vtop > vs)) {
-            const float m_new = top > m + 8.f ? top : m;
-            float alpha = m_new == m ? 1.f : exp2_fast(m - m_new);
+          const float above = C8 ? top_v - m + power : 0.f;  // of the largest weight times scale times k
+          // (fp16 keeps 11 bits down to 2^-14, so 4 bits of range for what lies below the largest)
+          const bool far_below = C8 && !first && !plain && above < -10.f && top_v > -CUDART_INF_F;
+          if (__any_sync(0xffffffffu, top > m + kLag || (C8 && above > 8.f + kTopPower) || far_below)) {
+            const float m_new = top > m + kLag ? top - kTopPower : m;
+            const float up = m_new == m ? 0.f : m_new - m;
             m = m_new;
-            l *= alpha;
+            l *= exp2_fast(-up);
+            float alpha = exp2_fast(-up);
             if (C8) {
-              alpha *= vtop > 0.f ? vs / vtop : 1.f;
-              vs = vtop;
+              const float held = floorf(power + up);  // the sums as large as they are
+              float most = first ? kMostPower : held;
+              if (__any_sync(0xffffffffu, far_below)) {
+                float a = 0.f;
+#pragma unroll 1
+                for (int c = 0; c < kD; c += 32) {
+                  uint32_t o[32];
+                  tmem_ld32_issue(ocol + t * kTile + c, o);
+                  tmem_wait_ld32(o);
+#pragma unroll
+                  for (int e = 0; e < 32; ++e) a = fmaxf(a, fabsf(__uint_as_float(o[e])));
+                }
+                const int room = a < CUDART_INF_F ? min(max(142 - static_cast<int>(__float_as_uint(a) >> 23), 0), 120) : 0;
+                if (far_below) most = held + static_cast<float>(room);  // they grow to 2^16 at most
+              }
+              if (top_v > -CUDART_INF_F) most = fminf(most, floorf(kTopPower - (top_v - m)));
+              most = fminf(most, kMostPower);
+              alpha = exp2_fast(most - power - up);
+              power = most;
             }
             if (!first) rescale(alpha);
           }
           const float nm = m == -CUDART_INF_F ? 0.f : -m;
-          const float inv = C8 ? (vs > 0.f ? 1.f / vs : 0.f) : 1.f;
+          const float nv = nm + power;
 #pragma unroll 1
           for (int b = 0; b < blocks; ++b) {
             float s[32];
@@ -908,9 +986,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
               float x = exp2_fast(fmaf(s[2 * e], f, nm)), y = exp2_fast(fmaf(s[2 * e + 1], f, nm));
               sum += x + y;
               if (C8) {
-                const float2 v = reinterpret_cast<const float2*>(vv)[16 * b + e];
-                x *= v.x * inv;
-                y *= v.y * inv;
+                const float2 v = reinterpret_cast<const float2*>(lv)[16 * b + e];
+                x = exp2_fast(fmaf(s[2 * e], f, v.x) + nv);
+                y = exp2_fast(fmaf(s[2 * e + 1], f, v.y) + nv);
               }
               pk[e] = pack16<kBf>(x, y);
             }
@@ -935,7 +1013,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
       tc_fence_after();
       if (!w.pair) {
         ml_of[t * kTile + r] = make_float2(m, l);
-        if (r == 0) group_vs[t] = vs;
+        if (C8) power_of[t * kTile + r] = power;
       }
       // both groups, also after an abort: all leave together
       int all_ok;
@@ -953,11 +1031,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
         w1 = weight_of(b.x, m);
         l = a.y * w0 + b.y * w1;
         if (C8) {
-          w0 *= group_vs[0];
-          w1 *= group_vs[1];
+          w0 = weight_of(a.x - power_of[r], m);
+          w1 = weight_of(b.x - power_of[kTile + r], m);
         }
       } else if (C8) {
-        w0 = vs;
+        w0 = exp2_fast(-power);
       }
       const bool whole = w.of == 1;
       const bool two = !w.pair && w.chunks > 1;

@@ -159,3 +159,96 @@ def test_rows_of_every_size_few_rows(shape):
         v *= torch.exp2(torch.randint(-60, 10, (v.shape[0], 1, 1), generator=torch.Generator().manual_seed(5)).float())
 
     agree(build([640, 200], *shape, BF16, 45, values=values, new_values=lambda v: v.mul_(1e-6)), slack=2.0)
+
+
+@pytest.mark.parametrize("zeros", ["none", "some", "most"])
+@pytest.mark.parametrize("dtype,scale", SMALL)
+@pytest.mark.parametrize("shape", MANY)
+def test_small_values_many_rows(shape, dtype, scale, zeros):
+    agree(small_values(shape, scale, dtype, zeros))
+
+
+@pytest.mark.parametrize("value", [1e4, 1e8])
+@pytest.mark.parametrize("shape", MANY)
+def test_a_large_row_of_little_weight_many_rows(shape, value):
+    keys, values = a_row_of_little_weight(value)
+    c = build([500, 150], *shape, BF16, 43, keys=keys, values=values)
+    c["q"] = c["q"].abs()
+    agree(c, v_max=6.0)
+
+
+@pytest.mark.parametrize("order", ["mixed", "first", "last"])
+@pytest.mark.parametrize("shape", MANY)
+def test_small_rows_that_carry_the_weight_many_rows(shape, order):
+    """`first` and `last`: whole chunks that need no scales behind or before whole chunks that do."""
+    keys, values = on_small_rows(order)
+    c = build([700, 260], *shape, BF16, 44, keys=keys, values=values)
+    c["q"] = c["q"].abs()
+    c["mask"] = [0] * len(c["mask"])
+    agree(c, v_max=6 * 2.0 ** -40, slack=2.0)
+
+
+@pytest.mark.parametrize("shape", MANY)
+def test_rows_of_every_size_many_rows(shape):
+    def values(v, own):
+        v *= torch.exp2(torch.randint(-60, 10, (v.shape[0], 1, 1), generator=torch.Generator().manual_seed(5)).float())
+
+    agree(build([640, 200], *shape, BF16, 45, values=values, new_values=lambda v: v.mul_(1e-6)), slack=2.0)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -8, 2.0 ** -30])
+@pytest.mark.parametrize("shape", MANY)
+def test_zeros_then_small_values(shape, scale):
+    """A cache that starts with chunks of zeros, whose scales say nothing; new tokens as small as the rest."""
+    def values(v, own):
+        v *= scale
+        for at in own:
+            v[at[:512]] = 0
+
+    agree(build([900, 640], *shape, BF16, 46, values=values, new_values=lambda v: v.mul_(scale)))
+
+
+@pytest.mark.parametrize("scale", [1.0, 1e-5])
+@pytest.mark.parametrize("shape", MANY + FEW[1:])
+def test_scales_of_any_kind(shape, scale):
+    """Scales that are no powers of two, over several chunks."""
+    c = build([900, 300], *shape, BF16, 47, values=lambda v, own: v.mul_(scale), new_values=lambda v: v.mul_(scale))
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    c["vs"] = c["vs"] * (0.6 + 0.3 * torch.rand(c["vs"].shape, generator=gen, device="cuda"))
+    c["ks"] = c["ks"] * (0.8 + 0.4 * torch.rand(c["ks"].shape, generator=gen, device="cuda"))
+    agree(c)
+
+
+@pytest.mark.parametrize("value", [1e5, 1e10, 1e30])
+@pytest.mark.parametrize("shape", MANY + FEW[1:])
+def test_an_unseen_draft_of_any_size_has_no_effect(shape, value):
+    c = build([300, 0], *shape, BF16, 48)
+    n, hidden = shape[0], 5
+    c["mask"] = [m & ~(1 << hidden) for m in c["mask"]]
+    c["mask"][hidden] |= 1 << hidden
+    clean, lse, _ = run(c)
+    for t in (hidden, n + hidden):
+        c["vn"][t] = c["vn"][t] * value
+    out, lse2, status = run(c)
+    blind = [i for i in range(2 * n) if i % n != hidden]
+    assert status == fsx.FSX_OK and torch.equal(out[blind], clean[blind]) and torch.equal(lse[:, blind], lse2[:, blind])
+    want, _ = oracle(c)
+    err = to64(out)[blind] - want[blind]
+    assert np.linalg.norm(err) <= U[BF16] * np.linalg.norm(want[blind])
+
+
+@pytest.mark.parametrize("value", [1e5, 1e10])
+@pytest.mark.parametrize("shape", MANY + FEW[1:])
+def test_a_large_draft_of_little_weight(shape, value):
+    """Everyone sees token 1, whose key is -12 against queries of positive components: a weight of e^-108."""
+    c = build([200, 0], *shape, BF16, 49)
+    n = shape[0]
+    c["q"] = c["q"].abs()
+    c["mask"] = [m | 2 for m in c["mask"]]
+    for t in (1, n + 1):
+        c["kn"][t] = -12
+        c["vn"][t] = c["vn"][t] * value
+    # (a row that sees nothing else takes it whole: none here, every token sees itself and token 1 another)
+    c["mask"][1] |= 1
+    c["mask"][n + 1] |= 1
+    agree(c, v_max=6.0)
