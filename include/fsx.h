@@ -504,8 +504,9 @@ void fsx_session_destroy(fsx_session s);
  * the smallest power of two s (at least 2^-126) with max|x| / s <= 448, and the code is x / s
  * rounded to e4m3 (nearest, ties to even). A row of zeros has scale 1.
  *   d_k, d_v   : DEVICE [n_rows] rows of `dtype` (FSX_F32, FSX_BF16, FSX_F16), kv_stride apart.
- *   d_rows     : DEVICE int64 [n_rows]: the cache row that row i goes to; NULL: row i. Rows that
- *                repeat leave one of their values.
+ *   d_rows     : DEVICE int64 [n_rows]: the cache row that row i goes to; NULL: row i. They are
+ *                distinct: a cache row that several go to holds codes and scales of any of them
+ *                afterwards, which need not belong together; the other rows are not affected.
  *   d_k_cache, d_v_cache : DEVICE e4m3 [cache_rows, n_kv_heads, 128].
  *   d_k_scale, d_v_scale : DEVICE fp32 [n_kv_heads, cache_rows].
  * A destination outside 0 .. cache_rows-1 sets the status to FSX_ERR_DEVICE_ARG and its row is

@@ -5,6 +5,9 @@
 // the scale max|x| / 448 it costs nothing in precision, since e4m3 keeps its relative step over the
 // range (only values 2^-14 of the maximum meet subnormals a bit earlier).
 // Scales lie as [head, row]: the attention of one head reads them along the rows.
+// Codes and scales of a row are stored by several lanes, and the rows of a call by warps in no order, so that destinations have
+// to be distinct: to order writers of one row would take a pass over the row numbers ahead of this one, as long as a small
+// write itself.
 //
 // Both kernels are bound by memory: 16 lanes hold a row of a head (8 values each, 16-byte loads or
 // stores of the 16-bit side, 8 bytes of codes), a warp takes 8 consecutive rows, all loads issued

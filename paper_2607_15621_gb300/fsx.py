@@ -405,7 +405,7 @@ def _cache8_call(k, v, rows, k_cache, v_cache, k_scale, v_scale):
 
 
 def cache_write(k, v, rows, k_cache, v_cache, k_scale, v_scale, status, stream=None):
-    """fsx_cache_write_e4m3: rows k, v [n, kv heads, 128] into cache rows `rows` (int64 [n]; None: 0 .. n - 1)."""
+    """fsx_cache_write_e4m3: rows k, v [n, kv heads, 128] into cache rows `rows` (int64 [n], distinct; None: 0 .. n - 1)."""
     code, shape, pitch, m = _cache8_call(k, v, rows, k_cache, v_cache, k_scale, v_scale)
     on = _raw_stream(_device()) if stream is None else _stream(stream)
     error = (_lib or lib()).fsx_cache_write_e4m3(

@@ -143,3 +143,26 @@ def test_no_rows_and_offsets_beyond_32_bits():
         want, scale = llm_oracle.cache_write(to64(x))
         assert np.array_equal(to64(got), want * scale[..., None])
     assert (kc.view(torch.uint8)[:-5] == 0x55).all()
+
+
+def test_rows_that_repeat_leave_the_others_alone():
+    """Destinations have to be distinct; where they are not, only the row that is named twice is unspecified."""
+    n, heads = 64, 3
+    k, v = values(n, heads, torch.bfloat16, 9), values(n, heads, torch.bfloat16, 10)
+    k[1::2] *= 2.0 ** 40
+    v[1::2] *= 2.0 ** -40
+    rows = torch.arange(n, device="cuda") + 2
+    rows[[5, 6, 30, 63]] = 40  # beside its own writer, row 38
+    (kc, vc), (ks, vs) = cache(n + 8, heads)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    fsx.cache_write(k, v, rows, kc, vc, ks, vs, status)
+    assert int(status) == fsx.FSX_OK
+    once = [i for i in range(n) if int(rows[i]) != 40]
+    at = rows[once]
+    for x, c, s in ((k, kc, ks), (v, vc, vs)):
+        want, scale = llm_oracle.cache_write(to64(x[once]))
+        assert same(c.view(torch.uint8)[at].view(torch.float8_e4m3fn), want)
+        assert np.array_equal(s[:, at].T.double().cpu().numpy(), scale)
+        rest = torch.ones(n + 8, dtype=torch.bool, device="cuda")
+        rest[rows] = False
+        assert (c.view(torch.uint8)[rest] == 0x55).all() and (s[:, rest] == 7).all()
