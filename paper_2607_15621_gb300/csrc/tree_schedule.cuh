@@ -46,7 +46,7 @@ struct TreeShape {
   int slots;             // of the workspace
 };
 
-__device__ __forceinline__ int tree_chunks(const TreeShape& s, int len) { return (len + s.chunk - 1) / s.chunk + 1; }
+__device__ __forceinline__ int tree_chunks(const TreeShape& s, int len) { return static_cast<int>((static_cast<uint32_t>(len) + s.chunk - 1) / s.chunk) + 1; }
 __device__ __forceinline__ int tree_pieces(const TreeShape& s, int n, int most) {
   return n <= s.few ? 1 : (n + most - 1) / most;
 }

@@ -40,6 +40,7 @@
 // Registers: 640 threads at 96 from launch; softmax warpgroups take 2 x 128, producers keep 2 x 80, MMA and scheduler 64
 // (with 104, 96 and 80 the softmax spilled into its loop, with 128, 88 and 48 the MMA warp into its own: the wide
 // tree 52.4 and 50.2 for 48.9 us).
+#include "chunk_line.h"
 #include "fsx.h"
 #include "kernels.h"
 #include "llm.h"
@@ -63,7 +64,6 @@ constexpr int kWorkUsers = 17;               // warps that read a piece's descri
 constexpr uint32_t kColS = 0, kColO = 256;
 constexpr int kMaxGrid = 256;
 constexpr int kPartials = 2 * kMaxGrid;      // slots of the workspace
-constexpr int kLeast = 4;                    // chunks of a range or of a piece of a cut item
 constexpr int kStart = 5;                    // chunks that a piece's start and end cost
 
 // A piece as every role sees it
@@ -160,15 +160,15 @@ __device__ __forceinline__ float row_max16(float t) {  // over the 16 lanes that
   return t;
 }
 
-// The line of work: pre[b] pieces (most > 0) or chunks (ranges) of the requests before b, pre[B] of all. Counted in 32 bits:
-// 2^32 chunks would take hours, and each 64-bit division is a hundred instructions that every CTA waits for.
+// The line of work: pre[b] pieces (most > 0) or chunks (ranges) of the requests before b, pre[B] of all, in 32 bits: each 64-bit
+// division is a hundred instructions that every CTA waits for. The chunks are counted first, in 64 bits (chunk_line.h); a line
+// that is too long for places of 32 bits goes by whole items, of which there are below 2^23.
 struct Line {
   uint32_t* pre;
   uint32_t most;  // chunks of a piece; 0: ranges
-  uint32_t per;   // chunks of a range
+  uint32_t per;   // chunks of a range; 0: no ranges
 };
-__device__ __forceinline__ uint32_t chunks_of(int len) { return (len + kTile - 1) / kTile + 1; }  // the last one: new tokens
-__device__ __forceinline__ uint32_t above(uint32_t a, uint32_t b) { return (a + b - 1) / b; }
+__device__ __forceinline__ uint32_t chunks_of(int len) { return above(static_cast<uint32_t>(len), kTile) + 1; }  // the last one: new tokens
 // By the whole CTA: a warp weighs a plan. `costs`: kPlans (cost, most), then the range and a value per warp
 template <int ROWS>
 __device__ __forceinline__ Line line_of(const TreeArgs& p, uint32_t* pre, uint32_t* chunks, uint32_t* costs) {
@@ -184,15 +184,16 @@ __device__ __forceinline__ Line line_of(const TreeArgs& p, uint32_t* pre, uint32
   }
   __syncthreads();
   if (warp < kPlans) {
-    uint32_t total = 0, longest = 0;
+    ChunkCount mine;
+    uint32_t longest = 0;
 #pragma unroll 1
     for (int b = lane; b < p.B; b += 32) {
-      total += pre[b] * chunks[b];
+      mine.add(pre[b], chunks[b]);
       longest = max(longest, chunks[b]);
     }
-    total = __reduce_add_sync(0xffffffffu, total);
+    const uint64_t total = ChunkCount::sum(__reduce_add_sync(0xffffffffu, mine.low()), __reduce_add_sync(0xffffffffu, mine.high()));
     longest = __reduce_max_sync(0xffffffffu, longest);
-    const uint32_t per = max(above(total, gridDim.x), static_cast<uint32_t>(kLeast));
+    const uint32_t per = range_of(total, gridDim.x);
     // whole items, then pieces of 1, 1.25, 1.5 and 2 ranges
     const uint32_t most = warp == 0 ? longest : per * (warp < 4 ? 3 + warp : 8) / 4;
     float cost = CUDART_INF_F;
@@ -213,7 +214,7 @@ __device__ __forceinline__ Line line_of(const TreeArgs& p, uint32_t* pre, uint32
   }
   __syncthreads();
   Line line{pre, 0, costs[2 * kPlans]};
-  float best = static_cast<float>(line.per + 2 * kStart);
+  float best = line.per > 0 ? static_cast<float>(line.per + 2 * kStart) : CUDART_INF_F;
 #pragma unroll
   for (int i = 0; i < kPlans; ++i) {
     const float cost = __uint_as_float(costs[2 * i]);
