@@ -115,7 +115,8 @@ __device__ __forceinline__ uint32_t try_bar(uint32_t addr, uint32_t parity) {
   return done;
 }
 // Waits for phase `parity` of an mbarrier; false once a wait of the CTA has given up (about one second:
-// the status word and `abort` are set). The timer's low word wraps after 4.3 s.
+// the status word and `abort` are set). The timer's low word wraps after 4.3 s. A lane whose time is up leaves by the flag, which
+// its whole warp reads at once: the lanes of a warp get the same answer.
 __device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, int* status, volatile int* abort) {
   const uint32_t addr = smem_addr(bar);
   if (__builtin_expect(try_bar(addr, parity) != 0u, 1)) return true;
@@ -130,7 +131,6 @@ __device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, in
     if (now - t0 > kWaitLimitNs && now - t0 < 0x80000000u) {
       set_status(status, kStatusTimeout);
       *abort = 1;
-      return false;
     }
   }
 }

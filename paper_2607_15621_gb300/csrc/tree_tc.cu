@@ -820,9 +820,20 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
     bool ok = true;
     int chunk0 = 0;
     uint32_t s_count = 0;
+    // What all 256 threads of both groups say. No group may go on to a piece, or to its end, that the other has given up: it
+    // would wait there for ever.
+    auto both_groups = [](bool mine) {
+      int all;
+      asm volatile(
+          "{\n .reg .pred p, q;\n setp.ne.s32 p, %1, 0;\n barrier.red.and.pred q, 1, 256, p;\n selp.s32 %0, 1, 0, q;\n}"
+          : "=r"(all)
+          : "r"(static_cast<int>(mine))
+          : "memory");
+      return all != 0;
+    };
 #pragma unroll 1
-    for (int ord = 0; ok; ++ord) {
-      if (!find_work(ord)) break;
+    for (int ord = 0;; ++ord) {
+      if (!both_groups(find_work(ord))) break;  // (and the sums of the piece before are read)
       const Work& w = works[ord % kWorkRing];
       const int my_row = w.pair ? t * kTile + r : r;
       const bool mine = my_row < w.rows;
@@ -1016,14 +1027,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
         ml_of[t * kTile + r] = make_float2(m, l);
         if (C8) power_of[t * kTile + r] = power;
       }
-      // both groups, also after an abort: all leave together
-      int all_ok;
-      asm volatile(
-          "{\n .reg .pred p, q;\n setp.ne.s32 p, %1, 0;\n barrier.red.and.pred q, 1, 256, p;\n selp.s32 %0, 1, 0, q;\n}"
-          : "=r"(all_ok)
-          : "r"(static_cast<int>(ok))
-          : "memory");
-      if (!all_ok) break;
+      if (!both_groups(ok)) break;
       float w0 = 1.f, w1 = 0.f;  // of the two accumulators, for `pair` of this group's own
       if (!w.pair) {
         const float2 a = ml_of[r], b = ml_of[kTile + r];
@@ -1119,7 +1123,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const TreeArgs p) 
       chunk0 += w.chunks;
       give_back(ord);
       fence_proxy_async();  // the queries' place goes back to the tensor core
-      asm volatile("bar.sync 1, 256;" ::: "memory");  // the groups' sums are read before they are written again
+      __syncwarp();
       if (lane == 0) mbar_arrive(qempty);
     }
   }
