@@ -373,15 +373,15 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
           ++c;
         }
       }
-      if (!ok)  // what is on its way lands before the CTA leaves
-        for (int d = c - 1; d >= 0 && d >= c - kStages; --d, guarded >>= 1) {
-          if (guarded & 1u) {
-            --g;
-            mbar_wait(gfull + g % kGuarded, (g / kGuarded) & 1, p.status);
-          } else {
-            mbar_wait(full + d % kStages, (d / kStages) & 1, p.status);
-          }
+      // What is on its way lands before the CTA leaves, also where all loads were issued before another role gave up
+      for (int d = c - 1; d >= 0 && d >= c - kStages; --d, guarded >>= 1) {
+        if (guarded & 1u) {
+          --g;
+          mbar_wait(gfull + g % kGuarded, (g / kGuarded) & 1, p.status);
+        } else {
+          mbar_wait(full + d % kStages, (d / kStages) & 1, p.status);
         }
+      }
     }
     __syncwarp();
   } else {
@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const PromptArgs p,
       c0 += 2 * n_all;
     }
     cp_async_wait<0>();
-    if (!ok && by_tma && lane == 0)  // queries on their way land before the CTA leaves
+    if (by_tma && lane == 0)  // queries on their way land before the CTA leaves
       for (int t = 0; t < 2; ++t)
         if (uses[t] > 0) mbar_wait(qfull + t, (uses[t] - 1) & 1, p.status);
   }
