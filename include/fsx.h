@@ -492,10 +492,12 @@ void fsx_session_destroy(fsx_session s);
  *     16 bytes); outputs and caches are contiguous. Offsets may exceed 32 bits in elements.
  *   - d_status: DEVICE int, not NULL, that the caller zeroes once and reads when it likes. A
  *     call that finds an error writes its code there unless one is there already; no call clears it.
- *   - Scores, softmax statistics and sums are fp32. Weights of the values are rounded to `dtype`. Over
- *     an 8-bit cache the products are in fp16: weights are rounded to fp16, codes are exact in it, and
- *     rows of bf16 that meet codes become fp16 times a power of two a row, exact for values of at
- *     least 2^-22 of the row's largest; smaller ones may lose their last bits.
+ *   - Scores, softmax statistics and sums are fp32. Weights of the values are rounded to `dtype`; in fp16
+ *     one below 2^-14 of the row's largest loses bits, one below 2^-24 all of them. Over an 8-bit cache
+ *     the products are in fp16: codes are exact in it, weights are rounded to it, alone or times the
+ *     scale of the values in a unit of each row's own, which follows what the row sees. Rows of bf16 that
+ *     meet codes become fp16 times a power of two a row, exact for values of at least 2^-22 of the row's
+ *     largest; smaller ones may lose their last bits.
  *   - A key that a row does not see has no effect on it, whatever the key and value hold (NaN and
  *     infinities too). A row that sees no key gets zeros and a log-sum-exp of -infinity.
  *   - Outputs overlap no input. Asynchronous on `stream`; nothing is allocated. */

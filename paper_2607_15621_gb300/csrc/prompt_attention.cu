@@ -24,7 +24,8 @@
 // the last; a chunk takes about 2,600). Items go longest first, mirrored from round to round; the rank of an item
 // in the order of chunks is found by counting (the host knows no lengths).
 //
-// Measured: 8192 tokens, 32 heads over 8, causal: 322 to 328 us, 1680 TFLOP/s (0.88 of the library's matrix product).
+// Measured: 8192 tokens, 32 heads over 8, causal: 323 to 326 us in a graph, 1690 TFLOP/s (0.89 of the library's matrix product), 368 us
+// call by call on changing inputs.
 // A chunk of two tiles takes 2,600 cycles, of which its MMAs need 2,048 (tensor pipe 74 % active over the kernel) and its
 // exponentials 1,024. 16 prompts of 139 to 452 tokens: 32 us, where items of one to four chunks pay 5,000 cycles each for
 // their start and outputs. Four chunks of 123 to 511 tokens behind 1277 to 1936 rows: 48 us; 160 items for 152 SMs, so

@@ -25,8 +25,8 @@
 // The 4 warps of a CTA take every fourth 16 keys of a chunk of 64 and are put together in shared memory. Items are cut
 // into pieces that CTAs take from a queue (tree_schedule.cuh); the last one to end joins the pieces of its item.
 //
-// Measured: single tokens of 128 requests, 1.08 GB of 8-bit cache, 168 to 176 us (6.2 TB/s, 0.90 of a copy's rate; DRAM
-// 80 % busy, issue slots 52 %). One token over 224 rows of a 16-bit cache 6.5 us, which is one launch and three
+// Measured: single tokens of 128 requests, 1.08 GB of 8-bit cache, 170 to 175 us (6.2 TB/s, 0.91 of a copy's rate; DRAM
+// 81 % busy, issue slots 53 %). One token over 224 rows of a 16-bit cache 6.5 us, which is one launch and three
 // dependent trips to memory: offsets, keys, results.
 #include <math_constants.h>
 
@@ -724,7 +724,7 @@ Kernel kernel_of(int nt) {
 }
 
 // 8-row tiles of an item, by the rows that a request has on average; 0: the kernel of tree_tc.cu. Measured over eight
-// 8-bit caches of 4096 to 8192 rows: 8 to 16 rows a request 42.4 us here, 51.8 there; 16 to 32 rows 53.0 us there,
+// 8-bit caches of 4096 to 8192 rows: 8 to 16 rows a request 42 to 44 us here, 51.8 there; 16 to 32 rows 51.5 us there,
 // 57.0 here, in items of 16 that read the cache twice. Two tiles where one will do: 7.6 for 6.5 us (one token over 224
 // rows), 205 for 168 us (128 tokens).
 int tile_count(int B, long long new_rows, int n_heads, int n_kv_heads) {

@@ -1,13 +1,16 @@
 // How the attention of drafted tokens shares its work out. Every (request, tile of its rows, kv head)
-// is an item of ceil(cache rows / chunk) chunks and one more for the new tokens. Items of more than
-// `most` chunks are cut into near-equal pieces; `most` follows from the number of all chunks (the host knows no
-// lengths), so that one long request fills the GPU as well as many short ones. CTAs take pieces from
-// one queue: equal shares fixed before left the SMs idle a quarter of the time (some read the caches faster
-// than others, and a short cache costs more per row). The pieces of a cut item are put together by
-// whichever comes last, in the order of its keys, so that results do not depend on the order of arrival.
+// is an item of ceil(cache rows / chunk) chunks and one more for the new tokens. The kernel for many rows
+// (tree_tc.cu) takes only the requests and the workspace's head from here; it plans, stores and joins its pieces itself.
 //
-// Workspace: the queue, one counter per cut item, one slot of partial results per piece of a cut item.
-// All counters are zero between calls.
+// The kernel for few rows (tree_attention.cu): items of up to `few` chunks stay whole; longer ones are cut into near-equal pieces
+// of `most` chunks at most, which follows from the number of all chunks (the host knows no lengths), so that one long request
+// fills the GPU as well as many short ones. CTAs take pieces from one queue: equal shares fixed before left the SMs idle a
+// quarter of the time (some read the caches faster than others, and a short cache costs more per row). The pieces of a cut
+// item are put together by whichever comes last, in the order of its keys, so that results do not depend on the order of
+// arrival.
+//
+// Workspace: the header, counters (one per cut item, at its first slot), one slot of partial results per piece of a cut
+// item. Header and counters are zero between calls.
 #pragma once
 
 #include "device_util.cuh"
@@ -15,7 +18,7 @@
 
 namespace fsx {
 
-constexpr int kTreeHeader = 64;      // ints: [0] next piece, [1] CTAs that are done
+constexpr int kTreeHeader = 64;      // ints: [0] pieces taken from the queue, beyond each CTA's first, [1] CTAs that are done
 constexpr int kTreeCounters = 8192;  // as many for every kernel: what follows them may hold anything
 
 struct TreeRequest {

@@ -6,7 +6,8 @@
 //   O += P V      A in tensor memory, V read N-contiguous, O in tensor memory
 // Two S / P / O sets and two groups of softmax warps: in an item of more than 128 rows each works on its
 // own 128 rows and every chunk; else both on the same rows, one on the even and one on the odd chunks, so that
-// the tensor core always has the other's work while one is at its exponentials; their two results meet at the end.
+// the tensor core always has the other's work while one is at its exponentials; their two results meet at the end. Where a wait
+// gives up, both groups leave together.
 //
 // Eight producer warps, four for K and four for V, copy the rows of a chunk by 16-byte asynchronous copies, each
 // thread its own units, and wait for nobody: 16-bit rows straight into their slot, 8-bit rows into a private stage, from where the thread that copied
@@ -30,16 +31,17 @@
 // warp finds the pieces and describes them in a ring for the other roles. Cut items are put together by a
 // second kernel, a warp a row: 256 rows are too many for the one CTA that comes last.
 //
-// Measured: one tree of 50 tokens, 32 heads over 8, behind 32768 8-bit rows: 49 us, of which the plan, the queries and
-// the first keys take 10 us, 13.5 chunks of 256 rows 28 us (about 3,900 cycles each, of which MMAs 2,048 and
+// Measured (calls in a graph): one tree of 50 tokens, 32 heads over 8, behind 32768 8-bit rows: 49 to 50 us, of which the plan, the
+// queries and the first keys take 10 us, 13.5 chunks of 256 rows 28 us (about 3,900 cycles each, of which MMAs 2,048 and
 // exponentials 1,024: a tile's S, softmax and P V follow each other, and their instructions share the schedulers with
-// the producers') and results and join 10 us. Eight requests of 24 tokens at most over 4096 to 8192 rows: 54 us with
-// 8-bit, 53 us with 16-bit caches (3.8 TB/s). 16 requests of 6 to 11 tokens over 96 to 480 rows: 21 us, mostly the latency
-// of the same steps: plan 2.5, first piece 1, queries 2.4, first keys 1, three chunks 6, results 4, join 2 us.
+// the producers') and results and join 10 us. Eight requests of 24 tokens at most over 4096 to 8192 rows: 55 us with
+// 8-bit, 52.5 us with 16-bit caches (3.9 TB/s). 16 requests of 6 to 11 tokens over 96 to 480 rows: 22 us, mostly the latency
+// of the same steps: plan 2.5, first piece 1, queries 2.4, first keys 1, three chunks 6, results 4, join 2 us. k costs 2 %
+// to 3 % of a call over an 8-bit cache.
 //
-// Registers: 640 threads at 96 from launch; softmax warpgroups take 2 x 128, producers keep 2 x 80, MMA and scheduler 64
-// (with 104, 96 and 80 the softmax spilled into its loop, with 128, 88 and 48 the MMA warp into its own: the wide
-// tree 52.4 and 50.2 for 48.9 us).
+// Registers: 640 threads at 96 from launch, which is what the compiler gives every role: a few words spill in all variants (24 to
+// 28 bytes stored). Softmax warpgroups take 2 x 128, producers keep 2 x 80, MMA and scheduler 64 (with 104, 96 and 80, and with
+// 128, 88 and 48, more spilled: the wide tree 52.4 and 50.2 us where this split took 48.9).
 #include "chunk_line.h"
 #include "fsx.h"
 #include "kernels.h"
