@@ -579,6 +579,133 @@ fsx_status fsx_tree_attention(const void* d_q, long long q_stride, const void* d
                               int n_heads, int n_kv_heads, int head_dim, void* d_out, float* d_lse,
                               void* d_workspace, size_t workspace_bytes, int* d_status, void* stream);
 
+/* ================================================================ a cache in pages
+ * The operators around a cache that many requests share over time: its rows belong to pages, a
+ * table names each request's, and pages are shared, copied, freed and moved.
+ *   - A page is page_rows consecutive rows (a power of two, 16 to 1024) of a cache as the operators above
+ *     have it, [cache_rows, n_kv_heads, 128] with scales [n_kv_heads, cache_rows]; cache_rows are whole pages.
+ *     Row r of page p is cache row p * page_rows + r, so fsx_cache_write_e4m3 writes into pages too.
+ *   - d_table: DEVICE int32 [B, width]: row j of request b lies in page d_table[b][j / page_rows]. Entries
+ *     behind a request's last page are not read. d_lengths: DEVICE int64 [B], rows of each request, 0 to
+ *     width * page_rows. B is 1 .. 1024; width * page_rows and cache_rows are below 2^31.
+ *   - The conventions above hold (heads, strides, status, roundings, asynchronous, nothing allocated). A request whose
+ *     length is out of range, or that has a page outside the cache, sets FSX_ERR_DEVICE_ARG and gets no output;
+ *     the others are written. */
+
+/* Rotary positions of one to four axes (say time, height, width), and the keys' and values' rows into a cache.
+ * Pair j (0 .. 63) of a head is its dims (j, j + 64), or (2 j, 2 j + 1) with FSX_ROTARY_ADJACENT; it turns by
+ * d_positions[axis[j]][row] * rate[j] radians: (a, b) -> (a cos - b sin, a sin + b cos). Angles are exact to
+ * 2^-32 of a turn at any position up to 2^31 (negative ones turn back); products are fp32, rounded once.
+ *   d_q, d_q_out : DEVICE [n_rows] rows of `dtype` (FSX_BF16 or FSX_F16), strides apart; or both NULL.
+ *   d_k, d_k_out : the same with n_kv_heads. Either result may be its input itself (same pointer and stride).
+ *                  d_k_out may be NULL where there is a cache; all NULL: queries only.
+ *   d_positions  : DEVICE int64 [n_axes, n_rows].
+ *   axis, rate   : HOST [64]; |rate| <= 2^20.
+ *   d_k_cache, d_v_cache, d_rows, scales, cache_rows : as fsx_cache_write_e4m3, or NULL for no cache; cache_dtype is
+ *                  `dtype` (then no scales) or FSX_E4M3. Row i of the rotated keys, as rounded to `dtype`, and of d_v (kv_stride
+ *                  apart like d_k) goes to cache row d_rows[i] (NULL: i), distinct ones; one outside 0 .. cache_rows-1 sets
+ *                  FSX_ERR_DEVICE_ARG and is left out of the cache. Values that are not finite: as fsx_cache_write_e4m3. */
+enum { FSX_ROTARY_HALVES = 0, FSX_ROTARY_ADJACENT = 1 };
+fsx_status fsx_rotary(const void* d_q, long long q_stride, const void* d_k, const void* d_v, long long kv_stride, int dtype,
+                      const int64_t* d_positions, int n_axes, const int* axis, const double* rate, int layout,
+                      long long n_rows, int n_heads, int n_kv_heads, int head_dim, void* d_q_out, long long q_out_stride,
+                      void* d_k_out, long long k_out_stride, const int64_t* d_rows, void* d_k_cache, void* d_v_cache,
+                      float* d_k_scale, float* d_v_scale, int cache_dtype, long long cache_rows, int* d_status,
+                      void* stream);
+
+/* Attention of one new token of each request over the request's rows, d_lengths[b] of them (its own, if it is to see
+ * itself, has been written already).
+ *   d_q        : DEVICE [B] rows of `dtype` (FSX_BF16 or FSX_F16), q_stride apart.
+ *   caches     : of `dtype` or FSX_E4M3 with scales, as fsx_tree_attention.
+ *   d_picked   : NULL, or DEVICE int32 [B, n_kv_heads, n_picked]: only these pages of the request are attended to by the
+ *                heads of that kv head. Entries are places in the request's table (0: its first page), distinct, in any order; of a request
+ *                with n pages the first min(n, n_picked) are read; -1: none. Any other entry that is no page of
+ *                the request sets FSX_ERR_DEVICE_ARG, and the heads of that kv head get no output. n_picked is 1 .. 4096.
+ *   d_out      : DEVICE [B, n_heads, 128] of `dtype`; d_lse : DEVICE fp32 [n_heads, B] or NULL. A request without rows gets
+ *                zeros and -infinity.
+ *   d_workspace : as fsx_tree_attention: fsx_paged_attention_workspace_bytes(...) bytes, 256-byte aligned, zeroed once; calls that
+ *                overlap on the GPU (graphs that may run at the same time, too) must not share it. Its size
+ *                does not depend on B. */
+size_t fsx_paged_attention_workspace_bytes(int B, int n_heads, int n_kv_heads);
+fsx_status fsx_paged_attention(const void* d_q, long long q_stride, int dtype, const void* d_k_cache, const void* d_v_cache,
+                               const float* d_k_scale, const float* d_v_scale, int cache_dtype, long long cache_rows,
+                               int page_rows, const int32_t* d_table, int width, const int64_t* d_lengths, int B,
+                               const int32_t* d_picked, int n_picked, int n_heads, int n_kv_heads, int head_dim, void* d_out,
+                               float* d_lse, void* d_workspace, size_t workspace_bytes, int* d_status, void* stream);
+
+/* Bounds of the keys of pages, which fsx_page_select goes by: for every request those of the pages that hold its rows from
+ * d_start[b] on (d_start: DEVICE int64 [B], or NULL: all). Per page, kv head and dimension the least and the largest
+ * key: scale s the smallest power of two (at least 2^-126) with max|key| / s <= 127, codes floor(least / s) and ceil(largest / s).
+ *   d_k_cache    : of cache_dtype FSX_BF16, FSX_F16 or FSX_E4M3 (with d_k_scale).
+ *   d_bounds     : DEVICE int8 [pages, n_kv_heads, 2, 128] (least, largest), d_bound_scale : DEVICE fp32 [n_kv_heads, pages],
+ *                  pages = cache_rows / page_rows; other pages stay as they are. A page that several requests share gets those of
+ *                  either's rows in it: let it be full, or take the bounds of one.
+ * Keys that are not finite are left out and set FSX_ERR_RANGE. */
+fsx_status fsx_page_bounds(const void* d_k_cache, const float* d_k_scale, int cache_dtype, long long cache_rows, int page_rows,
+                           const int32_t* d_table, int width, const int64_t* d_lengths, const int64_t* d_start, int B,
+                           int n_kv_heads, int head_dim, int8_t* d_bounds, float* d_bound_scale, int* d_status, void* stream);
+
+/* The pages that each kv head of each request attends to: its first `first` and last `last` pages and, up to n_picked (1 .. 4096)
+ * in all, those of the highest score, the lowest page first among equals.
+ *   score = max over the heads of the group of 2^e * sum_d max(c_d lo_d, c_d hi_d), with the bounds' codes lo and hi, c = the query
+ *   over its scale (as the bounds', one per head) rounded to the nearest whole number, ties to even, and 2^e the product
+ *   of both scales, e limited to -100 .. 100. This is exact in fp32: the choice is the same on every run.
+ *   d_picked : DEVICE int32 [B, n_kv_heads, n_picked]: places in the request's table, ascending, -1 behind the last.
+ * width is at most 65536. A value of a query that is not finite counts as 0 and sets FSX_ERR_RANGE; a page outside the cache
+ * sets FSX_ERR_DEVICE_ARG and comes last; a request of a bad length gets a list of -1 only. */
+fsx_status fsx_page_select(const void* d_q, long long q_stride, int dtype, const int8_t* d_bounds, const float* d_bound_scale,
+                           long long cache_rows, int page_rows, const int32_t* d_table, int width, const int64_t* d_lengths,
+                           int B, int n_heads, int n_kv_heads, int head_dim, int first, int last, int n_picked,
+                           int32_t* d_picked, int* d_status, void* stream);
+
+/* One step of the page tables: requests go on, are forked, are freed, and grow. d_refs: DEVICE int32 [n_pages], how often each page
+ * is held, by the tables and by whatever else the caller counts in; 0: free.
+ *   1. Request i of B takes on the pages and the length of request d_source[i] of B_in (DEVICE int32 [B]; -1: none, an empty
+ *      request; NULL: request i itself, B = B_in). Requests that nobody names are freed. Holders are counted anew.
+ *   2. It grows by n = d_new_offsets[i+1] - d_new_offsets[i] rows (DEVICE int64 [B+1], within 0 .. new_rows). New rows go on in its
+ *      last page if that has room. If others hold that page too, it gets a page in its place, and the pair (old, new) is
+ *      listed for fsx_pages_copy; of the requests that do so at once the last one keeps the page if nobody else
+ *      holds it. New pages are the lowest free ones, in the order of the requests.
+ *   d_table_out [B, width], d_lengths_out [B], d_refs_out [n_pages]: the new state. Without d_source each may be its input.
+ *                With d_source the table and the lengths need buffers of their own. A table in its own place changes only where
+ *                pages are new; one in another is written whole, -1 behind a request's last page.
+ *   d_rows     : DEVICE int64 [new_rows]: the cache row of every new row, for fsx_cache_write_e4m3 or fsx_rotary.
+ *   d_pairs    : DEVICE int32 [B, 2], d_n_pairs : DEVICE int32: pages to copy (before the new rows are written).
+ * If the free pages do not last, requests are served in order; the first that finds too few and those behind it that
+ * need pages do not grow, get rows of -1, and FSX_ERR_OOM is set. A request that would pass its table's width, whose source or
+ * offsets are out of range, or whose last page is none of the cache sets FSX_ERR_DEVICE_ARG and does not grow either (a bad
+ * source or length: comes out empty); other entries that name no page are taken along and counted nowhere. */
+fsx_status fsx_pages_step(const int32_t* d_table, const int64_t* d_lengths, const int32_t* d_refs, int B_in,
+                          const int32_t* d_source, const int64_t* d_new_offsets, int B, long long new_rows, int width,
+                          int n_pages, int page_rows, int32_t* d_table_out, int64_t* d_lengths_out, int32_t* d_refs_out,
+                          int64_t* d_rows, int32_t* d_pairs, int32_t* d_n_pairs, int* d_status, void* stream);
+
+/* Moves the pages in use to the front of the cache: with u pages held (refs > 0), the i-th held page from u on goes to
+ * the i-th free one below u. d_table_out and d_refs_out (each may be its input) are the new state, d_pairs (DEVICE int32 [max_pairs, 2],
+ * max_pairs >= n_pages / 2) and d_n_pairs the moves (old, new) for fsx_pages_copy; holders outside the tables find
+ * theirs there. Entries behind a request's last page are taken along as they are. */
+fsx_status fsx_pages_compact(const int32_t* d_table, const int64_t* d_lengths, const int32_t* d_refs, int B, int width,
+                             int n_pages, int page_rows, int32_t* d_table_out, int32_t* d_refs_out, int32_t* d_pairs,
+                             int max_pairs, int32_t* d_n_pairs, int* d_status, void* stream);
+
+/* Copies pages: for every pair (from, to) of the first *d_n_pairs, everything that the planes hold of page `from` to page `to`.
+ * A plane is an array with something for each page: a cache has page_bytes = page_rows * n_kv_heads * 128 * element and one
+ * segment; scales [n_kv_heads, cache_rows] have n_kv_heads segments of page_bytes = 4 * page_rows, segment_stride =
+ * 4 * cache_rows; bounds page_bytes = 256 * n_kv_heads and one segment, their scales page_bytes 4 and n_kv_heads segments.
+ * Page p of segment s begins at base + s * segment_stride + p * page_bytes.
+ *   planes     : HOST [n_planes], 1 .. 512. Bytes are multiples of 4, bases 4-byte aligned (16 for speed).
+ *   d_pairs    : DEVICE int32 [max_pairs, 2]; pages that are copied to are distinct and none that is copied from.
+ * A pair outside 0 .. n_pages-1 sets FSX_ERR_DEVICE_ARG and is left out; so does a count outside 0 .. max_pairs, and nothing is
+ * copied. */
+typedef struct {
+  void* base;                /* DEVICE                                     */
+  long long page_bytes;      /* of a page, in one segment                  */
+  long long segment_stride;  /* bytes between segments, if there are more  */
+  int segments;              /* of a page                                  */
+} fsx_page_plane;
+fsx_status fsx_pages_copy(const fsx_page_plane* planes, int n_planes, int n_pages, const int32_t* d_pairs,
+                          const int32_t* d_n_pairs, int max_pairs, int* d_status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

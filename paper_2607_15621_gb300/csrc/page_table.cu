@@ -1,0 +1,474 @@
+// Page tables: a step of them (requests forked, freed and grown), compaction, and the copies of pages that both ask for
+// (fsx_pages_step, fsx_pages_compact, fsx_pages_copy).
+//
+// A page is free when nobody holds it (refs 0). The free pages that a step hands out are the lowest ones, in the order of the requests, so
+// that equal states give equal tables: counts of holders are sums of atomics, which do not depend on their order, and every place is a
+// count of what lies before it.
+//
+// A step and a compaction are one launch each, of one cluster of 8 CTAs: their phases follow one another by cluster barriers (0.5 us),
+// each CTA takes an eighth of the pages, and the CTAs tell each other their counts through distributed shared memory.
+// Bound by latency: a handful of dependent trips to memory; the holders' counts are read twice.
+// The copies are bound by memory: both ends of every page move once, all layers in one launch.
+#include <cooperative_groups.h>
+
+#include "device_util.cuh"
+#include "fsx.h"
+#include "kernels.h"
+#include "pages.h"
+
+namespace cg = cooperative_groups;
+
+namespace fsx {
+
+namespace {
+
+constexpr int kCtas = 8;
+constexpr int kThreads = 512;
+constexpr int kWarps = kThreads / 32;
+constexpr int kPerThread = kMaxSequences / kThreads;  // requests
+
+enum : int { kStatusOom = 3 };
+
+struct TableShared {
+  int n[kMaxSequences];     // rows of a request before its new tokens
+  int add[kMaxSequences];   // new tokens, 0: none or not possible
+  int last[kMaxSequences];  // its last page, if new tokens go into it, else -1
+  long long end[kMaxSequences];  // pages that it and the requests before it need
+  unsigned char copies[kMaxSequences];
+  int nth[kMaxSequences];  // copies of the requests before
+  long long scan[kWarps];
+  int scan2[kWarps];
+  int counts[2][kCtas];
+};
+
+// sum over the threads before this one; `total`: of all
+__device__ __forceinline__ long long scan_before(long long x, long long* warps, long long& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  long long sum = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long up = __shfl_up_sync(0xffffffffu, sum, o);
+    if (lane >= o) sum += up;
+  }
+  __syncthreads();
+  if (lane == 31) warps[warp] = sum;
+  __syncthreads();
+  total = 0;
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) sum += warps[w];
+    total += warps[w];
+  }
+  return sum - x;
+}
+__device__ __forceinline__ int scan_before(int x, int* warps, int& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int sum = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int up = __shfl_up_sync(0xffffffffu, sum, o);
+    if (lane >= o) sum += up;
+  }
+  __syncthreads();
+  if (lane == 31) warps[warp] = sum;
+  __syncthreads();
+  total = 0;
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) sum += warps[w];
+    total += warps[w];
+  }
+  return sum - x;
+}
+
+// The pages first .. end - 1 of this CTA
+__device__ __forceinline__ void part_of(int n_pages, int rank, int& first, int& end) {
+  const int part = ((n_pages + kCtas - 1) / kCtas + 3) & ~3;
+  first = static_cast<int>(min(static_cast<long long>(n_pages), static_cast<long long>(rank) * part));
+  end = static_cast<int>(min(static_cast<long long>(n_pages), static_cast<long long>(first) + part));
+}
+
+// Every CTA's `mine`, where every CTA can read it
+__device__ __forceinline__ void tell(cg::cluster_group& cluster, int (&counts)[kCtas], int rank, int mine) {
+  if (threadIdx.x < kCtas) *cluster.map_shared_rank(&counts[rank], threadIdx.x) = mine;
+  cluster.sync();
+}
+
+// Rows of request `i` of a table of lengths; -1: more than its pages hold, or negative
+__device__ __forceinline__ int rows_at(const int64_t* lengths, int i, int width, int shift) {
+  const long long n = lengths[i];
+  return n < 0 || n > static_cast<long long>(width) << shift || n > 0x7fffffffll - 64 ? -1 : static_cast<int>(n);
+}
+__device__ __forceinline__ int pages_for(long long n, int shift) { return static_cast<int>((n + (1 << shift) - 1) >> shift); }
+
+__global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) step_kernel(const StepArgs a) {
+  extern __shared__ __align__(16) unsigned char raw_smem[];
+  TableShared& sm = *reinterpret_cast<TableShared*>(raw_smem);
+  cg::cluster_group cluster = cg::this_cluster();
+  const int rank = static_cast<int>(cluster.block_rank()), tid = threadIdx.x, lane = tid & 31;
+  const int thread = rank * kThreads + tid, warp = thread >> 5;
+  constexpr int kAllThreads = kCtas * kThreads, kAllWarps = kAllThreads / 32;
+  const bool moved = a.table_out != a.table;
+  if (a.refs_out != a.refs) {
+    for (int i = thread; i < a.n_pages; i += kAllThreads) a.refs_out[i] = a.refs[i];
+  }
+  cluster.sync();
+  // ---- rows of the table, and the holders of their pages: a request that goes on from itself changes none
+  auto source = [&](int i) { return a.source != nullptr ? a.source[i] : i; };
+  for (int i = warp; i < a.B; i += kAllWarps) {
+    const int src = source(i);
+    const bool fine = src >= -1 && src < a.B_in;
+    const int n = fine && src >= 0 ? rows_at(a.lengths, src, a.width, a.shift) : 0;
+    if ((!fine || n < 0) && lane == 0) set_status(a.status, kStatusDeviceArg);
+    const int had = n > 0 ? pages_for(n, a.shift) : 0;
+    if (!moved && src == i) continue;
+    const int32_t* from = a.table + static_cast<long long>(src) * a.width;
+    int32_t* to = a.table_out + static_cast<long long>(i) * a.width;
+    for (int j = lane; j < a.width; j += 32) {
+      const int page = j < had ? from[j] : -1;
+      to[j] = page;
+      if (src != i && j < had) {
+        if (page >= 0 && page < a.n_pages) atomicAdd(a.refs_out + page, 1);
+        else set_status(a.status, kStatusDeviceArg);
+      }
+    }
+  }
+  for (int i = warp; i < a.B_in; i += kAllWarps) {
+    if (i < a.B && source(i) == i) continue;
+    const int n = rows_at(a.lengths, i, a.width, a.shift);
+    if (n < 0 && lane == 0) set_status(a.status, kStatusDeviceArg);
+    const int had = n > 0 ? pages_for(n, a.shift) : 0;
+    for (int j = lane; j < had; j += 32) {
+      const int page = a.table[static_cast<long long>(i) * a.width + j];
+      if (page >= 0 && page < a.n_pages) atomicSub(a.refs_out + page, 1);
+      else set_status(a.status, kStatusDeviceArg);
+    }
+  }
+  cluster.sync();
+  // ---- what each request needs; every CTA for itself
+  for (int i = tid; i < a.B; i += kThreads) {
+    const int src = source(i);
+    int n = src >= 0 && src < a.B_in ? rows_at(a.lengths, src, a.width, a.shift) : 0;
+    long long add = 0;
+    const long long t0 = a.new_offsets[i], t1 = a.new_offsets[i + 1];
+    bool fine = t0 >= 0 && t1 >= t0 && t1 <= a.new_rows;
+    if (n < 0) n = 0;
+    else if (fine) add = t1 - t0;
+    if (n + add > static_cast<long long>(a.width) << a.shift || n + add > 0x7fffffffll - 64) {
+      add = 0;
+      fine = false;
+    }
+    int last = -1;
+    if (add > 0 && (n & ((1 << a.shift) - 1)) != 0) {
+      last = a.table[static_cast<long long>(src) * a.width + (n >> a.shift)];
+      if (last < 0 || last >= a.n_pages) {
+        add = 0;
+        last = -1;
+        fine = false;
+      }
+    }
+    if (!fine && rank == 0) set_status(a.status, kStatusDeviceArg);
+    sm.n[i] = n;
+    sm.add[i] = static_cast<int>(add);
+    sm.last[i] = last;
+  }
+  __syncthreads();
+  long long need[kPerThread], mine = 0;
+  int copy[kPerThread], my_copies = 0;
+  const int per = (a.B + kThreads - 1) / kThreads;  // requests of a thread, one behind another
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u) {
+    const int i = tid * per + u;
+    need[u] = 0;
+    copy[u] = 0;
+    if (u < per && i < a.B) {
+      const int last = sm.last[i], held = last >= 0 ? __ldcg(a.refs_out + last) : 0;
+      if (held > 1) {  // of all that write into it the last one keeps it, if nobody else holds it
+        int writers = 0, behind = 0;
+        for (int x = 0; x < a.B; ++x)
+          if (sm.last[x] == last) {
+            ++writers;
+            behind = x;
+          }
+        copy[u] = !(held == writers && i == behind);
+      }
+      if (sm.add[i] > 0) need[u] = pages_for(static_cast<long long>(sm.n[i]) + sm.add[i], a.shift) - (pages_for(sm.n[i], a.shift) - copy[u]);
+      mine += need[u];
+      my_copies += copy[u];
+    }
+  }
+  long long total;
+  int total_copies;
+  long long before = scan_before(mine, sm.scan, total);
+  int copies_before = scan_before(my_copies, sm.scan2, total_copies);
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u) {
+    const int i = tid * per + u;
+    if (u < per && i < a.B) {
+      before += need[u];
+      sm.end[i] = before;
+      sm.copies[i] = static_cast<unsigned char>(copy[u]);
+      sm.nth[i] = copies_before;
+      copies_before += copy[u];
+    }
+  }
+  // ---- the free pages before this CTA's, and all of them
+  int first, last_page;
+  part_of(a.n_pages, rank, first, last_page);
+  int free_pages = 0;
+  for (int i = first + tid; i < last_page; i += kThreads) free_pages += __ldcg(a.refs_out + i) <= 0;
+  int in_part;
+  scan_before(free_pages, sm.scan2, in_part);
+  tell(cluster, sm.counts[0], rank, in_part);
+  long long all_free = 0, nth_free = 0;
+  for (int r = 0; r < kCtas; ++r) {
+    if (r < rank) nth_free += sm.counts[0][r];
+    all_free += sm.counts[0][r];
+  }
+  // a request grows if the pages last for it and all before it, or if it needs none
+  auto start_of = [&](int i) { return i > 0 ? sm.end[i - 1] : 0ll; };
+  auto grows = [&](int i) { return sm.end[i] <= all_free || sm.end[i] == start_of(i); };
+  const long long wanted = min(total, all_free);
+  for (int base = first; base < last_page && nth_free < wanted; base += kThreads) {
+    const int page = base + tid;
+    const bool is_free = page < last_page && __ldcg(a.refs_out + page) <= 0;
+    int in_tile;
+    const long long nth = nth_free + scan_before(is_free ? 1 : 0, sm.scan2, in_tile);
+    nth_free += in_tile;
+    if (!is_free || nth >= wanted) continue;
+    int lo = 0, hi = a.B - 1;  // the first request whose end lies above nth
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (sm.end[mid] > nth) hi = mid;
+      else lo = mid + 1;
+    }
+    if (!grows(lo)) continue;
+    const int n = sm.n[lo], kept = pages_for(n, a.shift) - sm.copies[lo], col = kept + static_cast<int>(nth - start_of(lo));
+    a.table_out[static_cast<long long>(lo) * a.width + col] = page;
+    a.refs_out[page] = 1;
+    const long long t0 = a.new_offsets[lo], end = static_cast<long long>(n) + sm.add[lo];
+    for (long long x = max(static_cast<long long>(n), static_cast<long long>(col) << a.shift); x < min(end, static_cast<long long>(col + 1) << a.shift); ++x)
+      a.rows[t0 + x - n] = (static_cast<long long>(page) << a.shift) + (x - (static_cast<long long>(col) << a.shift));
+    if (sm.copies[lo] && col == kept) {
+      a.pairs[2 * sm.nth[lo]] = sm.last[lo];
+      a.pairs[2 * sm.nth[lo] + 1] = page;
+    }
+  }
+  // ---- lengths, rows in pages that are there already
+  if (rank == 0) {
+    int copied = 0;
+    for (int i = tid; i < a.B; i += kThreads) {
+      const bool grown = grows(i);
+      const int n = sm.n[i], add = sm.add[i];
+      const long long t0 = a.new_offsets[i], t1 = a.new_offsets[i + 1];
+      a.lengths_out[i] = n + (grown ? add : 0);
+      if (!grown) set_status(a.status, kStatusOom);
+      if (!grown || add == 0) {
+        for (long long t = max(t0, 0ll); t < min(t1, a.new_rows); ++t) a.rows[t] = -1;
+      } else if (sm.last[i] >= 0) {
+        if (sm.copies[i]) {
+          atomicSub(a.refs_out + sm.last[i], 1);
+          ++copied;
+        } else {
+          const int col = n >> a.shift;
+          const long long end = min(static_cast<long long>(n) + add, static_cast<long long>(col + 1) << a.shift);
+          for (long long x = n; x < end; ++x)
+            a.rows[t0 + x - n] = (static_cast<long long>(sm.last[i]) << a.shift) + (x - (static_cast<long long>(col) << a.shift));
+        }
+      }
+    }
+    int all_copied;
+    scan_before(copied, sm.scan2, all_copied);
+    if (tid == 0) *a.n_pairs = all_copied;
+  }
+}
+
+__global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) compact_kernel(const CompactArgs a) {
+  __shared__ int scan[kWarps];
+  __shared__ int counts[3][kCtas];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int rank = static_cast<int>(cluster.block_rank()), tid = threadIdx.x;
+  const int thread = rank * kThreads + tid;
+  constexpr int kAllThreads = kCtas * kThreads;
+  int first, end;
+  part_of(a.n_pages, rank, first, end);
+  int mine = 0;
+  for (int i = first + tid; i < end; i += kThreads) {
+    const int r = a.refs[i];
+    mine += r > 0;
+    if (r < 0 || a.refs_out != a.refs) a.refs_out[i] = max(r, 0);
+  }
+  int in_part;
+  scan_before(mine, scan, in_part);
+  tell(cluster, counts[0], rank, in_part);
+  int used = 0;
+  for (int r = 0; r < kCtas; ++r) used += counts[0][r];
+  // ---- the i-th page in use at `used` or above goes to the i-th free one below: as many as those
+  int moves = 0, room = 0;
+  for (int i = first + tid; i < end; i += kThreads) {
+    const bool in_use = __ldcg(a.refs_out + i) > 0;
+    moves += in_use && i >= used;
+    room += !in_use && i < used;
+  }
+  int all_moves, all_room;
+  scan_before(moves, scan, all_moves);
+  scan_before(room, scan, all_room);
+  if (tid < kCtas) *cluster.map_shared_rank(&counts[2][rank], tid) = all_room;
+  tell(cluster, counts[1], rank, all_moves);
+  int nth_move = 0, nth_room = 0, m = 0;
+  for (int r = 0; r < kCtas; ++r) {
+    if (r < rank) {
+      nth_move += counts[1][r];
+      nth_room += counts[2][r];
+    }
+    m += counts[1][r];
+  }
+  for (int base = first; base < end; base += kThreads) {
+    const int i = base + tid;
+    const bool there = i < end, in_use = there && __ldcg(a.refs_out + i) > 0;
+    const bool goes = in_use && i >= used, takes = there && !in_use && i < used;
+    int in_tile;
+    // a tile may hold both, in two runs: one scan for both, halves of a word
+    const int at = scan_before((goes ? 1 : 0) + (takes ? 1 << 16 : 0), scan, in_tile);
+    if (goes) a.pairs[2 * (nth_move + (at & 0xffff))] = i;
+    if (takes) a.pairs[2 * (nth_room + (at >> 16)) + 1] = i;
+    nth_move += in_tile & 0xffff;
+    nth_room += in_tile >> 16;
+  }
+  cluster.sync();
+  // ---- holders move; the old place keeps the new one for the tables, as -1 - page
+  for (int i = thread; i < m; i += kAllThreads) {
+    const int src = __ldcg(a.pairs + 2 * i), dst = __ldcg(a.pairs + 2 * i + 1);
+    a.refs_out[dst] = __ldcg(a.refs_out + src);
+    a.refs_out[src] = -1 - dst;
+  }
+  cluster.sync();
+  const long long entries = static_cast<long long>(a.B) * a.width;
+  for (long long e = thread; e < entries; e += kAllThreads) {
+    const int b = static_cast<int>(e / a.width), j = static_cast<int>(e - static_cast<long long>(b) * a.width);
+    const int n = rows_at(a.lengths, b, a.width, a.shift);
+    int page = a.table[e];
+    bool changed = a.table_out != a.table;
+    if (n < 0) {
+      if (j == 0) set_status(a.status, kStatusDeviceArg);
+    } else if (j < pages_for(n, a.shift)) {
+      if (page < 0 || page >= a.n_pages) {
+        set_status(a.status, kStatusDeviceArg);
+      } else if (page >= used) {
+        const int r = __ldcg(a.refs_out + page);
+        if (r < 0) {
+          page = -1 - r;
+          changed = true;
+        }
+      }
+    }
+    if (changed) a.table_out[e] = page;
+  }
+  cluster.sync();
+  for (int i = thread; i < m; i += kAllThreads) a.refs_out[__ldcg(a.pairs + 2 * i)] = 0;
+  if (thread == 0) *a.n_pairs = m;
+}
+
+// ---------------------------------------------------------------- copies
+
+constexpr int kCopyThreads = 256;
+constexpr int kUnit = 16384;  // bytes that a CTA moves at a time
+
+struct CopyPlane {
+  unsigned char* base;
+  long long page_bytes, stride;
+  int segments, units;  // units of a segment
+  int first;            // units of the planes before, of one page
+};
+struct CopyArgs {
+  const int32_t* pairs;
+  const int32_t* n_pairs;
+  int max_pairs, n_pages, n_planes, units;  // units of one page over all planes
+  int* status;
+  CopyPlane planes[kMaxPlanes];
+};
+
+__global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ CopyArgs a) {
+  const int tid = threadIdx.x;
+  int n = *a.n_pairs;
+  if (n < 0 || n > a.max_pairs) {
+    if (blockIdx.x == 0 && tid == 0) set_status(a.status, kStatusDeviceArg);
+    n = 0;
+  }
+  const long long total = static_cast<long long>(n) * a.units;
+  for (long long w = blockIdx.x; w < total; w += gridDim.x) {
+    const int pair = static_cast<int>(w / a.units), unit = static_cast<int>(w - static_cast<long long>(pair) * a.units);
+    const int src = __ldg(a.pairs + 2 * pair), dst = __ldg(a.pairs + 2 * pair + 1);
+    if (src < 0 || src >= a.n_pages || dst < 0 || dst >= a.n_pages) {
+      if (tid == 0) set_status(a.status, kStatusDeviceArg);
+      continue;
+    }
+    int lo = 0, hi = a.n_planes - 1;  // the last plane that begins at `unit` or before
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (a.planes[mid].first <= unit) lo = mid;
+      else hi = mid - 1;
+    }
+    const CopyPlane& p = a.planes[lo];
+    const int in_plane = unit - p.first, segment = in_plane / p.units;
+    const long long at = static_cast<long long>(in_plane - segment * p.units) * kUnit;
+    const long long bytes = min(static_cast<long long>(kUnit), p.page_bytes - at);
+    const unsigned char* from = p.base + segment * p.stride + src * p.page_bytes + at;
+    unsigned char* to = p.base + segment * p.stride + dst * p.page_bytes + at;
+    if (((reinterpret_cast<uintptr_t>(from) | reinterpret_cast<uintptr_t>(to) | static_cast<uintptr_t>(bytes)) & 15u) == 0) {
+      constexpr int kEach = kUnit / 16 / kCopyThreads;
+      const int n16 = static_cast<int>(bytes >> 4);
+      uint4 x[kEach];
+#pragma unroll
+      for (int i = 0; i < kEach; ++i)
+        if (tid + i * kCopyThreads < n16) x[i] = reinterpret_cast<const uint4*>(from)[tid + i * kCopyThreads];
+#pragma unroll
+      for (int i = 0; i < kEach; ++i)
+        if (tid + i * kCopyThreads < n16) reinterpret_cast<uint4*>(to)[tid + i * kCopyThreads] = x[i];
+    } else {
+      for (int i = tid; i < static_cast<int>(bytes >> 2); i += kCopyThreads)
+        reinterpret_cast<uint32_t*>(to)[i] = reinterpret_cast<const uint32_t*>(from)[i];
+    }
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_pages_step(const StepArgs& a, cudaStream_t stream) {
+  const void* fn = reinterpret_cast<const void*>(&step_kernel);
+  const cudaError_t e = allow_shared_memory(fn, sizeof(TableShared));
+  if (e != cudaSuccess) return e;
+  void* args[] = {const_cast<StepArgs*>(&a)};
+  return launch_ex(fn, dim3(kCtas), dim3(kThreads), sizeof(TableShared), stream, false, args);
+}
+
+cudaError_t launch_pages_compact(const CompactArgs& a, cudaStream_t stream) {
+  void* args[] = {const_cast<CompactArgs*>(&a)};
+  return launch_ex(reinterpret_cast<const void*>(&compact_kernel), dim3(kCtas), dim3(kThreads), 0, stream, false, args);
+}
+
+cudaError_t launch_pages_copy(const fsx_page_plane* planes, int n_planes, int n_pages, const int32_t* pairs,
+                              const int32_t* n_pairs, int max_pairs, int* status, cudaStream_t stream) {
+  CopyArgs a;
+  a.pairs = pairs;
+  a.n_pairs = n_pairs;
+  a.max_pairs = max_pairs;
+  a.n_pages = n_pages;
+  a.n_planes = n_planes;
+  a.status = status;
+  long long units = 0;
+  for (int i = 0; i < n_planes; ++i) {
+    const long long each = (planes[i].page_bytes + kUnit - 1) / kUnit;
+    a.planes[i] = CopyPlane{static_cast<unsigned char*>(planes[i].base), planes[i].page_bytes, planes[i].segment_stride,
+                            planes[i].segments, static_cast<int>(each), static_cast<int>(units)};
+    units += each * planes[i].segments;
+    if (units > 0x3fffffffll) return cudaErrorInvalidValue;
+  }
+  a.units = static_cast<int>(units);
+  const int sms = sm_count();
+  if (sms == 0) return cudaErrorNoDevice;
+  const long long most = units * max_pairs, want = static_cast<long long>(sms) * 8;
+  void* args[] = {&a};
+  return launch_ex(reinterpret_cast<const void*>(&copy_kernel), dim3(static_cast<unsigned>(most < want ? most : want)), dim3(kCopyThreads), 0, stream,
+                   false, args);
+}
+
+}  // namespace fsx

@@ -1,0 +1,229 @@
+// Rotary positions of one or several axes for queries and keys, and the keys' and values' rows written into a cache in the
+// same pass (fsx_rotary).
+//
+// Pair j of a head turns by pos[axis_j] rate_j: (a, b) -> (a cos - b sin, a sin + b cos). The angle is taken in whole turns as
+// 64-bit fixed point: turns_j = rate_j / (2 pi) in units of 2^-64, and pos * turns_j modulo 2^64 is the fraction of a turn,
+// exactly as far as turns_j is; its upper 32 bits go to sincospi. An angle in fp32 would be off by 2^-24 of itself, at
+// position 100,000 by half a percent of a turn. So results depend on the position only through the turn's 2^-32.
+// Products in fp32, rounded once to the type; keys go into an 8-bit cache from their rounded values, so that a cache written
+// here has the bits of one written from the rotated keys by fsx_cache_write_e4m3.
+//
+// Bound by memory (no product to speak of): 8 lanes hold a head of a row, 16 values each, the two halves of 8 pairs; a warp
+// takes 4 heads at a time, 16 in flight. Its lanes compute the row's 64 sines and cosines, two each, and share them through
+// shared memory: each is used by all heads of the row. Where rows are few they are shared out by heads over several warps.
+#include "fsx.h"
+#include "kernels.h"
+#include "pages.h"
+#include "rows8.cuh"
+#include "tc_attention.cuh"
+
+namespace fsx {
+
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kAhead = 4;  // groups of 4 heads that are loaded at once
+
+template <bool BF>
+__device__ __forceinline__ void unpack8(const uint4& v, float (&x)[8]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = unpack16<BF>(w[i]);
+    x[2 * i] = f.x;
+    x[2 * i + 1] = f.y;
+  }
+}
+template <bool BF>
+__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
+  return make_uint4(pack16<BF>(x[0], x[1]), pack16<BF>(x[2], x[3]), pack16<BF>(x[4], x[5]), pack16<BF>(x[6], x[7]));
+}
+
+// 16 values of a head's row, 8 lanes a row: codes and the row's scale as fsx_cache_write_e4m3 makes them. False: values
+// that are not finite.
+__device__ __forceinline__ bool quantise(const float (&x)[2][8], uint2 (&code)[2], float& scale) {
+  uint32_t top = 0;
+  bool wild = false;
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t m = __float_as_uint(x[h][j]) & 0x7fffffffu;
+      if (m < 0x7f800000u) top = max(top, m);
+      else wild = true;
+    }
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  int e = static_cast<int>(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
+  e = max(e, -126);
+  const bool zero = top == 0;
+  scale = zero ? 1.f : __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
+  const float inv = zero ? 1.f : __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint32_t c[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c[j] = pack_e4m3x2(x[h][2 * j] * inv, x[h][2 * j + 1] * inv);
+    if (wild) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if ((__float_as_uint(x[h][j]) & 0x7fffffffu) >= 0x7f800000u) c[j >> 1] |= 0x7fu << ((j & 1) * 8);
+    }
+    code[h] = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+  }
+  return !wild;
+}
+
+enum { kNoCache = 0, kCache16 = 1, kCache8 = 2 };
+
+// `parts` warps a row, `per` groups of 4 heads each
+template <bool BF, bool ADJACENT, int CACHE>
+__global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant__ RotaryArgs a, int parts, int per) {
+  __shared__ __align__(16) float2 turn[kWarps][kHeadDim / 2];  // cosine, sine
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane & 7;
+  const long long w = static_cast<long long>(blockIdx.x) * kWarps + warp;
+  const long long row = w / parts;
+  if (row >= a.rows) return;  // the whole warp
+  const int part = static_cast<int>(w - row * parts);
+  const int nq = a.q != nullptr ? a.n_heads : 0, nk = a.k != nullptr ? a.n_kv_heads : 0;
+  const int slots = nq + nk + (CACHE != kNoCache ? nk : 0);
+  const int group_end = min(part * per + per, (slots + 3) >> 2);
+  constexpr int kSecond = ADJACENT ? 8 : kHeadDim / 2;  // from a lane's first 8 values to its others
+  const int dim = ADJACENT ? 16 * l : 8 * l;
+  const uint16_t* const q = static_cast<const uint16_t*>(a.q) + row * a.q_stride + dim;
+  const uint16_t* const k = static_cast<const uint16_t*>(a.k) + row * a.kv_stride + dim;
+  const uint16_t* const v = static_cast<const uint16_t*>(a.v) + row * a.kv_stride + dim;
+  uint4 x[kAhead][2];
+  auto load = [&](int group, uint4 (&to)[2]) {  // plain loads: a result may replace its input
+    const int s = group * 4 + (lane >> 3);
+    if (group < group_end && s < slots) {
+      const uint16_t* src = s < nq ? q + s * kHeadDim : s < nq + nk ? k + (s - nq) * kHeadDim : v + (s - nq - nk) * kHeadDim;
+      to[0] = *reinterpret_cast<const uint4*>(src);
+      to[1] = *reinterpret_cast<const uint4*>(src + kSecond);
+    } else {
+      to[0] = to[1] = make_uint4(0u, 0u, 0u, 0u);
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) load(part * per + i, x[i]);
+  long long at = -1;
+  if (CACHE != kNoCache) {
+    const long long r = a.dst_rows != nullptr ? __ldg(reinterpret_cast<const long long*>(a.dst_rows) + row) : row;
+    if (r >= 0 && r < a.cache_rows) at = r;
+    else if (lane == 0) set_status(a.status, kStatusDeviceArg);
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int j = lane + 32 * h;
+    const uint64_t pos = static_cast<uint64_t>(__ldg(reinterpret_cast<const long long*>(a.positions) + a.axis[j] * a.rows + row));
+    float c, s;
+    sincospif(static_cast<float>(static_cast<int32_t>((pos * a.turns[j]) >> 32)) * (1.f / 2147483648.f), &s, &c);
+    turn[warp][j] = make_float2(c, s);
+  }
+  __syncwarp();
+  float2 t[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float4 y = reinterpret_cast<const float4*>(&turn[warp][8 * l])[i];
+    t[2 * i] = make_float2(y.x, y.y);
+    t[2 * i + 1] = make_float2(y.z, y.w);
+  }
+  bool wild = false;
+#pragma unroll 1
+  for (int base = part * per; base < group_end; base += kAhead) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int s = (base + i) * 4 + (lane >> 3);
+      const bool there = base + i < group_end && s < slots;
+      uint4 y[2] = {x[i][0], x[i][1]};
+      if (base + kAhead < group_end) load(base + kAhead + i, x[i]);
+      const bool is_v = s >= nq + nk;
+      float f[2][8];
+      unpack8<BF>(y[0], f[0]);
+      unpack8<BF>(y[1], f[1]);
+      if (!is_v) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          float& p0 = ADJACENT ? f[j >> 2][2 * (j & 3)] : f[0][j];
+          float& p1 = ADJACENT ? f[j >> 2][2 * (j & 3) + 1] : f[1][j];
+          const float c = t[j].x, z = t[j].y, u = p0, o = p1;
+          p0 = u * c - o * z;
+          p1 = u * z + o * c;
+        }
+        y[0] = pack8<BF>(f[0]);
+        y[1] = pack8<BF>(f[1]);
+      }
+      const int kv = s - (is_v ? nq + nk : nq);
+      if (there && !is_v) {
+        uint16_t* out = s < nq ? static_cast<uint16_t*>(a.q_out) + row * a.q_out_stride + s * kHeadDim
+                               : static_cast<uint16_t*>(a.k_out) + row * a.k_out_stride + kv * kHeadDim;
+        if (s < nq || a.k_out != nullptr) {
+          *reinterpret_cast<uint4*>(out + dim) = y[0];
+          *reinterpret_cast<uint4*>(out + dim + kSecond) = y[1];
+        }
+      }
+      if (CACHE == kCache16) {
+        if (there && s >= nq && at >= 0) {
+          uint16_t* out = static_cast<uint16_t*>(is_v ? a.v_cache : a.k_cache) + (at * nk + kv) * kHeadDim + dim;
+          *reinterpret_cast<uint4*>(out) = y[0];
+          *reinterpret_cast<uint4*>(out + kSecond) = y[1];
+        }
+      } else if (CACHE == kCache8) {
+        if (__any_sync(0xffffffffu, there && s >= nq)) {
+          unpack8<BF>(y[0], f[0]);
+          unpack8<BF>(y[1], f[1]);
+          uint2 code[2];
+          float scale;
+          const bool fine = quantise(f, code, scale);
+          if (there && s >= nq) {
+            wild = wild || !fine;
+            if (at >= 0) {
+              unsigned char* out = static_cast<unsigned char*>(is_v ? a.v_cache : a.k_cache) + (at * nk + kv) * kHeadDim + dim;
+              if (ADJACENT) {
+                *reinterpret_cast<uint4*>(out) = make_uint4(code[0].x, code[0].y, code[1].x, code[1].y);
+              } else {
+                *reinterpret_cast<uint2*>(out) = code[0];
+                *reinterpret_cast<uint2*>(out + kSecond) = code[1];
+              }
+              if (l == 0) (is_v ? a.v_scale : a.k_scale)[kv * a.cache_rows + at] = scale;
+            }
+          }
+        }
+      }
+    }
+  }
+  if (CACHE == kCache8 && wild) set_status(a.status, kStatusRange);
+}
+
+template <bool BF, bool ADJACENT>
+const void* kernel_of(int cache) {
+  return cache == kNoCache  ? reinterpret_cast<const void*>(&rotary_kernel<BF, ADJACENT, kNoCache>)
+         : cache == kCache16 ? reinterpret_cast<const void*>(&rotary_kernel<BF, ADJACENT, kCache16>)
+                             : reinterpret_cast<const void*>(&rotary_kernel<BF, ADJACENT, kCache8>);
+}
+
+}  // namespace
+
+cudaError_t launch_rotary(const RotaryArgs& a, int dtype, bool adjacent, bool cache8, cudaStream_t stream) {
+  const int cache = a.k_cache == nullptr ? kNoCache : cache8 ? kCache8 : kCache16;
+  const void* fn = dtype == FSX_BF16 ? (adjacent ? kernel_of<true, true>(cache) : kernel_of<true, false>(cache))
+                                     : (adjacent ? kernel_of<false, true>(cache) : kernel_of<false, false>(cache));
+  const int nk = a.k != nullptr ? a.n_kv_heads : 0;
+  const int slots = (a.q != nullptr ? a.n_heads : 0) + (cache != kNoCache ? 2 : 1) * nk;
+  if (slots == 0) return cudaSuccess;
+  const int sms = sm_count();
+  if (sms == 0) return cudaErrorNoDevice;
+  // enough warps for every SM, and no more than there are groups of heads
+  const int groups = (slots + 3) / 4;
+  const long long want = (static_cast<long long>(sms) * 32 + a.rows - 1) / a.rows;
+  const int split = static_cast<int>(want < groups ? want : groups);
+  int per = (groups + split - 1) / split;
+  int parts = (groups + per - 1) / per;
+  const long long blocks = (a.rows * parts + kWarps - 1) / kWarps;
+  if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+  void* args[] = {const_cast<RotaryArgs*>(&a), &parts, &per};
+  return launch_ex(fn, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, false, args);
+}
+
+}  // namespace fsx
