@@ -146,7 +146,8 @@ __global__ void __launch_bounds__(32 * kBoundsWarps) bounds_kernel(const BoundsA
         c[j] = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float y = sub == 0 ? floorf(lo[4 * j + i] * inv) : ceilf(hi[4 * j + i] * inv);
+          const float x = sub == 0 ? lo[4 * j + i] : hi[4 * j + i];  // outwards, also where the quotient is below fp32
+          const float y = sub == 0 ? fminf(floorf(x * inv), x < 0.f ? -1.f : 127.f) : fmaxf(ceilf(x * inv), x > 0.f ? 1.f : -127.f);
           c[j] |= (static_cast<uint32_t>(static_cast<int>(y)) & 0xffu) << (8 * i);
         }
       }

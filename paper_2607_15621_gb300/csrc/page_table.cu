@@ -150,7 +150,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) step_k
     long long add = 0;
     const long long t0 = a.new_offsets[i], t1 = a.new_offsets[i + 1];
     bool fine = t0 >= 0 && t1 >= t0 && t1 <= a.new_rows;
-    if (n < 0) n = 0;
+    if (n < 0 || src < -1 || src >= a.B_in) n = 0;  // reported above
     else if (fine) add = t1 - t0;
     if (n + add > static_cast<long long>(a.width) << a.shift || n + add > 0x7fffffffll - 64) {
       add = 0;

@@ -133,8 +133,8 @@ fsx_status fsx_rotary(const void* d_q, long long q_stride, const void* d_k, cons
     a.turns[j] = turns_of(rate[j]);
   }
   const bool cached = d_k_cache || d_v_cache;
-  if (!d_q && !d_k) return fail(FSX_ERR_INVALID_ARG, "neither queries nor keys");
   if (n_rows == 0) return FSX_OK;
+  if (!d_q && !d_k) return fail(FSX_ERR_INVALID_ARG, "neither queries nor keys");
   if (!d_positions) return fail(FSX_ERR_INVALID_ARG, "d_positions is NULL");
   if (!!d_q != !!d_q_out) return fail(FSX_ERR_INVALID_ARG, "d_q and d_q_out go together");
   if (d_q && ((s = check_rows("d_q", d_q, q_stride, n_heads)) != FSX_OK || (s = check_rows("d_q_out", d_q_out, q_out_stride, n_heads)) != FSX_OK)) return s;
