@@ -232,9 +232,20 @@ __device__ __forceinline__ void cache_step(State<NT>& st, const unsigned char* x
   }
 }
 
-// One tensor's 16 keys into a stage. `src`: this lane's unit of its first row of them; rows past `left` become zeros.
-template <bool C8, bool V>
-__device__ __forceinline__ void copy_rows(uint32_t dst, const unsigned char* src, long long row_bytes, int left) {
+// What is read once: first to leave L2, so that tables, queries, partial results and the kernel's own code stay there
+__device__ __forceinline__ uint64_t once_policy() {
+  uint64_t policy;
+  asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+  return policy;
+}
+__device__ __forceinline__ void copy16_once(uint32_t dst, const void* src, bool there, uint64_t policy) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0), "l"(policy) : "memory");
+}
+
+// One tensor's 16 keys into a stage. `src`: this lane's unit of its first row of them; rows past `left` become zeros. ONCE: by
+// `policy`.
+template <bool C8, bool V, bool ONCE = false>
+__device__ __forceinline__ void copy_rows(uint32_t dst, const unsigned char* src, long long row_bytes, int left, uint64_t policy = 0) {
   using S = Stage<C8>;
   constexpr int kPerRow = S::kRow / 16, kStep = 32 / kPerRow;  // lanes a row, rows a warp copies at once
   const int lane = threadIdx.x & 31, u = lane % kPerRow, r0 = lane / kPerRow;
@@ -242,7 +253,9 @@ __device__ __forceinline__ void copy_rows(uint32_t dst, const unsigned char* src
   for (int i = 0; i < 16 / kStep; ++i) {
     const int r = r0 + i * kStep;
     const int at = V ? u ^ (r & 6) : u ^ ((r & 1) << 2);
-    copy16(dst + (V ? S::kOffV : 0) + r * S::kRow + at * 16, src + i * kStep * row_bytes, r < left);
+    const uint32_t to = dst + (V ? S::kOffV : 0) + r * S::kRow + at * 16;
+    if (ONCE) copy16_once(to, src + i * kStep * row_bytes, r < left, policy);
+    else copy16(to, src + i * kStep * row_bytes, r < left);
   }
 }
 

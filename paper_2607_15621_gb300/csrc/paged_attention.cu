@@ -6,9 +6,14 @@
 // a warp needs one page number a step: at the start of a piece its lanes look up the pages of 32 steps at once, and a
 // step's comes by a shuffle, so that no copy waits for the table.
 //
-// Items (request, tile of the group, kv head) are cut into pieces of at most 28 chunks of 64 keys, by the count of all chunks, and
-// CTAs take pieces from one queue; the pieces of an item are joined by the CTA that ends last, in the order of the keys.
-// A piece that meets a page number outside the cache marks its result, and its item writes nothing.
+// Items (request, tile of the group, kv head) are shared out in one of two ways:
+//   line   few items. One CTA a SM with 12 or 16 warps; all steps of all items in one line, cut into as many equal ranges as there are CTAs, so
+//          that every SM reads the same number of bytes; a cut less than 32 steps from an item's end moves there. A CTA's ranges put 12 or 16
+//          warps together in shared memory, so an item that is spread over the whole GPU has few partial results to join.
+//   queue  many items. Four warps a CTA, three or four CTAs a SM, pieces of at most 28 chunks of 64 keys from one queue: SMs that
+//          read faster take more, and one CTA's end overlaps with the others' loads.
+// The pieces of a cut item are joined by the CTA that ends last, in the order of the keys. A piece that meets a page number
+// outside the cache marks its result, and its item writes nothing.
 #include <math_constants.h>
 
 #include "few_rows.cuh"
@@ -20,31 +25,35 @@ namespace fsx {
 
 namespace {
 
-constexpr int kFew = 8, kMany = 28;  // chunks of an item that is not cut, and of a piece
-constexpr int kHeader = 64;          // ints of the workspace: [0] pieces taken from the queue, [1] CTAs that are done
+constexpr int kFew = 8, kMany = 28;  // queue: chunks of an item that is not cut, and of a piece
+constexpr int kNear = 32;            // line: steps
+constexpr int kHeader = 64;          // ints of the workspace, queue: [0] pieces taken, [1] CTAs that are done
 constexpr int kCounters = 8192;      // then one for each slot
 
 struct Plan {
+  int* len;          // [B] rows of the requests, -1: not in order
   uint32_t* pieces;  // [B + 1] pieces of the requests before
   int* slots;        // [B + 1] slots of the requests before
   int most;          // chunks of a piece
 };
-__host__ __device__ constexpr size_t plan_bytes(int B) { return (B + 1) * 2 * sizeof(int); }
+__host__ __device__ constexpr size_t plan_bytes(int B) { return (B + (B + 1) * 2) * sizeof(int); }
 
 struct Request {
   int len;    // rows
   int pages;  // that hold them
   int steps;  // of 16 keys, over all pages or the picked ones
 };
-// false: the length is negative or more than the table's pages hold; no steps then and no items
-__device__ __forceinline__ bool request_of(const PagedArgs& p, int b, Request& r) {
+// -1: the length is negative or more than the table's pages hold; no items then
+__device__ __forceinline__ int length_of(const PagedArgs& p, int b) {
   const long long len = p.pages.lengths[b];
-  r.len = r.pages = r.steps = 0;
-  if (len < 0 || len > static_cast<long long>(p.pages.width) << p.pages.shift || len > 0x7fffffffll - 64) return false;
-  r.len = static_cast<int>(len);
-  r.pages = static_cast<int>((len + (1 << p.pages.shift) - 1) >> p.pages.shift);
-  r.steps = p.picked != nullptr ? min(r.pages, p.n_picked) << (p.pages.shift - 4) : (r.len + 15) >> 4;
-  return true;
+  return len < 0 || len > static_cast<long long>(p.pages.width) << p.pages.shift || len > 0x7fffffffll - 64 ? -1 : static_cast<int>(len);
+}
+__device__ __forceinline__ Request request_of(const PagedArgs& p, int len) {
+  Request r;
+  r.len = len;
+  r.pages = (len + (1 << p.pages.shift) - 1) >> p.pages.shift;
+  r.steps = p.picked != nullptr ? min(r.pages, p.n_picked) << (p.pages.shift - 4) : (len + 15) >> 4;
+  return r;
 }
 __device__ __forceinline__ int chunks_of(const Request& r) { return max(1, (r.steps + kWarps - 1) / kWarps); }
 __device__ __forceinline__ int pieces_of(int n, int most) { return n <= kFew ? 1 : (n + most - 1) / most; }
@@ -54,15 +63,15 @@ __device__ __forceinline__ Plan make_plan(const PagedArgs& p, long long items, i
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = p.pages.B;
   const int per = (B + kThreads - 1) / kThreads, b0 = min(B, tid * per), b1 = min(B, b0 + per);
   Plan plan;
-  plan.pieces = static_cast<uint32_t*>(at);
+  plan.len = static_cast<int*>(at);
+  plan.pieces = reinterpret_cast<uint32_t*>(plan.len + B);
   plan.slots = reinterpret_cast<int*>(plan.pieces + B + 1);
   long long total = 0;
   for (int b = b0; b < b1; ++b) {
-    Request r;
-    const bool fine = request_of(p, b, r);
-    if (!fine && blockIdx.x == 0) set_status(p.status, kStatusDeviceArg);
-    plan.slots[b] = fine ? chunks_of(r) : 0;  // for the second look
-    total += plan.slots[b];
+    const int len = length_of(p, b);
+    if (len < 0 && blockIdx.x == 0) set_status(p.status, kStatusDeviceArg);
+    plan.len[b] = len;
+    total += len < 0 ? 0 : chunks_of(request_of(p, len));
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
@@ -82,7 +91,7 @@ __device__ __forceinline__ Plan make_plan(const PagedArgs& p, long long items, i
   }
   long long mine = 0, mine_slots = 0;
   for (int b = b0; b < b1; ++b) {
-    const int n = plan.slots[b], of = n > 0 ? pieces_of(n, plan.most) : 0;
+    const int len = plan.len[b], of = len < 0 ? 0 : pieces_of(chunks_of(request_of(p, len)), plan.most);
     plan.pieces[b] = static_cast<uint32_t>(mine);  // within this thread's requests
     plan.slots[b] = static_cast<int>(mine_slots);
     mine += items * of;
@@ -121,31 +130,132 @@ __device__ __forceinline__ Plan make_plan(const PagedArgs& p, long long items, i
 struct Piece {
   Request r;
   int b, kvh, row0;  // request, kv head, first row (head of the group) of the tile
-  int from, to;      // chunks
-  int slot, j, of;   // piece j of `of`; `slot` is that of piece 0
+  int from, to;      // steps
+  int first, j, of;  // piece j of `of`; `first`: slot of piece 0 (line: its CTA)
 };
-__device__ __forceinline__ Piece piece_at(const PagedArgs& p, const Plan& plan, int tile_rows, uint32_t i) {
-  int lo = 0, hi = p.pages.B;  // pieces[lo] <= i < pieces[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (plan.pieces[mid] <= i) lo = mid;
-    else hi = mid;
-  }
-  Piece x;
-  x.b = lo;
-  request_of(p, lo, x.r);
-  const int n = chunks_of(x.r);
-  x.of = pieces_of(n, plan.most);
-  const uint32_t rel = i - plan.pieces[lo], item = rel / static_cast<uint32_t>(x.of);
-  x.j = static_cast<int>(rel - item * x.of);
-  x.slot = plan.slots[lo] + static_cast<int>(rel) - x.j;
-  const uint32_t least = static_cast<uint32_t>(n) / static_cast<uint32_t>(x.of), more = n - least * x.of;
-  x.from = static_cast<int>(x.j * least + min(static_cast<uint32_t>(x.j), more));
-  x.to = static_cast<int>(x.from + least + (static_cast<uint32_t>(x.j) < more ? 1 : 0));
+__device__ __forceinline__ void set_item(const PagedArgs& p, Piece& x, uint32_t item, int tile_rows) {
   const uint32_t tile = item / static_cast<uint32_t>(p.n_kv_heads);
   x.kvh = static_cast<int>(item - tile * p.n_kv_heads);
   x.row0 = static_cast<int>(tile) * tile_rows;
+}
+// the last b with at[b] <= x, of at[0 .. n]
+template <typename T>
+__device__ __forceinline__ int find(const T* at, int n, T x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (at[mid] <= x) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+__device__ __forceinline__ Piece piece_at(const PagedArgs& p, const Plan& plan, int tile_rows, uint32_t i) {
+  Piece x;
+  const int b = x.b = find(plan.pieces, p.pages.B, i);
+  x.r = request_of(p, plan.len[b]);
+  const int n = chunks_of(x.r);
+  x.of = pieces_of(n, plan.most);
+  const uint32_t rel = i - plan.pieces[b], item = rel / static_cast<uint32_t>(x.of);
+  x.j = static_cast<int>(rel - item * x.of);
+  x.first = plan.slots[b] + static_cast<int>(rel) - x.j;
+  const uint32_t least = static_cast<uint32_t>(n) / static_cast<uint32_t>(x.of), more = n - least * x.of;
+  x.from = static_cast<int>(x.j * least + min(static_cast<uint32_t>(x.j), more)) * kWarps;
+  x.to = min(x.from + static_cast<int>(least + (static_cast<uint32_t>(x.j) < more ? 1 : 0)) * kWarps, x.r.steps);
+  set_item(p, x, item, tile_rows);
   return x;
+}
+
+// The line of all steps: where each request's begin, and where the CTAs' ranges do. In 32 bits: the host sees to that.
+struct Line {
+  int* len;         // [B]
+  uint32_t* start;  // [B + 1]
+  uint32_t* cut;    // [CTAs + 1]
+  uint32_t ranges;  // the rest of the CTAs have none
+};
+__host__ __device__ constexpr size_t line_bytes(int B, int ctas) { return (B + B + 1 + ctas + 1) * sizeof(int); }
+__device__ __forceinline__ uint32_t line_steps(const Request& r) { return max(1, r.steps); }
+
+template <int W>
+__device__ __forceinline__ Line make_line(const PagedArgs& p, uint32_t items, void* at, uint32_t* scratch) {
+  constexpr int kThreadsLine = 32 * W;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = p.pages.B;
+  Line line;
+  line.len = static_cast<int*>(at);
+  line.start = reinterpret_cast<uint32_t*>(line.len + B);
+  line.cut = line.start + B + 1;
+  uint32_t before = 0;
+#pragma unroll 1
+  for (int b0 = 0; b0 < B; b0 += kThreadsLine) {  // a thread a request
+    const int b = b0 + tid;
+    uint32_t mine = 0;
+    if (b < B) {
+      const int len = length_of(p, b);
+      line.len[b] = len;
+      if (len >= 0) mine = items * line_steps(request_of(p, len));
+      else if (blockIdx.x == 0) set_status(p.status, kStatusDeviceArg);
+    }
+    uint32_t sum = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t up = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += up;
+    }
+    if (lane == 31) scratch[warp] = sum;
+    __syncthreads();
+    uint32_t all = 0;
+    const int warps = min(W, (B - b0 + 31) >> 5);
+#pragma unroll 1
+    for (int w = 0; w < warps; ++w) {
+      if (w < warp) sum += scratch[w];
+      all += scratch[w];
+    }
+    if (b < B) line.start[b] = before + sum - mine;
+    before += all;
+    if (b0 + kThreadsLine < B) __syncthreads();
+  }
+  if (tid == 0) line.start[B] = before;
+  __syncthreads();
+  // ranges of 32 steps and more, or one for each item; a cut near an item's end moves there
+  line.ranges = max(1u, min(gridDim.x, max(before / kNear, min(before, items * B))));
+  const uint32_t least = before / line.ranges, more = before - least * line.ranges;
+  for (uint32_t c = tid; c <= line.ranges; c += kThreadsLine) {
+    uint32_t x = c * least + min(c, more);
+    if (c < line.ranges && c > 0) {
+      const int b = find(line.start, B, x);
+      const uint32_t n = line_steps(request_of(p, line.len[b])), off = (x - line.start[b]) % n;
+      if (off < kNear) x -= off;
+      else if (n - off < kNear) x += n - off;
+    }
+    line.cut[c] = x;
+  }
+  __syncthreads();
+  return line;
+}
+// The part of the range that begins at step `at` of the line, up to its item's end; `at` moves on
+__device__ __forceinline__ Piece segment_at(const PagedArgs& p, const Line& line, int tile_rows, uint32_t end, uint32_t& at) {
+  Piece x;
+  const int b = x.b = find(line.start, p.pages.B, at);
+  x.r = request_of(p, line.len[b]);
+  const uint32_t n = line_steps(x.r), rel = at - line.start[b], item = rel / n;
+  x.from = static_cast<int>(rel - item * n);
+  x.to = static_cast<int>(min(n, x.from + (end - at)));
+  x.first = x.j = 0;
+  x.of = 1;
+  if (x.from > 0 || x.to < n) {
+    const uint32_t s = at - x.from;
+    x.first = find(line.cut, static_cast<int>(line.ranges), s);
+    x.of = find(line.cut, static_cast<int>(line.ranges), s + n - 1) - x.first + 1;
+    x.j = static_cast<int>(blockIdx.x) - x.first;
+  }
+  at += x.to - x.from;
+  x.to = min(x.to, x.r.steps);  // a request without rows has a step of none
+  set_item(p, x, item, tile_rows);
+  return x;
+}
+// Slot of an item's piece: a CTA of a line has two, for the item that began before its range and for the one that goes on behind it
+template <bool LINE>
+__device__ __forceinline__ int slot_of(const Piece& x, int j) {
+  return LINE ? 2 * (x.first + j) + (j == 0 ? 1 : 0) : x.first + j;
 }
 
 // First cache row of step `step` and how many of its 16 rows are keys of the request. False: no page of the cache.
@@ -173,14 +283,22 @@ __device__ __forceinline__ bool look_up(const PagedArgs& p, const Piece& it, int
   return true;
 }
 
-template <bool C8, int NT>
+// Warps of a CTA, rows that they put together at a time
+template <bool C8, int NT, bool LINE>
+struct Shape {
+  static constexpr int kWarps = LINE ? 4 * Fit<C8, NT>::kCtas : fsx::kWarps;
+  static constexpr int kCtas = LINE ? 1 : Fit<C8, NT>::kCtas;
+  static constexpr int kPass = LINE ? 2 : Fit<C8, NT>::kPass;
+};
+template <bool C8, int NT, bool LINE>
 struct Shared {  // and the plan behind it
-  long long scratch[2 * kWarps];
-  __align__(128) unsigned char ring[kWarps][Fit<C8, NT>::kStages * Stage<C8>::kBytes];
-  float m[kWarps][8 * NT], l[kWarps][8 * NT];
-  float o[kWarps][Fit<C8, NT>::kPass][kD];
-  int left[kWarps][4];  // keys of the ring's stages
-  int bad[kWarps];
+  static constexpr int kW = Shape<C8, NT, LINE>::kWarps;
+  long long scratch[2 * kW];
+  __align__(128) unsigned char ring[kW][Fit<C8, NT>::kStages * Stage<C8>::kBytes];
+  float m[kW][8 * NT], l[kW][8 * NT];
+  float o[kW][Shape<C8, NT, LINE>::kPass][kD];
+  int left[kW][4];  // keys of the ring's stages
+  int bad;          // of the piece
   uint32_t next;
   int last;
 };
@@ -213,24 +331,39 @@ __device__ __forceinline__ void load_queries(uint32_t (&qf)[NT][8][2], const Pag
   }
 }
 
-template <bool BF, bool C8, int NT>
-__global__ void __launch_bounds__(kThreads, Fit<C8, NT>::kCtas) paged_kernel(const PagedArgs p) {
+template <bool BF, bool C8, int NT, bool LINE>
+__global__ void __launch_bounds__(32 * Shape<C8, NT, LINE>::kWarps, Shape<C8, NT, LINE>::kCtas) paged_kernel(const PagedArgs p) {
   using S = Stage<C8>;
-  constexpr int kStages = Fit<C8, NT>::kStages, kPass = Fit<C8, NT>::kPass;
+  using Sm = Shared<C8, NT, LINE>;
+  constexpr int kStages = Fit<C8, NT>::kStages, kPass = Shape<C8, NT, LINE>::kPass, kW = Sm::kW;
   constexpr int kPerRow = S::kRow / 16;
   constexpr int kTile = 8 * NT;
   extern __shared__ __align__(128) unsigned char raw_smem[];
-  Shared<C8, NT>& sm = *reinterpret_cast<Shared<C8, NT>*>(raw_smem);
+  Sm& sm = *reinterpret_cast<Sm*>(raw_smem);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
   const int G = p.n_heads / p.n_kv_heads;
   int* header = static_cast<int*>(p.workspace);
   const long long items = static_cast<long long>((G + kTile - 1) / kTile) * p.n_kv_heads;
-  const Plan plan = make_plan(p, items, slots_of(NT), raw_smem + sizeof(sm), sm.scratch);
-  const uint32_t total = plan.pieces[p.pages.B];
+  Plan plan;
+  Line line;
+  uint32_t total = 0, i = blockIdx.x;  // queue: pieces, this CTA's
+  uint32_t at = 0, end = 0;            // line: where the next segment begins, and this CTA's range ends
+  if (tid == 0) sm.bad = 0;  // the plan has barriers
+  if constexpr (LINE) {
+    line = make_line<kW>(p, static_cast<uint32_t>(items), raw_smem + sizeof(sm), reinterpret_cast<uint32_t*>(sm.scratch));
+    if (blockIdx.x < line.ranges) {
+      at = line.cut[blockIdx.x];
+      end = line.cut[blockIdx.x + 1];
+    }
+  } else {
+    plan = make_plan(p, items, slots_of(NT), raw_smem + sizeof(sm), sm.scratch);
+    total = plan.pieces[p.pages.B];
+  }
   const long long row_bytes = static_cast<long long>(p.n_kv_heads) * S::kRow;
   const uint32_t ring = smem_addr(sm.ring[warp]);
+  const uint64_t policy = once_policy();
 
-  // this warp's copies of a piece: chunks staged .. count - 1, of which it takes every one's `warp`-th 16 keys
+  // this warp's copies of a piece: steps from + warp, from + warp + kW, ...: `count`
   Piece it;
   const unsigned char *kc = nullptr, *vc = nullptr;
   const float* scales = nullptr;
@@ -239,12 +372,12 @@ __global__ void __launch_bounds__(kThreads, Fit<C8, NT>::kCtas) paged_kernel(con
   auto copy_next = [&](const Piece& x) {
     if (staged < count) {
       if ((staged & 31) == 0)  // a lane a step
-        bad = !look_up(p, x, staged + lane < count ? (x.from + staged + lane) * kWarps + warp : 0x7fffffff, rows_of, left_of) || bad;
+        bad = !look_up(p, x, staged + lane < count ? x.from + (staged + lane) * kW + warp : 0x7fffffff, rows_of, left_of) || bad;
       const int row = __shfl_sync(0xffffffffu, rows_of, staged & 31), left = __shfl_sync(0xffffffffu, left_of, staged & 31);
       if (left > 0) {
         const uint32_t dst = ring + slot_in * S::kBytes;
-        copy_rows<C8, false>(dst, kc + row * row_bytes, row_bytes, left);
-        copy_rows<C8, true>(dst, vc + row * row_bytes, row_bytes, left);
+        copy_rows<C8, false, true>(dst, kc + row * row_bytes, row_bytes, left, policy);
+        copy_rows<C8, true, true>(dst, vc + row * row_bytes, row_bytes, left, policy);
         if (C8) copy4(dst + S::kOffScale + lane * 4, scales + row, (lane & 15) < left);
       }
       if (lane == 0) sm.left[warp][slot_in] = left;
@@ -255,27 +388,28 @@ __global__ void __launch_bounds__(kThreads, Fit<C8, NT>::kCtas) paged_kernel(con
   };
   auto begin = [&](const Piece& x) {
     staged = 0;
-    count = x.to - x.from;
-    const long long at = static_cast<long long>(lane / kPerRow) * row_bytes + x.kvh * S::kRow + (lane % kPerRow) * 16;
-    kc = static_cast<const unsigned char*>(p.k_cache) + at;
-    vc = static_cast<const unsigned char*>(p.v_cache) + at;
+    count = max(0, (x.to - x.from - warp + kW - 1) / kW);
+    const long long off = static_cast<long long>(lane / kPerRow) * row_bytes + x.kvh * S::kRow + (lane % kPerRow) * 16;
+    kc = static_cast<const unsigned char*>(p.k_cache) + off;
+    vc = static_cast<const unsigned char*>(p.v_cache) + off;
     if (C8) scales = (lane < 16 ? p.k_scale : p.v_scale) + x.kvh * p.cache_rows + (lane & 15);
     slot_in = 0;
     bad = false;
 #pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) copy_next(x);
+    for (int n = 0; n < kStages - 1; ++n) copy_next(x);
   };
 
-  uint32_t i = blockIdx.x;
+  bool more = LINE ? at < end : i < total;
   uint32_t qf[NT][8][2];
-  if (i < total) {
-    it = piece_at(p, plan, kTile, i);
-    load_queries<C8, NT>(qf, p, it, G);
+  if (more) {
+    if constexpr (LINE) it = segment_at(p, line, kTile, end, at);
+    else it = piece_at(p, plan, kTile, i);
     begin(it);
+    load_queries<C8, NT>(qf, p, it, G);
   }
 #pragma unroll 1
-  while (i < total) {
-    if (tid == 0) sm.next = gridDim.x + atomicAdd(reinterpret_cast<unsigned*>(header), 1u);
+  while (more) {
+    if (!LINE && tid == 0) sm.next = gridDim.x + atomicAdd(reinterpret_cast<unsigned*>(header), 1u);
     State<NT> st;
     float f[NT][2];
     make_queries<BF, C8, NT>(qf, f);
@@ -290,9 +424,9 @@ __global__ void __launch_bounds__(kThreads, Fit<C8, NT>::kCtas) paged_kernel(con
         for (int e = 0; e < 4; ++e) st.o[j][t][e] = 0.f;
     }
     int slot_out = 0;
-    const int chunks = it.to - it.from;
+    const int steps = count;
 #pragma unroll 1
-    for (int n = 0; n < chunks; ++n) {
+    for (int n = 0; n < steps; ++n) {
       cp_async_wait<kStages - 2>();
       __syncwarp();  // every lane's copies of the stage; and the stage before is read
       const int left = sm.left[warp][slot_out];
@@ -301,7 +435,7 @@ __global__ void __launch_bounds__(kThreads, Fit<C8, NT>::kCtas) paged_kernel(con
       slot_out = slot_out + 1 == kStages ? 0 : slot_out + 1;
     }
     cp_async_wait<0>();
-    const bool any_bad = __any_sync(0xffffffffu, bad);
+    if (__any_sync(0xffffffffu, bad) && lane == 0) sm.bad = 1;
     if (C8) {  // the sums without k
 #pragma unroll
       for (int t = 0; t < NT; ++t)
@@ -329,21 +463,27 @@ __global__ void __launch_bounds__(kThreads, Fit<C8, NT>::kCtas) paged_kernel(con
           sm.l[warp][8 * t + 2 * c + r] = l;
         }
       }
-    if (lane == 0) sm.bad[warp] = any_bad;
     __syncthreads();
     // ---- the next piece's first copies go out before this one's results are put together
-    const bool wrong = (sm.bad[0] | sm.bad[1] | sm.bad[2] | sm.bad[3]) != 0;
-    if (wrong && tid == 0) set_status(p.status, kStatusDeviceArg);
-    const uint32_t i_next = sm.next;
+    const bool wrong = sm.bad != 0;
     Piece next = it;
-    if (i_next < total) {
-      next = piece_at(p, plan, kTile, i_next);
+    bool goes_on;
+    if constexpr (LINE) {
+      goes_on = at < end;
+      if (goes_on) next = segment_at(p, line, kTile, end, at);
+    } else {
+      i = sm.next;
+      goes_on = i < total;
+      if (goes_on) next = piece_at(p, plan, kTile, i);
+    }
+    if (goes_on) {
       load_queries<C8, NT>(qf, p, next, G);
       begin(next);
     }
-    // ---- the four warps' results, kPass rows at a time; a thread a dim
+    // ---- the warps' results, kPass rows at a time; a thread a dim
     auto lse_at = [&](int head) -> float& { return p.lse[static_cast<long long>(head) * p.pages.B + it.b]; };
-    float* slot = slot_at<NT>(p, it.slot + it.j);
+    float* slot = slot_at<NT>(p, slot_of<LINE>(it, it.j));
+    const int dim = tid & (kD - 1);
 #pragma unroll
     for (int base = 0; base < kTile; base += kPass) {
       if (base >= rows) break;
@@ -360,88 +500,126 @@ __global__ void __launch_bounds__(kThreads, Fit<C8, NT>::kCtas) paged_kernel(con
         }
       __syncthreads();
 #pragma unroll 1
-      for (int row = base; row < min(rows, base + kPass); ++row) {
-        const float m = fmaxf(fmaxf(sm.m[0][row], sm.m[1][row]), fmaxf(sm.m[2][row], sm.m[3][row]));
+      for (int row = base + tid / kD; row < min(rows, base + kPass); row += kW * 32 / kD) {
+        float m = sm.m[0][row];
+#pragma unroll
+        for (int w = 1; w < kW; ++w) m = fmaxf(m, sm.m[w][row]);
         float l = 0.f, o = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
+        for (int w = 0; w < kW; ++w) {
           const float a = weight_of(sm.m[w][row], m);
           l += a * sm.l[w][row];
-          o += a * sm.o[w][row - base][tid];
+          o += a * sm.o[w][row - base][dim];
         }
         const int head = it.kvh * G + it.row0 + row;
         if (it.of > 1) {
-          __stcg(slot + row * kD + tid, o);
-          if (tid == 0) __stcg(reinterpret_cast<float2*>(slot + kTile * kD) + row, make_float2(m, wrong ? -1.f : l));
+          __stcg(slot + row * kD + dim, o);
+          if (dim == 0) __stcg(reinterpret_cast<float2*>(slot + kTile * kD) + row, make_float2(m, wrong ? -1.f : l));
         } else if (!wrong) {
           const float y = l == 0.f ? 0.f : o / l;
-          static_cast<uint16_t*>(p.out)[(static_cast<long long>(it.b) * p.n_heads + head) * kD + tid] = static_cast<uint16_t>(pack16<BF>(y, y));
-          if (p.lse != nullptr && tid == 0) lse_at(head) = l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * kLn2;
+          static_cast<uint16_t*>(p.out)[(static_cast<long long>(it.b) * p.n_heads + head) * kD + dim] = static_cast<uint16_t>(pack16<BF>(y, y));
+          if (p.lse != nullptr && dim == 0) lse_at(head) = l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * kLn2;
         }
       }
       __syncthreads();
+    }
+    if (tid == 0 && wrong) {
+      sm.bad = 0;
+      set_status(p.status, kStatusDeviceArg);
     }
     if (it.of > 1) {
       __threadfence();
       __syncthreads();
       if (tid == 0) {
-        int* counter = header + kHeader + it.slot;
+        int* counter = header + kHeader + it.first;
         sm.last = atomicAdd(counter, 1) == it.of - 1;
         if (sm.last) *counter = 0;
       }
       __syncthreads();
       if (sm.last) {
         __threadfence();
-        const float* first = slot_at<NT>(p, it.slot);
+        // `share` warps a row, each every share-th piece; 4 dims a lane
+        const int share = max(1, kW / rows), at_once = kW / share;
 #pragma unroll 1
-        for (int row = warp; row < rows; row += kWarps) {  // a warp a row, 4 dims a lane
+        for (int row0 = 0; row0 < rows; row0 += at_once) {
+          const int row = row0 + warp / share, part = warp % share;
           float m = -CUDART_INF_F, l = 0.f;
           float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
           bool refused = false;
+          if (row < rows && warp / share < at_once) {
 #pragma unroll 1
-          for (int j0 = 0; j0 < it.of; j0 += kJoin) {  // in the order of the keys; the loads of kJoin pieces at once
-            float2 x[kJoin];
-            float4 v[kJoin];
+            for (int j0 = part; j0 < it.of; j0 += kJoin * share) {  // in the order of the keys; the loads of kJoin pieces at once
+              float2 x[kJoin];
+              float4 v[kJoin];
 #pragma unroll
-            for (int j = 0; j < kJoin; ++j) {
-              const float* other = first + min(j0 + j, it.of - 1) * slot_floats(NT);
-              x[j] = __ldcg(reinterpret_cast<const float2*>(other + kTile * kD) + row);
-              v[j] = __ldcg(reinterpret_cast<const float4*>(other + row * kD) + lane);
-            }
-            float top = m;
+              for (int j = 0; j < kJoin; ++j) {
+                const float* other = slot_at<NT>(p, slot_of<LINE>(it, min(j0 + j * share, it.of - 1)));
+                x[j] = __ldcg(reinterpret_cast<const float2*>(other + kTile * kD) + row);
+                v[j] = __ldcg(reinterpret_cast<const float4*>(other + row * kD) + lane);
+              }
+              float top = m;
 #pragma unroll
-            for (int j = 0; j < kJoin; ++j) top = fmaxf(top, x[j].x);
-            const float old = weight_of(m, top);
-            m = top;
-            l *= old;
-            o = make_float4(o.x * old, o.y * old, o.z * old, o.w * old);
+              for (int j = 0; j < kJoin; ++j) top = fmaxf(top, x[j].x);
+              const float old = weight_of(m, top);
+              m = top;
+              l *= old;
+              o = make_float4(o.x * old, o.y * old, o.z * old, o.w * old);
 #pragma unroll
-            for (int j = 0; j < kJoin; ++j) {
-              const float a = weight_of(x[j].x, top);
-              refused = refused || x[j].y < 0.f;
-              if (j0 + j < it.of) {
-                l += a * x[j].y;
-                o.x += a * v[j].x;
-                o.y += a * v[j].y;
-                o.z += a * v[j].z;
-                o.w += a * v[j].w;
+              for (int j = 0; j < kJoin; ++j) {
+                const float a = weight_of(x[j].x, top);
+                refused = refused || x[j].y < 0.f;
+                if (j0 + j * share < it.of) {
+                  l += a * x[j].y;
+                  o.x += a * v[j].x;
+                  o.y += a * v[j].y;
+                  o.z += a * v[j].z;
+                  o.w += a * v[j].w;
+                }
               }
             }
           }
-          if (refused) continue;
-          const int head = it.kvh * G + it.row0 + row;
-          const float inv = l == 0.f ? 0.f : 1.f / l;
-          uint16_t* out = static_cast<uint16_t*>(p.out) + (static_cast<long long>(it.b) * p.n_heads + head) * kD + 4 * lane;
-          *reinterpret_cast<uint2*>(out) = make_uint2(pack16<BF>(o.x * inv, o.y * inv), pack16<BF>(o.z * inv, o.w * inv));
-          if (p.lse != nullptr && lane == 0) lse_at(head) = l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * kLn2;
+          if (share > 1) {  // the row's warps, by the first of them
+            *reinterpret_cast<float4*>(&sm.o[warp][0][4 * lane]) = o;
+            if (lane == 0) {
+              sm.m[warp][0] = m;
+              sm.l[warp][0] = refused ? -1.f : l;
+            }
+            __syncthreads();
+            if (part == 0 && row < rows) {
+              float top = m;
+              for (int w = 1; w < share; ++w) top = fmaxf(top, sm.m[warp + w][0]);
+              const float own = weight_of(m, top);
+              l *= own;
+              o = make_float4(o.x * own, o.y * own, o.z * own, o.w * own);
+              for (int w = 1; w < share; ++w) {
+                const float a = weight_of(sm.m[warp + w][0], top), lw = sm.l[warp + w][0];
+                const float4 v = *reinterpret_cast<const float4*>(&sm.o[warp + w][0][4 * lane]);
+                refused = refused || lw < 0.f;
+                l += a * lw;
+                o.x += a * v.x;
+                o.y += a * v.y;
+                o.z += a * v.z;
+                o.w += a * v.w;
+              }
+              m = top;
+            }
+            __syncthreads();
+          }
+          if (row < rows && part == 0 && warp / share < at_once && !refused) {
+            const int head = it.kvh * G + it.row0 + row;
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            uint16_t* out = static_cast<uint16_t*>(p.out) + (static_cast<long long>(it.b) * p.n_heads + head) * kD + 4 * lane;
+            *reinterpret_cast<uint2*>(out) = make_uint2(pack16<BF>(o.x * inv, o.y * inv), pack16<BF>(o.z * inv, o.w * inv));
+            if (p.lse != nullptr && lane == 0) lse_at(head) = l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * kLn2;
+          }
         }
       }
     }
     __syncthreads();  // before the next piece writes what was read here
     it = next;
-    i = i_next;
+    more = goes_on;
   }
-  if (tid == 0 && atomicAdd(reinterpret_cast<unsigned*>(header) + 1, 1u) == gridDim.x - 1) {
+  if (!LINE && tid == 0 && atomicAdd(reinterpret_cast<unsigned*>(header) + 1, 1u) == gridDim.x - 1) {
     header[0] = 0;  // every CTA has taken its last piece
     header[1] = 0;
   }
@@ -450,15 +628,17 @@ __global__ void __launch_bounds__(kThreads, Fit<C8, NT>::kCtas) paged_kernel(con
 struct Kernel {
   const void* fn;
   size_t smem;
-  int ctas;  // per SM
+  int ctas, threads;
 };
-template <bool BF, bool C8, int NT>
+template <bool BF, bool C8, int NT, bool LINE>
 Kernel kernel_for() {
-  return {reinterpret_cast<const void*>(&paged_kernel<BF, C8, NT>), sizeof(Shared<C8, NT>), Fit<C8, NT>::kCtas};
+  using F = Shape<C8, NT, LINE>;
+  return {reinterpret_cast<const void*>(&paged_kernel<BF, C8, NT, LINE>), sizeof(Shared<C8, NT, LINE>), F::kCtas, 32 * F::kWarps};
 }
 template <bool BF, bool C8>
-Kernel kernel_of(int nt) {
-  return nt == 1 ? kernel_for<BF, C8, 1>() : kernel_for<BF, C8, 2>();
+Kernel kernel_of(int nt, bool line) {
+  return nt == 1 ? (line ? kernel_for<BF, C8, 1, true>() : kernel_for<BF, C8, 1, false>())
+                 : (line ? kernel_for<BF, C8, 2, true>() : kernel_for<BF, C8, 2, false>());
 }
 
 int tile_count(int n_heads, int n_kv_heads) { return n_heads / n_kv_heads <= 8 ? 1 : 2; }
@@ -470,17 +650,22 @@ size_t paged_attention_workspace_bytes(int B, int n_heads, int n_kv_heads) {
   return (kHeader + kCounters) * sizeof(int) + slots_of(nt) * slot_floats(nt) * sizeof(float);
 }
 
+constexpr int kLineItems = 8;  // items a SM up to which the line is taken
+
 cudaError_t launch_paged_attention(const PagedArgs& a, int dtype, bool cache8, cudaStream_t stream) {
-  const int nt = tile_count(a.n_heads, a.n_kv_heads);
-  const Kernel k = dtype == FSX_BF16 ? (cache8 ? kernel_of<true, true>(nt) : kernel_of<true, false>(nt))
-                                     : (cache8 ? kernel_of<false, true>(nt) : kernel_of<false, false>(nt));
-  const size_t smem = k.smem + plan_bytes(a.pages.B);
+  const int nt = tile_count(a.n_heads, a.n_kv_heads), G = a.n_heads / a.n_kv_heads;
   const int sms = sm_count();
   if (sms == 0) return cudaErrorNoDevice;
+  const long long items = static_cast<long long>(a.pages.B) * a.n_kv_heads * ((G + 8 * nt - 1) / (8 * nt));
+  const long long steps = ((static_cast<long long>(a.pages.width) << a.pages.shift) >> 4) * items;  // at most
+  const bool line = items <= static_cast<long long>(kLineItems) * sms && steps < 0x7fffffffll && 2 * sms <= slots_of(nt);
+  const Kernel k = dtype == FSX_BF16 ? (cache8 ? kernel_of<true, true>(nt, line) : kernel_of<true, false>(nt, line))
+                                     : (cache8 ? kernel_of<false, true>(nt, line) : kernel_of<false, false>(nt, line));
+  const size_t smem = k.smem + (line ? line_bytes(a.pages.B, sms) : plan_bytes(a.pages.B));
   const cudaError_t e = allow_shared_memory(k.fn, smem);
   if (e != cudaSuccess) return e;
   void* args[] = {const_cast<PagedArgs*>(&a)};
-  return launch_ex(k.fn, dim3(static_cast<unsigned>(sms * k.ctas)), dim3(kThreads), smem, stream, false, args);
+  return launch_ex(k.fn, dim3(static_cast<unsigned>(sms * k.ctas)), dim3(static_cast<unsigned>(k.threads)), smem, stream, false, args);
 }
 
 }  // namespace fsx
