@@ -651,7 +651,7 @@ fsx_status fsx_page_bounds(const void* d_k_cache, const float* d_k_scale, int ca
  *   over its scale (as the bounds', one per head) rounded to the nearest whole number, ties to even, and 2^e the product
  *   of both scales, e limited to -100 .. 100. This is exact in fp32: the choice is the same on every run.
  *   d_picked : DEVICE int32 [B, n_kv_heads, n_picked]: places in the request's table, ascending, -1 behind the last.
- * width is at most 65536. A value of a query that is not finite counts as 0 and sets FSX_ERR_RANGE; a page outside the cache
+ * width is at most 32768. A value of a query that is not finite counts as 0 and sets FSX_ERR_RANGE; a page outside the cache
  * sets FSX_ERR_DEVICE_ARG and comes last; a request of a bad length gets a list of -1 only. */
 fsx_status fsx_page_select(const void* d_q, long long q_stride, int dtype, const int8_t* d_bounds, const float* d_bound_scale,
                            long long cache_rows, int page_rows, const int32_t* d_table, int width, const int64_t* d_lengths,

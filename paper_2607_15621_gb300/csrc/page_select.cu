@@ -54,6 +54,8 @@ __global__ void __launch_bounds__(32 * kBoundsWarps) bounds_kernel(const BoundsA
   constexpr int kAhead = 8;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane % kLanes, sub = lane / kLanes;
   const int b = blockIdx.y;
+  pdl_launch_dependents();
+  pdl_wait();
   int len, pages;
   const bool fine = rows_of(a.pages, b, len, pages);
   const long long start = a.start != nullptr ? a.start[b] : 0;
@@ -163,18 +165,18 @@ __global__ void __launch_bounds__(32 * kBoundsWarps) bounds_kernel(const BoundsA
 
 // ---------------------------------------------------------------- selection
 
-constexpr int kSelectThreads = 256;
+constexpr int kSelectThreads = 512;
 constexpr int kSelectWarps = kSelectThreads / 32;
-constexpr int kMaxSplit = 8;                              // CTAs of a cluster
-constexpr int kMaxKeys = kMaxPagesListed / kMaxSplit;     // pages of a CTA
+constexpr int kMaxSplit = 8;  // CTAs of a cluster
 constexpr int kHeadTile = 4;
+constexpr int kIdle = 1, kFewPages = 128;  // CTAs a SM, and pages of a CTA, from which on an item is not split further
+constexpr int kAtOnce = 2;  // times 8 pages of a warp
+constexpr int kDigit = 11, kBins = 1 << kDigit, kPerThread = kBins / kSelectThreads;
 
 struct __align__(16) SelectShared {
-  uint32_t hist[256];
-  uint32_t sum[256];
-  uint32_t counts[2][kMaxSplit];  // above the border, at it, of each CTA
+  uint32_t hist[kBins];
   uint32_t warps[2][kSelectWarps];
-  uint32_t border, above;  // of this pass: digit, keys above it
+  uint32_t border, above, whole;  // of a pass: digit, keys above it, whether all keys at it are taken
 };
 
 // order of floats as order of unsigned numbers
@@ -183,8 +185,8 @@ __device__ __forceinline__ uint32_t key_of(float x) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// A cluster a request and kv head; CTA r scores the r-th part of the pages and keeps their keys, the border is found by digits of 8
-// bits over all of them, and every CTA writes what it chose behind the choices of those before it.
+// A cluster a request and kv head: its CTAs score a part of the pages each and store the keys in the first CTA's shared
+// memory, which then finds the border alone, by digits of 11 bits counted from the lowest key, and writes the pages above it.
 template <bool BF>
 __global__ void __launch_bounds__(kSelectThreads) select_kernel(const SelectArgs a) {
   extern __shared__ __align__(16) unsigned char raw_smem[];
@@ -199,6 +201,8 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const SelectArgs
   int8_t* q_code = reinterpret_cast<int8_t*>(q_scale + tiles * kHeadTile);  // [G][2][128]: negative part, positive part
   uint32_t* keys = reinterpret_cast<uint32_t*>(q_code + tiles * kHeadTile * 256);
   int32_t* out = a.picked + static_cast<long long>(item) * a.n_picked;
+  pdl_launch_dependents();
+  pdl_wait();
   int len, pages;
   const bool fine = rows_of(a.pages, b, len, pages);
   if (!fine && rank == 0 && tid == 0) set_status(a.status, kStatusDeviceArg);
@@ -207,6 +211,15 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const SelectArgs
       for (int i = tid; i < a.n_picked; i += kSelectThreads) out[i] = i < pages ? i : -1;
     return;  // the whole cluster
   }
+  const int part = (pages + split - 1) / split, p0 = min(pages, rank * part), n = min(pages, p0 + part) - p0;
+  bool lost = false;
+  for (int i = tid; i < n; i += kSelectThreads) {  // where the pages are, in the keys' place
+    const int at = __ldg(a.pages.table + static_cast<long long>(b) * a.pages.width + p0 + i);
+    const bool there = at >= 0 && at < a.pages.n_pages;
+    lost = lost || !there;
+    keys[i] = there ? static_cast<uint32_t>(at) : 0xffffffffu;
+  }
+  if (lost) set_status(a.status, kStatusDeviceArg);
   // ---- the queries' codes; what is not finite counts as 0
   for (int h = warp; h < tiles * kHeadTile; h += kSelectWarps) {
     float x[4] = {0.f, 0.f, 0.f, 0.f}, top = 0.f;
@@ -240,71 +253,104 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const SelectArgs
     if (lane == 0) q_scale[h] = scale;
   }
   __syncthreads();
-  // ---- scores: 4 lanes a page, 8 pages a warp; unit 4 i + sub of a page's 16 units of 16 bytes
-  const int part = (pages + split - 1) / split, p0 = min(pages, rank * part), n = min(pages, p0 + part) - p0;
+  uint32_t* const all_keys = split > 1 ? cluster.map_shared_rank(keys, 0) : keys;
+  // ---- scores: 4 lanes a page, 8 pages a warp, kAtOnce times; unit 4 u + sub of a page's 16 units of 16 bytes
   const int sub = lane & 3;
-  bool lost = false;
-  for (int base = warp * 8; base < n; base += kSelectWarps * 8) {
-    const int i = base + (lane >> 2), page = p0 + i;
-    int at = i < n ? __ldg(a.pages.table + static_cast<long long>(b) * a.pages.width + page) : 0;
-    if (at < 0 || at >= a.pages.n_pages) {
-      lost = true;
-      at = -1;
-    }
-    const long long where = static_cast<long long>(max(at, 0)) * a.n_kv_heads + kvh;
-    const int4* src = reinterpret_cast<const int4*>(a.bounds + where * 256) + sub;
-    int4 x[4];
+  for (int base = warp * (8 * kAtOnce); base < n; base += kSelectWarps * (8 * kAtOnce)) {
+    int4 x[kAtOnce][4];
+    float scale[kAtOnce], best[kAtOnce];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) x[u] = __ldg(src + 4 * u);
-    const float scale = __ldg(a.bound_scale + static_cast<long long>(kvh) * a.pages.n_pages + max(at, 0));
-    float best = -CUDART_INF_F;
-    for (int t = 0; t < tiles; ++t) {
-      int acc[kHeadTile];
+    for (int t = 0; t < kAtOnce; ++t) {
+      const int i = base + 8 * t + (lane >> 2);
+      const uint32_t at = i < n ? keys[i] : 0u;
+      const long long page = at == 0xffffffffu ? 0 : at;
+      const int4* src = reinterpret_cast<const int4*>(a.bounds + (page * a.n_kv_heads + kvh) * 256) + sub;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) x[t][u] = __ldg(src + 4 * u);
+      scale[t] = __ldg(a.bound_scale + static_cast<long long>(kvh) * a.pages.n_pages + page);
+      best[t] = -CUDART_INF_F;
+    }
+    for (int head = 0; head < tiles * kHeadTile; head += kHeadTile) {
+      int acc[kAtOnce][kHeadTile];
 #pragma unroll
       for (int h = 0; h < kHeadTile; ++h) {
-        acc[h] = 0;
-        const int4* q = reinterpret_cast<const int4*>(q_code + (t * kHeadTile + h) * 256) + sub;
+        const int4* q = reinterpret_cast<const int4*>(q_code + (head + h) * 256) + sub;
+#pragma unroll
+        for (int t = 0; t < kAtOnce; ++t) acc[t][h] = 0;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const int4 y = q[4 * u];
-          acc[h] = __dp4a(x[u].x, y.x, acc[h]);
-          acc[h] = __dp4a(x[u].y, y.y, acc[h]);
-          acc[h] = __dp4a(x[u].z, y.z, acc[h]);
-          acc[h] = __dp4a(x[u].w, y.w, acc[h]);
-        }
-        acc[h] += __shfl_xor_sync(0xffffffffu, acc[h], 1);
-        acc[h] += __shfl_xor_sync(0xffffffffu, acc[h], 2);
-        if (t * kHeadTile + h < G) {
-          const int e = static_cast<int>(__float_as_uint(scale) >> 23) + static_cast<int>(__float_as_uint(q_scale[t * kHeadTile + h]) >> 23) - 254;
-          best = fmaxf(best, static_cast<float>(acc[h]) * __uint_as_float(static_cast<uint32_t>(127 + max(-100, min(100, e))) << 23));
+#pragma unroll
+          for (int t = 0; t < kAtOnce; ++t) {
+            acc[t][h] = __dp4a(x[t][u].x, y.x, acc[t][h]);
+            acc[t][h] = __dp4a(x[t][u].y, y.y, acc[t][h]);
+            acc[t][h] = __dp4a(x[t][u].z, y.z, acc[t][h]);
+            acc[t][h] = __dp4a(x[t][u].w, y.w, acc[t][h]);
+          }
         }
       }
+      // sums over the 4 lanes; lane `sub` ends with that of head `sub`
+      const int e_q = static_cast<int>(__float_as_uint(q_scale[head + sub]) >> 23) - 254;
+#pragma unroll
+      for (int t = 0; t < kAtOnce; ++t) {
+        const bool up = sub & 1, high = sub & 2;
+        int s0 = up ? acc[t][1] : acc[t][0], s1 = up ? acc[t][3] : acc[t][2];
+        s0 += __shfl_xor_sync(0xffffffffu, up ? acc[t][0] : acc[t][1], 1);
+        s1 += __shfl_xor_sync(0xffffffffu, up ? acc[t][2] : acc[t][3], 1);
+        const int sum = (high ? s1 : s0) + __shfl_xor_sync(0xffffffffu, high ? s0 : s1, 2);
+        const int e = max(-100, min(100, e_q + static_cast<int>(__float_as_uint(scale[t]) >> 23)));
+        if (head + sub < G) best[t] = fmaxf(best[t], static_cast<float>(sum) * __uint_as_float(static_cast<uint32_t>(127 + e) << 23));
+      }
     }
-    if (i < n && sub == 0)
-      keys[i] = page < a.first || page >= pages - a.last ? 0xffffffffu : at < 0 ? 0u : key_of(best);
+#pragma unroll
+    for (int t = 0; t < kAtOnce; ++t) {
+      best[t] = fmaxf(best[t], __shfl_xor_sync(0xffffffffu, best[t], 1));
+      best[t] = fmaxf(best[t], __shfl_xor_sync(0xffffffffu, best[t], 2));
+      const int i = base + 8 * t + (lane >> 2);
+      if (i < n && sub == 0) all_keys[p0 + i] = keys[i] == 0xffffffffu ? 0u : key_of(best[t]);
+    }
   }
-  if (lost) set_status(a.status, kStatusDeviceArg);
-  // ---- the border: the n_picked-th largest key, digit by digit
-  uint32_t prefix = 0, want = static_cast<uint32_t>(a.n_picked);  // digits found; keys still to take among those that share them
-#pragma unroll 1
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    sm.hist[tid] = 0;
+  if (split > 1) cluster.sync();  // the keys are in the first CTA; nothing is read from the others
+  else __syncthreads();
+  if (rank != 0) return;
+  // ---- the border among the pages that are not taken anyway: the want-th largest key
+  const int p_first = a.first, p_last = pages - a.last;
+  uint32_t want = static_cast<uint32_t>(a.n_picked - a.first - a.last);
+  uint32_t least = 0xffffffffu, most = 0;
+  for (int i = p_first + tid; i < p_last; i += kSelectThreads) {
+    least = min(least, keys[i]);
+    most = max(most, keys[i]);
+  }
+  least = __reduce_min_sync(0xffffffffu, least);
+  most = __reduce_max_sync(0xffffffffu, most);
+  if (lane == 0) {
+    sm.warps[0][warp] = least;
+    sm.warps[1][warp] = most;
+  }
+  __syncthreads();
+  for (int w = 0; w < kSelectWarps; ++w) {
+    least = min(least, sm.warps[0][w]);
+    most = max(most, sm.warps[1][w]);
+  }
+  // (key - least) >> shift: above `border` taken, at it the first `want` ones
+  uint32_t border = 0;
+  int shift = 32 - __clz(most - least);
+  bool whole = want == 0;
+  if (whole) border = 0xffffffffu, shift = 0;  // no key - least is as large: at least two pages lie between the first and the last
+  for (bool first = true; !whole && shift > 0; first = false) {
+    const int width = min(kDigit, shift), below = shift;
+    shift -= width;
+    for (int i = tid; i < kBins; i += kSelectThreads) sm.hist[i] = 0;
     __syncthreads();
-    for (int i = tid; i < n; i += kSelectThreads) {
-      const uint32_t k = keys[i];
-      if (shift == 24 || (k >> (shift + 8)) == prefix) atomicAdd(&sm.hist[(k >> shift) & 255u], 1u);
+    for (int i = p_first + tid; i < p_last; i += kSelectThreads) {
+      const uint32_t k = keys[i] - least;
+      if (first || (k >> below) == border) atomicAdd(&sm.hist[(k >> shift) & ((1u << width) - 1)], 1u);
     }
-    if (split > 1) cluster.sync();
-    else __syncthreads();
-    uint32_t mine = 0;
-    for (int r = 0; r < split; ++r) mine += split > 1 ? *cluster.map_shared_rank(&sm.hist[tid], r) : sm.hist[tid];
-    // keys in this digit and above, from the highest digit down
-    uint32_t sum = mine;
-    const int rev = 255 - tid;  // thread t sums digits t and above: lanes in reversed order
-    sm.sum[rev] = mine;
     __syncthreads();
-    sum = sm.sum[tid];
-    const uint32_t own = sum;
+    uint32_t mine[kPerThread], own = 0;  // thread t counts kPerThread digits, from the highest down
+#pragma unroll
+    for (int i = 0; i < kPerThread; ++i) own += mine[i] = sm.hist[kBins - 1 - (tid * kPerThread + i)];
+    uint32_t sum = own;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const uint32_t up = __shfl_up_sync(0xffffffffu, sum, o);
@@ -313,21 +359,37 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const SelectArgs
     if (lane == 31) sm.warps[0][warp] = sum;
     __syncthreads();
     for (int w = 0; w < warp; ++w) sum += sm.warps[0][w];
-    if (sum >= want && sum - own < want) {  // one thread: its digit is 255 - tid
-      sm.border = 255u - tid;
-      sm.above = sum - own;
+    uint32_t above = sum - own;
+    if (sum >= want && above < want) {  // one thread
+#pragma unroll
+      for (int i = 0; i < kPerThread; ++i) {
+        if (above < want && above + mine[i] >= want) {
+          sm.border = static_cast<uint32_t>(kBins - 1 - (tid * kPerThread + i));
+          sm.above = above;
+          sm.whole = above + mine[i] == want;
+          above = want;
+        } else {
+          above += mine[i];
+        }
+      }
     }
-    if (split > 1) cluster.sync();  // and every CTA has read the others' counts
-    else __syncthreads();
-    prefix = prefix << 8 | sm.border;
+    __syncthreads();
+    border = (first ? 0u : border << width) | sm.border;
     want -= sm.above;
+    whole = sm.whole != 0;
   }
-  // ---- every thread a run of keys; how many lie above the border and at it
-  const int per = (n + kSelectThreads - 1) / kSelectThreads, i0 = min(n, tid * per), i1 = min(n, i0 + per);
+  // ---- every thread a run of pages; how many lie above the border and at it
+  const int per = (pages + kSelectThreads - 1) / kSelectThreads, i0 = min(pages, tid * per), i1 = min(pages, i0 + per);
+  auto rank_of = [&](int i) {  // 2: above, 1: at the border
+    if (i < p_first || i >= p_last) return 2;
+    const uint32_t k = (keys[i] - least) >> shift;
+    return k > border ? 2 : k == border ? 1 : 0;
+  };
   uint32_t above = 0, at_it = 0;
   for (int i = i0; i < i1; ++i) {
-    above += keys[i] > prefix;
-    at_it += keys[i] == prefix;
+    const int r = rank_of(i);
+    above += r == 2;
+    at_it += r == 1;
   }
   uint32_t sa = above, sb = at_it;
 #pragma unroll
@@ -338,6 +400,7 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const SelectArgs
       sb += ub;
     }
   }
+  __syncthreads();
   if (lane == 31) {
     sm.warps[0][warp] = sa;
     sm.warps[1][warp] = sb;
@@ -347,25 +410,14 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const SelectArgs
     sa += sm.warps[0][w];
     sb += sm.warps[1][w];
   }
-  if (split > 1) {
-    if (tid == kSelectThreads - 1)
-      for (int r = 0; r < split; ++r) {
-        *cluster.map_shared_rank(&sm.counts[0][rank], r) = sa;
-        *cluster.map_shared_rank(&sm.counts[1][rank], r) = sb;
-      }
-    cluster.sync();
-    for (int r = 0; r < rank; ++r) {
-      sa += sm.counts[0][r];
-      sb += sm.counts[1][r];
-    }
-  }
   uint32_t before = sa - above, equal = sb - at_it;
   for (int i = i0; i < i1; ++i) {
-    if (keys[i] > prefix) {
-      out[before + min(equal, want)] = p0 + i;
+    const int r = rank_of(i);
+    if (r == 2) {
+      out[before + min(equal, want)] = i;
       ++before;
-    } else if (keys[i] == prefix) {
-      if (equal < want) out[before + equal] = p0 + i;
+    } else if (r == 1) {
+      if (equal < want) out[before + equal] = i;
       ++equal;
     }
   }
@@ -385,23 +437,23 @@ cudaError_t launch_page_bounds(const BoundsArgs& a, int cache_dtype, cudaStream_
   const void* fn = cache_dtype == FSX_E4M3   ? reinterpret_cast<const void*>(&bounds_kernel<FSX_E4M3>)
                    : cache_dtype == FSX_BF16 ? reinterpret_cast<const void*>(&bounds_kernel<FSX_BF16>)
                                              : reinterpret_cast<const void*>(&bounds_kernel<FSX_F16>);
-  return launch_ex(fn, dim3(x, static_cast<unsigned>(a.pages.B)), dim3(32 * kBoundsWarps), 0, stream, false, args);
+  return launch_ex(fn, dim3(x, static_cast<unsigned>(a.pages.B)), dim3(32 * kBoundsWarps), 0, stream, true, args);
 }
 
 cudaError_t launch_page_select(const SelectArgs& a, int dtype, cudaStream_t stream) {
   const int sms = sm_count();
   if (sms == 0) return cudaErrorNoDevice;
   const long long items = static_cast<long long>(a.pages.B) * a.n_kv_heads;
-  int split = 1;  // CTAs an item: while they leave SMs idle and have 64 pages and more each; no more pages a CTA than it keeps
-  while (split < kMaxSplit && ((items * split < sms && a.pages.width > 64 * split) || a.pages.width > kMaxKeys * split)) split *= 2;
+  int split = 1;  // CTAs an item: while SMs are left and each has 128 pages and more
+  while (split < kMaxSplit && items * split < sms * kIdle && a.pages.width > kFewPages * split) split *= 2;
   const int G = a.n_heads / a.n_kv_heads, tiles = (G + kHeadTile - 1) / kHeadTile;
   const size_t smem = sizeof(SelectShared) + static_cast<size_t>(tiles) * kHeadTile * (256 + sizeof(float)) +
-                      static_cast<size_t>((a.pages.width + split - 1) / split) * sizeof(uint32_t);
+                      static_cast<size_t>(a.pages.width) * sizeof(uint32_t);
   const void* fn = dtype == FSX_BF16 ? reinterpret_cast<const void*>(&select_kernel<true>) : reinterpret_cast<const void*>(&select_kernel<false>);
   const cudaError_t e = allow_shared_memory(fn, smem);
   if (e != cudaSuccess) return e;
   void* args[] = {const_cast<SelectArgs*>(&a)};
-  return launch_ex(fn, dim3(static_cast<unsigned>(items * split)), dim3(kSelectThreads), smem, stream, false, args, 1, split);
+  return launch_ex(fn, dim3(static_cast<unsigned>(items * split)), dim3(kSelectThreads), smem, stream, true, args, 1, split);
 }
 
 }  // namespace fsx

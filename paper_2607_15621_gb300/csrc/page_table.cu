@@ -107,6 +107,8 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) step_k
   const int thread = rank * kThreads + tid, warp = thread >> 5;
   constexpr int kAllThreads = kCtas * kThreads, kAllWarps = kAllThreads / 32;
   const bool moved = a.table_out != a.table;
+  pdl_launch_dependents();
+  pdl_wait();
   if (a.refs_out != a.refs) {
     for (int i = thread; i < a.n_pages; i += kAllThreads) a.refs_out[i] = a.refs[i];
   }
@@ -290,6 +292,8 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) compac
   constexpr int kAllThreads = kCtas * kThreads;
   int first, end;
   part_of(a.n_pages, rank, first, end);
+  pdl_launch_dependents();
+  pdl_wait();
   int mine = 0;
   for (int i = first + tid; i < end; i += kThreads) {
     const int r = a.refs[i];
@@ -388,6 +392,8 @@ struct CopyArgs {
 
 __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ CopyArgs a) {
   const int tid = threadIdx.x;
+  pdl_launch_dependents();
+  pdl_wait();
   int n = *a.n_pairs;
   if (n < 0 || n > a.max_pairs) {
     if (blockIdx.x == 0 && tid == 0) set_status(a.status, kStatusDeviceArg);
@@ -437,12 +443,12 @@ cudaError_t launch_pages_step(const StepArgs& a, cudaStream_t stream) {
   const cudaError_t e = allow_shared_memory(fn, sizeof(TableShared));
   if (e != cudaSuccess) return e;
   void* args[] = {const_cast<StepArgs*>(&a)};
-  return launch_ex(fn, dim3(kCtas), dim3(kThreads), sizeof(TableShared), stream, false, args);
+  return launch_ex(fn, dim3(kCtas), dim3(kThreads), sizeof(TableShared), stream, true, args);
 }
 
 cudaError_t launch_pages_compact(const CompactArgs& a, cudaStream_t stream) {
   void* args[] = {const_cast<CompactArgs*>(&a)};
-  return launch_ex(reinterpret_cast<const void*>(&compact_kernel), dim3(kCtas), dim3(kThreads), 0, stream, false, args);
+  return launch_ex(reinterpret_cast<const void*>(&compact_kernel), dim3(kCtas), dim3(kThreads), 0, stream, true, args);
 }
 
 cudaError_t launch_pages_copy(const fsx_page_plane* planes, int n_planes, int n_pages, const int32_t* pairs,
@@ -468,7 +474,7 @@ cudaError_t launch_pages_copy(const fsx_page_plane* planes, int n_planes, int n_
   const long long most = units * max_pairs, want = static_cast<long long>(sms) * 8;
   void* args[] = {&a};
   return launch_ex(reinterpret_cast<const void*>(&copy_kernel), dim3(static_cast<unsigned>(most < want ? most : want)), dim3(kCopyThreads), 0, stream,
-                   false, args);
+                   true, args);
 }
 
 }  // namespace fsx

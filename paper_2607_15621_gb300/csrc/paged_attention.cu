@@ -348,6 +348,8 @@ __global__ void __launch_bounds__(32 * Shape<C8, NT, LINE>::kWarps, Shape<C8, NT
   Line line;
   uint32_t total = 0, i = blockIdx.x;  // queue: pieces, this CTA's
   uint32_t at = 0, end = 0;            // line: where the next segment begins, and this CTA's range ends
+  pdl_launch_dependents();
+  pdl_wait();
   if (tid == 0) sm.bad = 0;  // the plan has barriers
   if constexpr (LINE) {
     line = make_line<kW>(p, static_cast<uint32_t>(items), raw_smem + sizeof(sm), reinterpret_cast<uint32_t*>(sm.scratch));
@@ -665,7 +667,7 @@ cudaError_t launch_paged_attention(const PagedArgs& a, int dtype, bool cache8, c
   const cudaError_t e = allow_shared_memory(k.fn, smem);
   if (e != cudaSuccess) return e;
   void* args[] = {const_cast<PagedArgs*>(&a)};
-  return launch_ex(k.fn, dim3(static_cast<unsigned>(sms * k.ctas)), dim3(static_cast<unsigned>(k.threads)), smem, stream, false, args);
+  return launch_ex(k.fn, dim3(static_cast<unsigned>(sms * k.ctas)), dim3(static_cast<unsigned>(k.threads)), smem, stream, true, args);
 }
 
 }  // namespace fsx

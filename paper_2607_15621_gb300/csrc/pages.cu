@@ -257,7 +257,7 @@ fsx_status fsx_page_select(const void* d_q, long long q_stride, int dtype, const
   if (s == FSX_OK) s = check_pages(d_table, d_lengths, B, width, page_rows, cache_rows, a.pages);
   if (s == FSX_OK) s = check_rows("d_q", d_q, q_stride, n_heads);
   if (s != FSX_OK) return s;
-  if (width > fsx::kMaxPagesListed) return fail(FSX_ERR_UNSUPPORTED, "at most 65536 pages a request");
+  if (width > fsx::kMaxPagesListed) return fail(FSX_ERR_UNSUPPORTED, "at most 32768 pages a request");
   if (n_picked < 1 || n_picked > fsx::kMaxPicked) return fail(FSX_ERR_INVALID_ARG, "n_picked must be in 1..4096");
   if (first < 0 || last < 0 || first > n_picked || last > n_picked - first)
     return fail(FSX_ERR_INVALID_ARG, "first and last must be >= 0 and n_picked at most together");

@@ -15,7 +15,7 @@ namespace fsx {
 
 constexpr int kMaxAxes = 4;          // of rotary positions
 constexpr int kMaxPicked = 4096;     // pages that a selection takes
-constexpr int kMaxPagesListed = 65536;  // pages of a request that a selection looks at
+constexpr int kMaxPagesListed = 32768;  // pages of a request that a selection looks at
 constexpr int kMaxPlanes = 512;      // of a copy of pages
 
 struct RotaryArgs {

@@ -81,6 +81,8 @@ enum { kNoCache = 0, kCache16 = 1, kCache8 = 2 };
 template <bool BF, bool ADJACENT, int CACHE>
 __global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant__ RotaryArgs a, int parts, int per) {
   __shared__ __align__(16) float2 turn[kWarps][kHeadDim / 2];  // cosine, sine
+  pdl_launch_dependents();
+  pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane & 7;
   const long long w = static_cast<long long>(blockIdx.x) * kWarps + warp;
   const long long row = w / parts;
@@ -223,7 +225,7 @@ cudaError_t launch_rotary(const RotaryArgs& a, int dtype, bool adjacent, bool ca
   const long long blocks = (a.rows * parts + kWarps - 1) / kWarps;
   if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
   void* args[] = {const_cast<RotaryArgs*>(&a), &parts, &per};
-  return launch_ex(fn, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, false, args);
+  return launch_ex(fn, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, true, args);
 }
 
 }  // namespace fsx

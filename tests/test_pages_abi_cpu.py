@@ -94,7 +94,7 @@ def test_page_bounds_refuse(lib, over, code):
 
 @pytest.mark.parametrize("over,code", PAGES + [
     (dict(q=None), BAD), (dict(dt=fsx.FSX_F32), BAD), (dict(b=None), BAD), (dict(bs=None), BAD), (dict(picked=None), BAD),
-    (dict(width=65537), UNS), (dict(np=0), BAD), (dict(np=4097), BAD), (dict(first=-1), BAD), (dict(last=-1), BAD),
+    (dict(width=32769), UNS), (dict(np=0), BAD), (dict(np=4097), BAD), (dict(first=-1), BAD), (dict(last=-1), BAD),
     (dict(first=3, last=2), BAD), (dict(qs=504), BAD), (dict(cr=0), BAD),
 ])
 def test_page_select_refuses(lib, over, code):
