@@ -2,7 +2,8 @@
 
 Each .cu translation unit is compiled in parallel with nvcc, then linked into
 ``paper_2607_15621_gb300/_lib/libfsx.so`` with the CUDA runtime linked
-statically, so the library loads on machines without a GPU.
+statically, so the library loads on machines without a GPU. ``_lib/_calls.so``
+is the Python extension that passes torch tensors to some of its entry points.
 
     python -m paper_2607_15621_gb300.build
 """
@@ -12,6 +13,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -20,6 +22,7 @@ CSRC = os.path.join(PKG, "csrc")
 OUT_DIR = os.path.join(PKG, "_lib")
 BUILD_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(OUT_DIR, "libfsx.so")
+CALLS = os.path.join(OUT_DIR, "_calls.so")
 SOURCES = ["fsx.cu", "launch.cu", "gemm_tc.cu", "gemm_stream.cu", "gemm_res.cu", "attention.cu", "attention_tc.cu", "embed_head.cu",
            "attention_noalloc.cu", "tick_persistent.cu", "append.cu", "paper_tokens.cu", "session.cu",
            "llm.cu", "cache8.cu", "prompt_attention.cu", "tree_attention.cu", "tree_tc.cu", "pages.cu",
@@ -43,6 +46,19 @@ def _run(cmd):
     return res.stdout + res.stderr
 
 
+def _build_calls() -> str:
+    """The extension module: plain C++ against this interpreter's and this torch's headers."""
+    import torch
+    at = os.path.dirname(torch.__file__)
+    include = [sysconfig.get_paths()["include"], os.path.join(at, "include"),
+               os.path.join(at, "include", "torch", "csrc", "api", "include"), os.path.join(ROOT, "include")]
+    out = _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", *(x for i in include for x in ("-I", i)),
+                os.path.join(CSRC, "calls.cpp"), "-o", CALLS + ".tmp", "-L" + os.path.join(at, "lib"), "-ltorch_python",
+                "-ltorch_cpu", "-ltorch", "-lc10", "-ldl"])
+    os.replace(CALLS + ".tmp", CALLS)
+    return out
+
+
 def build(verbose: bool = False, extra_flags=()) -> str:
     os.makedirs(OUT_DIR, exist_ok=True)
     os.makedirs(BUILD_DIR, exist_ok=True)
@@ -53,8 +69,10 @@ def build(verbose: bool = False, extra_flags=()) -> str:
         obj = os.path.join(BUILD_DIR, src.replace(".cu", ".o"))
         objs.append(obj)
         cmds.append([cc, *ARCH, *FLAGS, *extra_flags, "-c", os.path.join(CSRC, src), "-o", obj])
-    with ThreadPoolExecutor(max_workers=len(cmds)) as ex:
+    with ThreadPoolExecutor(max_workers=len(cmds) + 1) as ex:
+        calls = ex.submit(_build_calls)
         logs = list(ex.map(_run, cmds))
+        logs.append(calls.result())
     tmp = LIB + ".tmp"
     logs.append(_run([cc, *ARCH, "-shared", "-Xcompiler", "-pthread", "-o", tmp, *objs]))
     os.replace(tmp, LIB)

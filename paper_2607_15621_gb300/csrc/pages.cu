@@ -2,6 +2,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <cstring>
 
 #include "fsx.h"
 #include "kernels.h"
@@ -76,11 +77,14 @@ fsx_status check_pages(const int32_t* table, const int64_t* lengths, int B, int 
   return FSX_OK;
 }
 
-// Turns a position of a pair, as 64-bit fixed point: the fraction of rate / (2 pi), rounded down. `rate` is m 2^(e - 53) with whole
-// m; 1 / (2 pi) to 128 bits behind the point; of the product 64 bits behind the point are kept.
+// Turns a position of a pair, as 64-bit fixed point: the fraction of rate / (2 pi), rounded down. |rate| is m 2^(e - 53), m whole;
+// 1 / (2 pi) to 128 bits behind the point; of the product 64 bits behind the point are kept.
 uint64_t turns_of(double rate) {
-  int e = 0;
-  const uint64_t m = static_cast<uint64_t>(std::ldexp(std::frexp(std::fabs(rate), &e), 53));
+  uint64_t bits;
+  memcpy(&bits, &rate, sizeof(bits));
+  const int biased = static_cast<int>(bits >> 52 & 0x7ff), e = biased - 1022;
+  if (biased == 0) return 0;  // zero, or below 2^-1022
+  const uint64_t m = (bits & ((1ull << 52) - 1)) | 1ull << 52;
   constexpr uint64_t kHi = 0x28BE60DB9391054Aull, kLo = 0x7F09D5F47D4D3770ull;  // 1 / (2 pi) = 0.28BE60DB...
   const unsigned __int128 hi = static_cast<unsigned __int128>(m) * kHi, lo = static_cast<unsigned __int128>(m) * kLo;
   // m / (2 pi) as w2.w1..., then times 2^(e - 53)

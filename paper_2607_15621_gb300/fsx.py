@@ -16,6 +16,7 @@ from .synth import Dims
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "_lib", "libfsx.so")
+CALLS_PATH = os.path.join(_PKG, "_lib", "_calls.so")
 
 FSX_OK = 0
 FSX_ERR_INVALID_ARG = 1
@@ -369,14 +370,14 @@ def attention_noalloc_status(stream=None) -> int:
 # What the checks below ask for. A call of 10 to 20 us on the GPU waits for its caller: the conditions are one expression
 # of cheap attributes (12 to 23 us a call with a helper for each), and only a refusal looks for its reason.
 _CODES: dict = {}  # torch dtype -> fsx_dtype; e4m3 caches may be held as bytes
-_I64 = _I32 = _I8 = _F32 = _raw_stream = _device = None
+_I64 = _F32 = _raw_stream = _device = None
 
 
 def _codes() -> dict:
-    global _I64, _I32, _I8, _F32, _raw_stream, _device
+    global _I64, _F32, _raw_stream, _device
     if not _CODES:
         import torch
-        _I64, _I32, _I8, _F32 = torch.int64, torch.int32, torch.int8, torch.float32
+        _I64, _F32 = torch.int64, torch.float32
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # of tensors on the GPU: CUDA is at work
         _device = getattr(torch._C, "_cuda_getDevice", None)
         _CODES.update({torch.float32: FSX_F32, torch.bfloat16: FSX_BF16, torch.float16: FSX_F16,
@@ -527,6 +528,7 @@ class RotaryPairs:
         if len(axis) != 64 or len(rate) != 64:
             raise FsxError(FSX_ERR_INVALID_ARG, f"64 axes and rates are asked for; given: {len(axis)} and {len(rate)}")
         self.axis, self.rate = (ctypes.c_int * 64)(*axis), (ctypes.c_double * 64)(*rate)
+        self.axis_at, self.rate_at = ctypes.addressof(self.axis), ctypes.addressof(self.rate)
         self.n_axes = max(axis) + 1
         self.layout = FSX_ROTARY_ADJACENT if adjacent else FSX_ROTARY_HALVES
 
@@ -543,65 +545,54 @@ def rotary_pairs(sections: Sequence[int] = (64,), base: float = 10000.0, per_axi
     return RotaryPairs(axis, rate, adjacent)
 
 
+# The operators over a cache in pages are called through an extension module (csrc/calls.cpp), which reads the tensors and checks
+# that they go together; -1: they do not.
+_calls = _where = None
+
+
+def _native():
+    """The extension's functions, and what gives the current device (-1 on a machine without a GPU)."""
+    global _calls, _where
+    if _calls is None:
+        import importlib.util
+        import torch
+        lib()
+        if not os.path.exists(CALLS_PATH):
+            raise RuntimeError(f"{CALLS_PATH} is missing: build it with paper_2607_15621_gb300.build.build()")
+        spec = importlib.util.spec_from_file_location("_calls", CALLS_PATH)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        module.bind(LIB_PATH)
+        _codes()
+        if torch.cuda.is_available():
+            torch.cuda.init()
+            _where = torch._C._cuda_getDevice
+        else:
+            _where = lambda: -1
+        _calls = module
+    return _calls
+
+
+def _refused(error: int, what: str, **tensors):
+    if error > 0:
+        check(error)
+    _refuse(what + ", all on the current device", **tensors)
+
+
 def rotary(q, k, positions, pairs: RotaryPairs, status, q_out=None, k_out=None, v=None, rows=None, k_cache=None, v_cache=None,
            k_scale=None, v_scale=None, stream=None):
     """fsx_rotary: q [n, heads, 128] into q_out, k [n, kv heads, 128] into k_out (each may be its input; q or k may be None), by
     positions int64 [axes, n]; with caches [rows, kv heads, 128] of their dtype or e4m3 (then with scales [kv heads, rows])
     the rotated keys and v into cache rows `rows` (int64 [n], distinct; None: 0 .. n - 1)."""
-    codes = _CODES or _codes()
-    any_ = k if q is None else q
-    shape, dtype = any_.shape, any_.dtype
-    n = shape[0]
-    qs = qos = ks = kos = (0, 0, 1)
-    good = len(shape) == 3 and dtype in codes and positions.dtype is _I64 and positions.dim() == 2 and \
-        positions.shape[1] == n and positions.shape[0] >= pairs.n_axes and positions.is_contiguous() and (q is None) == (q_out is None)
-    if good and q is not None:
-        qs, qos = q.stride(), q_out.stride()
-        good = q_out.shape == shape and q_out.dtype is dtype and _rows(q, qs) and _rows(q_out, qos)
-    heads = kv_heads = shape[1] if good else 0
-    held, m = dtype, 0
-    if good and k is not None:
-        ks, kv_shape = k.stride(), k.shape
-        kv_heads = kv_shape[1] if len(kv_shape) == 3 else 0
-        good = kv_heads > 0 and kv_shape[0] == n and kv_shape[2] == shape[2] and k.dtype is dtype and _rows(k, ks)
-        if q is None:
-            heads = kv_heads
-        if good and k_out is not None:
-            kos = k_out.stride()
-            good = k_out.shape == kv_shape and k_out.dtype is dtype and _rows(k_out, kos)
-        if good and k_cache is not None:
-            cs, held = k_cache.shape, k_cache.dtype
-            m = cs[0]
-            good = (v is not None and v_cache is not None and v.shape == kv_shape and v.dtype is dtype and
-                    (v.stride() == ks or _alike(v, k)) and len(cs) == 3 and cs[1] == kv_heads and cs[2] == shape[2] and
-                    v_cache.shape == cs and v_cache.dtype is held and held in codes and k_cache.is_contiguous() and
-                    v_cache.is_contiguous() and
-                    (codes[held] != FSX_E4M3 or _scales(k_scale, v_scale, kv_heads, m)) and
-                    (rows is None or (rows.dtype is _I64 and rows.dim() == 1 and rows.shape[0] == n and rows.is_contiguous())))
-    if not good or (k is None and (k_out is not None or k_cache is not None)) or (k_cache is None and v_cache is not None):
-        _refuse("q, q_out [n, heads, 128], k, k_out, v [n, kv heads, 128] of one dtype, k and v of one stride, positions int64 "
-                "[axes, n], rows int64 [n], caches [rows, kv heads, 128] of that dtype or e4m3 with scales fp32 [kv heads, rows]",
-                q=q, k=k, v=v, positions=positions, q_out=q_out, k_out=k_out, rows=rows, k_cache=k_cache, v_cache=v_cache,
-                k_scale=k_scale, v_scale=v_scale)
-    eight = k_cache is not None and codes[held] == FSX_E4M3
-    on = _raw_stream(_device()) if stream is None else _stream(stream)
-    error = (_lib or lib()).fsx_rotary(
-        None if q is None else q.data_ptr(), 0 if q is None else _pitch(q, qs), None if k is None else k.data_ptr(),
-        None if v is None else v.data_ptr(), 0 if k is None else _pitch(k, ks), codes[dtype], positions.data_ptr(),
-        positions.shape[0], pairs.axis, pairs.rate, pairs.layout, n, heads, kv_heads, shape[2],
-        None if q is None else q_out.data_ptr(), 0 if q is None else _pitch(q_out, qos),
-        None if k_out is None else k_out.data_ptr(), 0 if k_out is None else _pitch(k_out, kos),
-        None if rows is None else rows.data_ptr(), None if k_cache is None else k_cache.data_ptr(),
-        None if k_cache is None else v_cache.data_ptr(), k_scale.data_ptr() if eight else None,
-        v_scale.data_ptr() if eight else None, codes[held], m, status.data_ptr(), on)
+    call = _calls or _native()
+    device = _where()
+    error = call.rotary(q, k, positions, pairs.axis_at, pairs.rate_at, pairs.n_axes, pairs.layout, status, q_out, k_out, v, rows, k_cache,
+                        v_cache, k_scale, v_scale, device, _raw_stream(device) if stream is None else _stream(stream))
     if error:
-        check(error)
-
-
-def _scales(k_scale, v_scale, kv_heads: int, rows: int) -> bool:
-    return (k_scale is not None and v_scale is not None and k_scale.dtype is _F32 and v_scale.dtype is _F32 and
-            k_scale.shape == (kv_heads, rows) and v_scale.shape == (kv_heads, rows) and k_scale.is_contiguous() and
-            v_scale.is_contiguous())
+        _refused(error, "q, q_out [n, heads, 128], k, k_out, v [n, kv heads, 128] of one dtype, k and v of one stride, positions int64 "
+                 "[axes, n], rows int64 [n], caches [rows, kv heads, 128] of that dtype or e4m3 with scales fp32 [kv heads, rows]",
+                 q=q, k=k, v=v, positions=positions, q_out=q_out, k_out=k_out, rows=rows, k_cache=k_cache, v_cache=v_cache,
+                 k_scale=k_scale, v_scale=v_scale)
 
 
 def paged_attention_workspace_bytes(B: int, n_heads: int, n_kv_heads: int) -> int:
@@ -613,93 +604,43 @@ def paged_attention(q, k_cache, v_cache, table, lengths, page_rows: int, out, st
     """fsx_paged_attention: one token a request, q [B, heads, 128], over caches [rows, kv heads, 128] of q's dtype or e4m3
     (then with scales [kv heads, rows]) in pages of page_rows rows: table int32 [B, width], lengths int64 [B]; over all pages or
     those of `picked`, int32 [B, kv heads, n]."""
-    codes = _CODES or _codes()
-    dtype, held, qs, shape, cs, ts = q.dtype, k_cache.dtype, q.stride(), q.shape, k_cache.shape, table.shape
-    code = codes.get(held)
-    good = (len(shape) == 3 and len(cs) == 3 and len(ts) == 2 and dtype in codes and code is not None and qs[2] == 1 and
-            (qs[1] == shape[2] or shape[1] == 1) and out.dtype is dtype and out.shape == shape and out.is_contiguous() and
-            table.dtype is _I32 and table.is_contiguous() and ts[0] == shape[0] and lengths.dtype is _I64 and
-            lengths.dim() == 1 and lengths.shape[0] == shape[0] and lengths.is_contiguous() and v_cache.dtype is held and
-            v_cache.shape == cs and cs[2] == shape[2] and k_cache.is_contiguous() and v_cache.is_contiguous() and
-            (code != FSX_E4M3 or _scales(k_scale, v_scale, cs[1], cs[0])) and
-            (picked is None or (picked.dtype is _I32 and picked.dim() == 3 and picked.shape[:2] == (shape[0], cs[1]) and
-                                picked.is_contiguous())) and
-            (lse is None or (lse.dtype is _F32 and lse.shape == (shape[1], shape[0]) and lse.is_contiguous())))
-    if not good:
-        _refuse("q, out [B, heads, 128] of one dtype, out contiguous, caches [rows, kv heads, 128] of that dtype or e4m3 with "
-                "scales fp32 [kv heads, rows], table int32 [B, width], lengths int64 [B], picked int32 [B, kv heads, n], lse "
-                "fp32 [heads, B]", q=q, k_cache=k_cache, v_cache=v_cache, table=table, lengths=lengths, out=out,
-                k_scale=k_scale, v_scale=v_scale, picked=picked, lse=lse)
-    eight = code == FSX_E4M3
-    on = _raw_stream(_device()) if stream is None else _stream(stream)
-    error = (_lib or lib()).fsx_paged_attention(
-        q.data_ptr(), qs[0] if shape[0] > 1 else _pitch(q, qs), codes[dtype], k_cache.data_ptr(), v_cache.data_ptr(),
-        k_scale.data_ptr() if eight else None, v_scale.data_ptr() if eight else None, code, cs[0], page_rows,
-        table.data_ptr(), ts[1], lengths.data_ptr(), shape[0], None if picked is None else picked.data_ptr(),
-        0 if picked is None else picked.shape[2], shape[1], cs[1], shape[2], out.data_ptr(),
-        None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-        status.data_ptr(), on)
+    call = _calls or _native()
+    device = _where()
+    error = call.paged_attention(q, k_cache, v_cache, table, lengths, page_rows, out, status, workspace, k_scale, v_scale, picked, lse,
+                                 device, _raw_stream(device) if stream is None else _stream(stream))
     if error:
-        check(error)
+        _refused(error, "q, out [B, heads, 128] of one dtype, out contiguous, caches [rows, kv heads, 128] of that dtype or e4m3 with "
+                 "scales fp32 [kv heads, rows], table int32 [B, width], lengths int64 [B], picked int32 [B, kv heads, n], lse fp32 "
+                 "[heads, B]", q=q, k_cache=k_cache, v_cache=v_cache, table=table, lengths=lengths, out=out, k_scale=k_scale,
+                 v_scale=v_scale, picked=picked, lse=lse)
     return out
-
-
-def _pages_call(cs, table, lengths, page_rows, bounds, bound_scale) -> bool:
-    """A cache's pages, their table and their bounds."""
-    bs, n = bounds.shape, cs[0] // page_rows if page_rows > 0 else 0
-    return (len(cs) == 3 and table.dim() == 2 and table.dtype is _I32 and table.is_contiguous() and lengths.dtype is _I64 and
-            lengths.dim() == 1 and lengths.shape[0] == table.shape[0] and lengths.is_contiguous() and bounds.dtype is _I8 and
-            bs == (n, cs[1], 2, cs[2]) and bounds.is_contiguous() and bound_scale.dtype is _F32 and
-            bound_scale.shape == (cs[1], n) and bound_scale.is_contiguous())
 
 
 def page_bounds(k_cache, table, lengths, page_rows: int, bounds, bound_scale, status, k_scale=None, start=None, stream=None):
     """fsx_page_bounds: least and largest keys of the requests' pages (from row start int64 [B] on) into bounds int8
     [pages, kv heads, 2, 128] and bound_scale fp32 [kv heads, pages]."""
-    codes = _CODES or _codes()
-    cs, code = k_cache.shape, codes.get(k_cache.dtype)
-    good = (code is not None and _pages_call(cs, table, lengths, page_rows, bounds, bound_scale) and k_cache.is_contiguous() and
-            (code != FSX_E4M3 or (k_scale is not None and k_scale.dtype is _F32 and k_scale.shape == (cs[1], cs[0]) and
-                                  k_scale.is_contiguous())) and
-            (start is None or (start.dtype is _I64 and start.shape == lengths.shape and start.is_contiguous())))
-    if not good:
-        _refuse("a cache [rows, kv heads, 128] (e4m3: with scales fp32 [kv heads, rows]), table int32 [B, width], lengths and start "
-                "int64 [B], bounds int8 [pages, kv heads, 2, 128], bound_scale fp32 [kv heads, pages]", k_cache=k_cache,
-                table=table, lengths=lengths, bounds=bounds, bound_scale=bound_scale, k_scale=k_scale, start=start)
-    on = _raw_stream(_device()) if stream is None else _stream(stream)
-    error = (_lib or lib()).fsx_page_bounds(
-        k_cache.data_ptr(), k_scale.data_ptr() if code == FSX_E4M3 else None, code, cs[0], page_rows, table.data_ptr(),
-        table.shape[1], lengths.data_ptr(), None if start is None else start.data_ptr(), table.shape[0], cs[1], cs[2],
-        bounds.data_ptr(), bound_scale.data_ptr(), status.data_ptr(), on)
+    call = _calls or _native()
+    device = _where()
+    error = call.page_bounds(k_cache, table, lengths, page_rows, bounds, bound_scale, status, k_scale, start, device,
+                             _raw_stream(device) if stream is None else _stream(stream))
     if error:
-        check(error)
+        _refused(error, "a cache [rows, kv heads, 128] (e4m3: with scales fp32 [kv heads, rows]), table int32 [B, width], lengths and "
+                 "start int64 [B], bounds int8 [pages, kv heads, 2, 128], bound_scale fp32 [kv heads, pages]", k_cache=k_cache,
+                 table=table, lengths=lengths, bounds=bounds, bound_scale=bound_scale, k_scale=k_scale, start=start)
 
 
 def page_select(q, bounds, bound_scale, table, lengths, page_rows: int, picked, status, first: int = 1, last: int = 1, stream=None):
     """fsx_page_select: the pages that q [B, heads, 128] attends to into picked int32 [B, kv heads, n]: the request's `first` first
     and `last` last ones and those of the highest scores."""
-    codes = _CODES or _codes()
-    shape, qs, bs = q.shape, q.stride(), bounds.shape
-    good = (len(shape) == 3 and len(bs) == 4 and q.dtype in codes and _rows(q, qs) and shape[2] == bs[3] and
-            _pages_call((bs[0] * page_rows, bs[1], bs[3]), table, lengths, page_rows, bounds, bound_scale) and
-            table.shape[0] == shape[0] and picked.dtype is _I32 and picked.dim() == 3 and
-            picked.shape[:2] == (shape[0], bs[1]) and picked.is_contiguous())
-    if not good:
-        _refuse("q [B, heads, 128], bounds int8 [pages, kv heads, 2, 128], bound_scale fp32 [kv heads, pages], table int32 "
-                "[B, width], lengths int64 [B], picked int32 [B, kv heads, n]", q=q, bounds=bounds, bound_scale=bound_scale,
-                table=table, lengths=lengths, picked=picked)
-    on = _raw_stream(_device()) if stream is None else _stream(stream)
-    error = (_lib or lib()).fsx_page_select(
-        q.data_ptr(), _pitch(q, qs), codes[q.dtype], bounds.data_ptr(), bound_scale.data_ptr(), bs[0] * page_rows, page_rows,
-        table.data_ptr(), table.shape[1], lengths.data_ptr(), shape[0], shape[1], bs[1], shape[2], first, last,
-        picked.shape[2], picked.data_ptr(), status.data_ptr(), on)
+    call = _calls or _native()
+    device = _where()
+    error = call.page_select(q, bounds, bound_scale, table, lengths, page_rows, picked, status, first, last, device,
+                             _raw_stream(device) if stream is None else _stream(stream))
     if error:
-        check(error)
+        _refused(error, "q [B, heads, 128], bounds int8 [pages, kv heads, 2, 128], bound_scale fp32 [kv heads, pages], table int32 "
+                 "[B, width], lengths int64 [B], picked int32 [B, kv heads, n]", q=q, bounds=bounds, bound_scale=bound_scale,
+                 table=table, lengths=lengths, picked=picked)
     return picked
-
-
-def _ints(t, dtype, *shape) -> bool:
-    return t.dtype is dtype and t.shape == shape and t.is_contiguous()
 
 
 def pages_step(table, lengths, refs, new_offsets, page_rows: int, table_out, lengths_out, refs_out, rows, pairs, n_pairs, status,
@@ -707,46 +648,27 @@ def pages_step(table, lengths, refs, new_offsets, page_rows: int, table_out, len
     """fsx_pages_step: the state table int32 [B_in, width], lengths int64 [B_in], refs int32 [pages] into table_out, lengths_out,
     refs_out, where request i takes on request source[i] (int32 [B]; None: itself) and grows by the rows of new_offsets (int64
     [B + 1]); rows int64 [new rows], pairs int32 [B, 2] and n_pairs int32 [1] for cache_write and pages_copy."""
-    _CODES or _codes()
-    good = table.dim() == 2 and table_out.dim() == 2 and refs.dim() == 1 and rows.dim() == 1
-    if good:
-        B_in, B, width, n = table.shape[0], table_out.shape[0], table.shape[1], refs.shape[0]
-        good = (_ints(table, _I32, B_in, width) and _ints(lengths, _I64, B_in) and _ints(refs, _I32, n) and
-                _ints(new_offsets, _I64, B + 1) and _ints(table_out, _I32, B, width) and _ints(lengths_out, _I64, B) and
-                _ints(refs_out, _I32, n) and _ints(rows, _I64, rows.shape[0]) and _ints(pairs, _I32, B, 2) and
-                _ints(n_pairs, _I32, 1) and (source is None or _ints(source, _I32, B)))
-    if not good:
-        _refuse("table int32 [B_in, width], lengths int64 [B_in], refs int32 [pages], new_offsets int64 [B + 1], the same of B "
-                "requests, rows int64 [new rows], pairs int32 [B, 2], n_pairs int32 [1], source int32 [B]", table=table,
-                lengths=lengths, refs=refs, new_offsets=new_offsets, table_out=table_out, lengths_out=lengths_out,
-                refs_out=refs_out, rows=rows, pairs=pairs, n_pairs=n_pairs, source=source)
-    on = _raw_stream(_device()) if stream is None else _stream(stream)
-    error = (_lib or lib()).fsx_pages_step(
-        table.data_ptr(), lengths.data_ptr(), refs.data_ptr(), B_in, None if source is None else source.data_ptr(),
-        new_offsets.data_ptr(), B, rows.shape[0], width, n, page_rows, table_out.data_ptr(), lengths_out.data_ptr(),
-        refs_out.data_ptr(), rows.data_ptr(), pairs.data_ptr(), n_pairs.data_ptr(), status.data_ptr(), on)
+    call = _calls or _native()
+    device = _where()
+    error = call.pages_step(table, lengths, refs, new_offsets, page_rows, table_out, lengths_out, refs_out, rows, pairs, n_pairs, status,
+                            source, device, _raw_stream(device) if stream is None else _stream(stream))
     if error:
-        check(error)
+        _refused(error, "table int32 [B_in, width], lengths int64 [B_in], refs int32 [pages], new_offsets int64 [B + 1], the same of B "
+                 "requests, rows int64 [new rows], pairs int32 [B, 2], n_pairs int32 [1], source int32 [B]", table=table,
+                 lengths=lengths, refs=refs, new_offsets=new_offsets, table_out=table_out, lengths_out=lengths_out,
+                 refs_out=refs_out, rows=rows, pairs=pairs, n_pairs=n_pairs, source=source)
 
 
 def pages_compact(table, lengths, refs, page_rows: int, table_out, refs_out, pairs, n_pairs, status, stream=None):
     """fsx_pages_compact: pages in use to the front; pairs int32 [pages / 2 or more, 2], n_pairs int32 [1] for pages_copy."""
-    _CODES or _codes()
-    good = table.dim() == 2 and refs.dim() == 1 and pairs.dim() == 2
-    if good:
-        B, width, n, m = table.shape[0], table.shape[1], refs.shape[0], pairs.shape[0]
-        good = (_ints(table, _I32, B, width) and _ints(lengths, _I64, B) and _ints(refs, _I32, n) and
-                _ints(table_out, _I32, B, width) and _ints(refs_out, _I32, n) and _ints(pairs, _I32, m, 2) and _ints(n_pairs, _I32, 1))
-    if not good:
-        _refuse("table, table_out int32 [B, width], lengths int64 [B], refs, refs_out int32 [pages], pairs int32 [pages / 2 or "
-                "more, 2], n_pairs int32 [1]", table=table, lengths=lengths, refs=refs, table_out=table_out, refs_out=refs_out,
-                pairs=pairs, n_pairs=n_pairs)
-    on = _raw_stream(_device()) if stream is None else _stream(stream)
-    error = (_lib or lib()).fsx_pages_compact(
-        table.data_ptr(), lengths.data_ptr(), refs.data_ptr(), B, width, n, page_rows, table_out.data_ptr(),
-        refs_out.data_ptr(), pairs.data_ptr(), m, n_pairs.data_ptr(), status.data_ptr(), on)
+    call = _calls or _native()
+    device = _where()
+    error = call.pages_compact(table, lengths, refs, page_rows, table_out, refs_out, pairs, n_pairs, status, device,
+                               _raw_stream(device) if stream is None else _stream(stream))
     if error:
-        check(error)
+        _refused(error, "table, table_out int32 [B, width], lengths int64 [B], refs, refs_out int32 [pages], pairs int32 [pages / 2 or "
+                 "more, 2], n_pairs int32 [1]", table=table, lengths=lengths, refs=refs, table_out=table_out, refs_out=refs_out,
+                 pairs=pairs, n_pairs=n_pairs)
 
 
 class PagePlanes:
@@ -754,6 +676,7 @@ class PagePlanes:
 
     def __init__(self, planes: Sequence, n_pages: int, keep: Sequence):
         self.array, self.n, self.n_pages, self._keep = (PagePlane * len(planes))(*planes), len(planes), n_pages, list(keep)
+        self.at, self.device = ctypes.addressof(self.array), self._keep[0].get_device()  # -1: not on a GPU
 
 
 def page_planes(page_rows: int, caches: Sequence = (), scales: Sequence = (), bounds: Sequence = (),
@@ -762,8 +685,8 @@ def page_planes(page_rows: int, caches: Sequence = (), scales: Sequence = (), bo
     [kv heads, pages], of all layers, keys and values: made once, used by every pages_copy."""
     each = [(c, c.shape[0] // page_rows) for c in caches] + [(s, s.shape[1] // page_rows) for s in scales] + \
         [(b, b.shape[0]) for b in bounds] + [(s, s.shape[1]) for s in bound_scales]
-    if not each or len({n for _, n in each}) != 1 or not all(t.is_contiguous() for t, _ in each):
-        _refuse("contiguous tensors of as many pages each", **{f"planes[{i}]": t for i, (t, _) in enumerate(each)})
+    if not each or len({n for _, n in each}) != 1 or len({t.device for t, _ in each}) != 1 or not all(t.is_contiguous() for t, _ in each):
+        _refuse("contiguous tensors of as many pages each on one device", **{f"planes[{i}]": t for i, (t, _) in enumerate(each)})
     n_pages, planes = each[0][1], []
     for group, by_row in ((caches, True), (scales, False), (bounds, True), (bound_scales, False)):
         for t in group:
@@ -777,14 +700,12 @@ def page_planes(page_rows: int, caches: Sequence = (), scales: Sequence = (), bo
 
 def pages_copy(planes: PagePlanes, pairs, n_pairs, status, stream=None):
     """fsx_pages_copy: page pairs[i, 0] to page pairs[i, 1] in every plane, for the first n_pairs of them."""
-    _CODES or _codes()
-    if not (pairs.dim() == 2 and _ints(pairs, _I32, pairs.shape[0], 2) and _ints(n_pairs, _I32, 1)):
-        _refuse("pairs int32 [n, 2] and n_pairs int32 [1]", pairs=pairs, n_pairs=n_pairs)
-    on = _raw_stream(_device()) if stream is None else _stream(stream)
-    error = (_lib or lib()).fsx_pages_copy(planes.array, planes.n, planes.n_pages, pairs.data_ptr(), n_pairs.data_ptr(),
-                                           pairs.shape[0], status.data_ptr(), on)
+    call = _calls or _native()
+    device = _where()
+    error = -1 if planes.device != device else call.pages_copy(
+        planes.at, planes.n, planes.n_pages, pairs, n_pairs, status, device, _raw_stream(device) if stream is None else _stream(stream))
     if error:
-        check(error)
+        _refused(error, "planes, pairs int32 [n, 2] and n_pairs int32 [1]", pairs=pairs, n_pairs=n_pairs)
 
 
 class Append:
