@@ -46,95 +46,262 @@ __device__ __forceinline__ bool rows_of(const PagedCache& p, int b, int& len, in
 
 constexpr int kBoundsWarps = 8;
 
-// A warp a page and kv head: 16 lanes a row of 16-bit keys (two rows at once), 8 lanes a row of codes (four).
-template <int TYPE>
-__global__ void __launch_bounds__(32 * kBoundsWarps) bounds_kernel(const BoundsArgs a) {
+// Least and largest of packed 16-bit values; a NaN stays
+template <bool BF>
+__device__ __forceinline__ void bound2(uint32_t& lo, uint32_t& hi, uint32_t low, uint32_t high) {
+  if (BF) {
+    asm("min.NaN.bf16x2 %0, %0, %1;" : "+r"(lo) : "r"(low));
+    asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(hi) : "r"(high));
+  } else {
+    asm("min.NaN.f16x2 %0, %0, %1;" : "+r"(lo) : "r"(low));
+    asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(hi) : "r"(high));
+  }
+}
+
+// Ends of a lane's values over rows from, from + step, ... below `filled` of a page, kAhead of them loaded at once; `src`, `scales`: at the
+// lane's own row `sub` of the first. CAREFUL: values that are not finite change neither end, and are reported; else they
+// show in the ends (16 bits: NaN and infinities; codes: infinities, and NaN codes by `wild`).
+template <int TYPE, int AHEAD, bool CAREFUL>
+struct Ends {
+  static constexpr bool kC8 = TYPE == FSX_E4M3, kBf = TYPE == FSX_BF16;
+  static constexpr int kLanes = kC8 ? 8 : 16, kValues = kHeadDim / kLanes, kAtOnce = 32 / kLanes;
+  static __device__ __forceinline__ void scan(const unsigned char* src, const float* scales, long long row_bytes, int sub, int from, int step, int filled,
+                                              float (&lo)[kValues], float (&hi)[kValues], bool& wild) {
+    constexpr uint32_t kInf = kBf ? 0x7f807f80u : 0x7c007c00u;
+    uint32_t lo2[4], hi2[4];
+    if constexpr (kC8) {
+#pragma unroll
+      for (int j = 0; j < kValues; ++j) {
+        lo[j] = CUDART_INF_F;
+        hi[j] = -CUDART_INF_F;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        lo2[j] = kInf;
+        hi2[j] = kInf | 0x80008000u;
+      }
+    }
+#pragma unroll 1
+    for (int r0 = from; r0 < filled; r0 += AHEAD * step) {
+      uint4 x[AHEAD];
+      float s[AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const int r = r0 + i * step;  // rows behind the last: the page's first, once more
+        const int take = r + sub < filled ? r : -sub;
+        x[i] = __ldg(reinterpret_cast<const uint4*>(src + take * row_bytes));
+        s[i] = kC8 ? __ldg(scales + take) : 1.f;
+      }
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+        if constexpr (!kC8) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint32_t low = w[j], high = w[j];
+            if (CAREFUL) {
+              const uint32_t bad = not_finite2<kBf>(w[j]), mask = (bad >> 15) * 0xffffu;
+              wild = wild || bad != 0u;
+              low = (w[j] & ~mask) | (kInf & mask);
+              high = (w[j] & ~mask) | ((kInf | 0x80008000u) & mask);
+            }
+            bound2<kBf>(lo2[j], hi2[j], low, high);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            wild = wild || (((w[j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0u;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              float2 y = unpack_e4m3x2(w[j] >> (t * 16));
+              y.x *= s[i];
+              y.y *= s[i];
+              float2 z = y;
+              if (CAREFUL) {
+                const bool bad_x = !(fabsf(y.x) < CUDART_INF_F), bad_y = !(fabsf(y.y) < CUDART_INF_F);
+                wild = wild || bad_x || bad_y;
+                if (bad_x) y.x = CUDART_INF_F, z.x = -CUDART_INF_F;
+                if (bad_y) y.y = CUDART_INF_F, z.y = -CUDART_INF_F;
+              }
+              const int v = 4 * j + 2 * t;
+              lo[v] = fminf(lo[v], y.x);
+              hi[v] = fmaxf(hi[v], z.x);
+              lo[v + 1] = fminf(lo[v + 1], y.y);
+              hi[v + 1] = fmaxf(hi[v + 1], z.y);
+            }
+          }
+        }
+      }
+    }
+    if constexpr (!kC8) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        bound2<kBf>(lo2[j], hi2[j], __shfl_xor_sync(0xffffffffu, lo2[j], 16), __shfl_xor_sync(0xffffffffu, hi2[j], 16));
+        const float2 x = unpack16<kBf>(lo2[j]), y = unpack16<kBf>(hi2[j]);
+        lo[2 * j] = x.x, lo[2 * j + 1] = x.y, hi[2 * j] = y.x, hi[2 * j + 1] = y.y;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kValues; ++j)
+#pragma unroll
+        for (int o = kLanes; o < 32; o <<= 1) {
+          lo[j] = fminf(lo[j], __shfl_xor_sync(0xffffffffu, lo[j], o));
+          hi[j] = fmaxf(hi[j], __shfl_xor_sync(0xffffffffu, hi[j], o));
+        }
+    }
+  }
+};
+
+// The same of rows of codes whose scales are powers of two within 2^14 of one another: a code times its scale over the largest so far is
+// exact in fp16 (a code's last bit is 2^-9, fp16's 2^-24), so that two values are scaled and compared at once. In fp32 it takes
+// 2.5 times the instructions (131,000 rows of 8 heads 57 us, of which all but 17 for them). A NaN code shows in the ends. False:
+// the scales are not like that.
+template <int AHEAD>
+__device__ __forceinline__ bool scan_plain(const unsigned char* src, const float* scales, long long row_bytes, int sub, int from, int step, int filled,
+                                           float (&lo)[16], float (&hi)[16]) {
+  uint32_t lo2[8], hi2[8], top = 0, low = 0xffffffffu, all = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    lo2[j] = 0x7c007c00u;
+    hi2[j] = 0xfc00fc00u;
+  }
+#pragma unroll 1
+  for (int r0 = from; r0 < filled; r0 += AHEAD * step) {
+    uint4 x[AHEAD];
+    uint32_t s[AHEAD], most = 0, least = 0xffffffffu;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int r = r0 + i * step;  // rows behind the last: the page's first, once more
+      const int take = r + sub < filled ? r : -sub;
+      x[i] = __ldg(reinterpret_cast<const uint4*>(src + take * row_bytes));
+      s[i] = __float_as_uint(__ldg(scales + take));
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      most = max(most, s[i]);
+      least = min(least, s[i]);
+      all |= s[i];
+    }
+    most = __reduce_max_sync(0xffffffffu, most);
+    low = min(low, __reduce_min_sync(0xffffffffu, least));
+    if (most > top) {  // the ends so far, in the new unit
+      const uint32_t d = top == 0 ? 0u : (most - top) >> 23, q = d < 15u ? (15u - d) << 10 : 0u, q2 = q | q << 16;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (top != 0) {
+          const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&lo2[j]), *reinterpret_cast<const __half2*>(&q2));
+          const __half2 z = __hmul2(*reinterpret_cast<const __half2*>(&hi2[j]), *reinterpret_cast<const __half2*>(&q2));
+          lo2[j] = *reinterpret_cast<const uint32_t*>(&y);
+          hi2[j] = *reinterpret_cast<const uint32_t*>(&z);
+        }
+      top = most;
+    }
+    if (top - low > 14u << 23) return false;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+      const uint32_t q = (15u - ((top - s[i]) >> 23)) << 10, q2 = q | q << 16;  // the quotient, 2^0 to 2^-14
+      const __half2 f = *reinterpret_cast<const __half2*>(&q2);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        uint32_t y;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y) : "h"(static_cast<uint16_t>(w[j >> 1] >> ((j & 1) * 16))));
+        const __half2 z = __hmul2(*reinterpret_cast<const __half2*>(&y), f);
+        y = *reinterpret_cast<const uint32_t*>(&z);
+        bound2<false>(lo2[j], hi2[j], y, y);
+      }
+    }
+  }
+  if (__any_sync(0xffffffffu, (all & 0x807fffffu) != 0u) || top >= 0x7f800000u || low == 0u) return false;
+  const float unit = __uint_as_float(top);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+#pragma unroll
+    for (int o = 8; o < 32; o <<= 1)
+      bound2<false>(lo2[j], hi2[j], __shfl_xor_sync(0xffffffffu, lo2[j], o), __shfl_xor_sync(0xffffffffu, hi2[j], o));
+    const float2 x = unpack16<false>(lo2[j]), y = unpack16<false>(hi2[j]);
+    lo[2 * j] = x.x * unit, lo[2 * j + 1] = x.y * unit, hi[2 * j] = y.x * unit, hi[2 * j + 1] = y.y * unit;
+  }
+  return true;
+}
+
+// `share` warps a page and kv head, 1 or 8: 8 where pages are few (those that new rows went into), for a shorter chain.
+// 16 lanes a row of 16-bit keys (two rows at once), 8 lanes a row of codes (four).
+template <int TYPE, int SHARE>
+__global__ void __launch_bounds__(32 * kBoundsWarps, TYPE == FSX_E4M3 ? 3 : 4) bounds_kernel(const BoundsArgs a) {
   constexpr bool kC8 = TYPE == FSX_E4M3, kBf = TYPE == FSX_BF16;
   constexpr int kLanes = kC8 ? 8 : 16, kValues = kHeadDim / kLanes, kAtOnce = 32 / kLanes;
-  constexpr int kAhead = 8;
+  constexpr int kAhead = SHARE > 1 ? 2 : 8;
+  __shared__ float part[SHARE > 1 ? kBoundsWarps : 1][2][kHeadDim];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane % kLanes, sub = lane / kLanes;
   const int b = blockIdx.y;
   pdl_launch_dependents();
   pdl_wait();
   int len, pages;
-  const bool fine = rows_of(a.pages, b, len, pages);
   const long long start = a.start != nullptr ? a.start[b] : 0;
+  const bool fine = rows_of(a.pages, b, len, pages);
   if (!fine || start < 0) {
     if (blockIdx.x == 0 && threadIdx.x == 0) set_status(a.status, kStatusDeviceArg);
     return;
   }
   const int shift = a.pages.shift;
   const int first = start >= len ? pages : static_cast<int>(start >> shift);
-  const long long units = static_cast<long long>(pages - first) * a.n_kv_heads;
+  const uint32_t units = static_cast<uint32_t>(pages - first) * a.n_kv_heads;  // below 2^31: see the host
   const long long row_bytes = static_cast<long long>(a.n_kv_heads) * kHeadDim * (kC8 ? 1 : 2);
+  const uint32_t stride = gridDim.x * (kBoundsWarps / SHARE);
   bool wild = false, lost = false;
-  for (long long u = static_cast<long long>(blockIdx.x) * kBoundsWarps + warp; u < units; u += static_cast<long long>(gridDim.x) * kBoundsWarps) {
-    const int page = first + static_cast<int>(u / a.n_kv_heads), kvh = static_cast<int>(u % a.n_kv_heads);
-    const int at = __ldg(a.pages.table + static_cast<long long>(b) * a.pages.width + page);
+  const int32_t* const table = a.pages.table + static_cast<long long>(b) * a.pages.width + first;
+  uint32_t u = blockIdx.x * (kBoundsWarps / SHARE) + (SHARE > 1 ? 0 : warp);
+  int ahead = u < units ? __ldg(table + u / a.n_kv_heads) : 0;
+  for (; u < units; u += stride) {
+    const uint32_t nth = u / a.n_kv_heads;
+    const int page = first + static_cast<int>(nth), kvh = static_cast<int>(u - nth * a.n_kv_heads), at = ahead;
+    if (u + stride < units) ahead = __ldg(table + (u + stride) / a.n_kv_heads);
     if (at < 0 || at >= a.pages.n_pages) {
       lost = true;
-      continue;
+      continue;  // the same for all of the unit's warps
     }
     const int filled = min(len - (page << shift), 1 << shift);
     const long long row0 = static_cast<long long>(at) << shift;
     const unsigned char* src = static_cast<const unsigned char*>(a.k_cache) + (row0 + sub) * row_bytes + kvh * (kHeadDim * (kC8 ? 1 : 2)) + l * 16;
     const float* scales = kC8 ? a.k_scale + kvh * a.cache_rows + row0 + sub : nullptr;
     float lo[kValues], hi[kValues];
+    const int from = SHARE > 1 ? warp * kAtOnce : 0;
+    bool plain = false;
+    if constexpr (kC8) plain = scan_plain<kAhead>(src, scales, row_bytes, sub, from, kAtOnce * SHARE, filled, lo, hi);
+    if (!plain) Ends<TYPE, kC8 ? 1 : kAhead, kC8>::scan(src, scales, row_bytes, sub, from, kAtOnce * SHARE, filled, lo, hi, wild);
+    bool bad = false;  // an end that is not finite; of a warp without rows both are infinite
 #pragma unroll
-    for (int j = 0; j < kValues; ++j) {
-      lo[j] = CUDART_INF_F;
-      hi[j] = -CUDART_INF_F;
-    }
-    for (int r0 = 0; r0 < filled; r0 += kAhead * kAtOnce) {
-      uint4 x[kAhead];
-      float s[kAhead];
+    for (int j = 0; j < kValues; ++j) bad = bad || !(fabsf(lo[j]) < CUDART_INF_F) || !(fabsf(hi[j]) < CUDART_INF_F);
+    if (__any_sync(0xffffffffu, bad) && from < filled) Ends<TYPE, 1, true>::scan(src, scales, row_bytes, sub, from, kAtOnce * SHARE, filled, lo, hi, wild);
+    if constexpr (SHARE > 1) {  // the warps' ends, by the first warp
+      if (sub == 0) {
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int r = r0 + i * kAtOnce;  // rows behind the last: the page's first, once more
-        const int take = r + sub < filled ? r : -sub;
-        x[i] = __ldg(reinterpret_cast<const uint4*>(src + take * row_bytes));
-        s[i] = kC8 ? __ldg(scales + take) : 1.f;
-      }
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-        for (int j = 0; j < kValues / 2; ++j) {
-          float2 y;
-          if (kC8) {
-            y = unpack_e4m3x2(w[j >> 1] >> ((j & 1) * 16));
-            y.x *= s[i];
-            y.y *= s[i];
-          } else {
-            y = unpack16<kBf>(w[j & 3]);
-          }
-          if (!(fabsf(y.x) < CUDART_INF_F && fabsf(y.y) < CUDART_INF_F)) {  // left out
-            wild = true;
-            if (fabsf(y.x) < CUDART_INF_F) {
-              lo[2 * j] = fminf(lo[2 * j], y.x);
-              hi[2 * j] = fmaxf(hi[2 * j], y.x);
-            }
-            if (fabsf(y.y) < CUDART_INF_F) {
-              lo[2 * j + 1] = fminf(lo[2 * j + 1], y.y);
-              hi[2 * j + 1] = fmaxf(hi[2 * j + 1], y.y);
-            }
-            continue;
-          }
-          lo[2 * j] = fminf(lo[2 * j], y.x);
-          hi[2 * j] = fmaxf(hi[2 * j], y.x);
-          lo[2 * j + 1] = fminf(lo[2 * j + 1], y.y);
-          hi[2 * j + 1] = fmaxf(hi[2 * j + 1], y.y);
+        for (int j = 0; j < kValues / 4; ++j) {
+          reinterpret_cast<float4*>(&part[warp][0][l * kValues])[j] = make_float4(lo[4 * j], lo[4 * j + 1], lo[4 * j + 2], lo[4 * j + 3]);
+          reinterpret_cast<float4*>(&part[warp][1][l * kValues])[j] = make_float4(hi[4 * j], hi[4 * j + 1], hi[4 * j + 2], hi[4 * j + 3]);
         }
       }
+      __syncthreads();
+      if (warp == 0) {
+#pragma unroll
+        for (int w = 1; w < kBoundsWarps; ++w)
+#pragma unroll
+          for (int j = 0; j < kValues / 4; ++j) {
+            const float4 x = reinterpret_cast<const float4*>(&part[w][0][l * kValues])[j], y = reinterpret_cast<const float4*>(&part[w][1][l * kValues])[j];
+            lo[4 * j] = fminf(lo[4 * j], x.x), lo[4 * j + 1] = fminf(lo[4 * j + 1], x.y);
+            lo[4 * j + 2] = fminf(lo[4 * j + 2], x.z), lo[4 * j + 3] = fminf(lo[4 * j + 3], x.w);
+            hi[4 * j] = fmaxf(hi[4 * j], y.x), hi[4 * j + 1] = fmaxf(hi[4 * j + 1], y.y);
+            hi[4 * j + 2] = fmaxf(hi[4 * j + 2], y.z), hi[4 * j + 3] = fmaxf(hi[4 * j + 3], y.w);
+          }
+      }
+      __syncthreads();
+      if (warp != 0) continue;
     }
     float top = 0.f;
 #pragma unroll
     for (int j = 0; j < kValues; ++j) {
-#pragma unroll
-      for (int o = kLanes; o < 32; o <<= 1) {
-        lo[j] = fminf(lo[j], __shfl_xor_sync(0xffffffffu, lo[j], o));
-        hi[j] = fmaxf(hi[j], __shfl_xor_sync(0xffffffffu, hi[j], o));
-      }
       if (lo[j] > hi[j]) lo[j] = hi[j] = 0.f;  // no finite key
       top = fmaxf(top, fmaxf(fabsf(lo[j]), fabsf(hi[j])));
     }
@@ -425,19 +592,26 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const SelectArgs
 
 }  // namespace
 
+template <int SHARE>
+static const void* bounds_of(int cache_dtype) {
+  return cache_dtype == FSX_E4M3   ? reinterpret_cast<const void*>(&bounds_kernel<FSX_E4M3, SHARE>)
+         : cache_dtype == FSX_BF16 ? reinterpret_cast<const void*>(&bounds_kernel<FSX_BF16, SHARE>)
+                                   : reinterpret_cast<const void*>(&bounds_kernel<FSX_F16, SHARE>);
+}
+
 cudaError_t launch_page_bounds(const BoundsArgs& a, int cache_dtype, cudaStream_t stream) {
   const int sms = sm_count();
   if (sms == 0) return cudaErrorNoDevice;
-  // warps for the whole GPU over all requests, and no more than a request's pages can have
-  const long long most = (static_cast<long long>(a.pages.width) * a.n_kv_heads + kBoundsWarps - 1) / kBoundsWarps;
-  const long long want = (static_cast<long long>(sms) * 8 + a.pages.B - 1) / a.pages.B;
+  // With a start, pages are few: the ones that new rows went into. Without, twice as many warps as run at once over all requests, and no
+  // more than a request's pages can have.
+  const bool few = a.start != nullptr;
+  const int each = few ? 1 : kBoundsWarps;
+  const long long most = (static_cast<long long>(a.pages.width) * a.n_kv_heads + each - 1) / each;
+  const long long want = (static_cast<long long>(sms) * (few ? 8 : 16) + a.pages.B - 1) / a.pages.B;
   const unsigned x = static_cast<unsigned>(want < most ? want : most);
-  if (x == 0) return cudaSuccess;
   void* args[] = {const_cast<BoundsArgs*>(&a)};
-  const void* fn = cache_dtype == FSX_E4M3   ? reinterpret_cast<const void*>(&bounds_kernel<FSX_E4M3>)
-                   : cache_dtype == FSX_BF16 ? reinterpret_cast<const void*>(&bounds_kernel<FSX_BF16>)
-                                             : reinterpret_cast<const void*>(&bounds_kernel<FSX_F16>);
-  return launch_ex(fn, dim3(x, static_cast<unsigned>(a.pages.B)), dim3(32 * kBoundsWarps), 0, stream, true, args);
+  return launch_ex(few ? bounds_of<kBoundsWarps>(cache_dtype) : bounds_of<1>(cache_dtype), dim3(x, static_cast<unsigned>(a.pages.B)), dim3(32 * kBoundsWarps),
+                   0, stream, true, args);
 }
 
 cudaError_t launch_page_select(const SelectArgs& a, int dtype, cudaStream_t stream) {

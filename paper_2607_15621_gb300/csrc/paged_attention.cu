@@ -26,7 +26,7 @@ namespace fsx {
 namespace {
 
 constexpr int kFew = 8, kMany = 28;  // queue: chunks of an item that is not cut, and of a piece
-constexpr int kNear = 32;            // line: steps
+constexpr int kNear = 32, kWhole = 64, kShort = 128;  // line: steps
 constexpr int kHeader = 64;          // ints of the workspace, queue: [0] pieces taken, [1] CTAs that are done
 constexpr int kCounters = 8192;      // then one for each slot
 
@@ -172,8 +172,10 @@ struct Line {
   uint32_t* cut;    // [CTAs + 1]
   uint32_t ranges;  // the rest of the CTAs have none
 };
-__host__ __device__ constexpr size_t line_bytes(int B, int ctas) { return (B + B + 1 + ctas + 1) * sizeof(int); }
+__host__ __device__ constexpr size_t line_bytes(int B, int ctas) { return (B + 2 * (B + 1) + ctas + 1) * sizeof(int); }
 __device__ __forceinline__ uint32_t line_steps(const Request& r) { return max(1, r.steps); }
+
+__device__ __forceinline__ uint32_t short_pieces(uint32_t n, uint32_t most) { return n <= kWhole ? 1u : (n + most - 1) / most; }
 
 template <int W>
 __device__ __forceinline__ Line make_line(const PagedArgs& p, uint32_t items, void* at, uint32_t* scratch) {
@@ -215,8 +217,44 @@ __device__ __forceinline__ Line make_line(const PagedArgs& p, uint32_t items, vo
   }
   if (tid == 0) line.start[B] = before;
   __syncthreads();
-  // ranges of 32 steps and more, or one for each item; a cut near an item's end moves there
-  line.ranges = max(1u, min(gridDim.x, max(before / kNear, min(before, items * B))));
+  const uint32_t ctas = gridDim.x, all_items = items * B;
+  if (before < ctas * kShort && all_items <= ctas) {
+    // little work: near-equal pieces of whole items, at most one a CTA, as many as there are CTAs for
+    const uint32_t most = max(static_cast<uint32_t>(kNear), (before + ctas - all_items) / max(1u, ctas - all_items));
+    uint32_t* first = line.cut + ctas + 1;  // [B + 1] pieces of the requests before
+    if (warp == 0) {
+      uint32_t sum = 0;
+#pragma unroll 1
+      for (int b0 = 0; b0 < B; b0 += 32) {
+        const int b = b0 + lane;
+        const uint32_t mine = b < B && line.len[b] >= 0 ? items * short_pieces(line_steps(request_of(p, line.len[b])), most) : 0;
+        uint32_t up_to = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const uint32_t up = __shfl_up_sync(0xffffffffu, up_to, o);
+          if (lane >= o) up_to += up;
+        }
+        if (b < B) first[b] = sum + up_to - mine;
+        sum += __shfl_sync(0xffffffffu, up_to, 31);
+      }
+      if (lane == 0) first[B] = sum;
+    }
+    __syncthreads();
+    line.ranges = max(1u, first[B]);
+    for (uint32_t c = tid; c <= line.ranges; c += kThreadsLine) {
+      uint32_t x = before;
+      if (c < first[B]) {
+        const int b = find(first, B, c);
+        const uint32_t n = line_steps(request_of(p, line.len[b])), of = short_pieces(n, most), rel = c - first[b], item = rel / of;
+        x = line.start[b] + item * n + (rel - item * of) * n / of;
+      }
+      line.cut[c] = x;
+    }
+    __syncthreads();
+    return line;
+  }
+  // equal ranges; a cut less than 32 steps from an item's end moves there
+  line.ranges = max(1u, min(ctas, before / kNear));
   const uint32_t least = before / line.ranges, more = before - least * line.ranges;
   for (uint32_t c = tid; c <= line.ranges; c += kThreadsLine) {
     uint32_t x = c * least + min(c, more);
@@ -652,7 +690,7 @@ size_t paged_attention_workspace_bytes(int B, int n_heads, int n_kv_heads) {
   return (kHeader + kCounters) * sizeof(int) + slots_of(nt) * slot_floats(nt) * sizeof(float);
 }
 
-constexpr int kLineItems = 8;  // items a SM up to which the line is taken
+constexpr int kLineItems = 2;  // items a SM up to which the line is taken
 
 cudaError_t launch_paged_attention(const PagedArgs& a, int dtype, bool cache8, cudaStream_t stream) {
   const int nt = tile_count(a.n_heads, a.n_kv_heads), G = a.n_heads / a.n_kv_heads;

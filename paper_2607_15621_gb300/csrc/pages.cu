@@ -238,6 +238,7 @@ fsx_status fsx_page_bounds(const void* d_k_cache, const float* d_k_scale, int ca
   if (cache_rows > 0 && !d_k_cache) return fail(FSX_ERR_INVALID_ARG, "NULL pointer argument");
   if (cache_dtype == FSX_E4M3 && cache_rows > 0 && !d_k_scale) return fail(FSX_ERR_INVALID_ARG, "an e4m3 cache needs its scales");
   if (!aligned(d_k_cache, 16) || !aligned(d_bounds, 16)) return fail(FSX_ERR_INVALID_ARG, "the cache and the bounds must be 16-byte aligned");
+  if (static_cast<long long>(width) * n_kv_heads > kMaxRows / 2) return fail(FSX_ERR_UNSUPPORTED, "width times n_kv_heads must be below 2^30");
   a.k_cache = d_k_cache;
   a.k_scale = d_k_scale;
   a.cache_rows = cache_rows;
