@@ -321,6 +321,16 @@ __device__ __forceinline__ bool look_up(const PagedArgs& p, const Piece& it, int
   return true;
 }
 
+// Rows of sums in shared memory: where dim d lies, and floats from row to row. A warp stores two dims of 8 lane groups g for 4 rows at
+// once; turned by g within its 16 (8) dims and with this pitch they fall on different banks but for two (as they are, 16 at
+// once on the same: 2 us for 7 rows of 16 warps).
+template <bool C8>
+constexpr int kPitch = C8 ? kD + 4 : kD + 2;
+template <bool C8>
+__device__ __forceinline__ int place_of(int d) {
+  return C8 ? (d & ~15) | ((d + 2 * (d >> 5)) & 15) : (d & ~7) | ((d + 2 * ((d >> 5) & 1)) & 7);
+}
+
 // Warps of a CTA, rows that they put together at a time
 template <bool C8, int NT, bool LINE>
 struct Shape {
@@ -333,8 +343,9 @@ struct Shared {  // and the plan behind it
   static constexpr int kW = Shape<C8, NT, LINE>::kWarps;
   long long scratch[2 * kW];
   __align__(128) unsigned char ring[kW][Fit<C8, NT>::kStages * Stage<C8>::kBytes];
-  float m[kW][8 * NT], l[kW][8 * NT];
-  float o[kW][Shape<C8, NT, LINE>::kPass][kD];
+  float m[kW][8 * NT], l[kW][8 * NT];  // of each warp
+  float weight[kW][8 * NT], top[8 * NT], total[8 * NT];
+  __align__(16) float o[kW][Shape<C8, NT, LINE>::kPass][kPitch<C8>];
   int left[kW][4];  // keys of the ring's stages
   int bad;          // of the piece
   uint32_t next;
@@ -520,37 +531,52 @@ __global__ void __launch_bounds__(32 * Shape<C8, NT, LINE>::kWarps, Shape<C8, NT
       load_queries<C8, NT>(qf, p, next, G);
       begin(next);
     }
-    // ---- the warps' results, kPass rows at a time; a thread a dim
+    // ---- the warps' results: kPass rows at a time, or all of them where no copies are on their way into the rings
     auto lse_at = [&](int head) -> float& { return p.lse[static_cast<long long>(head) * p.pages.B + it.b]; };
     float* slot = slot_at<NT>(p, slot_of<LINE>(it, it.j));
-    const int dim = tid & (kD - 1);
+    const bool all = LINE && !goes_on;
+    const int pass = all ? kTile : kPass;
+    float* const sums = all ? reinterpret_cast<float*>(&sm.ring[0][0]) : &sm.o[0][0][0];  // [kW][pass][kPitch]
+    for (int row = tid >> 4; row < rows; row += 2 * kW) {  // 16 lanes a row, one a warp
+      const int w = tid & 15;
+      const float m = w < kW ? sm.m[w][row] : -CUDART_INF_F, l = w < kW ? sm.l[w][row] : 0.f;
+      const uint32_t lanes = 0xffffu << (lane & 16);
+      float top = m;
 #pragma unroll
-    for (int base = 0; base < kTile; base += kPass) {
-      if (base >= rows) break;
+      for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(lanes, top, o));
+      const float a = weight_of(m, top);
+      float total = a * l;
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) total += __shfl_xor_sync(lanes, total, o);
+      if (w < kW) sm.weight[w][row] = a;
+      if (w == 0) {
+        sm.top[row] = top;
+        sm.total[row] = total;
+      }
+    }
+#pragma unroll 1
+    for (int base = 0; base < rows; base += pass) {
+      const int here = min(rows, base + pass);
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const int row = 8 * t + 2 * c + r;
-          if (row >= base && row < base + kPass && row < rows) {
+          if (row >= base && row < here) {
+            float* to = sums + (warp * pass + row - base) * kPitch<C8>;
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-              *reinterpret_cast<float2*>(&sm.o[warp][row - base][out_dim<C8>(g, j, 0)]) = make_float2(st.o[j][t][r], st.o[j][t][2 + r]);
+            for (int j = 0; j < 8; ++j) *reinterpret_cast<float2*>(to + place_of<C8>(out_dim<C8>(g, j, 0))) = make_float2(st.o[j][t][r], st.o[j][t][2 + r]);
           }
         }
       __syncthreads();
 #pragma unroll 1
-      for (int row = base + tid / kD; row < min(rows, base + kPass); row += kW * 32 / kD) {
-        float m = sm.m[0][row];
+      for (int i = tid; i < (here - base) * kD; i += 32 * kW) {  // a thread a dim
+        const int row = base + i / kD, dim = i & (kD - 1);
+        const float* from = sums + (row - base) * kPitch<C8> + place_of<C8>(dim);
+        float o = 0.f;
 #pragma unroll
-        for (int w = 1; w < kW; ++w) m = fmaxf(m, sm.m[w][row]);
-        float l = 0.f, o = 0.f;
-#pragma unroll
-        for (int w = 0; w < kW; ++w) {
-          const float a = weight_of(sm.m[w][row], m);
-          l += a * sm.l[w][row];
-          o += a * sm.o[w][row - base][dim];
-        }
+        for (int w = 0; w < kW; ++w) o += sm.weight[w][row] * from[w * pass * kPitch<C8>];
+        const float m = sm.top[row], l = sm.total[row];
         const int head = it.kvh * G + it.row0 + row;
         if (it.of > 1) {
           __stcg(slot + row * kD + dim, o);
