@@ -26,14 +26,15 @@ constexpr int kCtas = 8;
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kPerThread = kMaxSequences / kThreads;  // requests
+constexpr int kAtOnce = 8;                           // entries of a table's row that a lane loads at once
 
 enum : int { kStatusOom = 3 };
 
 struct TableShared {
-  int n[kMaxSequences];     // rows of a request before its new tokens
-  int add[kMaxSequences];   // new tokens, 0: none or not possible
-  int last[kMaxSequences];  // its last page, if new tokens go into it, else -1
-  long long end[kMaxSequences];  // pages that it and the requests before it need
+  __align__(16) int last[kMaxSequences];  // a request's last page, if new tokens go into it, else -1
+  int n[kMaxSequences];                   // its rows before its new tokens
+  int add[kMaxSequences];                 // new tokens, 0: none or not possible
+  long long end[kMaxSequences];           // pages that it and the requests before it need
   unsigned char copies[kMaxSequences];
   int nth[kMaxSequences];  // copies of the requests before
   long long scan[kWarps];
@@ -42,24 +43,6 @@ struct TableShared {
 };
 
 // sum over the threads before this one; `total`: of all
-__device__ __forceinline__ long long scan_before(long long x, long long* warps, long long& total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  long long sum = x;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long up = __shfl_up_sync(0xffffffffu, sum, o);
-    if (lane >= o) sum += up;
-  }
-  __syncthreads();
-  if (lane == 31) warps[warp] = sum;
-  __syncthreads();
-  total = 0;
-  for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) sum += warps[w];
-    total += warps[w];
-  }
-  return sum - x;
-}
 __device__ __forceinline__ int scan_before(int x, int* warps, int& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int sum = x;
@@ -112,48 +95,20 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) step_k
   if (a.refs_out != a.refs) {
     for (int i = thread; i < a.n_pages; i += kAllThreads) a.refs_out[i] = a.refs[i];
   }
-  cluster.sync();
-  // ---- rows of the table, and the holders of their pages: a request that goes on from itself changes none
+  // ---- every request's rows, new tokens and last page; every CTA for itself
   auto source = [&](int i) { return a.source != nullptr ? a.source[i] : i; };
-  for (int i = warp; i < a.B; i += kAllWarps) {
-    const int src = source(i);
-    const bool fine = src >= -1 && src < a.B_in;
-    const int n = fine && src >= 0 ? rows_at(a.lengths, src, a.width, a.shift) : 0;
-    if ((!fine || n < 0) && lane == 0) set_status(a.status, kStatusDeviceArg);
-    const int had = n > 0 ? pages_for(n, a.shift) : 0;
-    if (!moved && src == i) continue;
-    const int32_t* from = a.table + static_cast<long long>(src) * a.width;
-    int32_t* to = a.table_out + static_cast<long long>(i) * a.width;
-    for (int j = lane; j < a.width; j += 32) {
-      const int page = j < had ? from[j] : -1;
-      to[j] = page;
-      if (src != i && j < had) {
-        if (page >= 0 && page < a.n_pages) atomicAdd(a.refs_out + page, 1);
-        else set_status(a.status, kStatusDeviceArg);
-      }
-    }
-  }
-  for (int i = warp; i < a.B_in; i += kAllWarps) {
-    if (i < a.B && source(i) == i) continue;
-    const int n = rows_at(a.lengths, i, a.width, a.shift);
-    if (n < 0 && lane == 0) set_status(a.status, kStatusDeviceArg);
-    const int had = n > 0 ? pages_for(n, a.shift) : 0;
-    for (int j = lane; j < had; j += 32) {
-      const int page = a.table[static_cast<long long>(i) * a.width + j];
-      if (page >= 0 && page < a.n_pages) atomicSub(a.refs_out + page, 1);
-      else set_status(a.status, kStatusDeviceArg);
-    }
-  }
-  cluster.sync();
-  // ---- what each request needs; every CTA for itself
   for (int i = tid; i < a.B; i += kThreads) {
     const int src = source(i);
-    int n = src >= 0 && src < a.B_in ? rows_at(a.lengths, src, a.width, a.shift) : 0;
-    long long add = 0;
     const long long t0 = a.new_offsets[i], t1 = a.new_offsets[i + 1];
+    const bool known = src >= -1 && src < a.B_in;
+    int n = known && src >= 0 ? rows_at(a.lengths, src, a.width, a.shift) : 0;
     bool fine = t0 >= 0 && t1 >= t0 && t1 <= a.new_rows;
-    if (n < 0 || src < -1 || src >= a.B_in) n = 0;  // reported above
-    else if (fine) add = t1 - t0;
+    long long add = fine ? t1 - t0 : 0;
+    if (!known || n < 0) {  // comes out empty
+      n = 0;
+      add = 0;
+      fine = false;
+    }
     if (n + add > static_cast<long long>(a.width) << a.shift || n + add > 0x7fffffffll - 64) {
       add = 0;
       fine = false;
@@ -172,7 +127,58 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) step_k
     sm.add[i] = static_cast<int>(add);
     sm.last[i] = last;
   }
-  __syncthreads();
+  for (int i = a.B + tid; i < ((a.B + 3) & ~3); i += kThreads) sm.last[i] = -1;
+  cluster.sync();
+  // ---- rows of the table, and the holders of their pages: a warp a new or an old row; a request that goes on from itself changes none
+  for (int w = warp; w < a.B + a.B_in; w += kAllWarps) {
+    if (w < a.B) {
+      const int src = source(w);
+      if (!moved && src == w) continue;
+      const int had = pages_for(sm.n[w], a.shift);
+      const int32_t* from = a.table + static_cast<long long>(src) * a.width;  // not read where had is 0
+      int32_t* to = a.table_out + static_cast<long long>(w) * a.width;
+      for (int j0 = lane; j0 < a.width; j0 += 32 * kAtOnce) {
+        int page[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) page[u] = j0 + 32 * u < had ? from[j0 + 32 * u] : -1;
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          const int j = j0 + 32 * u;
+          if (j < a.width) to[j] = page[u];
+          if (src != w && j < had) {
+            if (page[u] >= 0 && page[u] < a.n_pages) atomicAdd(a.refs_out + page[u], 1);
+            else set_status(a.status, kStatusDeviceArg);
+          }
+        }
+      }
+    } else {
+      const int i = w - a.B;
+      if (i < a.B && source(i) == i) continue;
+      const int n = rows_at(a.lengths, i, a.width, a.shift);
+      if (n < 0 && lane == 0) set_status(a.status, kStatusDeviceArg);
+      const int had = n > 0 ? pages_for(n, a.shift) : 0;
+      const int32_t* from = a.table + static_cast<long long>(i) * a.width;
+      for (int j0 = lane; j0 < had; j0 += 32 * kAtOnce) {
+        int page[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) page[u] = j0 + 32 * u < had ? from[j0 + 32 * u] : 0;
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+          if (j0 + 32 * u < had) {
+            if (page[u] >= 0 && page[u] < a.n_pages) atomicSub(a.refs_out + page[u], 1);
+            else set_status(a.status, kStatusDeviceArg);
+          }
+      }
+    }
+  }
+  cluster.sync();
+  // ---- what each request needs, and the free pages of this CTA's part
+  int first, last_page;
+  part_of(a.n_pages, rank, first, last_page);
+  int free_pages = 0;
+  for (int i = first + 4 * tid; i < last_page; i += 4 * kThreads)  // parts begin at multiples of 4
+#pragma unroll
+    for (int j = 0; j < 4; ++j) free_pages += i + j < last_page && __ldcg(a.refs_out + i + j) <= 0;
   long long need[kPerThread], mine = 0;
   int copy[kPerThread], my_copies = 0;
   const int per = (a.B + kThreads - 1) / kThreads;  // requests of a thread, one behind another
@@ -185,11 +191,11 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) step_k
       const int last = sm.last[i], held = last >= 0 ? __ldcg(a.refs_out + last) : 0;
       if (held > 1) {  // of all that write into it the last one keeps it, if nobody else holds it
         int writers = 0, behind = 0;
-        for (int x = 0; x < a.B; ++x)
-          if (sm.last[x] == last) {
-            ++writers;
-            behind = x;
-          }
+        for (int x = 0; x < a.B; x += 4) {
+          const int4 other = *reinterpret_cast<const int4*>(&sm.last[x]);
+          writers += (other.x == last) + (other.y == last) + (other.z == last) + (other.w == last);
+          behind = other.w == last ? x + 3 : other.z == last ? x + 2 : other.y == last ? x + 1 : other.x == last ? x : behind;
+        }
         copy[u] = !(held == writers && i == behind);
       }
       if (sm.add[i] > 0) need[u] = pages_for(static_cast<long long>(sm.n[i]) + sm.add[i], a.shift) - (pages_for(sm.n[i], a.shift) - copy[u]);
@@ -197,10 +203,31 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) step_k
       my_copies += copy[u];
     }
   }
-  long long total;
-  int total_copies;
-  long long before = scan_before(mine, sm.scan, total);
-  int copies_before = scan_before(my_copies, sm.scan2, total_copies);
+  // sums over the threads before: pages in the upper bits, at most 1024 copies below
+  long long packed = mine << 11 | my_copies;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long up = __shfl_up_sync(0xffffffffu, packed, o);
+    if (lane >= o) packed += up;
+  }
+  free_pages = __reduce_add_sync(0xffffffffu, free_pages);
+  if (lane == 31) {
+    sm.scan[tid >> 5] = packed;
+    sm.scan2[tid >> 5] = free_pages;
+  }
+  __syncthreads();
+  long long all = 0;
+  int in_part = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < (tid >> 5)) packed += sm.scan[w];
+    all += sm.scan[w];
+    in_part += sm.scan2[w];
+  }
+  const long long total = all >> 11;
+  const int total_copies = static_cast<int>(all & 2047);
+  long long before = (packed >> 11) - mine;
+  int copies_before = static_cast<int>(packed & 2047) - my_copies;
 #pragma unroll
   for (int u = 0; u < kPerThread; ++u) {
     const int i = tid * per + u;
@@ -212,13 +239,6 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) step_k
       copies_before += copy[u];
     }
   }
-  // ---- the free pages before this CTA's, and all of them
-  int first, last_page;
-  part_of(a.n_pages, rank, first, last_page);
-  int free_pages = 0;
-  for (int i = first + tid; i < last_page; i += kThreads) free_pages += __ldcg(a.refs_out + i) <= 0;
-  int in_part;
-  scan_before(free_pages, sm.scan2, in_part);
   tell(cluster, sm.counts[0], rank, in_part);
   long long all_free = 0, nth_free = 0;
   for (int r = 0; r < kCtas; ++r) {
@@ -254,33 +274,35 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) step_k
       a.pairs[2 * sm.nth[lo] + 1] = page;
     }
   }
-  // ---- lengths, rows in pages that are there already
-  if (rank == 0) {
-    int copied = 0;
-    for (int i = tid; i < a.B; i += kThreads) {
-      const bool grown = grows(i);
-      const int n = sm.n[i], add = sm.add[i];
-      const long long t0 = a.new_offsets[i], t1 = a.new_offsets[i + 1];
-      a.lengths_out[i] = n + (grown ? add : 0);
-      if (!grown) set_status(a.status, kStatusOom);
-      if (!grown || add == 0) {
-        for (long long t = max(t0, 0ll); t < min(t1, a.new_rows); ++t) a.rows[t] = -1;
-      } else if (sm.last[i] >= 0) {
-        if (sm.copies[i]) {
-          atomicSub(a.refs_out + sm.last[i], 1);
-          ++copied;
-        } else {
-          const int col = n >> a.shift;
-          const long long end = min(static_cast<long long>(n) + add, static_cast<long long>(col + 1) << a.shift);
-          for (long long x = n; x < end; ++x)
-            a.rows[t0 + x - n] = (static_cast<long long>(sm.last[i]) << a.shift) + (x - (static_cast<long long>(col) << a.shift));
-        }
+  // ---- lengths, rows in pages that are there already; one CTA
+  if (rank != kCtas - 1) return;
+  int copied = 0;
+  for (int i = tid; i < a.B; i += kThreads) {
+    const bool grown = grows(i);
+    const int n = sm.n[i], add = sm.add[i];
+    const long long t0 = a.new_offsets[i], t1 = a.new_offsets[i + 1];
+    a.lengths_out[i] = n + (grown ? add : 0);
+    if (!grown) set_status(a.status, kStatusOom);
+    if (!grown || add == 0) {
+      for (long long t = max(t0, 0ll); t < min(t1, a.new_rows); ++t) a.rows[t] = -1;
+    } else if (sm.last[i] >= 0) {
+      if (sm.copies[i]) {
+        atomicSub(a.refs_out + sm.last[i], 1);
+        ++copied;
+      } else {
+        const int col = n >> a.shift;
+        const long long end = min(static_cast<long long>(n) + add, static_cast<long long>(col + 1) << a.shift);
+        for (long long x = n; x < end; ++x)
+          a.rows[t0 + x - n] = (static_cast<long long>(sm.last[i]) << a.shift) + (x - (static_cast<long long>(col) << a.shift));
       }
     }
-    int all_copied;
-    scan_before(copied, sm.scan2, all_copied);
-    if (tid == 0) *a.n_pairs = all_copied;
   }
+  if (total > all_free) {  // not all of them
+    scan_before(copied, sm.scan2, copied);
+  } else {
+    copied = total_copies;
+  }
+  if (tid == 0) *a.n_pairs = copied;
 }
 
 __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) compact_kernel(const CompactArgs a) {
