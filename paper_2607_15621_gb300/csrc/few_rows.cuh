@@ -87,9 +87,10 @@ __device__ __forceinline__ uint2 zero_rows(const unsigned char* v) {
 }
 
 // Scores s[nt][key half * 2 + row] of 16 keys -> weights into the state, P^T packed for O^T. BF: type of the weights.
-// C8: vs are the scales of values of keys g, g + 8, `v` their rows.
-template <bool BF, bool C8, int NT>
-__device__ __forceinline__ void softmax_step(State<NT>& st, float (&s)[NT][4], float (&vs)[2], const unsigned char* v, uint32_t (&pt)[NT][2]) {
+// C8: vs are the scales of values of keys g, g + 8, `v` their rows. SPLIT: pt[nt][2 ..] is what rounding took off the weights,
+// itself in that type, for a second product (cache_step: if `second`).
+template <bool BF, bool C8, int NT, bool SPLIT = false>
+__device__ __forceinline__ void softmax_step(State<NT>& st, float (&s)[NT][4], float (&vs)[2], const unsigned char* v, uint32_t (&pt)[NT][SPLIT ? 4 : 2]) {
   float w[NT][4], p[NT][4];
   auto weigh = [&](int t, int e) {
     const int r = e & 1;
@@ -152,14 +153,20 @@ __device__ __forceinline__ void softmax_step(State<NT>& st, float (&s)[NT][4], f
       if (!C8) weigh(t, e);
       st.l[t][e & 1] += w[t][e];
     }
-    pt[t][0] = transpose8x8(pack16<BF>(p[t][0], p[t][1]));
-    pt[t][1] = transpose8x8(pack16<BF>(p[t][2], p[t][3]));
+    const uint32_t first = pack16<BF>(p[t][0], p[t][1]), second = pack16<BF>(p[t][2], p[t][3]);
+    pt[t][0] = transpose8x8(first);
+    pt[t][1] = transpose8x8(second);
+    if (SPLIT) {
+      const float2 x = unpack16<BF>(first), y = unpack16<BF>(second);
+      pt[t][SPLIT ? 2 : 0] = transpose8x8(pack16<BF>(p[t][0] - x.x, p[t][1] - x.y));
+      pt[t][SPLIT ? 3 : 1] = transpose8x8(pack16<BF>(p[t][2] - y.x, p[t][3] - y.y));
+    }
   }
 }
 
-template <bool BF, bool C8, int NT>
+template <bool BF, bool C8, int NT, bool SPLIT = false>
 __device__ __forceinline__ void cache_step(State<NT>& st, const unsigned char* x, const uint32_t (&q)[NT][8][2],
-                                           const float (&f)[NT][2], int left) {
+                                           const float (&f)[NT][2], int left, bool second = true) {
   using S = Stage<C8>;
   constexpr bool kBf = BF && !C8;
   const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
@@ -209,8 +216,8 @@ __device__ __forceinline__ void cache_step(State<NT>& st, const unsigned char* x
         const float y = s[t][2 * h + r] * (C8 ? f[t][r] * ks[h] : kScaleLog2);
         s[t][2 * h + r] = g + 8 * h < left ? y : -CUDART_INF_F;
       }
-  uint32_t pt[NT][2];
-  softmax_step<kBf, C8, NT>(st, s, vs, x + S::kOffV, pt);
+  uint32_t pt[NT][SPLIT ? 4 : 2];
+  softmax_step<kBf, C8, NT, SPLIT>(st, s, vs, x + S::kOffV, pt);
   uint4 xv[4][S::kV];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -228,7 +235,10 @@ __device__ __forceinline__ void cache_step(State<NT>& st, const unsigned char* x
     const uint32_t a0 = __byte_perm(h[0], h[1], 0x5410), a1 = __byte_perm(h[0], h[1], 0x7632);
     const uint32_t a2 = __byte_perm(h[2], h[3], 0x5410), a3 = __byte_perm(h[2], h[3], 0x7632);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) mma<kBf>(st.o[j][t], a0, a1, a2, a3, pt[t][0], pt[t][1]);
+    for (int t = 0; t < NT; ++t) {
+      mma<kBf>(st.o[j][t], a0, a1, a2, a3, pt[t][0], pt[t][1]);
+      if (SPLIT && second) mma<kBf>(st.o[j][t], a0, a1, a2, a3, pt[t][SPLIT ? 2 : 0], pt[t][SPLIT ? 3 : 1]);
+    }
   }
 }
 

@@ -464,28 +464,45 @@ __global__ void __launch_bounds__(32 * Shape<C8, NT, LINE>::kWarps, Shape<C8, NT
     State<NT> st;
     float f[NT][2];
     make_queries<BF, C8, NT>(qf, f);
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      st.m[t][0] = st.m[t][1] = -CUDART_INF_F;
-      st.l[t][0] = st.l[t][1] = 0.f;
-      st.k[t][0] = st.k[t][1] = power_of(kMostPower);
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) st.o[j][t][e] = 0.f;
-    }
-    int slot_out = 0;
-    const int steps = count;
+    // Weights over a 16-bit cache go into the product in two parts of that type. An infinity among the values times a second part of
+    // zero or less is none any more: sums that are not finite are made again from the first parts alone.
+    bool second = !C8;
 #pragma unroll 1
-    for (int n = 0; n < steps; ++n) {
-      cp_async_wait<kStages - 2>();
-      __syncwarp();  // every lane's copies of the stage; and the stage before is read
-      const int left = sm.left[warp][slot_out];
-      copy_next(it);
-      if (left > 0) cache_step<BF, C8, NT>(st, sm.ring[warp] + slot_out * S::kBytes, qf, f, left);
-      slot_out = slot_out + 1 == kStages ? 0 : slot_out + 1;
+    for (;;) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        st.m[t][0] = st.m[t][1] = -CUDART_INF_F;
+        st.l[t][0] = st.l[t][1] = 0.f;
+        st.k[t][0] = st.k[t][1] = power_of(kMostPower);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) st.o[j][t][e] = 0.f;
+      }
+      int slot_out = 0;
+      const int steps = count;
+#pragma unroll 1
+      for (int n = 0; n < steps; ++n) {
+        cp_async_wait<kStages - 2>();
+        __syncwarp();  // every lane's copies of the stage; and the stage before is read
+        const int left = sm.left[warp][slot_out];
+        copy_next(it);
+        if (left > 0) cache_step<BF, C8, NT, !C8>(st, sm.ring[warp] + slot_out * S::kBytes, qf, f, left, second);
+        slot_out = slot_out + 1 == kStages ? 0 : slot_out + 1;
+      }
+      cp_async_wait<0>();
+      if (C8 || !second) break;
+      bool wild = false;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) wild = wild || !(fabsf(st.o[j][t][e]) < CUDART_INF_F);
+      if (!__any_sync(0xffffffffu, wild)) break;
+      second = false;
+      begin(it);
     }
-    cp_async_wait<0>();
     if (__any_sync(0xffffffffu, bad) && lane == 0) sm.bad = 1;
     if (C8) {  // the sums without k
 #pragma unroll
