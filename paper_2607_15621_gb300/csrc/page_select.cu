@@ -355,7 +355,7 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 // A cluster a request and kv head: its CTAs score a part of the pages each and store the keys in the first CTA's shared
 // memory, which then finds the border alone, by digits of 11 bits counted from the lowest key, and writes the pages above it.
 template <bool BF>
-__global__ void __launch_bounds__(kSelectThreads) select_kernel(const SelectArgs a) {
+__global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const SelectArgs a) {
   extern __shared__ __align__(16) unsigned char raw_smem[];
   cg::cluster_group cluster = cg::this_cluster();
   const int split = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
