@@ -694,7 +694,7 @@ fsx_status fsx_pages_compact(const int32_t* d_table, const int64_t* d_lengths, c
  * 4 * cache_rows; bounds page_bytes = 256 * n_kv_heads and one segment, their scales page_bytes 4 and n_kv_heads segments.
  * Page p of segment s begins at base + s * segment_stride + p * page_bytes.
  *   planes     : HOST [n_planes], 1 .. 512. Bytes are multiples of 4, bases 4-byte aligned (16 for speed).
- *   d_pairs    : DEVICE int32 [max_pairs, 2]; pages that are copied to are distinct and none that is copied from.
+ *   d_pairs    : DEVICE int32 [max_pairs, 2], 8-byte aligned; pages that are copied to are distinct and none that is copied from.
  * A pair outside 0 .. n_pages-1 sets FSX_ERR_DEVICE_ARG and is left out; so does a count outside 0 .. max_pairs, and nothing is
  * copied. */
 typedef struct {

@@ -401,30 +401,62 @@ constexpr int kUnit = 16384;  // bytes that a CTA moves at a time
 struct CopyPlane {
   unsigned char* base;
   long long page_bytes, stride;
-  int segments, units;  // units of a segment
+  int segments, units;  // units of a segment; with `together` > 1 of all of them
+  int together;         // segments of a unit: short ones go many at a time
   int first;            // units of the planes before, of one page
 };
+// `segs` segments of `bytes` each, `stride` apart, from one page to another
+template <typename T>
+__device__ __forceinline__ void copy_segments(unsigned char* base, long long stride, long long from, long long to, int segs, int bytes) {
+  constexpr int kAhead = 4;
+  const uint32_t each = static_cast<uint32_t>(bytes) / sizeof(T), all = each * segs;
+  for (uint32_t i0 = threadIdx.x; i0 < all; i0 += kCopyThreads * kAhead) {
+    T x[kAhead];
+    unsigned char* at[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const uint32_t i = i0 + u * kCopyThreads, seg = i / each;
+      at[u] = base + seg * stride + static_cast<long long>(i - seg * each) * sizeof(T);
+      if (i < all) x[u] = *reinterpret_cast<const T*>(at[u] + from);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (i0 + u * kCopyThreads < all) *reinterpret_cast<T*>(at[u] + to) = x[u];
+  }
+}
+
+// PLANES: room in the kernel's parameters, 2.6 or 20 KB
+template <int PLANES>
 struct CopyArgs {
   const int32_t* pairs;
   const int32_t* n_pairs;
   int max_pairs, n_pages, n_planes, units;  // units of one page over all planes
   int* status;
-  CopyPlane planes[kMaxPlanes];
+  CopyPlane planes[PLANES];
 };
 
-__global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ CopyArgs a) {
+template <int PLANES>
+__global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ CopyArgs<PLANES> a) {
   const int tid = threadIdx.x;
   pdl_launch_dependents();
   pdl_wait();
+  // the first pair is read beside the count: there are max_pairs of them in memory
+  const long long most = static_cast<long long>(a.max_pairs) * a.units;
+  long long w = blockIdx.x;
+  int pair = static_cast<int>(w / a.units);
+  int2 ends = w < most ? __ldg(reinterpret_cast<const int2*>(a.pairs) + pair) : make_int2(0, 0);
   int n = *a.n_pairs;
   if (n < 0 || n > a.max_pairs) {
     if (blockIdx.x == 0 && tid == 0) set_status(a.status, kStatusDeviceArg);
     n = 0;
   }
   const long long total = static_cast<long long>(n) * a.units;
-  for (long long w = blockIdx.x; w < total; w += gridDim.x) {
-    const int pair = static_cast<int>(w / a.units), unit = static_cast<int>(w - static_cast<long long>(pair) * a.units);
-    const int src = __ldg(a.pairs + 2 * pair), dst = __ldg(a.pairs + 2 * pair + 1);
+  for (; w < total; w += gridDim.x) {
+    const int unit = static_cast<int>(w - static_cast<long long>(pair) * a.units), src = ends.x, dst = ends.y;
+    if (w + gridDim.x < total) {
+      pair = static_cast<int>((w + gridDim.x) / a.units);
+      ends = __ldg(reinterpret_cast<const int2*>(a.pairs) + pair);
+    }
     if (src < 0 || src >= a.n_pages || dst < 0 || dst >= a.n_pages) {
       if (tid == 0) set_status(a.status, kStatusDeviceArg);
       continue;
@@ -436,7 +468,18 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constan
       else hi = mid - 1;
     }
     const CopyPlane& p = a.planes[lo];
-    const int in_plane = unit - p.first, segment = in_plane / p.units;
+    const int in_plane = unit - p.first;
+    if (p.together > 1) {
+      const int seg0 = in_plane * p.together, segs = min(p.together, p.segments - seg0);
+      unsigned char* const base = p.base + seg0 * p.stride;
+      const long long from = src * p.page_bytes, to = dst * p.page_bytes;
+      if (((reinterpret_cast<uintptr_t>(p.base) | static_cast<uintptr_t>(p.stride) | static_cast<uintptr_t>(p.page_bytes)) & 15u) == 0)
+        copy_segments<uint4>(base, p.stride, from, to, segs, static_cast<int>(p.page_bytes));
+      else
+        copy_segments<uint32_t>(base, p.stride, from, to, segs, static_cast<int>(p.page_bytes));
+      continue;
+    }
+    const int segment = in_plane / p.units;
     const long long at = static_cast<long long>(in_plane - segment * p.units) * kUnit;
     const long long bytes = min(static_cast<long long>(kUnit), p.page_bytes - at);
     const unsigned char* from = p.base + segment * p.stride + src * p.page_bytes + at;
@@ -473,9 +516,10 @@ cudaError_t launch_pages_compact(const CompactArgs& a, cudaStream_t stream) {
   return launch_ex(reinterpret_cast<const void*>(&compact_kernel), dim3(kCtas), dim3(kThreads), 0, stream, true, args);
 }
 
-cudaError_t launch_pages_copy(const fsx_page_plane* planes, int n_planes, int n_pages, const int32_t* pairs,
-                              const int32_t* n_pairs, int max_pairs, int* status, cudaStream_t stream) {
-  CopyArgs a;
+template <int PLANES>
+static cudaError_t copy_with(const fsx_page_plane* planes, int n_planes, int n_pages, const int32_t* pairs, const int32_t* n_pairs, int max_pairs,
+                             int* status, cudaStream_t stream) {
+  CopyArgs<PLANES> a;
   a.pairs = pairs;
   a.n_pairs = n_pairs;
   a.max_pairs = max_pairs;
@@ -484,10 +528,12 @@ cudaError_t launch_pages_copy(const fsx_page_plane* planes, int n_planes, int n_
   a.status = status;
   long long units = 0;
   for (int i = 0; i < n_planes; ++i) {
-    const long long each = (planes[i].page_bytes + kUnit - 1) / kUnit;
-    a.planes[i] = CopyPlane{static_cast<unsigned char*>(planes[i].base), planes[i].page_bytes, planes[i].segment_stride,
-                            planes[i].segments, static_cast<int>(each), static_cast<int>(units)};
-    units += each * planes[i].segments;
+    const long long bytes = planes[i].page_bytes, segments = planes[i].segments;
+    const long long together = bytes * 2 <= kUnit && segments > 1 ? (kUnit / bytes < segments ? kUnit / bytes : segments) : 1;
+    const long long each = together > 1 ? (segments + together - 1) / together : (bytes + kUnit - 1) / kUnit;
+    a.planes[i] = CopyPlane{static_cast<unsigned char*>(planes[i].base), bytes, planes[i].segment_stride, static_cast<int>(segments),
+                            static_cast<int>(each), static_cast<int>(together), static_cast<int>(units)};
+    units += together > 1 ? each : each * segments;
     if (units > 0x3fffffffll) return cudaErrorInvalidValue;
   }
   a.units = static_cast<int>(units);
@@ -495,8 +541,14 @@ cudaError_t launch_pages_copy(const fsx_page_plane* planes, int n_planes, int n_
   if (sms == 0) return cudaErrorNoDevice;
   const long long most = units * max_pairs, want = static_cast<long long>(sms) * 8;
   void* args[] = {&a};
-  return launch_ex(reinterpret_cast<const void*>(&copy_kernel), dim3(static_cast<unsigned>(most < want ? most : want)), dim3(kCopyThreads), 0, stream,
-                   true, args);
+  return launch_ex(reinterpret_cast<const void*>(&copy_kernel<PLANES>), dim3(static_cast<unsigned>(most < want ? most : want)), dim3(kCopyThreads), 0,
+                   stream, true, args);
+}
+
+cudaError_t launch_pages_copy(const fsx_page_plane* planes, int n_planes, int n_pages, const int32_t* pairs,
+                              const int32_t* n_pairs, int max_pairs, int* status, cudaStream_t stream) {
+  return n_planes <= 64 ? copy_with<64>(planes, n_planes, n_pages, pairs, n_pairs, max_pairs, status, stream)
+                        : copy_with<kMaxPlanes>(planes, n_planes, n_pages, pairs, n_pairs, max_pairs, status, stream);
 }
 
 }  // namespace fsx

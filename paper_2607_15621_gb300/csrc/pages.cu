@@ -345,6 +345,7 @@ fsx_status fsx_pages_copy(const fsx_page_plane* planes, int n_planes, int n_page
                           int max_pairs, int* d_status, void* stream) {
   fsx::set_error_message("");
   if (!planes || !d_n_pairs || !d_status || (max_pairs > 0 && !d_pairs)) return fail(FSX_ERR_INVALID_ARG, "NULL pointer argument");
+  if (!aligned(d_pairs, 8)) return fail(FSX_ERR_INVALID_ARG, "d_pairs must be 8-byte aligned");
   if (n_planes < 1 || n_planes > fsx::kMaxPlanes) return fail(FSX_ERR_INVALID_ARG, "n_planes must be in 1..512");
   if (n_pages < 1 || max_pairs < 0) return fail(FSX_ERR_INVALID_ARG, "n_pages must be positive and max_pairs >= 0");
   for (int i = 0; i < n_planes; ++i) {

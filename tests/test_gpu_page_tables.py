@@ -207,7 +207,7 @@ def test_compaction_reports_bad_entries():
     assert refs_out.tolist() == [1, 1, 1, 1, 0, 0, 0, 0] and pairs[:int(n)].tolist() == [[5, 1], [7, 2]]
 
 
-@pytest.mark.parametrize("page_rows,kv_heads,layers", [(16, 1, 1), (16, 8, 3), (64, 3, 2), (1024, 2, 1)])
+@pytest.mark.parametrize("page_rows,kv_heads,layers", [(16, 1, 1), (16, 8, 3), (64, 3, 2), (1024, 2, 1), (16, 300, 1), (512, 20, 1)])
 def test_copies_of_every_plane(page_rows, kv_heads, layers):
     n_pages, g = 21, torch.Generator(device="cuda").manual_seed(1)
     rows = n_pages * page_rows

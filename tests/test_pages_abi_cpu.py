@@ -126,7 +126,7 @@ def test_pages_compact_refuses(lib, over, code):
 
 @pytest.mark.parametrize("over,code", [
     (dict(planes=None), BAD), (dict(np=0), BAD), (dict(np=513), BAD), (dict(n=0), BAD), (dict(pairs=None), BAD), (dict(npairs=None), BAD),
-    (dict(mp=-1), BAD), (dict(status=None), BAD), (dict(planes=planes(base=None)), BAD), (dict(planes=planes(base=FAKE + 2)), BAD),
+    (dict(pairs=FAKE + 4), BAD), (dict(mp=-1), BAD), (dict(status=None), BAD), (dict(planes=planes(base=None)), BAD), (dict(planes=planes(base=FAKE + 2)), BAD),
     (dict(planes=planes(page_bytes=0)), BAD), (dict(planes=planes(page_bytes=6)), BAD), (dict(planes=planes(segments=0)), BAD),
     (dict(planes=planes(segments=2, stride=4096 * 20 - 4)), BAD), (dict(planes=planes(segments=2, stride=4096 * 20 + 2)), BAD),
 ])
