@@ -90,8 +90,8 @@ struct Ends {
       for (int i = 0; i < AHEAD; ++i) {
         const int r = r0 + i * step;  // rows behind the last: the page's first, once more
         const int take = r + sub < filled ? r : -sub;
-        x[i] = __ldg(reinterpret_cast<const uint4*>(src + take * row_bytes));
-        s[i] = kC8 ? __ldg(scales + take) : 1.f;
+        x[i] = *reinterpret_cast<const uint4*>(src + take * row_bytes);
+        s[i] = kC8 ? scales[take] : 1.f;
       }
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) {
@@ -174,8 +174,8 @@ __device__ __forceinline__ bool scan_plain(const unsigned char* src, const float
     for (int i = 0; i < AHEAD; ++i) {
       const int r = r0 + i * step;  // rows behind the last: the page's first, once more
       const int take = r + sub < filled ? r : -sub;
-      x[i] = __ldg(reinterpret_cast<const uint4*>(src + take * row_bytes));
-      s[i] = __float_as_uint(__ldg(scales + take));
+      x[i] = *reinterpret_cast<const uint4*>(src + take * row_bytes);
+      s[i] = __float_as_uint(scales[take]);
     }
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
@@ -253,11 +253,11 @@ __global__ void __launch_bounds__(32 * kBoundsWarps, TYPE == FSX_E4M3 ? 3 : 4) b
   bool wild = false, lost = false;
   const int32_t* const table = a.pages.table + static_cast<long long>(b) * a.pages.width + first;
   uint32_t u = blockIdx.x * (kBoundsWarps / SHARE) + (SHARE > 1 ? 0 : warp);
-  int ahead = u < units ? __ldg(table + u / a.n_kv_heads) : 0;
+  int ahead = u < units ? table[u / a.n_kv_heads] : 0;
   for (; u < units; u += stride) {
     const uint32_t nth = u / a.n_kv_heads;
     const int page = first + static_cast<int>(nth), kvh = static_cast<int>(u - nth * a.n_kv_heads), at = ahead;
-    if (u + stride < units) ahead = __ldg(table + (u + stride) / a.n_kv_heads);
+    if (u + stride < units) ahead = table[(u + stride) / a.n_kv_heads];
     if (at < 0 || at >= a.pages.n_pages) {
       lost = true;
       continue;  // the same for all of the unit's warps
@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const SelectA
   const int part = (pages + split - 1) / split, p0 = min(pages, rank * part), n = min(pages, p0 + part) - p0;
   bool lost = false;
   for (int i = tid; i < n; i += kSelectThreads) {  // where the pages are, in the keys' place
-    const int at = __ldg(a.pages.table + static_cast<long long>(b) * a.pages.width + p0 + i);
+    const int at = a.pages.table[static_cast<long long>(b) * a.pages.width + p0 + i];
     const bool there = at >= 0 && at < a.pages.n_pages;
     lost = lost || !there;
     keys[i] = there ? static_cast<uint32_t>(at) : 0xffffffffu;
@@ -391,7 +391,7 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const SelectA
   for (int h = warp; h < tiles * kHeadTile; h += kSelectWarps) {
     float x[4] = {0.f, 0.f, 0.f, 0.f}, top = 0.f;
     if (h < G) {
-      const uint2 w = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(a.q) + b * a.q_stride + (kvh * G + h) * kHeadDim) + lane);
+      const uint2 w = *(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(a.q) + b * a.q_stride + (kvh * G + h) * kHeadDim) + lane);
       const float2 u = unpack16<BF>(w.x), v = unpack16<BF>(w.y);
       x[0] = u.x, x[1] = u.y, x[2] = v.x, x[3] = v.y;
     }
@@ -433,8 +433,8 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const SelectA
       const long long page = at == 0xffffffffu ? 0 : at;
       const int4* src = reinterpret_cast<const int4*>(a.bounds + (page * a.n_kv_heads + kvh) * 256) + sub;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) x[t][u] = __ldg(src + 4 * u);
-      scale[t] = __ldg(a.bound_scale + static_cast<long long>(kvh) * a.pages.n_pages + page);
+      for (int u = 0; u < 4; ++u) x[t][u] = src[4 * u];
+      scale[t] = a.bound_scale[static_cast<long long>(kvh) * a.pages.n_pages + page];
       best[t] = -CUDART_INF_F;
     }
     for (int head = 0; head < tiles * kHeadTile; head += kHeadTile) {

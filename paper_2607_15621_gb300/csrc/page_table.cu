@@ -178,7 +178,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) step_k
   int free_pages = 0;
   for (int i = first + 4 * tid; i < last_page; i += 4 * kThreads)  // parts begin at multiples of 4
 #pragma unroll
-    for (int j = 0; j < 4; ++j) free_pages += i + j < last_page && __ldcg(a.refs_out + i + j) <= 0;
+    for (int j = 0; j < 4; ++j) free_pages += i + j < last_page && load_l2(a.refs_out + i + j) <= 0;
   long long need[kPerThread], mine = 0;
   int copy[kPerThread], my_copies = 0;
   const int per = (a.B + kThreads - 1) / kThreads;  // requests of a thread, one behind another
@@ -188,7 +188,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) step_k
     need[u] = 0;
     copy[u] = 0;
     if (u < per && i < a.B) {
-      const int last = sm.last[i], held = last >= 0 ? __ldcg(a.refs_out + last) : 0;
+      const int last = sm.last[i], held = last >= 0 ? load_l2(a.refs_out + last) : 0;
       if (held > 1) {  // of all that write into it the last one keeps it, if nobody else holds it
         int writers = 0, behind = 0;
         for (int x = 0; x < a.B; x += 4) {
@@ -251,7 +251,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) step_k
   const long long wanted = min(total, all_free);
   for (int base = first; base < last_page && nth_free < wanted; base += kThreads) {
     const int page = base + tid;
-    const bool is_free = page < last_page && __ldcg(a.refs_out + page) <= 0;
+    const bool is_free = page < last_page && load_l2(a.refs_out + page) <= 0;
     int in_tile;
     const long long nth = nth_free + scan_before(is_free ? 1 : 0, sm.scan2, in_tile);
     nth_free += in_tile;
@@ -330,7 +330,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) compac
   // ---- the i-th page in use at `used` or above goes to the i-th free one below: as many as those
   int moves = 0, room = 0;
   for (int i = first + tid; i < end; i += kThreads) {
-    const bool in_use = __ldcg(a.refs_out + i) > 0;
+    const bool in_use = load_l2(a.refs_out + i) > 0;
     moves += in_use && i >= used;
     room += !in_use && i < used;
   }
@@ -349,7 +349,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) compac
   }
   for (int base = first; base < end; base += kThreads) {
     const int i = base + tid;
-    const bool there = i < end, in_use = there && __ldcg(a.refs_out + i) > 0;
+    const bool there = i < end, in_use = there && load_l2(a.refs_out + i) > 0;
     const bool goes = in_use && i >= used, takes = there && !in_use && i < used;
     int in_tile;
     // a tile may hold both, in two runs: one scan for both, halves of a word
@@ -362,8 +362,8 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) compac
   cluster.sync();
   // ---- holders move; the old place keeps the new one for the tables, as -1 - page
   for (int i = thread; i < m; i += kAllThreads) {
-    const int src = __ldcg(a.pairs + 2 * i), dst = __ldcg(a.pairs + 2 * i + 1);
-    a.refs_out[dst] = __ldcg(a.refs_out + src);
+    const int src = load_l2(a.pairs + 2 * i), dst = load_l2(a.pairs + 2 * i + 1);
+    a.refs_out[dst] = load_l2(a.refs_out + src);
     a.refs_out[src] = -1 - dst;
   }
   cluster.sync();
@@ -379,7 +379,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) compac
       if (page < 0 || page >= a.n_pages) {
         set_status(a.status, kStatusDeviceArg);
       } else if (page >= used) {
-        const int r = __ldcg(a.refs_out + page);
+        const int r = load_l2(a.refs_out + page);
         if (r < 0) {
           page = -1 - r;
           changed = true;
@@ -389,7 +389,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) compac
     if (changed) a.table_out[e] = page;
   }
   cluster.sync();
-  for (int i = thread; i < m; i += kAllThreads) a.refs_out[__ldcg(a.pairs + 2 * i)] = 0;
+  for (int i = thread; i < m; i += kAllThreads) a.refs_out[load_l2(a.pairs + 2 * i)] = 0;
   if (thread == 0) *a.n_pairs = m;
 }
 
@@ -444,7 +444,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constan
   const long long most = static_cast<long long>(a.max_pairs) * a.units;
   long long w = blockIdx.x;
   int pair = static_cast<int>(w / a.units);
-  int2 ends = w < most ? __ldg(reinterpret_cast<const int2*>(a.pairs) + pair) : make_int2(0, 0);
+  int2 ends = w < most ? *(reinterpret_cast<const int2*>(a.pairs) + pair) : make_int2(0, 0);
   int n = *a.n_pairs;
   if (n < 0 || n > a.max_pairs) {
     if (blockIdx.x == 0 && tid == 0) set_status(a.status, kStatusDeviceArg);
@@ -455,7 +455,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constan
     const int unit = static_cast<int>(w - static_cast<long long>(pair) * a.units), src = ends.x, dst = ends.y;
     if (w + gridDim.x < total) {
       pair = static_cast<int>((w + gridDim.x) / a.units);
-      ends = __ldg(reinterpret_cast<const int2*>(a.pairs) + pair);
+      ends = *(reinterpret_cast<const int2*>(a.pairs) + pair);
     }
     if (src < 0 || src >= a.n_pages || dst < 0 || dst >= a.n_pages) {
       if (tid == 0) set_status(a.status, kStatusDeviceArg);

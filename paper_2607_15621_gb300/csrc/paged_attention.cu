@@ -303,7 +303,7 @@ __device__ __forceinline__ bool look_up(const PagedArgs& p, const Piece& it, int
   const int shift = p.pages.shift, in_page = step & ((1 << (shift - 4)) - 1);
   int page = step >> (shift - 4);
   if (p.picked != nullptr) {
-    page = __ldg(p.picked + (static_cast<long long>(it.b) * p.n_kv_heads + it.kvh) * p.n_picked + page);
+    page = p.picked[(static_cast<long long>(it.b) * p.n_kv_heads + it.kvh) * p.n_picked + page];
     if (page == -1) return true;
     if (page < 0 || page >= it.r.pages) return false;
   }
@@ -312,7 +312,7 @@ __device__ __forceinline__ bool look_up(const PagedArgs& p, const Piece& it, int
     left = 0;
     return true;
   }
-  const int at = __ldg(p.pages.table + static_cast<long long>(it.b) * p.pages.width + page);
+  const int at = p.pages.table[static_cast<long long>(it.b) * p.pages.width + page];
   if (at < 0 || at >= p.pages.n_pages) {
     left = 0;
     return false;
@@ -373,7 +373,7 @@ __device__ __forceinline__ void load_queries(uint32_t (&qf)[NT][8][2], const Pag
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const int d = C8 ? (k >> 2) * 64 + 16 * c + 4 * (k & 3) : 8 * (c + 4 * (k >> 1)) + 4 * (k & 1);
-      const uint2 w = there ? __ldg(reinterpret_cast<const uint2*>(q + row * kD + d)) : make_uint2(0u, 0u);
+      const uint2 w = there ? *reinterpret_cast<const uint2*>(q + row * kD + d) : make_uint2(0u, 0u);
       qf[t][k][0] = w.x;
       qf[t][k][1] = w.y;
     }
@@ -637,8 +637,8 @@ __global__ void __launch_bounds__(32 * Shape<C8, NT, LINE>::kWarps, Shape<C8, NT
 #pragma unroll
               for (int j = 0; j < kJoin; ++j) {
                 const float* other = slot_at<NT>(p, slot_of<LINE>(it, min(j0 + j * share, it.of - 1)));
-                x[j] = __ldcg(reinterpret_cast<const float2*>(other + kTile * kD) + row);
-                v[j] = __ldcg(reinterpret_cast<const float4*>(other + row * kD) + lane);
+                x[j] = load_l2(reinterpret_cast<const float2*>(other + kTile * kD) + row);
+                v[j] = load_l2(reinterpret_cast<const float4*>(other + row * kD) + lane);
               }
               float top = m;
 #pragma unroll

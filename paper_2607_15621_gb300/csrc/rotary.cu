@@ -111,14 +111,14 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant_
   for (int i = 0; i < kAhead; ++i) load(part * per + i, x[i]);
   long long at = -1;
   if (CACHE != kNoCache) {
-    const long long r = a.dst_rows != nullptr ? __ldg(reinterpret_cast<const long long*>(a.dst_rows) + row) : row;
+    const long long r = a.dst_rows != nullptr ? a.dst_rows[row] : row;
     if (r >= 0 && r < a.cache_rows) at = r;
     else if (lane == 0) set_status(a.status, kStatusDeviceArg);
   }
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int j = lane + 32 * h;
-    const uint64_t pos = static_cast<uint64_t>(__ldg(reinterpret_cast<const long long*>(a.positions) + a.axis[j] * a.rows + row));
+    const uint64_t pos = static_cast<uint64_t>(a.positions[a.axis[j] * a.rows + row]);
     float c, s;
     sincospif(static_cast<float>(static_cast<int32_t>((pos * a.turns[j]) >> 32)) * (1.f / 2147483648.f), &s, &c);
     turn[warp][j] = make_float2(c, s);
