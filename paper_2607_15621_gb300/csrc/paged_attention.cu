@@ -7,9 +7,10 @@
 // step's comes by a shuffle, so that no copy waits for the table.
 //
 // Items (request, tile of the group, kv head) are shared out in one of two ways:
-//   line   few items. One CTA a SM with 12 or 16 warps; all steps of all items in one line, cut into as many equal ranges as there are CTAs, so
-//          that every SM reads the same number of bytes; a cut less than 32 steps from an item's end moves there. A CTA's ranges put 12 or 16
-//          warps together in shared memory, so an item that is spread over the whole GPU has few partial results to join.
+//   line   few items. One CTA a SM with 8 warps and long rings; all steps of all items in one line, cut into as many equal ranges as there
+//          are CTAs, so that every SM reads the same number of bytes; a cut less than 16 steps from an item's end moves there. Little work
+//          goes in whole items or near-equal pieces of them, one a CTA. A CTA puts 8 warps together in shared memory, so an item that
+//          is spread over the whole GPU has few partial results to join.
 //   queue  many items. Four warps a CTA, three or four CTAs a SM, pieces of at most 28 chunks of 64 keys from one queue: SMs that
 //          read faster take more, and one CTA's end overlaps with the others' loads.
 // The pieces of a cut item are joined by the CTA that ends last, in the order of the keys. A piece that meets a page number
@@ -26,7 +27,7 @@ namespace fsx {
 namespace {
 
 constexpr int kFew = 8, kMany = 28;  // queue: chunks of an item that is not cut, and of a piece
-constexpr int kNear = 32, kWhole = 64, kShort = 128;  // line: steps
+constexpr int kLeast = 32, kSnap = 16, kWhole = 64, kShort = 128;  // line: steps
 constexpr int kHeader = 64;          // ints of the workspace, queue: [0] pieces taken, [1] CTAs that are done
 constexpr int kCounters = 8192;      // then one for each slot
 
@@ -220,7 +221,7 @@ __device__ __forceinline__ Line make_line(const PagedArgs& p, uint32_t items, vo
   const uint32_t ctas = gridDim.x, all_items = items * B;
   if (before < ctas * kShort && all_items <= ctas) {
     // little work: near-equal pieces of whole items, at most one a CTA, as many as there are CTAs for
-    const uint32_t most = max(static_cast<uint32_t>(kNear), (before + ctas - all_items) / max(1u, ctas - all_items));
+    const uint32_t most = max(static_cast<uint32_t>(kLeast), (before + ctas - all_items) / max(1u, ctas - all_items));
     uint32_t* first = line.cut + ctas + 1;  // [B + 1] pieces of the requests before
     if (warp == 0) {
       uint32_t sum = 0;
@@ -253,16 +254,16 @@ __device__ __forceinline__ Line make_line(const PagedArgs& p, uint32_t items, vo
     __syncthreads();
     return line;
   }
-  // equal ranges; a cut less than 32 steps from an item's end moves there
-  line.ranges = max(1u, min(ctas, before / kNear));
+  // equal ranges; a cut less than 16 steps from an item's end moves there
+  line.ranges = max(1u, min(ctas, before / kLeast));
   const uint32_t least = before / line.ranges, more = before - least * line.ranges;
   for (uint32_t c = tid; c <= line.ranges; c += kThreadsLine) {
-    uint32_t x = c * least + min(c, more);
+    uint32_t x = c * least + c * more / line.ranges;
     if (c < line.ranges && c > 0) {
       const int b = find(line.start, B, x);
       const uint32_t n = line_steps(request_of(p, line.len[b])), off = (x - line.start[b]) % n;
-      if (off < kNear) x -= off;
-      else if (n - off < kNear) x += n - off;
+      if (off < kSnap) x -= off;
+      else if (n - off < kSnap) x += n - off;
     }
     line.cut[c] = x;
   }
@@ -334,7 +335,8 @@ __device__ __forceinline__ int place_of(int d) {
 // Warps of a CTA, rows that they put together at a time
 template <bool C8, int NT, bool LINE>
 struct Shape {
-  static constexpr int kWarps = LINE ? 4 * Fit<C8, NT>::kCtas : fsx::kWarps;
+  static constexpr int kWarps = LINE ? 8 : fsx::kWarps;
+  static constexpr int kStages = LINE ? (C8 ? 6 : 3) : Fit<C8, NT>::kStages;
   static constexpr int kCtas = LINE ? 1 : Fit<C8, NT>::kCtas;
   static constexpr int kPass = LINE ? 2 : Fit<C8, NT>::kPass;
 };
@@ -342,11 +344,11 @@ template <bool C8, int NT, bool LINE>
 struct Shared {  // and the plan behind it
   static constexpr int kW = Shape<C8, NT, LINE>::kWarps;
   long long scratch[2 * kW];
-  __align__(128) unsigned char ring[kW][Fit<C8, NT>::kStages * Stage<C8>::kBytes];
+  __align__(128) unsigned char ring[kW][Shape<C8, NT, LINE>::kStages * Stage<C8>::kBytes];
   float m[kW][8 * NT], l[kW][8 * NT];  // of each warp
   float weight[kW][8 * NT], top[8 * NT], total[8 * NT];
   __align__(16) float o[kW][Shape<C8, NT, LINE>::kPass][kPitch<C8>];
-  int left[kW][4];  // keys of the ring's stages
+  int left[kW][8];  // keys of the ring's stages
   int bad;          // of the piece
   uint32_t next;
   int last;
@@ -384,7 +386,7 @@ template <bool BF, bool C8, int NT, bool LINE>
 __global__ void __launch_bounds__(32 * Shape<C8, NT, LINE>::kWarps, Shape<C8, NT, LINE>::kCtas) paged_kernel(const PagedArgs p) {
   using S = Stage<C8>;
   using Sm = Shared<C8, NT, LINE>;
-  constexpr int kStages = Fit<C8, NT>::kStages, kPass = Shape<C8, NT, LINE>::kPass, kW = Sm::kW;
+  constexpr int kStages = Shape<C8, NT, LINE>::kStages, kPass = Shape<C8, NT, LINE>::kPass, kW = Sm::kW;
   constexpr int kPerRow = S::kRow / 16;
   constexpr int kTile = 8 * NT;
   extern __shared__ __align__(128) unsigned char raw_smem[];
