@@ -521,6 +521,20 @@ __global__ void __launch_bounds__(32 * Shape<C8, NT, LINE>::kWarps, Shape<C8, NT
     }
 
     const int rows = min(kTile, G - it.row0);
+    // ---- the next piece's first copies go out before this one's results are put together
+    Piece next = it;
+    bool goes_on = false;
+    auto go_on = [&] {
+      load_queries<C8, NT>(qf, p, next, G);
+      begin(next);
+    };
+    if constexpr (LINE) {
+      goes_on = at < end;
+      if (goes_on) {
+        next = segment_at(p, line, kTile, end, at);
+        go_on();
+      }
+    }
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -534,21 +548,14 @@ __global__ void __launch_bounds__(32 * Shape<C8, NT, LINE>::kWarps, Shape<C8, NT
         }
       }
     __syncthreads();
-    // ---- the next piece's first copies go out before this one's results are put together
     const bool wrong = sm.bad != 0;
-    Piece next = it;
-    bool goes_on;
-    if constexpr (LINE) {
-      goes_on = at < end;
-      if (goes_on) next = segment_at(p, line, kTile, end, at);
-    } else {
+    if constexpr (!LINE) {
       i = sm.next;
       goes_on = i < total;
-      if (goes_on) next = piece_at(p, plan, kTile, i);
-    }
-    if (goes_on) {
-      load_queries<C8, NT>(qf, p, next, G);
-      begin(next);
+      if (goes_on) {
+        next = piece_at(p, plan, kTile, i);
+        go_on();
+      }
     }
     // ---- the warps' results: kPass rows at a time, or all of them where no copies are on their way into the rings
     auto lse_at = [&](int head) -> float& { return p.lse[static_cast<long long>(head) * p.pages.B + it.b]; };
