@@ -457,8 +457,8 @@ __global__ void __launch_bounds__(32 * Shape<C8, NT, LINE>::kWarps, Shape<C8, NT
   if (more) {
     if constexpr (LINE) it = segment_at(p, line, kTile, end, at);
     else it = piece_at(p, plan, kTile, i);
+    load_queries<C8, NT>(qf, p, it, G);  // in front of the cache's copies, which would keep them waiting
     begin(it);
-    load_queries<C8, NT>(qf, p, it, G);
   }
 #pragma unroll 1
   while (more) {
@@ -622,16 +622,16 @@ __global__ void __launch_bounds__(32 * Shape<C8, NT, LINE>::kWarps, Shape<C8, NT
       set_status(p.status, kStatusDeviceArg);
     }
     if (it.of > 1) {
-      __threadfence();
-      __syncthreads();
+      // the barrier behind the results, then one thread's fence for all of the CTA's
       if (tid == 0) {
         int* counter = header + kHeader + it.first;
+        __threadfence();
         sm.last = atomicAdd(counter, 1) == it.of - 1;
+        __threadfence();
         if (sm.last) *counter = 0;
       }
       __syncthreads();
       if (sm.last) {
-        __threadfence();
         // `share` warps a row, each every share-th piece; 4 dims a lane
         const int share = max(1, kW / rows), at_once = kW / share;
 #pragma unroll 1
