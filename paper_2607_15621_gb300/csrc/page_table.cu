@@ -397,6 +397,8 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) compac
 
 constexpr int kCopyThreads = 256;
 constexpr int kUnit = 16384;  // bytes that a CTA moves at a time
+constexpr int kSmall = 2048;  // bytes of a page in a plane, all segments, up to which a warp moves them, eight planes a CTA: 800 pages of
+// 8-bit rows of 8 heads with scales over 4 layers take 37 us, with a CTA a segment 151
 
 struct CopyPlane {
   unsigned char* base;
@@ -405,32 +407,41 @@ struct CopyPlane {
   int together;         // segments of a unit: short ones go many at a time
   int first;            // units of the planes before, of one page
 };
-// `segs` segments of `bytes` each, `stride` apart, from one page to another
-template <typename T>
+// `segs` segments of `bytes` each, `stride` apart, from one page to another, by THREADS threads
+template <int THREADS, typename T>
 __device__ __forceinline__ void copy_segments(unsigned char* base, long long stride, long long from, long long to, int segs, int bytes) {
-  constexpr int kAhead = 4;
   const uint32_t each = static_cast<uint32_t>(bytes) / sizeof(T), all = each * segs;
-  for (uint32_t i0 = threadIdx.x; i0 < all; i0 += kCopyThreads * kAhead) {
-    T x[kAhead];
-    unsigned char* at[kAhead];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const uint32_t i = i0 + u * kCopyThreads, seg = i / each;
-      at[u] = base + seg * stride + static_cast<long long>(i - seg * each) * sizeof(T);
-      if (i < all) x[u] = *reinterpret_cast<const T*>(at[u] + from);
-    }
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-      if (i0 + u * kCopyThreads < all) *reinterpret_cast<T*>(at[u] + to) = x[u];
+#pragma unroll 1
+  for (uint32_t i = threadIdx.x % THREADS; i < all; i += 2 * THREADS) {  // two at once: few registers, which the long copies need
+    const uint32_t j = i + THREADS, seg_i = i / each, seg_j = j / each;
+    unsigned char* const at_i = base + seg_i * stride + static_cast<long long>(i - seg_i * each) * sizeof(T);
+    unsigned char* const at_j = base + seg_j * stride + static_cast<long long>(j - seg_j * each) * sizeof(T);
+    const T x = *reinterpret_cast<const T*>(at_i + from);
+    T y;
+    if (j < all) y = *reinterpret_cast<const T*>(at_j + from);
+    *reinterpret_cast<T*>(at_i + to) = x;
+    if (j < all) *reinterpret_cast<T*>(at_j + to) = y;
   }
 }
 
-// PLANES: room in the kernel's parameters, 2.6 or 20 KB
+template <int THREADS>
+__device__ __forceinline__ void copy_some(const CopyPlane& p, int seg0, int segs, int src, int dst) {
+  unsigned char* const base = p.base + seg0 * p.stride;
+  const long long from = src * p.page_bytes, to = dst * p.page_bytes;
+  const int bytes = static_cast<int>(p.page_bytes);
+  if (((reinterpret_cast<uintptr_t>(p.base) | static_cast<uintptr_t>(p.segments > 1 ? p.stride : 0) | static_cast<uintptr_t>(bytes)) & 15u) == 0)
+    copy_segments<THREADS, uint4>(base, p.stride, from, to, segs, bytes);
+  else
+    copy_segments<THREADS, uint32_t>(base, p.stride, from, to, segs, bytes);
+}
+
+// PLANES: room in the kernel's parameters, 2.6 or 20 KB (2.4 or 2.9 us of the caller's time)
 template <int PLANES>
 struct CopyArgs {
   const int32_t* pairs;
   const int32_t* n_pairs;
   int max_pairs, n_pages, n_planes, units;  // units of one page over all planes
+  int n_large, large_units;                 // the planes whose pages are more than kSmall bytes come first
   int* status;
   CopyPlane planes[PLANES];
 };
@@ -461,7 +472,12 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constan
       if (tid == 0) set_status(a.status, kStatusDeviceArg);
       continue;
     }
-    int lo = 0, hi = a.n_planes - 1;  // the last plane that begins at `unit` or before
+    if (unit >= a.large_units) {
+      const int small = a.n_large + (unit - a.large_units) * (kCopyThreads / 32) + (tid >> 5);
+      if (small < a.n_planes) copy_some<32>(a.planes[small], 0, a.planes[small].segments, src, dst);
+      continue;
+    }
+    int lo = 0, hi = a.n_large - 1;  // the last plane that begins at `unit` or before
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
       if (a.planes[mid].first <= unit) lo = mid;
@@ -470,13 +486,8 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constan
     const CopyPlane& p = a.planes[lo];
     const int in_plane = unit - p.first;
     if (p.together > 1) {
-      const int seg0 = in_plane * p.together, segs = min(p.together, p.segments - seg0);
-      unsigned char* const base = p.base + seg0 * p.stride;
-      const long long from = src * p.page_bytes, to = dst * p.page_bytes;
-      if (((reinterpret_cast<uintptr_t>(p.base) | static_cast<uintptr_t>(p.stride) | static_cast<uintptr_t>(p.page_bytes)) & 15u) == 0)
-        copy_segments<uint4>(base, p.stride, from, to, segs, static_cast<int>(p.page_bytes));
-      else
-        copy_segments<uint32_t>(base, p.stride, from, to, segs, static_cast<int>(p.page_bytes));
+      const int seg0 = in_plane * p.together;
+      copy_some<kCopyThreads>(p, seg0, min(p.together, p.segments - seg0), src, dst);
       continue;
     }
     const int segment = in_plane / p.units;
@@ -527,15 +538,21 @@ static cudaError_t copy_with(const fsx_page_plane* planes, int n_planes, int n_p
   a.n_planes = n_planes;
   a.status = status;
   long long units = 0;
+  int large = 0, small = n_planes;
   for (int i = 0; i < n_planes; ++i) {
     const long long bytes = planes[i].page_bytes, segments = planes[i].segments;
+    const bool is_small = bytes * segments <= kSmall;
     const long long together = bytes * 2 <= kUnit && segments > 1 ? (kUnit / bytes < segments ? kUnit / bytes : segments) : 1;
     const long long each = together > 1 ? (segments + together - 1) / together : (bytes + kUnit - 1) / kUnit;
-    a.planes[i] = CopyPlane{static_cast<unsigned char*>(planes[i].base), bytes, planes[i].segment_stride, static_cast<int>(segments),
-                            static_cast<int>(each), static_cast<int>(together), static_cast<int>(units)};
-    units += together > 1 ? each : each * segments;
+    a.planes[is_small ? --small : large++] =
+        CopyPlane{static_cast<unsigned char*>(planes[i].base), bytes, planes[i].segment_stride, static_cast<int>(segments),
+                  static_cast<int>(each), static_cast<int>(together), static_cast<int>(units)};
+    if (!is_small) units += together > 1 ? each : each * segments;
     if (units > 0x3fffffffll) return cudaErrorInvalidValue;
   }
+  a.n_large = large;
+  a.large_units = static_cast<int>(units);
+  units += (n_planes - large + kCopyThreads / 32 - 1) / (kCopyThreads / 32);
   a.units = static_cast<int>(units);
   const int sms = sm_count();
   if (sms == 0) return cudaErrorNoDevice;

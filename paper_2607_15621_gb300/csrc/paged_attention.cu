@@ -11,7 +11,7 @@
 //          are CTAs, so that every SM reads the same number of bytes; a cut less than 16 steps from an item's end moves there. Little work
 //          goes in whole items or near-equal pieces of them, one a CTA. A CTA puts 8 warps together in shared memory, so an item that
 //          is spread over the whole GPU has few partial results to join.
-//   queue  many items. Four warps a CTA, three or four CTAs a SM, pieces of at most 28 chunks of 64 keys from one queue: SMs that
+//   queue  many items. Four warps a CTA, three or four CTAs a SM, pieces of at most 14 chunks of 64 keys from one queue: SMs that
 //          read faster take more, and one CTA's end overlaps with the others' loads.
 // The pieces of a cut item are joined by the CTA that ends last, in the order of the keys. A piece that meets a page number
 // outside the cache marks its result, and its item writes nothing.
@@ -26,7 +26,7 @@ namespace fsx {
 
 namespace {
 
-constexpr int kFew = 8, kMany = 28;  // queue: chunks of an item that is not cut, and of a piece
+constexpr int kFew = 8, kMany = 14;  // queue: chunks of an item that is not cut, and of a piece
 constexpr int kLeast = 32, kSnap = 16, kWhole = 64, kShort = 128;  // line: steps
 constexpr int kHeader = 64;          // ints of the workspace, queue: [0] pieces taken, [1] CTAs that are done
 constexpr int kCounters = 8192;      // then one for each slot
