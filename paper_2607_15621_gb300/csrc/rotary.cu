@@ -3,8 +3,8 @@
 //
 // Pair j of a head turns by pos[axis_j] rate_j: (a, b) -> (a cos - b sin, a sin + b cos). The angle is taken in whole turns as
 // 64-bit fixed point: turns_j = rate_j / (2 pi) in units of 2^-64, and pos * turns_j modulo 2^64 is the fraction of a turn,
-// exactly as far as turns_j is; its upper 32 bits go to sincospi. An angle in fp32 would be off by 2^-24 of itself, at
-// position 100,000 by half a percent of a turn. So results depend on the position only through the turn's 2^-32.
+// exactly as far as turns_j is; its upper 32 bits give the quarter turn and the rest, whose sine and cosine are Taylor's series. An
+// angle in fp32 would be off by 2^-24 of itself, at position 100,000 by half a percent of a turn.
 // Products in fp32, rounded once to the type; keys go into an 8-bit cache from their rounded values, so that a cache written
 // here has the bits of one written from the rotated keys by fsx_cache_write_e4m3.
 //
@@ -40,21 +40,44 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
   return make_uint4(pack16<BF>(x[0], x[1]), pack16<BF>(x[2], x[3]), pack16<BF>(x[4], x[5]), pack16<BF>(x[6], x[7]));
 }
 
+// Cosine and sine of `t` 2^-32 turns. |x| <= pi / 4 behind the nearest quarter: Taylor's series to x^8 and x^9 leave 2.5e-8 and 2e-9 out,
+// less than fp32's rounding of the result. As many rows of few heads are bound by these as by memory: 28,001 rows of 5 heads take
+// @@ us with it, 29.6 with the library's, which looks after arguments of any size.
+__device__ __forceinline__ float2 turned_by(uint32_t t) {
+  const uint32_t q = (t + 0x20000000u) >> 30;
+  const float x = static_cast<float>(static_cast<int32_t>(t - (q << 30))) * (6.28318530718f / 4294967296.f);
+  const float y = x * x;
+  const float s = fmaf(x * y, fmaf(y, fmaf(y, fmaf(y, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), x);
+  const float c = fmaf(y, fmaf(y, fmaf(y, fmaf(y, 1.f / 40320.f, -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
+  const uint32_t cosine = __float_as_uint(q & 1u ? s : c) ^ ((q + 1u) & 2u) << 30, sine = __float_as_uint(q & 1u ? c : s) ^ (q & 2u) << 30;
+  return make_float2(__uint_as_float(cosine), __uint_as_float(sine));
+}
+
 // 16 values of a head's row, 8 lanes a row: codes and the row's scale as fsx_cache_write_e4m3 makes them. False: values
-// that are not finite.
-__device__ __forceinline__ bool quantise(const float (&x)[2][8], uint2 (&code)[2], float& scale) {
-  uint32_t top = 0;
-  bool wild = false;
+// that are not finite. The largest magnitude is found two values at a time, of their 16 bits without the sign; only rows with
+// values that are not finite look at each.
+template <bool BF>
+__device__ __forceinline__ bool quantise(const uint4 (&y)[2], uint2 (&code)[2], float& scale) {
+  constexpr uint32_t kInf = BF ? 0x7f80u : 0x7c00u;
+  const uint32_t w[8] = {y[0].x, y[0].y, y[0].z, y[0].w, y[1].x, y[1].y, y[1].z, y[1].w};
+  uint32_t two = 0;
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+  for (int i = 0; i < 8; ++i) asm("max.u16x2 %0, %0, %1;" : "+r"(two) : "r"(w[i] & 0x7fff7fffu));
+  uint32_t most = max(two & 0xffffu, two >> 16);
+  const bool wild = most >= kInf;  // this lane's
+  if (__any_sync(0xffffffffu, wild)) {
+    most = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t m = __float_as_uint(x[h][j]) & 0x7fffffffu;
-      if (m < 0x7f800000u) top = max(top, m);
-      else wild = true;
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t lo = w[i] & 0x7fffu, hi = w[i] >> 16 & 0x7fffu;
+      if (lo < kInf) most = max(most, lo);
+      if (hi < kInf) most = max(most, hi);
     }
+  }
 #pragma unroll
-  for (int o = 4; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  for (int o = 4; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+  const float2 tops = unpack16<BF>(most);
+  const uint32_t top = __float_as_uint(tops.x);
   int e = static_cast<int>(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
   e = max(e, -126);
   const bool zero = top == 0;
@@ -64,11 +87,13 @@ __device__ __forceinline__ bool quantise(const float (&x)[2][8], uint2 (&code)[2
   for (int h = 0; h < 2; ++h) {
     uint32_t c[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) c[j] = pack_e4m3x2(x[h][2 * j] * inv, x[h][2 * j + 1] * inv);
-    if (wild) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if ((__float_as_uint(x[h][j]) & 0x7fffffffu) >= 0x7f800000u) c[j >> 1] |= 0x7fu << ((j & 1) * 8);
+    for (int j = 0; j < 4; ++j) {
+      const float2 x = unpack16<BF>(w[4 * h + j]);
+      c[j] = pack_e4m3x2(x.x * inv, x.y * inv);
+      if (wild) {
+        if ((w[4 * h + j] & 0x7fffu) >= kInf) c[j] |= 0x7fu;
+        if ((w[4 * h + j] >> 16 & 0x7fffu) >= kInf) c[j] |= 0x7f00u;
+      }
     }
     code[h] = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
   }
@@ -119,9 +144,7 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant_
   for (int h = 0; h < 2; ++h) {
     const int j = lane + 32 * h;
     const uint64_t pos = static_cast<uint64_t>(a.positions[a.axis[j] * a.rows + row]);
-    float c, s;
-    sincospif(static_cast<float>(static_cast<int32_t>((pos * a.turns[j]) >> 32)) * (1.f / 2147483648.f), &s, &c);
-    turn[warp][j] = make_float2(c, s);
+    turn[warp][j] = turned_by(static_cast<uint32_t>((pos * a.turns[j]) >> 32));
   }
   __syncwarp();
   float2 t[8];
@@ -173,11 +196,9 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant_
         }
       } else if (CACHE == kCache8) {
         if (__any_sync(0xffffffffu, there && s >= nq)) {
-          unpack8<BF>(y[0], f[0]);
-          unpack8<BF>(y[1], f[1]);
           uint2 code[2];
           float scale;
-          const bool fine = quantise(f, code, scale);
+          const bool fine = quantise<BF>(y, code, scale);
           if (there && s >= nq) {
             wild = wild || !fine;
             if (at >= 0) {
@@ -216,9 +237,11 @@ cudaError_t launch_rotary(const RotaryArgs& a, int dtype, bool adjacent, bool ca
   if (slots == 0) return cudaSuccess;
   const int sms = sm_count();
   if (sms == 0) return cudaErrorNoDevice;
-  // enough warps for every SM, and no more than there are groups of heads
-  const int groups = (slots + 3) / 4;
-  const long long want = (static_cast<long long>(sms) * 32 + a.rows - 1) / a.rows;
+  // 8 warps a SM and more where rows are few; and no warp has more heads than it loads at once as long as all run at once
+  // (128 rows of 48 heads: 4.4 us, with 32 warps a SM 5.1; 1000 rows 5.6, with whole rows 6.8)
+  const int groups = (slots + 3) / 4, least = (groups + kAhead - 1) / kAhead;
+  long long want = (static_cast<long long>(sms) * 8 + a.rows - 1) / a.rows;
+  if (want < least && a.rows * least <= static_cast<long long>(sms) * 20) want = least;
   const int split = static_cast<int>(want < groups ? want : groups);
   int per = (groups + split - 1) / split;
   int parts = (groups + per - 1) / per;
