@@ -220,3 +220,26 @@ def test_selection_is_captured_and_replayed():
     q.neg_()
     graph.replay()
     assert picked.cpu().tolist() == c.want(12)
+
+
+def test_bounds_of_codes_whose_scales_are_far_apart_or_no_powers_of_two():
+    """Rows of a page with scales that one fp16 unit holds, and with scales that it does not."""
+    g = torch.Generator().manual_seed(4)
+    code = torch.from_numpy(llm_oracle.E4M3[:127])[torch.randint(0, 127, (6 * 64, 1, 128), generator=g)] * (torch.randint(0, 2, (6 * 64, 1, 128), generator=g) * 2 - 1)
+    scale = torch.ones(6 * 64, 1)
+    scale[64:128] = 2.0 ** torch.randint(-7, 8, (64, 1), generator=g)    # 14 powers: just held
+    scale[128:192] = 2.0 ** torch.randint(-8, 8, (64, 1), generator=g)   # 15
+    scale[192:256] = 2.0 ** torch.randint(-120, 100, (64, 1), generator=g)
+    scale[256:320] = torch.rand(64, 1, generator=g) + 0.01
+    scale[320 + 40] = 2.0 ** 13  # late in the page: the ends so far change their unit
+    cache = code.float().to(torch.float8_e4m3fn).cuda()
+    bounds, bs, st = torch.empty(6, 1, 2, 128, dtype=torch.int8, device="cuda"), torch.empty(1, 6, device="cuda"), status()
+    for start in (None, torch.zeros(1, dtype=torch.int64, device="cuda")):  # a warp a page, eight warps a page
+        fsx.page_bounds(cache, torch.arange(6, dtype=torch.int32, device="cuda")[None], torch.tensor([6 * 64 - 5], device="cuda"), 64, bounds, bs,
+                        st, k_scale=scale.T.contiguous().cuda(), start=start)
+        assert int(st) == 0
+        value = to64(cache) * scale.double().numpy()[..., None]
+        value = value.astype(np.float32).astype(np.float64)  # codes times scales are fp32
+        for p in range(6):
+            want, s = po.page_bounds(value[p * 64:min(p * 64 + 64, 6 * 64 - 5), 0])
+            assert np.array_equal(bounds[p, 0].cpu().numpy(), want) and float(bs[0, p]) == s

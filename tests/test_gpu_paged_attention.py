@@ -17,6 +17,12 @@ pytestmark = pytest.mark.gpu
 BF, HF = torch.bfloat16, torch.float16
 
 
+def coded(x):
+    """Codes as values and powers of two as scales that hold the rows, whatever they are: for caches of many rows."""
+    s = 2.0 ** (torch.frexp(x.float().abs().amax(-1))[1].double() - 8)
+    return (x.double() / s[..., None]).float().to(torch.float8_e4m3fn).double().numpy(), s.numpy()
+
+
 class Case:
     """Requests over a cache of shuffled pages; every row that belongs to none is NaN."""
 
@@ -41,7 +47,7 @@ class Case:
         if cache == "e4m3":
             self.cache, self.scale, self.value = [], [], []
             for x in kv:
-                code, s = llm_oracle.cache_write(to64(x))
+                code, s = llm_oracle.cache_write(to64(x)) if rows * kv_heads < 50000 else coded(x)
                 code[~used.numpy()] = math.nan
                 s[~used.numpy()] = math.nan
                 self.value.append(code * s[..., None])
@@ -130,6 +136,30 @@ def test_picked_pages(page_rows, most, cache):
     c.run(picked=picked.cuda())
     assert int(c.status) == 0
     c.compare(picked.numpy())
+
+
+@pytest.mark.parametrize("cache", ["same", "e4m3"])
+@pytest.mark.parametrize("B,heads,kv_heads", [(310, 1, 1), (160, 20, 2), (100, 8, 4)])
+def test_many_items_some_of_them_cut(B, heads, kv_heads, cache):
+    g = torch.Generator().manual_seed(B)
+    lens = torch.randint(0, 1100, (B,), generator=g).tolist()
+    lens[7] = 2900
+    c = Case(lens, heads, kv_heads, 64, BF, BF if cache == "same" else cache, B)
+    c.run()
+    assert int(c.status) == 0
+    c.compare()
+    first = c.out.clone()
+    for _ in range(3):
+        c.out.fill_(7)
+        c.run()
+        assert torch.equal(c.out, first)
+    page = int(c.table[7, 30])
+    c.table[7, 30] = -1  # in one of several pieces: the others' results are as before
+    c.out.fill_(7)
+    c.run()
+    assert int(c.status) == fsx.FSX_ERR_DEVICE_ARG and (c.out[7] == 7).all()
+    c.out[7], c.table[7, 30] = first[7], page
+    assert torch.equal(c.out, first)
 
 
 def test_picked_none_gives_zeros():

@@ -167,3 +167,30 @@ def test_strides_none_rows_another_stream_and_a_graph():
     graph.replay()
     fsx.rotary(q, None, pos, pairs, st, q_out=qo)
     assert torch.equal(again, qo) and int(st) == 0
+
+
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("kind", [None, "e4m3", BF])
+@pytest.mark.parametrize("n,heads,kv_heads", [(30001, 2, 1), (30001, 5, 1), (13000, 1, 1), (1301, 32, 8), (3001, 16, 4), (1001, 40, 8)])
+def test_many_rows_are_what_few_of_them_are(n, heads, kv_heads, kind, adjacent):
+    """Several rows a warp, whole rows a warp and rows shared out over warps give the same bits."""
+    q, k, v, pos = inputs(n, heads, kv_heads, BF, heads, 3, far=100000)
+    pairs = fsx.rotary_pairs((16, 24, 24), adjacent=adjacent)
+    m = n + 11
+    rows = torch.randperm(m, generator=torch.Generator().manual_seed(n))[:n].cuda()
+    rows[n // 2] = -1  # one that has no place
+
+    def run(parts):
+        qo, ko, st = torch.empty_like(q).contiguous(), torch.empty_like(k).contiguous(), status()
+        (kc, vc), (ks, vs) = caches(m, kv_heads, kind) if kind else ([None, None], [None, None])
+        for a in range(0, n, parts):
+            b = min(n, a + parts)
+            write = dict(v=v[a:b], rows=rows[a:b], k_cache=kc, v_cache=vc, k_scale=ks, v_scale=vs) if kind else {}
+            fsx.rotary(q[a:b], k[a:b], pos[:, a:b].contiguous(), pairs, st, q_out=qo[a:b], k_out=ko[a:b], **write)
+        assert int(st) == (fsx.FSX_ERR_DEVICE_ARG if kind else 0)
+        return [qo, ko] + [x.view(torch.uint8) for x in (kc, vc, ks, vs) if x is not None]
+
+    whole, few = run(n), run(97)
+    assert all(torch.equal(a, b) for a, b in zip(whole, few))
+    some = torch.arange(0, n, n // 7, device="cuda")
+    near(whole[0][some], to64(q[some]), po.rotary(to64(q[some]), pos[:, some].cpu().numpy(), list(pairs.axis), list(pairs.rate), adjacent), BF, adjacent)
