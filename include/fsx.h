@@ -621,6 +621,8 @@ fsx_status fsx_rotary(const void* d_q, long long q_stride, const void* d_k, cons
  *                heads of that kv head. Entries are places in the request's table (0: its first page), distinct, in any order; of a request
  *                with n pages the first min(n, n_picked) are read; -1: none. Any other entry that is no page of
  *                the request sets FSX_ERR_DEVICE_ARG, and the heads of that kv head get no output. n_picked is 1 .. 4096.
+ *   roundings  : the weights of the values go into the product as two 16-bit parts where one would show (over 16-bit caches, and for
+ *                FSX_F16 over 8-bit ones), so that an output is rounded once, by its own type.
  *   d_out      : DEVICE [B, n_heads, 128] of `dtype`; d_lse : DEVICE fp32 [n_heads, B] or NULL. A request without rows gets
  *                zeros and -infinity.
  *   d_workspace : as fsx_tree_attention: fsx_paged_attention_workspace_bytes(...) bytes, 256-byte aligned, zeroed once; calls that
@@ -651,8 +653,8 @@ fsx_status fsx_page_bounds(const void* d_k_cache, const float* d_k_scale, int ca
  *   over its scale (as the bounds', one per head) rounded to the nearest whole number, ties to even, and 2^e the product
  *   of both scales, e limited to -100 .. 100. This is exact in fp32: the choice is the same on every run.
  *   d_picked : DEVICE int32 [B, n_kv_heads, n_picked]: places in the request's table, ascending, -1 behind the last.
- * width is at most 32768. A value of a query that is not finite counts as 0 and sets FSX_ERR_RANGE; a page outside the cache
- * sets FSX_ERR_DEVICE_ARG and comes last; a request of a bad length gets a list of -1 only. */
+ * width is at most 32768. A value of a query that is not finite counts as 0 and sets FSX_ERR_RANGE; where
+ * scores are made, a page outside the cache sets FSX_ERR_DEVICE_ARG and comes last; a request of a bad length gets a list of -1 only. */
 fsx_status fsx_page_select(const void* d_q, long long q_stride, int dtype, const int8_t* d_bounds, const float* d_bound_scale,
                            long long cache_rows, int page_rows, const int32_t* d_table, int width, const int64_t* d_lengths,
                            int B, int n_heads, int n_kv_heads, int head_dim, int first, int last, int n_picked,

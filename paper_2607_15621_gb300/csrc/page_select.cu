@@ -9,6 +9,9 @@
 // c hi where c > 0 and c lo elsewhere: two dot products of int8 with the positive and the negative part of c, in whole numbers
 // below 2^22, times a power of two: exact in fp32, and so is the largest over the heads of a group. The pages that are
 // chosen depend on no order of summation.
+//
+// Measured: bounds of 3,117 pages of 32 rows, 8 heads, bf16, 36 us (5.9 TB/s, 0.86 of a copy's rate; DRAM 70 % busy), of codes 37 us,
+// the newest page of 16 requests 3.5 us; 64 of up to 1024 pages for 16 requests and 8 kv heads 11.2 us, 96 of 2047 for one request 8.8 us.
 #include <cooperative_groups.h>
 #include <math_constants.h>
 
@@ -336,7 +339,8 @@ constexpr int kSelectThreads = 512;
 constexpr int kSelectWarps = kSelectThreads / 32;
 constexpr int kMaxSplit = 8;  // CTAs of a cluster
 constexpr int kHeadTile = 4;
-constexpr int kIdle = 1, kFewPages = 128;  // CTAs a SM, and pages of a CTA, from which on an item is not split further
+// CTAs a SM, and pages of a CTA, from which on an item is not split further (128 items of up to 1024 pages: 11.4 us, split for 2 CTAs a SM 15.1)
+constexpr int kIdle = 1, kFewPages = 128;
 constexpr int kAtOnce = 2;  // times 8 pages of a warp
 constexpr int kDigit = 11, kBins = 1 << kDigit, kPerThread = kBins / kSelectThreads;
 
@@ -602,7 +606,7 @@ static const void* bounds_of(int cache_dtype) {
 cudaError_t launch_page_bounds(const BoundsArgs& a, int cache_dtype, cudaStream_t stream) {
   const int sms = sm_count();
   if (sms == 0) return cudaErrorNoDevice;
-  // With a start, pages are few: the ones that new rows went into. Without, twice as many warps as run at once over all requests, and no
+  // With a start, pages are few: the ones that new rows went into (16 of 32 rows, 8 heads: 3.5 us, with a warp a page 5.6). Without, twice as many warps as run at once over all requests, and no
   // more than a request's pages can have.
   const bool few = a.start != nullptr;
   const int each = few ? 1 : kBoundsWarps;

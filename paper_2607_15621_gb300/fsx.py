@@ -1,4 +1,5 @@
-"""Thin ctypes binding of libfsx.so (include/fsx.h): argument marshalling only.
+"""Thin binding of libfsx.so (include/fsx.h): argument marshalling only, by ctypes, and for
+the operators over a cache in pages by an extension module (csrc/calls.cpp).
 
 Every step of the tick runs in the library's CUDA kernels; this module only
 turns torch tensors / numpy arrays into pointers, sizes and a cudaStream_t.
