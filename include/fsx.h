@@ -640,9 +640,9 @@ fsx_status fsx_paged_attention(const void* d_q, long long q_stride, int dtype, c
  * key: scale s the smallest power of two (at least 2^-126) with max|key| / s <= 127, codes floor(least / s) and ceil(largest / s).
  *   d_k_cache    : of cache_dtype FSX_BF16, FSX_F16 or FSX_E4M3 (with d_k_scale).
  *   d_bounds     : DEVICE int8 [pages, n_kv_heads, 2, 128] (least, largest), d_bound_scale : DEVICE fp32 [n_kv_heads, pages],
- *                  pages = cache_rows / page_rows; other pages stay as they are. A page that several requests share gets those of
- *                  either's rows in it: let it be full, or take the bounds of one.
- * Keys that are not finite are left out and set FSX_ERR_RANGE. */
+ *                  pages = cache_rows / page_rows; other pages stay as they are. A page that several requests share needs as many
+ *                  rows of each (a full one, or a last one of equal lengths): else its bounds may be of none of them.
+ * Keys that are not finite are left out and set FSX_ERR_RANGE. width times n_kv_heads is below 2^30. */
 fsx_status fsx_page_bounds(const void* d_k_cache, const float* d_k_scale, int cache_dtype, long long cache_rows, int page_rows,
                            const int32_t* d_table, int width, const int64_t* d_lengths, const int64_t* d_start, int B,
                            int n_kv_heads, int head_dim, int8_t* d_bounds, float* d_bound_scale, int* d_status, void* stream);

@@ -48,6 +48,12 @@ class Args {
     if (good && t.numel() > 0 && t.data_ptr() == nullptr) good = false;  // throws where there is no memory behind the tensor
     return &t;
   }
+  // the status word
+  const Tensor* word() {
+    const Tensor* t = tensor();
+    if (good && (t->scalar_type() != ScalarType::Int || t->numel() < 1)) good = false;
+    return t;
+  }
   long long number() {
     if (!good) return 0;
     const long long v = PyLong_AsLongLong(*at_++);
@@ -122,7 +128,7 @@ PyObject* rotary(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const int* axis = reinterpret_cast<const int*>(a.number());
   const double* rate = reinterpret_cast<const double*>(a.number());
   const int n_axes = a.small(), layout = a.small();
-  const Tensor *status = a.tensor(), *q_out = a.tensor(true), *k_out = a.tensor(true), *v = a.tensor(true), *dst = a.tensor(true),
+  const Tensor *status = a.word(), *q_out = a.tensor(true), *k_out = a.tensor(true), *v = a.tensor(true), *dst = a.tensor(true),
                *kc = a.tensor(true), *vc = a.tensor(true), *ks = a.tensor(true), *vs = a.tensor(true);
   const Tensor* any = q ? q : k;
   int64_t count = 0, heads = 0, kv_heads = 0, dim = 0;
@@ -156,10 +162,10 @@ PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Args a(args, n, 15);
   const Tensor *q = a.tensor(), *kc = a.tensor(), *vc = a.tensor(), *table = a.tensor(), *lengths = a.tensor();
   const int page_rows = a.small();
-  const Tensor *out = a.tensor(), *status = a.tensor(), *ws = a.tensor(), *ks = a.tensor(true), *vs = a.tensor(true), *picked = a.tensor(true),
+  const Tensor *out = a.tensor(), *status = a.word(), *ws = a.tensor(), *ks = a.tensor(true), *vs = a.tensor(true), *picked = a.tensor(true),
                *lse = a.tensor(true);
   int64_t B = 0, heads = 0, dim = 0;
-  if (a.check(a.good && rows(q) && table->dim() == 2)) {
+  if (a.check(a.good && rows(q) && table->dim() == 2 && ws->is_contiguous())) {
     B = q->size(0), heads = q->size(1), dim = q->size(2);
     a.check(code_of(*q) >= 0 && out->scalar_type() == q->scalar_type() && out->sizes() == q->sizes() && out->is_contiguous() &&
             is(table, ScalarType::Int, {B, table->size(1)}) && is(lengths, ScalarType::Long, {B}) && two_caches(kc, vc, dim));
@@ -188,7 +194,7 @@ PyObject* page_bounds(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Args a(args, n, 11);
   const Tensor *kc = a.tensor(), *table = a.tensor(), *lengths = a.tensor();
   const int page_rows = a.small();
-  const Tensor *bounds = a.tensor(), *scale = a.tensor(), *status = a.tensor(), *ks = a.tensor(true), *start = a.tensor(true);
+  const Tensor *bounds = a.tensor(), *scale = a.tensor(), *status = a.word(), *ks = a.tensor(true), *start = a.tensor(true);
   a.check(a.good && page_rows > 0 && kc->dim() == 3 && kc->is_contiguous() && code_of(*kc) >= 0 &&
           paged(table, lengths, bounds, scale, kc->size(0) / page_rows, kc->size(1), kc->size(2)));
   a.check(a.good && (code_of(*kc) != FSX_E4M3 || (ks && is(ks, ScalarType::Float, {kc->size(1), kc->size(0)}))));
@@ -205,7 +211,7 @@ PyObject* page_select(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Args a(args, n, 12);
   const Tensor *q = a.tensor(), *bounds = a.tensor(), *scale = a.tensor(), *table = a.tensor(), *lengths = a.tensor();
   const int page_rows = a.small();
-  const Tensor *picked = a.tensor(), *status = a.tensor();
+  const Tensor *picked = a.tensor(), *status = a.word();
   const int first = a.small(), last = a.small();
   a.check(a.good && rows(q) && bounds->dim() == 4 && code_of(*q) >= 0 && q->size(2) == bounds->size(3) &&
           paged(table, lengths, bounds, scale, bounds->size(0), bounds->size(1), bounds->size(3)) && table->size(0) == q->size(0) &&
@@ -224,7 +230,7 @@ PyObject* pages_step(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const Tensor *table = a.tensor(), *lengths = a.tensor(), *refs = a.tensor(), *offsets = a.tensor();
   const int page_rows = a.small();
   const Tensor *table_out = a.tensor(), *lengths_out = a.tensor(), *refs_out = a.tensor(), *to = a.tensor(), *pairs = a.tensor(), *n_pairs = a.tensor(),
-               *status = a.tensor(), *source = a.tensor(true);
+               *status = a.word(), *source = a.tensor(true);
   int64_t B_in = 0, B = 0, width = 0, pages = 0, total = 0;
   if (a.check(a.good && table->dim() == 2 && table_out->dim() == 2 && refs->dim() == 1 && to->dim() == 1)) {
     B_in = table->size(0), B = table_out->size(0), width = table->size(1), pages = refs->size(0), total = to->size(0);
@@ -246,7 +252,7 @@ PyObject* pages_compact(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Args a(args, n, 11);
   const Tensor *table = a.tensor(), *lengths = a.tensor(), *refs = a.tensor();
   const int page_rows = a.small();
-  const Tensor *table_out = a.tensor(), *refs_out = a.tensor(), *pairs = a.tensor(), *n_pairs = a.tensor(), *status = a.tensor();
+  const Tensor *table_out = a.tensor(), *refs_out = a.tensor(), *pairs = a.tensor(), *n_pairs = a.tensor(), *status = a.word();
   int64_t B = 0, width = 0, pages = 0;
   if (a.check(a.good && table->dim() == 2 && refs->dim() == 1 && pairs->dim() == 2)) {
     B = table->size(0), width = table->size(1), pages = refs->size(0);
@@ -267,7 +273,7 @@ PyObject* pages_copy(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Args a(args, n, 8);
   const fsx_page_plane* planes = reinterpret_cast<const fsx_page_plane*>(a.number());
   const int n_planes = a.small(), n_pages = a.small();
-  const Tensor *pairs = a.tensor(), *n_pairs = a.tensor(), *status = a.tensor();
+  const Tensor *pairs = a.tensor(), *n_pairs = a.tensor(), *status = a.word();
   a.check(a.good && pairs->dim() == 2 && is(pairs, ScalarType::Int, {pairs->size(0), 2}) && is(n_pairs, ScalarType::Int, {1}) &&
           pairs->size(0) <= INT32_MAX);
   return answer(a, [&] {

@@ -85,7 +85,7 @@ def test_paged_attention_refuses(lib, over, code):
 
 @pytest.mark.parametrize("over,code", PAGES + [
     (dict(kc=None), BAD), (dict(ks=None), BAD), (dict(cdt=fsx.FSX_F32), BAD), (dict(b=None), BAD), (dict(bs=None), BAD),
-    (dict(b=FAKE + 8), BAD), (dict(kc=FAKE + 8), BAD),
+    (dict(b=FAKE + 8), BAD), (dict(kc=FAKE + 8), BAD), (dict(width=1 << 20, Hk=1024), UNS),
 ])
 def test_page_bounds_refuse(lib, over, code):
     assert lib.fsx_page_bounds(*dict(BOUNDS, **over).values()) == code
@@ -168,7 +168,8 @@ def test_binding_refuses_tensors_that_do_not_fit():
              dict(positions=z(1, 4, dtype=i64)), dict(positions=z(1, 5, dtype=i32)), dict(positions=z(5, dtype=i64)),
              dict(pairs=fsx.rotary_pairs((32, 32))), dict(rows=z(5, dtype=i32)), dict(rows=z(4, dtype=i64)), dict(k_scale=None),
              dict(k_scale=z(160, 2, dtype=f32)), dict(v_cache=None), dict(k_cache=None), dict(k_cache=z(160, 3, 128, dtype=torch.uint8)),
-             dict(v_cache=z(160, 2, 128)), dict(k=None), dict(q=q.float(), q_out=q.float())])
+             dict(v_cache=z(160, 2, 128)), dict(k=None), dict(q=q.float(), q_out=q.float()), dict(status=st.long()),
+             dict(status=None), dict(status=st[:0])])
     refuses(fsx.paged_attention, dict(q=q, k_cache=cache, v_cache=cache, table=table, lengths=lengths, page_rows=16, out=q, status=st,
                                       workspace=z(256, dtype=torch.uint8), k_scale=scale, v_scale=scale),
             [dict(q=z(5, 4, 64)), dict(out=z(5, 128, 4).transpose(1, 2)), dict(out=q.half()), dict(table=table.long()),
