@@ -382,6 +382,7 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const SelectA
       for (int i = tid; i < a.n_picked; i += kSelectThreads) out[i] = i < pages ? i : -1;
     return;  // the whole cluster
   }
+  if (split > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // this CTA runs
   const int part = (pages + split - 1) / split, p0 = min(pages, rank * part), n = min(pages, p0 + part) - p0;
   bool lost = false;
   for (int i = tid; i < n; i += kSelectThreads) {  // where the pages are, in the keys' place
@@ -424,6 +425,7 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const SelectA
     if (lane == 0) q_scale[h] = scale;
   }
   __syncthreads();
+  if (split > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // every CTA of the cluster runs
   uint32_t* const all_keys = split > 1 ? cluster.map_shared_rank(keys, 0) : keys;
   // ---- scores: 4 lanes a page, 8 pages a warp, kAtOnce times; unit 4 u + sub of a page's 16 units of 16 bytes
   const int sub = lane & 3;
@@ -507,7 +509,7 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const SelectA
   uint32_t border = 0;
   int shift = 32 - __clz(most - least);
   bool whole = want == 0;
-  if (whole) border = 0xffffffffu, shift = 0;  // no key - least is as large: at least two pages lie between the first and the last
+  if (whole) border = 0xffffffffu, shift = 0;  // no key - least is as large: scores are finite
   for (bool first = true; !whole && shift > 0; first = false) {
     const int width = min(kDigit, shift), below = shift;
     shift -= width;

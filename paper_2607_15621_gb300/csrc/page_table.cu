@@ -72,7 +72,7 @@ __device__ __forceinline__ void part_of(int n_pages, int rank, int& first, int& 
   end = static_cast<int>(min(static_cast<long long>(n_pages), static_cast<long long>(first) + part));
 }
 
-// Every CTA's `mine`, where every CTA can read it
+// Every CTA's `mine`, where every CTA can read it. All of them run already.
 __device__ __forceinline__ void tell(cg::cluster_group& cluster, int (&counts)[kCtas], int rank, int mine) {
   if (threadIdx.x < kCtas) *cluster.map_shared_rank(&counts[rank], threadIdx.x) = mine;
   cluster.sync();
@@ -317,6 +317,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) compac
   constexpr int kAllThreads = kCtas * kThreads;
   int first, end;
   part_of(a.n_pages, rank, first, end);
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // this CTA runs
   pdl_launch_dependents();
   pdl_wait();
   int mine = 0;
@@ -327,6 +328,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) compac
   }
   int in_part;
   scan_before(mine, scan, in_part);
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // every CTA of the cluster runs
   tell(cluster, counts[0], rank, in_part);
   int used = 0;
   for (int r = 0; r < kCtas; ++r) used += counts[0][r];
