@@ -684,10 +684,12 @@ def page_planes(page_rows: int, caches: Sequence = (), scales: Sequence = (), bo
                 bound_scales: Sequence = ()) -> PagePlanes:
     """The planes of caches [rows, kv heads, 128], scales [kv heads, rows], bounds [pages, kv heads, 2, 128] and bound scales
     [kv heads, pages], of all layers, keys and values: made once, used by every pages_copy."""
-    each = [(c, c.shape[0] // page_rows) for c in caches] + [(s, s.shape[1] // page_rows) for s in scales] + \
-        [(b, b.shape[0]) for b in bounds] + [(s, s.shape[1]) for s in bound_scales]
-    if not each or len({n for _, n in each}) != 1 or len({t.device for t, _ in each}) != 1 or not all(t.is_contiguous() for t, _ in each):
-        _refuse("contiguous tensors of as many pages each on one device", **{f"planes[{i}]": t for i, (t, _) in enumerate(each)})
+    groups = ((caches, 3, 0, page_rows), (scales, 2, 1, page_rows), (bounds, 4, 0, 1), (bound_scales, 2, 1, 1))
+    each = [(t, t.shape[axis] // rows if t.dim() == dim and rows > 0 and t.numel() > 0 and t.shape[axis] % rows == 0 else 0)
+            for group, dim, axis, rows in groups for t in group]
+    if len({n for _, n in each}) != 1 or each[0][1] < 1 or len({t.device for t, _ in each}) != 1 or not all(t.is_contiguous() for t, _ in each):
+        _refuse("caches [rows, kv heads, 128], scales [kv heads, rows], bounds [pages, kv heads, 2, 128], bound scales [kv heads, pages], "
+                "contiguous, of as many whole pages each, on one device", **{f"planes[{i}]": t for i, (t, _) in enumerate(each)})
     n_pages, planes = each[0][1], []
     for group, by_row in ((caches, True), (scales, False), (bounds, True), (bound_scales, False)):
         for t in group:

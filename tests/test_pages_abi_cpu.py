@@ -203,6 +203,11 @@ def test_binding_refuses_tensors_that_do_not_fit():
         fsx.page_planes(16, [cache], [z(2, 320, dtype=f32)])
     with pytest.raises(fsx.FsxError):
         fsx.page_planes(16)
+    for page_rows, wrong in ((48, dict(caches=[cache])), (48, dict(scales=[scale])), (0, dict(caches=[cache])), (512, dict(caches=[cache])),
+                             (16, dict(caches=[cache[:0]])), (16, dict(bounds=[bounds[:0]])), (16, dict(scales=[scale[0]])),
+                             (16, dict(caches=[torch.zeros(())])), (16, dict(bound_scales=[bs[:0]]))):
+        with pytest.raises(fsx.FsxError):  # parts of pages, no pages, too few axes, nothing of a page
+            fsx.page_planes(page_rows, **wrong)
 
 
 def test_rotary_pairs():
