@@ -140,7 +140,7 @@ PyObject* rotary(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (k && a.check(k->dim() == 3 && k->size(0) == count && k->size(2) == dim && k->scalar_type() == any->scalar_type() && rows(k))) {
       kv_heads = k->size(1);
       if (k_out) a.check(k_out->sizes() == k->sizes() && k_out->scalar_type() == k->scalar_type() && rows(k_out));
-      if (kc && a.check(v && two_caches(kc, vc, dim) && kc->size(1) == kv_heads)) {
+      if (kc && a.check(v && two_caches(kc, vc, dim) && kc->size(1) == kv_heads && kc->size(0) > 0)) {
         a.check(v->sizes() == k->sizes() && v->scalar_type() == k->scalar_type() && rows(v) && (count < 2 || v->stride(0) == k->stride(0)));
         a.check(code_of(*kc) != FSX_E4M3 || scales(ks, vs, kv_heads, kc->size(0)));
         a.check(!dst || is(dst, ScalarType::Long, {count}));
@@ -170,7 +170,7 @@ PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
     a.check(code_of(*q) >= 0 && out->scalar_type() == q->scalar_type() && out->sizes() == q->sizes() && out->is_contiguous() &&
             is(table, ScalarType::Int, {B, table->size(1)}) && is(lengths, ScalarType::Long, {B}) && two_caches(kc, vc, dim));
     a.check(a.good && (code_of(*kc) != FSX_E4M3 || scales(ks, vs, kc->size(1), kc->size(0))));
-    a.check(a.good && (!picked || (picked->dim() == 3 && is(picked, ScalarType::Int, {B, kc->size(1), picked->size(2)}))));
+    a.check(a.good && (!picked || (picked->dim() == 3 && picked->size(2) > 0 && is(picked, ScalarType::Int, {B, kc->size(1), picked->size(2)}))));
     a.check(!lse || is(lse, ScalarType::Float, {heads, B}));
   }
   return answer(a, [&] {

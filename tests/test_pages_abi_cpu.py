@@ -210,6 +210,20 @@ def test_binding_refuses_tensors_that_do_not_fit():
             fsx.page_planes(page_rows, **wrong)
 
 
+def test_binding_refuses_lists_of_no_pages_and_caches_of_no_rows():
+    """Tensors of nothing have no memory: they must not be taken for ones that were not given."""
+    i32, i64 = torch.int32, torch.int64
+    st, cache, q, k = z(1, dtype=i32), z(160, 2, 128), z(5, 4, 128), z(5, 2, 128)
+    with pytest.raises(fsx.FsxError) as e:
+        fsx.paged_attention(q, cache, cache, z(5, 7, dtype=i32), z(5, dtype=i64), 16, q, st, z(1, dtype=torch.uint8),
+                            picked=z(5, 2, 0, dtype=i32), stream=0)
+    assert "picked" in str(e.value)
+    with pytest.raises(fsx.FsxError) as e:
+        fsx.rotary(q, k, z(1, 5, dtype=i64), fsx.rotary_pairs(), st, q_out=q, k_out=k, v=k, rows=z(5, dtype=i64), k_cache=cache[:0],
+                   v_cache=cache[:0], stream=0)
+    assert "caches" in str(e.value)
+
+
 def test_rotary_pairs():
     p = fsx.rotary_pairs((16, 24, 24))
     assert list(p.axis) == [0] * 16 + [1] * 24 + [2] * 24 and p.n_axes == 3 and p.layout == fsx.FSX_ROTARY_HALVES
