@@ -587,7 +587,7 @@ fsx_status fsx_tree_attention(const void* d_q, long long q_stride, const void* d
  *     Row r of page p is cache row p * page_rows + r, so fsx_cache_write_e4m3 writes into pages too.
  *   - d_table: DEVICE int32 [B, width]: row j of request b lies in page d_table[b][j / page_rows]. Entries
  *     behind a request's last page are not read. d_lengths: DEVICE int64 [B], rows of each request, 0 to
- *     width * page_rows. B is 1 .. 1024; width * page_rows and cache_rows are below 2^31.
+ *     width * page_rows and below 2^31 - 64. B is 1 .. 1024; width * page_rows and cache_rows are below 2^31.
  *   - The conventions above hold (heads, strides, status, roundings, asynchronous, nothing allocated). A request whose
  *     length is out of range, or that has a page outside the cache, sets FSX_ERR_DEVICE_ARG and gets no output;
  *     the others are written. */
@@ -625,9 +625,9 @@ fsx_status fsx_rotary(const void* d_q, long long q_stride, const void* d_k, cons
  *                FSX_F16 over 8-bit ones), so that an output is rounded once, by its own type.
  *   d_out      : DEVICE [B, n_heads, 128] of `dtype`; d_lse : DEVICE fp32 [n_heads, B] or NULL. A request without rows gets
  *                zeros and -infinity.
- *   d_workspace : as fsx_tree_attention: fsx_paged_attention_workspace_bytes(...) bytes, 256-byte aligned, zeroed once; calls that
- *                overlap on the GPU (graphs that may run at the same time, too) must not share it. Its size
- *                does not depend on B. */
+ *   d_workspace : as fsx_tree_attention: fsx_paged_attention_workspace_bytes(...) bytes, 256-byte aligned, zeroed once, for calls of
+ *                this operator only; calls that overlap on the GPU (graphs that may run at the same time, too) must not
+ *                share it. Its size does not depend on B. */
 size_t fsx_paged_attention_workspace_bytes(int B, int n_heads, int n_kv_heads);
 fsx_status fsx_paged_attention(const void* d_q, long long q_stride, int dtype, const void* d_k_cache, const void* d_v_cache,
                                const float* d_k_scale, const float* d_v_scale, int cache_dtype, long long cache_rows,
