@@ -344,10 +344,14 @@ constexpr int kIdle = 1, kFewPages = 128;
 constexpr int kAtOnce = 2;  // times 8 pages of a warp
 constexpr int kDigit = 11, kBins = 1 << kDigit, kPerThread = kBins / kSelectThreads;
 
+constexpr uint32_t kFewKeys = 256;  // at the border, which are compared with one another
+
 struct __align__(16) SelectShared {
-  uint32_t hist[kBins];
+  uint32_t hist[kBins];  // and the keys at the border
+  uint32_t least[kMaxSplit * kSelectWarps], most[kMaxSplit * kSelectWarps];  // keys that the warps of all CTAs have found
   uint32_t warps[2][kSelectWarps];
-  uint32_t border, above, whole;  // of a pass: digit, keys above it, whether all keys at it are taken
+  uint32_t border, above, at_it;  // of a pass: digit, keys above it, keys at it
+  uint32_t gathered;
 };
 
 // order of floats as order of unsigned numbers
@@ -391,6 +395,10 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const SelectA
     lost = lost || !there;
     keys[i] = there ? static_cast<uint32_t>(at) : 0xffffffffu;
   }
+  if (rank == 0) {
+    for (int i = tid; i < kBins; i += kSelectThreads) sm.hist[i] = 0;
+    if (tid == 0) sm.gathered = 0;
+  }
   if (lost) set_status(a.status, kStatusDeviceArg);
   // ---- the queries' codes; what is not finite counts as 0
   for (int h = warp; h < tiles * kHeadTile; h += kSelectWarps) {
@@ -429,6 +437,8 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const SelectA
   uint32_t* const all_keys = split > 1 ? cluster.map_shared_rank(keys, 0) : keys;
   // ---- scores: 4 lanes a page, 8 pages a warp, kAtOnce times; unit 4 u + sub of a page's 16 units of 16 bytes
   const int sub = lane & 3;
+  const int p_first = a.first, p_last = pages - a.last;  // the pages that are not taken anyway
+  uint32_t least = 0xffffffffu, most = 0;                // keys of theirs
   for (int base = warp * (8 * kAtOnce); base < n; base += kSelectWarps * (8 * kAtOnce)) {
     int4 x[kAtOnce][4];
     float scale[kAtOnce], best[kAtOnce];
@@ -480,31 +490,34 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const SelectA
       best[t] = fmaxf(best[t], __shfl_xor_sync(0xffffffffu, best[t], 1));
       best[t] = fmaxf(best[t], __shfl_xor_sync(0xffffffffu, best[t], 2));
       const int i = base + 8 * t + (lane >> 2);
-      if (i < n && sub == 0) all_keys[p0 + i] = keys[i] == 0xffffffffu ? 0u : key_of(best[t]);
+      if (i < n && sub == 0) {
+        const uint32_t key = keys[i] == 0xffffffffu ? 0u : key_of(best[t]);
+        all_keys[p0 + i] = key;
+        if (p0 + i >= p_first && p0 + i < p_last) {
+          least = min(least, key);
+          most = max(most, key);
+        }
+      }
     }
+  }
+  least = __reduce_min_sync(0xffffffffu, least);
+  most = __reduce_max_sync(0xffffffffu, most);
+  if (lane == 0) {
+    SelectShared* const to = split > 1 ? cluster.map_shared_rank(&sm, 0) : &sm;
+    to->least[rank * kSelectWarps + warp] = least;
+    to->most[rank * kSelectWarps + warp] = most;
   }
   if (split > 1) cluster.sync();  // the keys are in the first CTA; nothing is read from the others
   else __syncthreads();
   if (rank != 0) return;
   // ---- the border among the pages that are not taken anyway: the want-th largest key
-  const int p_first = a.first, p_last = pages - a.last;
   uint32_t want = static_cast<uint32_t>(a.n_picked - a.first - a.last);
-  uint32_t least = 0xffffffffu, most = 0;
-  for (int i = p_first + tid; i < p_last; i += kSelectThreads) {
-    least = min(least, keys[i]);
-    most = max(most, keys[i]);
+  for (int w = lane; w < split * kSelectWarps; w += 32) {
+    least = min(least, sm.least[w]);
+    most = max(most, sm.most[w]);
   }
   least = __reduce_min_sync(0xffffffffu, least);
   most = __reduce_max_sync(0xffffffffu, most);
-  if (lane == 0) {
-    sm.warps[0][warp] = least;
-    sm.warps[1][warp] = most;
-  }
-  __syncthreads();
-  for (int w = 0; w < kSelectWarps; ++w) {
-    least = min(least, sm.warps[0][w]);
-    most = max(most, sm.warps[1][w]);
-  }
   // (key - least) >> shift: above `border` taken, at it the first `want` ones
   uint32_t border = 0;
   int shift = 32 - __clz(most - least);
@@ -513,8 +526,10 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const SelectA
   for (bool first = true; !whole && shift > 0; first = false) {
     const int width = min(kDigit, shift), below = shift;
     shift -= width;
-    for (int i = tid; i < kBins; i += kSelectThreads) sm.hist[i] = 0;
-    __syncthreads();
+    if (!first) {
+      for (int i = tid; i < kBins; i += kSelectThreads) sm.hist[i] = 0;
+      __syncthreads();
+    }
     for (int i = p_first + tid; i < p_last; i += kSelectThreads) {
       const uint32_t k = keys[i] - least;
       if (first || (k >> below) == border) atomicAdd(&sm.hist[(k >> shift) & ((1u << width) - 1)], 1u);
@@ -539,7 +554,7 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const SelectA
         if (above < want && above + mine[i] >= want) {
           sm.border = static_cast<uint32_t>(kBins - 1 - (tid * kPerThread + i));
           sm.above = above;
-          sm.whole = above + mine[i] == want;
+          sm.at_it = mine[i];
           above = want;
         } else {
           above += mine[i];
@@ -549,7 +564,31 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const SelectA
     __syncthreads();
     border = (first ? 0u : border << width) | sm.border;
     want -= sm.above;
-    whole = sm.whole != 0;
+    const uint32_t at_border = sm.at_it;
+    whole = at_border == want;
+    if (!whole && shift > 0 && at_border <= kFewKeys) {  // a handful as a rule: each is compared with all
+      for (int i = p_first + tid; i < p_last; i += kSelectThreads) {
+        const uint32_t k = keys[i] - least;
+        if ((k >> shift) == border) sm.hist[atomicAdd(&sm.gathered, 1u)] = k;
+      }
+      __syncthreads();
+      if (tid < at_border) {
+        const uint32_t own_key = sm.hist[tid];
+        uint32_t larger = 0, equal_too = 0;
+        for (uint32_t i = 0; i < at_border; ++i) {
+          larger += sm.hist[i] > own_key;
+          equal_too += sm.hist[i] >= own_key;
+        }
+        if (larger < want && equal_too >= want) {  // equal keys write the same
+          sm.border = own_key;
+          sm.above = larger;
+        }
+      }
+      __syncthreads();
+      border = sm.border;
+      want -= sm.above;
+      shift = 0;
+    }
   }
   // ---- every thread a run of pages; how many lie above the border and at it
   const int per = (pages + kSelectThreads - 1) / kSelectThreads, i0 = min(pages, tid * per), i1 = min(pages, i0 + per);
@@ -573,7 +612,6 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const SelectA
       sb += ub;
     }
   }
-  __syncthreads();
   if (lane == 31) {
     sm.warps[0][warp] = sa;
     sm.warps[1][warp] = sb;

@@ -243,3 +243,20 @@ def test_bounds_of_codes_whose_scales_are_far_apart_or_no_powers_of_two():
         for p in range(6):
             want, s = po.page_bounds(value[p * 64:min(p * 64 + 64, 6 * 64 - 5), 0])
             assert np.array_equal(bounds[p, 0].cpu().numpy(), want) and float(bs[0, p]) == s
+
+
+@pytest.mark.parametrize("pages", [300, 2500])
+def test_many_pages_at_the_border(pages):
+    """Scores that one page far above squeezes into few digits: hundreds at the border, told apart by their last bits or not at all."""
+    c = Choice([16 * pages] * 2, 2, 1, 16, 10)
+    g = torch.Generator().manual_seed(11)
+    c.q[:] = 1
+    c.bounds[:] = 0
+    c.bounds[:, 0, 1, 0] = 127
+    c.bounds[:, 0, 1, 1:9] = torch.randint(0, 3, (len(c.bounds), 8), generator=g).to(torch.int8)
+    c.scale[:] = 2.0 ** -30
+    c.scale[0, c.table[0, 5]] = 2.0 ** 30
+    c.bounds[c.table[1, 40]] = -1  # and one below zero
+    for most in (3, 100, pages // 2, pages - 1):
+        assert c.run(most) == c.want(most)
+        assert c.run(most, 0, 0) == c.want(most, 0, 0)
