@@ -667,14 +667,15 @@ fsx_status fsx_page_select(const void* d_q, long long q_stride, int dtype, const
  *   2. It grows by n = d_new_offsets[i+1] - d_new_offsets[i] rows (DEVICE int64 [B+1], within 0 .. new_rows). New rows go on in its
  *      last page if that has room. If others hold that page too, it gets a page in its place, and the pair (old, new) is
  *      listed for fsx_pages_copy; of the requests that do so at once the last one keeps the page if nobody else
- *      holds it. New pages are the lowest free ones, in the order of the requests.
+ *      holds it, and all others leave it. New pages are the lowest free ones, in the order of the requests.
  *   d_table_out [B, width], d_lengths_out [B], d_refs_out [n_pages]: the new state. Without d_source each may be its input.
  *                With d_source the table and the lengths need buffers of their own. A table in its own place changes only where
  *                pages are new; one in another is written whole, -1 behind a request's last page.
  *   d_rows     : DEVICE int64 [new_rows]: the cache row of every new row, for fsx_cache_write_e4m3 or fsx_rotary.
  *   d_pairs    : DEVICE int32 [B, 2], d_n_pairs : DEVICE int32: pages to copy (before the new rows are written).
  * If the free pages do not last, requests are served in order; the first that finds too few and those behind it that
- * need pages do not grow, get rows of -1, and FSX_ERR_OOM is set. A request that would pass its table's width, whose source or
+ * need pages do not grow, get rows of -1, and FSX_ERR_OOM is set; nor does one that would have kept a page which one of these
+ * goes on holding. A request that would pass its table's width, whose source or
  * offsets are out of range, or whose last page is none of the cache sets FSX_ERR_DEVICE_ARG and does not grow either (a bad
  * source or length: comes out empty); other entries that name no page are taken along and counted nowhere. */
 fsx_status fsx_pages_step(const int32_t* d_table, const int64_t* d_lengths, const int32_t* d_refs, int B_in,

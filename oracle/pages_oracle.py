@@ -124,10 +124,13 @@ class Pages:
             copies.append(p is not None and refs[p] > 1 and not (refs[p] == len(others) and b == others[-1]))
         free = [p for p, r in enumerate(refs) if r <= 0]
         taken, short, pairs, rows = 0, False, [], []
+        stay = set()  # pages that a request which found no page for its copy goes on holding
         for b, (n, a) in enumerate(zip(list(out.lengths), grow)):
             wants = self.need(n + a) - (self.need(n) - copies[b]) if a else 0
             fits = not wants or (not short and taken + wants <= len(free))
-            if not fits:
+            if copies[b] and not fits:
+                stay.add(writes[b])
+            if not fits or (a and not copies[b] and writes[b] in stay):
                 short = True
                 rows += [-1] * new[b]
                 continue

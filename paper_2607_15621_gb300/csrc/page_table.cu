@@ -39,7 +39,8 @@ struct TableShared {
   int add[kMaxSequences];                 // new tokens, 0: none or not possible
   long long end[kMaxSequences];           // pages that it and the requests before it need
   unsigned char copies[kMaxSequences];
-  int nth[kMaxSequences];  // copies of the requests before
+  short leaves[kMaxSequences];  // the last of the others that write into the page that it keeps, if any, else -1
+  int nth[kMaxSequences];       // copies of the requests before
   long long scan[kWarps];
   int scan2[kWarps];
   int counts[2][kCtas];
@@ -183,23 +184,34 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) step_k
 #pragma unroll
     for (int j = 0; j < 4; ++j) free_pages += i + j < last_page && load_l2(a.refs_out + i + j) <= 0;
   long long need[kPerThread], mine = 0;
-  int copy[kPerThread], my_copies = 0;
+  int copy[kPerThread], leaves[kPerThread], my_copies = 0;
   const int per = (a.B + kThreads - 1) / kThreads;  // requests of a thread, one behind another
 #pragma unroll
   for (int u = 0; u < kPerThread; ++u) {
     const int i = tid * per + u;
     need[u] = 0;
     copy[u] = 0;
+    leaves[u] = -1;
     if (u < per && i < a.B) {
       const int last = sm.last[i], held = last >= 0 ? load_l2(a.refs_out + last) : 0;
       if (held > 1) {  // of all that write into it the last one keeps it, if nobody else holds it
-        int writers = 0, behind = 0;
+        int writers = 0, behind = -1, next = -1;  // the last one, and the one before it
+        auto see = [&](int page, int x) {
+          if (page == last) {
+            ++writers;
+            next = behind;
+            behind = x;
+          }
+        };
         for (int x = 0; x < a.B; x += 4) {
           const int4 other = *reinterpret_cast<const int4*>(&sm.last[x]);
-          writers += (other.x == last) + (other.y == last) + (other.z == last) + (other.w == last);
-          behind = other.w == last ? x + 3 : other.z == last ? x + 2 : other.y == last ? x + 1 : other.x == last ? x : behind;
+          see(other.x, x);
+          see(other.y, x + 1);
+          see(other.z, x + 2);
+          see(other.w, x + 3);
         }
         copy[u] = !(held == writers && i == behind);
+        if (!copy[u]) leaves[u] = next;
       }
       if (sm.add[i] > 0) need[u] = pages_for(static_cast<long long>(sm.n[i]) + sm.add[i], a.shift) - (pages_for(sm.n[i], a.shift) - copy[u]);
       mine += need[u];
@@ -238,6 +250,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) step_k
       before += need[u];
       sm.end[i] = before;
       sm.copies[i] = static_cast<unsigned char>(copy[u]);
+      sm.leaves[i] = static_cast<short>(leaves[u]);
       sm.nth[i] = copies_before;
       copies_before += copy[u];
     }
@@ -248,9 +261,12 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) step_k
     if (r < rank) nth_free += sm.counts[0][r];
     all_free += sm.counts[0][r];
   }
-  // a request grows if the pages last for it and all before it, or if it needs none
+  // A request grows if the pages last for it and all before it, or if it needs none. One that keeps a page which others write into grows only if
+  // they leave it: where the last of them gets a page for its copy, those before it have theirs.
   auto start_of = [&](int i) { return i > 0 ? sm.end[i - 1] : 0ll; };
-  auto grows = [&](int i) { return sm.end[i] <= all_free || sm.end[i] == start_of(i); };
+  auto grows = [&](int i) {
+    return (sm.end[i] <= all_free || sm.end[i] == start_of(i)) && (sm.leaves[i] < 0 || sm.end[sm.leaves[i]] <= all_free);
+  };
   const long long wanted = min(total, all_free);
   for (int base = first; base < last_page && nth_free < wanted; base += kThreads) {
     const int page = base + tid;
