@@ -621,8 +621,7 @@ fsx_status fsx_rotary(const void* d_q, long long q_stride, const void* d_k, cons
  *                heads of that kv head. Entries are places in the request's table (0: its first page), distinct, in any order; of a request
  *                with n pages the first min(n, n_picked) are read; -1: none. Any other entry that is no page of
  *                the request sets FSX_ERR_DEVICE_ARG, and the heads of that kv head get no output. n_picked is 1 .. 4096.
- *   roundings  : the weights of the values go into the product as two 16-bit parts where one would show (over 16-bit caches, and for
- *                FSX_F16 over 8-bit ones), so that an output is rounded once, by its own type.
+ *   roundings  : the weights of the values go into the product as two 16-bit parts, so that an output is rounded once, by its own type.
  *   d_out      : DEVICE [B, n_heads, 128] of `dtype`; d_lse : DEVICE fp32 [n_heads, B] or NULL. A request without rows gets
  *                zeros and -infinity.
  *   d_workspace : as fsx_tree_attention: fsx_paged_attention_workspace_bytes(...) bytes, 256-byte aligned, zeroed once, for calls of

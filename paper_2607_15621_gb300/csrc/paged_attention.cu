@@ -476,11 +476,10 @@ __global__ void __launch_bounds__(32 * Shape<C8, NT, LINE>::kWarps, Shape<C8, NT
     State<NT> st;
     float f[NT][2];
     make_queries<BF, C8, NT>(qf, f);
-    // Weights as fine as the output's type, bf16 over bf16 and fp16 over anything, go into the product in two parts, so that their
-    // rounding does not show. An infinity among the values of a 16-bit cache times a second part of zero or less is none any more: sums
-    // that are not finite are made again from the first parts alone.
-    constexpr bool kSplit = !C8 || !BF;
-    bool second = kSplit;
+    // Weights go into the product in two parts of its type, bf16 over bf16 and fp16 otherwise, so that their rounding does not
+    // show. An infinity among the values of a 16-bit cache times a second part of zero or less is none any more: sums that are not
+    // finite are made again from the first parts alone.
+    bool second = true;
 #pragma unroll 1
     for (;;) {
 #pragma unroll
@@ -501,7 +500,7 @@ __global__ void __launch_bounds__(32 * Shape<C8, NT, LINE>::kWarps, Shape<C8, NT
         __syncwarp();  // every lane's copies of the stage; and the stage before is read
         const int left = sm.left[warp][slot_out];
         copy_next(it);
-        if (left > 0) cache_step<BF, C8, NT, kSplit>(st, sm.ring[warp] + slot_out * S::kBytes, qf, f, left, second);
+        if (left > 0) cache_step<BF, C8, NT, true>(st, sm.ring[warp] + slot_out * S::kBytes, qf, f, left, second);
         slot_out = slot_out + 1 == kStages ? 0 : slot_out + 1;
       }
       cp_async_wait<0>();
