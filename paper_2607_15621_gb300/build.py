@@ -9,6 +9,7 @@ is the Python extension that passes torch tensors to some of its entry points.
 """
 from __future__ import annotations
 
+import importlib.util
 import os
 import shutil
 import subprocess
@@ -46,10 +47,31 @@ def _run(cmd):
     return res.stdout + res.stderr
 
 
+def _torch() -> str:
+    """Where torch lies; empty: nowhere. It is not imported."""
+    spec = importlib.util.find_spec("torch")
+    return os.path.dirname(spec.origin) if spec is not None and spec.origin else ""
+
+
+def calls_lacks() -> str:
+    """What a build of the extension module lacks on this machine; empty: nothing."""
+    at, python, cxx = _torch(), os.path.join(sysconfig.get_paths()["include"], "Python.h"), os.environ.get("CXX", "g++")
+    header = os.path.join(at, "include", "torch", "csrc", "autograd", "python_variable.h")
+    lacks = ["torch" if not at else "" if os.path.exists(header) else header,
+             "" if os.path.exists(python) else python, "" if shutil.which(cxx) else cxx]
+    return ", ".join(x for x in lacks if x)
+
+
 def _build_calls() -> str:
-    """The extension module: plain C++ against this interpreter's and this torch's headers."""
-    import torch
-    at = os.path.dirname(torch.__file__)
+    """The extension module: plain C++ against this interpreter's and this torch's headers. Where they are missing it is left out:
+    the library has no use for them."""
+    lacks = calls_lacks()
+    if os.path.exists(CALLS):
+        os.remove(CALLS)  # of an earlier build
+    if lacks:
+        print(f"{CALLS} is not built: no {lacks}", file=sys.stderr)
+        return ""
+    at = _torch()
     include = [sysconfig.get_paths()["include"], os.path.join(at, "include"),
                os.path.join(at, "include", "torch", "csrc", "api", "include"), os.path.join(ROOT, "include")]
     out = _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", *(x for i in include for x in ("-I", i)),
@@ -72,10 +94,10 @@ def build(verbose: bool = False, extra_flags=()) -> str:
     with ThreadPoolExecutor(max_workers=len(cmds) + 1) as ex:
         calls = ex.submit(_build_calls)
         logs = list(ex.map(_run, cmds))
+        tmp = LIB + ".tmp"
+        logs.append(_run([cc, *ARCH, "-shared", "-Xcompiler", "-pthread", "-o", tmp, *objs]))
+        os.replace(tmp, LIB)
         logs.append(calls.result())
-    tmp = LIB + ".tmp"
-    logs.append(_run([cc, *ARCH, "-shared", "-Xcompiler", "-pthread", "-o", tmp, *objs]))
-    os.replace(tmp, LIB)
     if verbose:
         print("".join(logs))
     return LIB

@@ -559,7 +559,10 @@ def _native():
         import torch
         lib()
         if not os.path.exists(CALLS_PATH):
-            raise RuntimeError(f"{CALLS_PATH} is missing: build it with paper_2607_15621_gb300.build.build()")
+            from .build import calls_lacks
+            lacks = calls_lacks()
+            raise RuntimeError(f"{CALLS_PATH} is missing: build it with paper_2607_15621_gb300.build.build()"
+                               + (f" (not here: {lacks})" if lacks else ""))
         spec = importlib.util.spec_from_file_location("_calls", CALLS_PATH)
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
