@@ -594,8 +594,8 @@ fsx_status fsx_tree_attention(const void* d_q, long long q_stride, const void* d
 
 /* Rotary positions of one to four axes (say time, height, width), and the keys' and values' rows into a cache.
  * Pair j (0 .. 63) of a head is its dims (j, j + 64), or (2 j, 2 j + 1) with FSX_ROTARY_ADJACENT; it turns by
- * d_positions[axis[j]][row] * rate[j] radians: (a, b) -> (a cos - b sin, a sin + b cos). Angles are exact to
- * 2^-32 of a turn at any position up to 2^31 (negative ones turn back); products are fp32, rounded once.
+ * d_positions[axis[j]][row] * rate[j] radians: (a, b) -> (a cos - b sin, a sin + b cos). Angles are off by less
+ * than 2^-31 of a turn at any position up to 2^31 (negative ones turn back); products are fp32, rounded once.
  *   d_q, d_q_out : DEVICE [n_rows] rows of `dtype` (FSX_BF16 or FSX_F16), strides apart; or both NULL.
  *   d_k, d_k_out : the same with n_kv_heads. Either result may be its input itself (same pointer and stride).
  *                  d_k_out may be NULL where there is a cache; all NULL: queries only.

@@ -2,8 +2,9 @@
 // same pass (fsx_rotary).
 //
 // Pair j of a head turns by pos[axis_j] rate_j: (a, b) -> (a cos - b sin, a sin + b cos). The angle is taken in whole turns as
-// 64-bit fixed point: turns_j = rate_j / (2 pi) in units of 2^-64, and pos * turns_j modulo 2^64 is the fraction of a turn,
-// exactly as far as turns_j is; its upper 32 bits give the quarter turn and the rest, whose sine and cosine are Taylor's series. An
+// 64-bit fixed point: turns_j = rate_j / (2 pi) in units of 2^-64, rounded down, and pos * turns_j modulo 2^64 is the fraction of a turn,
+// exactly as far as turns_j is (2^-33 at a position of 2^31); its upper 32 bits, less than 2^-32 below it, give the quarter turn and the
+// rest, whose sine and cosine are Taylor's series. An
 // angle in fp32 would be off by 2^-24 of itself, at position 100,000 by half a percent of a turn.
 // Products in fp32, rounded once to the type; keys go into an 8-bit cache from their rounded values, so that a cache written
 // here has the bits of one written from the rotated keys by fsx_cache_write_e4m3.
@@ -43,7 +44,7 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
 }
 
 // Cosine and sine of `t` 2^-32 turns. |x| <= pi / 4 behind the nearest quarter: Taylor's series to x^8 and x^9 leave 2.5e-8 and 2e-9 out,
-// less than fp32's rounding of the result (28,001 rows of 5 heads 28.6 us, with sincospif, which takes arguments of any size, 29.6).
+// about fp32's rounding of the result (28,001 rows of 5 heads 19.4 us, with sincospif, which takes arguments of any size, 19.7).
 __device__ __forceinline__ float2 turned_by(uint32_t t) {
   const uint32_t q = (t + 0x20000000u) >> 30;
   const float x = static_cast<float>(static_cast<int32_t>(t - (q << 30))) * (6.28318530718f / 4294967296.f);
