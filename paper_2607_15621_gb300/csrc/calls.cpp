@@ -76,6 +76,16 @@ class Args {
   void* stream = nullptr;
 };
 
+// Other threads run meanwhile: a full launch queue waits. Also where torch throws of a tensor, what catches it holds the lock again.
+class Unlocked {
+ public:
+  Unlocked() : state_(PyEval_SaveThread()) {}
+  ~Unlocked() { PyEval_RestoreThread(state_); }
+
+ private:
+  PyThreadState* state_;
+};
+
 template <typename F>
 PyObject* answer(Args& a, F call) {
   if (!a.good) {
@@ -83,9 +93,10 @@ PyObject* answer(Args& a, F call) {
     return PyLong_FromLong(-1);
   }
   long status;
-  Py_BEGIN_ALLOW_THREADS;  // a full launch queue waits
-  status = call();
-  Py_END_ALLOW_THREADS;
+  {
+    Unlocked meanwhile;
+    status = call();
+  }
   return PyLong_FromLong(status);
 }
 
