@@ -113,6 +113,8 @@ int code_of(const Tensor& t) {
 bool is(const Tensor* t, ScalarType type, std::initializer_list<int64_t> shape) {
   return t->scalar_type() == type && t->sizes() == at::IntArrayRef(shape) && t->is_contiguous();
 }
+// sizes that the entry points take in 32 bits
+bool fit(std::initializer_list<int64_t> sizes) { return std::max(sizes) <= INT32_MAX; }
 // [rows, heads, head_dim] whose rows are contiguous
 bool rows(const Tensor* t) {
   return t->dim() == 3 && t->stride(2) == 1 && (t->stride(1) == t->size(2) || t->size(1) == 1);
@@ -182,6 +184,7 @@ PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
             is(table, ScalarType::Int, {B, table->size(1)}) && is(lengths, ScalarType::Long, {B}) && two_caches(kc, vc, dim));
     a.check(a.good && (code_of(*kc) != FSX_E4M3 || scales(ks, vs, kc->size(1), kc->size(0))));
     a.check(a.good && (!picked || (picked->dim() == 3 && picked->size(2) > 0 && is(picked, ScalarType::Int, {B, kc->size(1), picked->size(2)}))));
+    a.check(a.good && fit({B, table->size(1), picked ? picked->size(2) : 0}));
     a.check(!lse || is(lse, ScalarType::Float, {heads, B}));
   }
   return answer(a, [&] {
@@ -197,7 +200,8 @@ PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
 // a table of requests, their lengths, and the bounds of `pages` pages
 bool paged(const Tensor* table, const Tensor* lengths, const Tensor* bounds, const Tensor* scale, int64_t pages, int64_t kv_heads, int64_t dim) {
   return table->dim() == 2 && is(table, ScalarType::Int, {table->size(0), table->size(1)}) && is(lengths, ScalarType::Long, {table->size(0)}) &&
-         is(bounds, ScalarType::Char, {pages, kv_heads, 2, dim}) && is(scale, ScalarType::Float, {kv_heads, pages});
+         is(bounds, ScalarType::Char, {pages, kv_heads, 2, dim}) && is(scale, ScalarType::Float, {kv_heads, pages}) &&
+         fit({table->size(0), table->size(1)});
 }
 
 // k_cache, table, lengths, page_rows, bounds, bound_scale, status, k_scale, start
@@ -226,7 +230,7 @@ PyObject* page_select(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const int first = a.small(), last = a.small();
   a.check(a.good && rows(q) && bounds->dim() == 4 && code_of(*q) >= 0 && q->size(2) == bounds->size(3) &&
           paged(table, lengths, bounds, scale, bounds->size(0), bounds->size(1), bounds->size(3)) && table->size(0) == q->size(0) &&
-          picked->dim() == 3 && is(picked, ScalarType::Int, {q->size(0), bounds->size(1), picked->size(2)}));
+          picked->dim() == 3 && is(picked, ScalarType::Int, {q->size(0), bounds->size(1), picked->size(2)}) && fit({picked->size(2)}));
   return answer(a, [&] {
     return f_page_select(ptr(q), pitch(q), code_of(*q), ptr<int8_t>(bounds), ptr<float>(scale), bounds->size(0) * page_rows, page_rows,
                          ptr<int32_t>(table), static_cast<int>(table->size(1)), ptr<int64_t>(lengths), static_cast<int>(q->size(0)),
@@ -248,7 +252,7 @@ PyObject* pages_step(PyObject*, PyObject* const* args, Py_ssize_t n) {
     a.check(is(table, ScalarType::Int, {B_in, width}) && is(lengths, ScalarType::Long, {B_in}) && is(refs, ScalarType::Int, {pages}) &&
             is(offsets, ScalarType::Long, {B + 1}) && is(table_out, ScalarType::Int, {B, width}) && is(lengths_out, ScalarType::Long, {B}) &&
             is(refs_out, ScalarType::Int, {pages}) && is(to, ScalarType::Long, {total}) && is(pairs, ScalarType::Int, {B, 2}) &&
-            is(n_pairs, ScalarType::Int, {1}) && (!source || is(source, ScalarType::Int, {B})) && width <= INT32_MAX && pages <= INT32_MAX);
+            is(n_pairs, ScalarType::Int, {1}) && (!source || is(source, ScalarType::Int, {B})) && fit({B_in, B, width, pages}));
   }
   return answer(a, [&] {
     return f_pages_step(ptr<int32_t>(table), ptr<int64_t>(lengths), ptr<int32_t>(refs), static_cast<int>(B_in), ptr<int32_t>(source),
@@ -269,8 +273,7 @@ PyObject* pages_compact(PyObject*, PyObject* const* args, Py_ssize_t n) {
     B = table->size(0), width = table->size(1), pages = refs->size(0);
     a.check(is(table, ScalarType::Int, {B, width}) && is(lengths, ScalarType::Long, {B}) && is(refs, ScalarType::Int, {pages}) &&
             is(table_out, ScalarType::Int, {B, width}) && is(refs_out, ScalarType::Int, {pages}) &&
-            is(pairs, ScalarType::Int, {pairs->size(0), 2}) && is(n_pairs, ScalarType::Int, {1}) && width <= INT32_MAX && pages <= INT32_MAX &&
-            pairs->size(0) <= INT32_MAX);
+            is(pairs, ScalarType::Int, {pairs->size(0), 2}) && is(n_pairs, ScalarType::Int, {1}) && fit({B, width, pages, pairs->size(0)}));
   }
   return answer(a, [&] {
     return f_pages_compact(ptr<int32_t>(table), ptr<int64_t>(lengths), ptr<int32_t>(refs), static_cast<int>(B), static_cast<int>(width),
@@ -286,7 +289,7 @@ PyObject* pages_copy(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const int n_planes = a.small(), n_pages = a.small();
   const Tensor *pairs = a.tensor(), *n_pairs = a.tensor(), *status = a.word();
   a.check(a.good && pairs->dim() == 2 && is(pairs, ScalarType::Int, {pairs->size(0), 2}) && is(n_pairs, ScalarType::Int, {1}) &&
-          pairs->size(0) <= INT32_MAX);
+          fit({pairs->size(0)}));
   return answer(a, [&] {
     return f_pages_copy(planes, n_planes, n_pages, ptr<int32_t>(pairs), ptr<int32_t>(n_pairs), static_cast<int>(pairs->size(0)), ptr<int>(status),
                         a.stream);
