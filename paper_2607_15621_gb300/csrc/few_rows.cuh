@@ -158,8 +158,13 @@ __device__ __forceinline__ void softmax_step(State<NT>& st, float (&s)[NT][4], f
     pt[t][1] = transpose8x8(second);
     if (SPLIT) {
       const float2 x = unpack16<BF>(first), y = unpack16<BF>(second);
-      pt[t][SPLIT ? 2 : 0] = transpose8x8(pack16<BF>(p[t][0] - x.x, p[t][1] - x.y));
-      pt[t][SPLIT ? 3 : 1] = transpose8x8(pack16<BF>(p[t][2] - y.x, p[t][3] - y.y));
+      float rest[4] = {p[t][0] - x.x, p[t][1] - x.y, p[t][2] - y.x, p[t][3] - y.y};
+      if (C8) {  // weights are 2^15 at most, second parts 8; an infinite scale's weight is infinite in its first part, and has a second one too
+#pragma unroll
+        for (int e = 0; e < 4; ++e) rest[e] = fminf(rest[e], 32.f);
+      }
+      pt[t][SPLIT ? 2 : 0] = transpose8x8(pack16<BF>(rest[0], rest[1]));
+      pt[t][SPLIT ? 3 : 1] = transpose8x8(pack16<BF>(rest[2], rest[3]));
     }
   }
 }

@@ -61,3 +61,28 @@ def test_the_weights_rounding_does_not_show(dtype, cache, heads, kv_heads, repea
     slack = abs(to64(out) - want) - U[dtype] * abs(want) - 2.0 ** -25
     print("slack %.3g" % slack.max())
     assert int(st) == 0 and slack.max() <= (2.0 ** -15 if dtype == BF and cache == "same" else 2.0 ** -16)
+
+
+@pytest.mark.parametrize("repeat", [1, 60])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_infinite_scales_of_values_are_carried(dtype, repeat):
+    """A value is its code times its row's scale: infinite, or NaN where the code is 0."""
+    n, B = 50, 2 * repeat
+    g = torch.Generator().manual_seed(4)
+    k, v = (torch.randint(1, 60, (64, 4, 128), generator=g, dtype=torch.uint8) for _ in "kv")  # positive codes
+    v[:, 0, 3], v[7, 1, 5] = 0, 0x80 | 9
+    ks, vs = torch.full((4, 64), 0.25), torch.full((4, 64), 0.5)
+    vs[:, 7], vs[2, 40] = float("inf"), float("inf")
+    table = torch.arange(4, dtype=torch.int32).repeat(B, 1)
+    lengths = torch.tensor([n, 7] * repeat)  # every second request ends before that row
+    out, st = torch.empty(B, 8, 128, dtype=dtype, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    q = normal(g, B, 8, 128, dtype=dtype)
+    ws = torch.zeros(fsx.paged_attention_workspace_bytes(B, 8, 4), dtype=torch.uint8, device="cuda")
+    f8 = lambda x: x.cuda().view(torch.float8_e4m3fn)
+    fsx.paged_attention(q.cuda(), f8(k), f8(v), table.cuda(), lengths.cuda(), 16, out, st, ws, k_scale=ks.cuda(), v_scale=vs.cuda())
+    got = out.float().cpu().view(B, 4, 2, 128)
+    assert int(st) == 0 and got[1::2].isfinite().all()
+    got = got[0::2]
+    assert got[:, 0, :, 3].isnan().all() and (got[:, 1, :, 5] == -float("inf")).all()
+    got[:, 0, :, 3], got[:, 1, :, 5] = float("inf"), float("inf")
+    assert (got == float("inf")).all()
