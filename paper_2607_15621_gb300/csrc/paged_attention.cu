@@ -18,8 +18,8 @@
 // The pieces of a cut item are joined by the CTA that ends last, in the order of the keys. A piece that meets a page number
 // outside the cache marks its result, and its item writes nothing.
 //
-// Measured: 128 requests of 64 to 2048 8-bit rows, 32 heads, 170 to 182 us (5.9 to 6.3 TB/s, 0.87 to 0.94 of a copy's rate; DRAM 76 %
-// busy, issue slots 54 %); one of 131,072 8-bit rows, 32 heads over 8, 49 to 52 us (5.3 to 5.6 TB/s: 4 us before the first products, 5
+// Measured: 128 requests of 64 to 2048 8-bit rows, 32 heads, 179 to 187 us (5.8 to 6.0 TB/s, 0.85 to 0.89 of a copy's rate; DRAM 73 %
+// busy, issue slots 55 %; with weights in one part 173 to 183); one of 131,072 8-bit rows, 32 heads over 8, 49 to 52 us (5.3 to 5.6 TB/s: 4 us before the first products, 5
 // after the last, SMs that differ by 12 %); 16 of 1000 to 8192 16-bit rows 44 us (5.2 TB/s); one of 224 rows 5.6 us.
 #include <math_constants.h>
 
@@ -32,10 +32,10 @@ namespace fsx {
 
 namespace {
 
-// queue: chunks of an item that is not cut, and of a piece (64 requests of 500 to 4096 rows, 8 kv heads: 66 us, with 28 chunks 70)
+// queue: chunks of an item that is not cut, and of a piece (64 requests of 500 to 4096 rows, 8 kv heads: 70 us, with 28 chunks 74)
 constexpr int kFew = 8, kMany = 14;
-// line, in steps: the least range; how near an item's end a cut moves there (32 requests of 500 to 4096 rows: 56 us, with 8 or 32 steps 63); the longest
-// item that stays whole where there is little work (8 requests of 100 to 700 rows, 4 kv heads: 8.9 us, with 32 steps 10.4); how many a CTA that is
+// line, in steps: the least range; how near an item's end a cut moves there (32 requests of 500 to 4096 rows: 56 us, with 8 or 32 steps 61); the longest
+// item that stays whole where there is little work (8 requests of 100 to 700 rows, 4 kv heads: 9.0 us, with 32 steps 10.5); how many a CTA that is
 // (4 requests of 500 to 2000 rows, 32 kv heads: 18.5 us, 22.8 as a line)
 constexpr int kLeast = 32, kSnap = 16, kWhole = 64, kShort = 128;
 constexpr int kHeader = 64;          // ints of the workspace, queue: [0] pieces taken, [1] CTAs that are done
@@ -754,7 +754,7 @@ size_t paged_attention_workspace_bytes(int B, int n_heads, int n_kv_heads) {
   return (kHeader + kCounters) * sizeof(int) + slots_of(nt) * slot_floats(nt) * sizeof(float);
 }
 
-// Items a SM up to which the line is taken: 256 items of 500 to 4096 rows 63 us, in the queue 65; 512 of them 82 to 92 and 66.
+// Items a SM up to which the line is taken: 256 items of 500 to 4096 rows 56 us, in the queue 60; 512 of them 84 and 70.
 constexpr int kLineItems = 2;
 
 cudaError_t launch_paged_attention(const PagedArgs& a, int dtype, bool cache8, cudaStream_t stream) {
