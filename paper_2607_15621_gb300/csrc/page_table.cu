@@ -10,7 +10,7 @@
 // Bound by latency: a handful of dependent trips to memory; the holders' counts are read twice.
 // The copies are bound by memory: both ends of every page move once, all layers in one launch.
 //
-// Measured: a step of 64 requests over 8192 pages 8.5 us; a compaction of 48 over 4096 pages 7.7 us; 803 pages of 32 KB in 8 planes
+// Measured: a step of 64 requests over 8192 pages 7.9 us; a compaction of 48 over 4096 pages 7.7 us; 803 pages of 32 KB in 8 planes
 // 68 us (6.2 TB/s, 0.91 of a copy's rate); 39 of them 4.1 us.
 #include <cooperative_groups.h>
 
